@@ -511,6 +511,91 @@ malib_status malib_meta_sample_device(const float* sigma, int32_t n_sigma, int32
                                       int64_t env_offset, int32_t* pair_assign_out,
                                       void* stream);
 
+/* ------------------------------------------------------ learner operators */
+
+/*
+ * What a learner runs between the trajectory records (malib_rollout_batch_traj)
+ * and the next policy of the pool (malib_pop_extend): the linear layer of an
+ * MLP policy with its backward pass, the clipped policy loss with a
+ * divergence term, and the distillation of teachers' top logits, each loss
+ * with its gradient (the Learner of Sec. 3.1, and the training interfaces of
+ * Sec. 3.3).  The calls hold no state: every buffer is the caller's,
+ * workspaces included, all work is asynchronous on `stream`, and nothing is
+ * allocated, so they may be captured into a HIP graph.  Strides are in
+ * elements; rows are contiguous (column stride 1) and may start at any
+ * element, but rows on 16-byte boundaries are faster.  Outputs must not
+ * overlap each other or an input unless a call says so.
+ */
+enum { MALIB_DT_F32 = 0, MALIB_DT_BF16 = 1 };
+
+enum {
+    MALIB_ACT_NONE = 0,
+    MALIB_ACT_RELU = 1,  /* max(z, 0); NaN stays NaN; derivative 0 at 0 */
+    MALIB_ACT_GELU = 2,  /* z Phi(z), Phi the normal distribution function */
+    MALIB_ACT_SILU = 3   /* z / (1 + e^-z) */
+};
+
+/* A matrix per group: element (r, c) of group g at ptr[g * group_stride +
+ * r * row_stride + c].  A group stride of 0 in an input shares it between the
+ * groups. */
+typedef struct {
+    void* ptr;
+    int64_t row_stride;
+    int64_t group_stride;
+} malib_mat;
+
+/* A linear layer of `groups` policies side by side (each with weights of its
+ * own), applied to `rows` inputs of each.
+ * 1 <= groups <= 65535, 0 <= rows < 2^31, 1 <= in, out <= 2^24. */
+typedef struct {
+    int32_t dtype;       /* MALIB_DT_*: type of every matrix */
+    int32_t act;         /* MALIB_ACT_* */
+    int64_t groups, rows, in, out;
+} malib_linear_desc;
+
+/*
+ * y = act(x W^T + b) + residual.
+ *  x: [rows][in]; w: [out][in] (row = output unit, as the populations');
+ *  bias: device fp32 [groups][out], contiguous, or NULL (zero);
+ *  residual: [rows][out] or NULL; may be y itself (same address and strides);
+ *  pre: [rows][out] or NULL: receives z = x W^T + b, which the backward pass
+ *       of a layer with an activation needs;
+ *  y: [rows][out].
+ *  work, work_bytes: device workspace of at least the bytes that
+ *       malib_linear_work reports (NULL and 0 where it reports 0), aligned to
+ *       16 bytes.
+ * Sums are formed in fp32 (bf16 on the bf16 matrix cores, fp32 on the fp32
+ * ones), each output rounded once; bias, activation and residual are applied
+ * before that rounding.  Results do not depend on the run: the order of every
+ * sum is fixed by the sizes.
+ */
+malib_status malib_linear(const malib_linear_desc* desc, const malib_mat* x, const malib_mat* w,
+                          const float* bias, const malib_mat* residual, const malib_mat* pre,
+                          const malib_mat* y, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * The gradients of malib_linear: dz = dy act'(z), dx = dz W, dw = dz^T x
+ * (summed over the rows), dbias = the sum of dz over the rows.  The
+ * residual's gradient is dy itself.
+ *  dy: [rows][out]; x, w: as in malib_linear (x may be NULL without dw, w
+ *  without dx); pre: [rows][out], the z that malib_linear wrote, required
+ *  with an activation;
+ *  dx: [rows][in], dw: [out][in], dbias: device fp32 [groups][out]; each may
+ *  be NULL (not computed).  An x or w shared by the groups (stride 0) gets
+ *  each group's own gradient; their sum is the caller's.
+ * dz enters the two products in the layer's type (with bf16 and GELU or SiLU a
+ * rounding of its own; none, relu: exact), dbias sums it unrounded.
+ */
+malib_status malib_linear_backward(const malib_linear_desc* desc, const malib_mat* dy,
+                                   const malib_mat* x, const malib_mat* w, const malib_mat* pre,
+                                   const malib_mat* dx, const malib_mat* dw, float* dbias,
+                                   void* work, int64_t work_bytes, void* stream);
+
+/* Workspace bytes of malib_linear (backward == 0) or malib_linear_backward
+ * with every output (backward != 0) for this description.  Host only. */
+malib_status malib_linear_work(const malib_linear_desc* desc, int32_t backward,
+                               int64_t* work_bytes);
+
 /* Message for the last non-OK status returned on this thread. */
 const char* malib_last_error(void);
 

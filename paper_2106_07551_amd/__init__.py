@@ -8,9 +8,10 @@ fallback: importing the binding without the built library raises.
 from .binding import (  # noqa: F401
     MalibError, ArgumentError, Population, Env, Trace, Traj, meta_sample,
     meta_sample_device, solve_fp, solve_alpharank, solve_lp,
-    expansion_pairs, aggregate,
+    expansion_pairs, aggregate, linear, linear_backward,
     debug_tanh_ref, debug_bf16, debug_philox,
     lib, LIB_PATH, POLICY_TABULAR, POLICY_MLP_F32, POLICY_MLP_BF16, ENV_MATRIX,
     ENV_ITER_MATRIX, ENV_PURSUIT, ENV_FEATURE, INIT_PER_ENV, INIT_SHARED, K_POLICY,
-    K_SAMPLE, K_ENV, K_SETUP, K_PAYOFF, EXPORTS,
+    K_SAMPLE, K_ENV, K_SETUP, K_PAYOFF, DT_F32, DT_BF16, ACT_NONE, ACT_RELU, ACT_GELU,
+    ACT_SILU, EXPORTS,
 )

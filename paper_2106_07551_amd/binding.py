@@ -20,6 +20,8 @@ POLICY_TABULAR, POLICY_MLP_F32, POLICY_MLP_BF16 = 0, 1, 2
 ENV_MATRIX, ENV_ITER_MATRIX, ENV_PURSUIT, ENV_FEATURE = 0, 1, 2, 3
 INIT_PER_ENV, INIT_SHARED = 0, 1
 K_POLICY, K_SAMPLE, K_ENV, K_SETUP, K_PAYOFF = 0, 1, 2, 3, 4
+DT_F32, DT_BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 # every function declared in include/malib.h
 EXPORTS = [
@@ -30,6 +32,7 @@ EXPORTS = [
     "malib_pop_extend", "malib_expansion_pairs", "malib_aggregate", "malib_rollout_batch_traj",
     "malib_pop_policy_ids", "malib_rollout_batch_noalloc", "malib_pop_set_graph",
     "malib_solve_alpharank", "malib_solve_lp",
+    "malib_linear", "malib_linear_backward", "malib_linear_work",
 ]
 
 
@@ -71,6 +74,15 @@ class TraceDesc(C.Structure):
 class TrajDesc(C.Structure):
     _fields_ = [("actions", C.c_void_p), ("rewards", C.c_void_p), ("flags", C.c_void_p),
                 ("obs", C.c_void_p), ("capacity", C.c_int64), ("cursor", C.c_int64)]
+
+
+class Mat(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("row_stride", C.c_int64), ("group_stride", C.c_int64)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("groups", C.c_int64),
+                ("rows", C.c_int64), ("inputs", C.c_int64), ("outputs", C.c_int64)]
 
 
 class EvalStats(C.Structure):
@@ -138,6 +150,13 @@ def lib():
         L.malib_pop_set_graph.restype = i32
         L.malib_pop_policy_ids.argtypes = [vp, vp, i32, C.POINTER(i32)]
         L.malib_pop_policy_ids.restype = i32
+        mp, lp = C.POINTER(Mat), C.POINTER(LinearDesc)
+        L.malib_linear.argtypes = [lp, mp, mp, vp, mp, mp, mp, vp, i64, vp]
+        L.malib_linear.restype = i32
+        L.malib_linear_backward.argtypes = [lp, mp, mp, mp, mp, mp, mp, vp, vp, i64, vp]
+        L.malib_linear_backward.restype = i32
+        L.malib_linear_work.argtypes = [lp, i32, C.POINTER(i64)]
+        L.malib_linear_work.restype = i32
         _lib = L
     return _lib
 
@@ -634,6 +653,149 @@ def meta_sample_device(sigma, n_policies: int, n_envs: int, n_agents: int, seed:
                                           None if sr is None else sr.ctypes.data, seed,
                                           env_offset, op, _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------ learner operators
+
+def _empty(shape, dtype, device, stream):
+    """A tensor from the memory pool of the stream the call runs on (the caching
+    allocator hands memory out again in the order of one stream only)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _dtype_code(t, what):
+    import torch
+    if t.dtype == torch.float32:
+        return DT_F32
+    if t.dtype == torch.bfloat16:
+        return DT_BF16
+    raise ArgumentError(f"{what}: expected dtype float32 or bfloat16, got {t.dtype}")
+
+
+def _mat(t, dtype, shape, what, out: bool = False):
+    """A malib_mat over a tensor [rows][cols] or [groups][rows][cols] whose rows
+    are contiguous; `shape` is (groups, rows, cols), groups None for one group.
+    An input without the group dimension is shared by the groups."""
+    if t is None:
+        return None
+    G, rows, cols = shape
+    want = (rows, cols) if G is None else (G, rows, cols)
+    shared = not out and G is not None and t.dim() == 2
+    if tuple(t.shape) != ((rows, cols) if shared else want):
+        raise ArgumentError(f"{what}: expected shape {want}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ArgumentError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    if cols > 1 and t.stride(-1) != 1:
+        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {t.stride(-1)}")
+    row = t.stride(-2) if rows > 1 else cols
+    group = 0 if G is None or shared else t.stride(0) if G > 1 else rows * row
+    return Mat(t.data_ptr(), row, group)
+
+
+def _on_device(*named):
+    for t, what in named:
+        if t is not None and not t.is_cuda:
+            raise ArgumentError(f"{what}: expected a device tensor, got one on {t.device}")
+
+
+def _layer(x_like, w, act):
+    """(groups or None, out, in) of a layer from its weight, and its checks."""
+    if w.dim() not in (2, 3):
+        raise ArgumentError(f"w: expected [out][in] or [groups][out][in], got shape "
+                            f"{tuple(w.shape)}")
+    if x_like.dim() not in (2, 3) or x_like.dim() > w.dim():
+        raise ArgumentError(f"x: expected [rows][in] or, with weights per group, "
+                            f"[groups][rows][in], got shape {tuple(x_like.shape)}")
+    if act not in (ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU):
+        raise ArgumentError(f"act: unknown activation {act!r}")
+    G = w.shape[0] if w.dim() == 3 else None
+    return G, w.shape[-2], w.shape[-1]
+
+
+def _work(desc, backward, work, device, stream):
+    """The workspace a call needs (allocated unless the caller's is given)."""
+    import torch
+    need = C.c_int64()
+    _check(lib().malib_linear_work(C.byref(desc), backward, C.byref(need)))
+    if work is None and need.value:
+        work = _empty(need.value, torch.uint8, device, stream)
+    if work is not None:
+        _dbytes(work, need.value, "work")
+    return work, 0 if work is None else work.numel() * work.element_size()
+
+
+def _ref(m):
+    return None if m is None else C.byref(m)
+
+
+def linear(x, w, bias=None, *, act: int = ACT_NONE, residual=None, pre=None, out=None, work=None,
+           stream=None):
+    """malib_linear: act(x w^T + bias) + residual for x [rows][in] and w
+    [out][in], or [groups][rows][in] and [groups][out][in] (x without the
+    group dimension is shared by the groups); float32 or bfloat16, bias
+    float32.  `pre` receives the values before the activation, which
+    linear_backward needs.  Returns [..][rows][out]."""
+    import torch
+    code = _dtype_code(x, "x")
+    G, n_out, n_in = _layer(x, w, act)
+    rows, dt = x.shape[-2], x.dtype
+    full = (rows, n_out) if G is None else (G, rows, n_out)
+    mx = _mat(x, dt, (G, rows, n_in), "x")
+    mw = _mat(w, dt, (G, n_out, n_in), "w")
+    mr = _mat(residual, dt, (G, rows, n_out), "residual")
+    mp = _mat(pre, dt, (G, rows, n_out), "pre", True)
+    _check_buf(bias, torch.float32, n_out * (G or 1), False, "bias")
+    _on_device((x, "x"), (w, "w"), (bias, "bias"), (residual, "residual"), (pre, "pre"),
+               (out, "out"))
+    if out is None:
+        out = _empty(full, dt, x.device, stream)
+    my = _mat(out, dt, (G, rows, n_out), "out", True)
+    d = LinearDesc(code, act, G or 1, rows, n_in, n_out)
+    work, nbytes = _work(d, 0, work, x.device, stream)
+    _check(lib().malib_linear(C.byref(d), C.byref(mx), C.byref(mw), _dptr(bias), _ref(mr),
+                              _ref(mp), C.byref(my), _dptr(work), nbytes, _stream(stream)))
+    return out
+
+
+def linear_backward(dy, x, w, *, act: int = ACT_NONE, pre=None, want=(True, True, True), dx=None,
+                    dw=None, dbias=None, work=None, stream=None):
+    """malib_linear_backward: (dx, dw, dbias) of linear for the gradient dy of
+    its output; `pre` is what linear wrote there (needed with an activation).
+    `want` leaves outputs out (None is returned for them).  The residual's
+    gradient is dy."""
+    import torch
+    code = _dtype_code(dy, "dy")
+    G, n_out, n_in = _layer(dy, w, act)
+    rows, dt = dy.shape[-2], dy.dtype
+    lead = () if G is None else (G,)
+    mdy = _mat(dy, dt, (G, rows, n_out), "dy")
+    mx = _mat(x, dt, (G, rows, n_in), "x")
+    mw = _mat(w, dt, (G, n_out, n_in), "w")
+    mp = _mat(pre, dt, (G, rows, n_out), "pre") if act != ACT_NONE else None
+    if act != ACT_NONE and pre is None:
+        raise ArgumentError("pre: the backward pass of an activation needs the values before it")
+    _on_device((dy, "dy"), (x, "x"), (w, "w"), (pre, "pre"), (dx, "dx"), (dw, "dw"),
+               (dbias, "dbias"))
+    if want[0] and dx is None:
+        dx = _empty(lead + (rows, n_in), dt, dy.device, stream)
+    if want[1] and dw is None:
+        dw = _empty(lead + (n_out, n_in), dt, dy.device, stream)
+    if want[2] and dbias is None:
+        dbias = _empty(lead + (n_out,), torch.float32, dy.device, stream)
+    dx, dw, dbias = (t if ok else None for t, ok in zip((dx, dw, dbias), want))
+    mdx = _mat(dx, dt, (G, rows, n_in), "dx", True)
+    mdw = _mat(dw, dt, (G, n_out, n_in), "dw", True)
+    _check_buf(dbias, torch.float32, n_out * (G or 1), False, "dbias")
+    d = LinearDesc(code, act, G or 1, rows, n_in, n_out)
+    work, nbytes = _work(d, 1, work, dy.device, stream)
+    _check(lib().malib_linear_backward(
+        C.byref(d), C.byref(mdy), _ref(mx), C.byref(mw), _ref(mp), _ref(mdx), _ref(mdw),
+        _dptr(dbias), _dptr(work), nbytes, _stream(stream)))
+    return dx, dw, dbias
 
 
 def debug_tanh_ref(x, y=None, stream=None):

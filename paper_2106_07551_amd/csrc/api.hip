@@ -71,6 +71,19 @@ malib_status fail(malib_status code, const char* fmt, ...)
     return code;
 }
 
+}  // namespace
+
+malib_status malib::set_error(malib_status code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+namespace {
+
 #define HIP_TRY(expr)                                                                     \
     do {                                                                                  \
         hipError_t e_ = (expr);                                                           \

@@ -1,0 +1,240 @@
+// C entry points of the learner operators: argument checks, workspaces and
+// launch sequences.
+#include "internal.hpp"
+
+using namespace malib;
+
+namespace {
+
+#define HIP_TRY(expr)                                                                     \
+    do {                                                                                  \
+        hipError_t e_ = (expr);                                                           \
+        if (e_ != hipSuccess)                                                             \
+            return set_error(e_ == hipErrorOutOfMemory ? MALIB_E_NOMEM : MALIB_E_HIP,     \
+                             "%s failed: %s", #expr, hipGetErrorString(e_));              \
+    } while (0)
+
+#define TRY(expr)                  \
+    do {                           \
+        malib_status s_ = (expr);  \
+        if (s_ != MALIB_OK)        \
+            return s_;             \
+    } while (0)
+
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxWidth = (int64_t)1 << 24;
+
+int type_size(int dtype) { return dtype == MALIB_DT_BF16 ? 2 : 4; }
+
+int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
+
+malib_status check_linear(const malib_linear_desc* d)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    if (d->dtype != MALIB_DT_F32 && d->dtype != MALIB_DT_BF16)
+        return set_error(MALIB_E_INVAL, "unknown dtype %d", d->dtype);
+    if (d->act < MALIB_ACT_NONE || d->act > MALIB_ACT_SILU)
+        return set_error(MALIB_E_INVAL, "unknown activation %d", d->act);
+    if (d->groups < 1 || d->groups > 65535)
+        return set_error(MALIB_E_INVAL, "groups must be in [1, 65535]");
+    if (d->rows < 0 || d->rows > kMaxRows)
+        return set_error(MALIB_E_INVAL, "rows must be in [0, 2^31)");
+    if (d->in < 1 || d->in > kMaxWidth || d->out < 1 || d->out > kMaxWidth)
+        return set_error(MALIB_E_INVAL, "in and out must be in [1, 2^24]");
+    return MALIB_OK;
+}
+
+// A matrix argument: alignment to its element, a row stride that holds its
+// columns; an output's groups must lie apart.
+malib_status check_mat(const malib_mat* m, const char* what, int64_t rows, int64_t cols,
+                       int64_t groups, int size, bool output)
+{
+    if (!m || !m->ptr)
+        return set_error(MALIB_E_INVAL, "%s is NULL", what);
+    if ((uintptr_t)m->ptr % size)
+        return set_error(MALIB_E_INVAL, "%s is not aligned to its elements", what);
+    if (rows > 1 && m->row_stride < (output ? cols : 0))
+        return set_error(MALIB_E_INVAL, "%s: row stride %lld is below %lld columns", what,
+                         (long long)m->row_stride, (long long)cols);
+    if (m->group_stride < 0)
+        return set_error(MALIB_E_INVAL, "%s: negative group stride", what);
+    if (m->row_stride > ((int64_t)1 << 40) || m->group_stride > ((int64_t)1 << 46))
+        return set_error(MALIB_E_INVAL, "%s: stride too large", what);
+    if (output && groups > 1 && rows > 0 &&
+        m->group_stride < (rows - 1) * (rows > 1 ? m->row_stride : 0) + cols &&
+        (rows == 1 || m->row_stride < groups * cols || m->group_stride < cols))
+        return set_error(MALIB_E_INVAL, "%s: the groups overlap", what);
+    return MALIB_OK;
+}
+
+MatArg arg(const malib_mat* m)
+{
+    return m ? MatArg{m->ptr, m->row_stride, m->group_stride} : MatArg{nullptr, 0, 0};
+}
+
+malib_status check_work(void* work, int64_t have, int64_t need)
+{
+    if (need > 0 && (!work || have < need))
+        return set_error(MALIB_E_INVAL, "the workspace needs %lld bytes, got %lld",
+                         (long long)need, (long long)(work ? have : 0));
+    if (need > 0 && (uintptr_t)work % 16)
+        return set_error(MALIB_E_INVAL, "the workspace is not aligned to 16 bytes");
+    return MALIB_OK;
+}
+
+// Workgroups of one product fit a launch
+malib_status check_grid(const malib_linear_desc* d, const GemmPlan& p, int64_t M, int64_t N)
+{
+    const int64_t mt = (M + p.tile - 1) / p.tile, nt = (N + p.tile - 1) / p.tile;
+    if (mt * nt > kMaxRows / ((int64_t)d->groups * p.splits))
+        return set_error(MALIB_E_UNSUPPORTED, "the layer has more tiles than one launch takes");
+    return MALIB_OK;
+}
+
+// The backward pass's launches and the layout of its workspace: dz (rows padded to
+// 16 bytes), the column sums' parts, the parts of the products' splits (dx and dW
+// in turn use the same).
+struct BackwardPlan {
+    GemmPlan dx, dw;
+    DzPlan dz;
+    int64_t dz_ld, dz_at, sum_at, part_at, bytes;
+};
+
+BackwardPlan backward_plan(const malib_linear_desc* d)
+{
+    const int size = type_size(d->dtype), ch = 16 / size;
+    BackwardPlan p;
+    p.dx = gemm_plan(d->groups, d->rows, d->in, d->out, size);
+    p.dw = gemm_plan(d->groups, d->out, d->in, d->rows, size);
+    p.dz = dz_plan(d->groups, d->rows, d->out, size);
+    p.dz_ld = (d->out + ch - 1) / ch * ch;
+    p.dz_at = 0;
+    p.sum_at =
+        d->act != MALIB_ACT_NONE ? align256(d->groups * d->rows * p.dz_ld * (int64_t)size) : 0;
+    p.part_at = p.sum_at + align256(p.dz.sum_bytes);
+    p.bytes = p.part_at + align256(std::max(p.dx.part_bytes, p.dw.part_bytes));
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+malib_status malib_linear_work(const malib_linear_desc* d, int32_t backward, int64_t* work_bytes)
+{
+    TRY(check_linear(d));
+    if (!work_bytes)
+        return set_error(MALIB_E_INVAL, "work_bytes is NULL");
+    *work_bytes = backward ? backward_plan(d).bytes
+                           : gemm_plan(d->groups, d->rows, d->out, d->in, type_size(d->dtype))
+                                 .part_bytes;
+    return MALIB_OK;
+}
+
+malib_status malib_linear(const malib_linear_desc* d, const malib_mat* x, const malib_mat* w,
+                          const float* bias, const malib_mat* residual, const malib_mat* pre,
+                          const malib_mat* y, void* work, int64_t work_bytes, void* stream)
+{
+    TRY(check_linear(d));
+    if (d->rows == 0)
+        return MALIB_OK;
+    const int size = type_size(d->dtype);
+    TRY(check_mat(x, "x", d->rows, d->in, d->groups, size, false));
+    TRY(check_mat(w, "w", d->out, d->in, d->groups, size, false));
+    TRY(check_mat(y, "y", d->rows, d->out, d->groups, size, true));
+    if (residual)
+        TRY(check_mat(residual, "residual", d->rows, d->out, d->groups, size, false));
+    if (pre)
+        TRY(check_mat(pre, "pre", d->rows, d->out, d->groups, size, true));
+    if (bias && (uintptr_t)bias % 4)
+        return set_error(MALIB_E_INVAL, "bias is not aligned to its elements");
+    const GemmPlan p = gemm_plan(d->groups, d->rows, d->out, d->in, size);
+    TRY(check_grid(d, p, d->rows, d->out));
+    TRY(check_work(work, work_bytes, p.part_bytes));
+    GemmArgs a{};
+    a.a = arg(x);
+    a.b = arg(w);
+    a.c = arg(y);
+    a.res = arg(residual);
+    a.pre = arg(pre);
+    a.bias = bias;
+    a.M = (int)d->rows;
+    a.N = (int)d->out;
+    a.K = (int)d->in;
+    a.groups = (int)d->groups;
+    a.act = d->act;
+    HIP_TRY(launch_gemm(kGemmForward, d->dtype, a, p, (float*)work, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* dy,
+                                   const malib_mat* x, const malib_mat* w, const malib_mat* pre,
+                                   const malib_mat* dx, const malib_mat* dw, float* dbias,
+                                   void* work, int64_t work_bytes, void* stream)
+{
+    TRY(check_linear(d));
+    const int size = type_size(d->dtype);
+    const bool act = d->act != MALIB_ACT_NONE;
+    if (d->rows > 0) {   // without rows the inputs may be empty: only sums of nothing are written
+        TRY(check_mat(dy, "dy", d->rows, d->out, d->groups, size, false));
+        if (act)
+            TRY(check_mat(pre, "pre", d->rows, d->out, d->groups, size, false));
+        if (dw)
+            TRY(check_mat(x, "x", d->rows, d->in, d->groups, size, false));
+        if (dx) {
+            TRY(check_mat(w, "w", d->out, d->in, d->groups, size, false));
+            TRY(check_mat(dx, "dx", d->rows, d->in, d->groups, size, true));
+        }
+    }
+    if (dw)
+        TRY(check_mat(dw, "dw", d->out, d->in, d->groups, size, true));
+    if (dbias && (uintptr_t)dbias % 4)
+        return set_error(MALIB_E_INVAL, "dbias is not aligned to its elements");
+    const BackwardPlan p = backward_plan(d);
+    if (dx)
+        TRY(check_grid(d, p.dx, d->rows, d->in));
+    if (dw)
+        TRY(check_grid(d, p.dw, d->out, d->in));
+    TRY(check_work(work, work_bytes, p.bytes));
+    hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)work;
+    MatArg dz = arg(dy);
+    if (d->rows == 0)
+        dz = MatArg{nullptr, d->out, 0};
+    const bool need_dz = act && (dx || dw) && d->rows > 0;
+    if (need_dz || dbias) {
+        MatArg to{nullptr, 0, 0};
+        if (need_dz)
+            to = MatArg{ws + p.dz_at, p.dz_ld, d->rows * p.dz_ld};
+        HIP_TRY(launch_dz(d->dtype, p.dz, arg(dy), arg(pre), to, d->act, (int)d->groups,
+                          (int)d->rows, (int)d->out, dbias ? (float*)(ws + p.sum_at) : nullptr,
+                          dbias, s));
+        if (need_dz)
+            dz = to;
+    }
+    float* part = (float*)(ws + p.part_at);
+    GemmArgs a{};
+    a.groups = (int)d->groups;
+    if (dx && d->rows > 0) {
+        a.a = dz;
+        a.b = arg(w);
+        a.c = arg(dx);
+        a.M = (int)d->rows;
+        a.N = (int)d->in;
+        a.K = (int)d->out;
+        HIP_TRY(launch_gemm(kGemmDx, d->dtype, a, p.dx, part, s));
+    }
+    if (dw) {
+        a.a = dz;
+        a.b = d->rows > 0 ? arg(x) : MatArg{nullptr, d->in, 0};
+        a.c = arg(dw);
+        a.M = (int)d->out;
+        a.N = (int)d->in;
+        a.K = (int)d->rows;
+        HIP_TRY(launch_gemm(kGemmDw, d->dtype, a, p.dw, part, s));
+    }
+    return MALIB_OK;
+}
+
+}  // extern "C"

@@ -359,6 +359,45 @@ hipError_t launch_finite_logits(const FiniteLaunch& L, float* out, hipStream_t s
 hipError_t launch_read_table(unsigned long long* acc, int64_t PP, int reset,
                              unsigned long long* out, hipStream_t s);
 
+// The learner's linear layer (k_linear.hip).  A matrix of a group: element (r, c) at
+// p[g * gs + r * ld + c].
+struct MatArg {
+    const void* p;
+    int64_t ld, gs;
+};
+// C[m][n] = sum_k A(m, k) B(n, k) for every group, with the forward's epilogue
+// (bias, activation, residual, the values before the activation) where given.
+struct GemmArgs {
+    MatArg a, b, c, res, pre;
+    const float* bias;   // [groups][N] or null
+    int M, N, K, groups, act;
+    // set by launch_gemm
+    int mt, nt, splits;
+    int64_t k_split;
+    float* part;
+};
+// Tile side, number of splits of k (each k_split long) and the bytes of their parts.
+struct GemmPlan {
+    int tile, splits;
+    int64_t k_split, part_bytes;
+};
+// Which index is contiguous in memory: forward k and k, dx k and n, dW m and n.
+enum { kGemmForward, kGemmDx, kGemmDw };
+GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
+hipError_t launch_gemm(int form, int dtype, GemmArgs a, const GemmPlan& p, float* part,
+                       hipStream_t s);
+struct DzPlan {
+    int rows_per_block, parts, col_blocks;
+    int64_t sum_bytes;
+};
+DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size);
+hipError_t launch_dz(int dtype, const DzPlan& p, const MatArg& dy, const MatArg& pre,
+                     const MatArg& dz, int act, int groups, int M, int N, float* sums, float* db,
+                     hipStream_t s);
+
+// The message of malib_last_error and its status (api.hip).
+malib_status set_error(malib_status code, const char* fmt, ...);
+
 // Diagnostics.
 hipError_t launch_debug_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t s);
 hipError_t launch_debug_tanh(const float* x, float* y, int64_t n, hipStream_t s);

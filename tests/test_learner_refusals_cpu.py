@@ -1,0 +1,112 @@
+"""What the learner operators refuse, on the host and before any device work:
+the library's own checks (pointers are never dereferenced) and the binding's
+checks of shapes, types, strides and devices."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2106_07551_amd as M
+from paper_2106_07551_amd import binding as B
+
+P = 4096          # an address that is never read
+
+
+def _linear(L, *, dtype=B.DT_BF16, act=B.ACT_NONE, groups=1, rows=8, n_in=16, n_out=24, x=None,
+            w=None, y=None, bias=None, residual=None, pre=None, work=None, nbytes=0):
+    d = B.LinearDesc(dtype, act, groups, rows, n_in, n_out)
+    x = B.Mat(P, n_in, rows * n_in) if x is None else x
+    w = B.Mat(P, n_in, n_out * n_in) if w is None else w
+    y = B.Mat(P, n_out, rows * n_out) if y is None else y
+    ref = [None if m is None or m == 0 else C.byref(m) for m in (x, w, residual, pre, y)]
+    return L.malib_linear(C.byref(d), ref[0], ref[1], bias, ref[2], ref[3], ref[4], work, nbytes,
+                          None)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=7), b"dtype"), (dict(act=9), b"activation"), (dict(groups=0), b"groups"),
+    (dict(groups=65536), b"groups"), (dict(rows=-1), b"rows"), (dict(rows=1 << 31), b"rows"),
+    (dict(n_in=0), b"in and out"), (dict(n_out=(1 << 24) + 1), b"in and out"),
+    (dict(x=0), b"x is NULL"), (dict(w=0), b"w is NULL"), (dict(y=0), b"y is NULL"),
+    (dict(x=B.Mat(None, 16, 0)), b"x is NULL"), (dict(x=B.Mat(P + 1, 16, 0)), b"aligned"),
+    (dict(y=B.Mat(P, 23, 0)), b"row stride"), (dict(x=B.Mat(P, -1, 0)), b"row stride"),
+    (dict(x=B.Mat(P, 16, -4)), b"group stride"), (dict(x=B.Mat(P, 1 << 41, 0)), b"too large"),
+    (dict(groups=2, y=B.Mat(P, 24, 0)), b"overlap"),
+    (dict(groups=2, y=B.Mat(P, 24, 24)), b"overlap"),
+    (dict(groups=2, pre=B.Mat(P, 24, 100)), b"overlap"),
+    (dict(bias=P + 2), b"bias"), (dict(residual=B.Mat(P + 1, 24, 0)), b"residual"),
+    (dict(n_in=4096), b"workspace"), (dict(n_in=4096, work=P, nbytes=16), b"workspace"),
+    (dict(n_in=4096, work=P + 8, nbytes=1 << 30), b"16 bytes"),
+])
+def test_linear_refuses(kw, word):
+    L = M.lib()
+    assert _linear(L, **kw) == B.E_INVAL
+    assert word in L.malib_last_error()
+
+
+def test_linear_desc_and_work_refused():
+    L = M.lib()
+    n = C.c_int64()
+    assert L.malib_linear_work(None, 0, C.byref(n)) == B.E_INVAL
+    d = B.LinearDesc(B.DT_F32, B.ACT_RELU, 1, 8, 16, 24)
+    assert L.malib_linear_work(C.byref(d), 0, None) == B.E_INVAL
+    assert L.malib_linear_work(C.byref(d), 1, C.byref(n)) == B.MALIB_OK and n.value > 0
+    # more tiles than one launch takes
+    d = B.LinearDesc(B.DT_F32, B.ACT_NONE, 65535, (1 << 31) - 1, 8, 1 << 24)
+    m = B.Mat(P, 1 << 24, 1 << 45)
+    assert L.malib_linear(C.byref(d), C.byref(m), C.byref(m), None, None, None,
+                          C.byref(B.Mat(P, 1 << 40, 1 << 24)), P, 1 << 62,
+                          None) in (B.E_UNSUPPORTED, B.E_INVAL)
+    assert L.malib_linear_backward(None, None, None, None, None, None, None, None, None, 0,
+                                   None) == B.E_INVAL
+
+
+def test_linear_without_rows_does_nothing():
+    L = M.lib()
+    d = B.LinearDesc(B.DT_F32, B.ACT_NONE, 1, 0, 16, 24)
+    assert L.malib_linear(C.byref(d), None, None, None, None, None, None, None, 0,
+                          None) == B.MALIB_OK
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dy=None), b"dy is NULL"), (dict(x=None), b"x is NULL"), (dict(w=None), b"w is NULL"),
+    (dict(act=B.ACT_GELU), b"pre is NULL"), (dict(dw=B.Mat(P, 15, 0)), b"dw"),
+    (dict(dx=B.Mat(P, 15, 0)), b"dx"), (dict(dbias=P + 1), b"dbias"),
+    (dict(nbytes=0), b"workspace"), (dict(work=None), b"workspace"),
+])
+def test_linear_backward_refuses(kw, word):
+    L = M.lib()
+    a = dict(act=B.ACT_NONE, dy=B.Mat(P, 24, 0), x=B.Mat(P, 16, 0), w=B.Mat(P, 16, 0), pre=None,
+             dx=B.Mat(P, 16, 0), dw=B.Mat(P, 16, 0), dbias=P, work=P, nbytes=1 << 30)
+    a.update(kw)
+    d = B.LinearDesc(B.DT_F32, a["act"], 1, 8, 16, 24)
+    ref = [None if a[k] is None else C.byref(a[k]) for k in ("dy", "x", "w", "pre", "dx", "dw")]
+    assert L.malib_linear_backward(C.byref(d), *ref, a["dbias"], a["work"], a["nbytes"],
+                                   None) == B.E_INVAL
+    assert word in L.malib_last_error()
+
+
+def test_linear_binding_checks():
+    x, w = torch.zeros(4, 8), torch.zeros(6, 8)
+    with pytest.raises(M.ArgumentError, match="device tensor"):
+        M.linear(x, w)
+    for bad, match in ((dict(x=x.half()), "dtype"), (dict(w=w.bfloat16()), "w: expected dtype"),
+                       (dict(w=torch.zeros(6, 9)), "x: expected shape"),
+                       (dict(w=torch.zeros(6)), "w: expected"),
+                       (dict(x=torch.zeros(2, 4, 8)), "x: expected"),
+                       (dict(x=torch.zeros(8, 4).t()), "contiguous rows"),
+                       (dict(bias=torch.zeros(5)), "bias"),
+                       (dict(bias=torch.zeros(6).double()), "bias"),
+                       (dict(residual=torch.zeros(4, 5)), "residual"),
+                       (dict(pre=torch.zeros(3, 6)), "pre"), (dict(act=5), "act")):
+        kw = dict(x=x, w=w)
+        kw.update(bad)
+        with pytest.raises(M.ArgumentError, match=match):
+            M.linear(**kw)
+    dy = torch.zeros(4, 6)
+    with pytest.raises(M.ArgumentError, match="pre"):
+        M.linear_backward(dy, x, w, act=M.ACT_RELU)
+    with pytest.raises(M.ArgumentError, match="dy: expected shape"):
+        M.linear_backward(torch.zeros(4, 5), x, w)
+    with pytest.raises(M.ArgumentError, match="x: expected shape"):
+        M.linear_backward(dy, torch.zeros(5, 8), w)
