@@ -596,6 +596,85 @@ malib_status malib_linear_backward(const malib_linear_desc* desc, const malib_ma
 malib_status malib_linear_work(const malib_linear_desc* desc, int32_t backward,
                                int64_t* work_bytes);
 
+/*
+ * The clipped policy loss over rows of logits, with its gradient.  A row is one
+ * decision: logits x over `actions` entries, the action taken, its log
+ * probability under the policy that took it (old) and its advantage.  With p
+ * the softmax over the legal entries, l = log p[action], r = exp(l - old):
+ *   loss = -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv)
+ *          + kl_coef KL - entropy_coef H
+ *   H = -sum_j p_j log p_j
+ *   KL = sum_j p_j (log p_j - log q_j) where reference logits are given (q:
+ *        their softmax over the same entries), else e^d - 1 - d with
+ *        d = ref_logp - l where the reference's log probability of the action
+ *        is given, else 0
+ *   total = sum over rows of w loss
+ *  logits, ref_logits, dlogits: [rows][actions] of `dtype`, rows the strides
+ *       apart; ref_logits may be NULL.
+ *  actions: device uint8, int32 or int64 [rows] (action_bytes 1, 4 or 8).
+ *  old_logp, advantage: device fp32 [rows]; ref_logp: the same or NULL (not
+ *       together with ref_logits).
+ *  mask: device uint8 [rows][actions], rows mask_stride apart, 0 where an
+ *       entry is not legal, or NULL.  What logits hold there is not used.
+ *  weight: device fp32 [rows], w of each row, or NULL (1 / rows each).
+ *  total: device fp32 [1] or NULL; stats: device fp32 [4][rows] or NULL: loss,
+ *       l, KL and H of each row; dlogits: the gradient of total, or NULL.
+ * A row counts if its action is a legal entry in [0, actions) (255 and -1,
+ * say, stand for no action), its weight is not 0 and any legal logit is above
+ * -inf; the others give zeros.  Sums are formed in fp32 (total in fp64) in an
+ * order fixed by the sizes, each output is rounded once.
+ * 0 <= rows < 2^31, 1 <= actions <= 2^24.  work: as malib_loss_work
+ * says, aligned to 16 bytes.
+ */
+typedef struct {
+    int32_t dtype;           /* MALIB_DT_* of logits, ref_logits, dlogits */
+    int32_t action_bytes;    /* 1, 4 or 8 */
+    int64_t rows, n_actions;
+    int64_t logits_stride, ref_stride, dlogits_stride, mask_stride;
+    float clip_low, clip_high;   /* >= 0; infinite: no clipping on that side */
+    float kl_coef, entropy_coef; /* finite */
+} malib_policy_loss_desc;
+
+malib_status malib_policy_loss(const malib_policy_loss_desc* desc, const void* logits,
+                               const void* actions, const float* old_logp,
+                               const float* advantage, const float* ref_logp,
+                               const void* ref_logits, const uint8_t* mask, const float* weight,
+                               float* total, float* stats, void* dlogits, void* work,
+                               int64_t work_bytes, void* stream);
+
+/*
+ * Distillation from teachers' top logits, with its gradient (e.g. of a
+ * meta-strategy's policies into one).  With t the softmax of a row's listed
+ * teacher logits over temperature T and q the softmax of the student's legal
+ * logits over T:
+ *   loss = T^2 sum_k t_k (log t_k - log q[idx_k]),  total = sum_rows w loss
+ *  teacher_idx, teacher_logits: device int32 and fp32 [rows][top], 1 <= top <=
+ *       256.  An entry counts if its index is a legal entry in [0, n_actions)
+ *       (-1, say, pads a short list); an index may be listed more than once
+ *       (the lists of several teachers side by side): its probabilities add.
+ *  loss: device fp32 [rows] or NULL.  The rest as in malib_policy_loss.
+ * A row counts if any of its entries does, with a logit above -inf, its weight
+ * is not 0 and any legal logit is above -inf; the others give zeros.
+ */
+typedef struct {
+    int32_t dtype;           /* MALIB_DT_* of logits, dlogits */
+    int32_t top;
+    int64_t rows, n_actions;
+    int64_t logits_stride, dlogits_stride, mask_stride;
+    float temperature;       /* > 0, finite */
+} malib_distill_desc;
+
+malib_status malib_distill_loss(const malib_distill_desc* desc, const void* logits,
+                                const int32_t* teacher_idx, const float* teacher_logits,
+                                const uint8_t* mask, const float* weight, float* total,
+                                float* loss, void* dlogits, void* work, int64_t work_bytes,
+                                void* stream);
+
+/* Workspace bytes of malib_policy_loss and malib_distill_loss for these sizes.
+ * Host only. */
+malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t n_actions,
+                             int64_t* work_bytes);
+
 /* Message for the last non-OK status returned on this thread. */
 const char* malib_last_error(void);
 

@@ -33,6 +33,7 @@ EXPORTS = [
     "malib_pop_policy_ids", "malib_rollout_batch_noalloc", "malib_pop_set_graph",
     "malib_solve_alpharank", "malib_solve_lp",
     "malib_linear", "malib_linear_backward", "malib_linear_work",
+    "malib_policy_loss", "malib_distill_loss", "malib_loss_work",
 ]
 
 
@@ -83,6 +84,21 @@ class Mat(C.Structure):
 class LinearDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("groups", C.c_int64),
                 ("rows", C.c_int64), ("inputs", C.c_int64), ("outputs", C.c_int64)]
+
+
+class PolicyLossDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("action_bytes", C.c_int32), ("rows", C.c_int64),
+                ("n_actions", C.c_int64), ("logits_stride", C.c_int64), ("ref_stride", C.c_int64),
+                ("dlogits_stride", C.c_int64), ("mask_stride", C.c_int64),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float),
+                ("entropy_coef", C.c_float)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("top", C.c_int32), ("rows", C.c_int64),
+                ("n_actions", C.c_int64), ("logits_stride", C.c_int64),
+                ("dlogits_stride", C.c_int64), ("mask_stride", C.c_int64),
+                ("temperature", C.c_float)]
 
 
 class EvalStats(C.Structure):
@@ -157,6 +173,12 @@ def lib():
         L.malib_linear_backward.restype = i32
         L.malib_linear_work.argtypes = [lp, i32, C.POINTER(i64)]
         L.malib_linear_work.restype = i32
+        L.malib_policy_loss.argtypes = [C.POINTER(PolicyLossDesc)] + [vp] * 12 + [i64, vp]
+        L.malib_policy_loss.restype = i32
+        L.malib_distill_loss.argtypes = [C.POINTER(DistillDesc)] + [vp] * 9 + [i64, vp]
+        L.malib_distill_loss.restype = i32
+        L.malib_loss_work.argtypes = [i32, i64, i64, C.POINTER(i64)]
+        L.malib_loss_work.restype = i32
         _lib = L
     return _lib
 
@@ -796,6 +818,132 @@ def linear_backward(dy, x, w, *, act: int = ACT_NONE, pre=None, want=(True, True
         C.byref(d), C.byref(mdy), _ref(mx), C.byref(mw), _ref(mp), _ref(mdx), _ref(mdw),
         _dptr(dbias), _dptr(work), nbytes, _stream(stream)))
     return dx, dw, dbias
+
+
+def _rows(t, dtype, shape, what) -> int:
+    """Row stride of a tensor [rows][n] whose rows are contiguous, checked."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != tuple(shape):
+        raise ArgumentError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise ArgumentError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {t.stride(1)}")
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _loss_args(logits, mask, weight, dlogits):
+    """What both losses check: (rows, n_actions, dtype code, strides of logits,
+    dlogits and mask)."""
+    import torch
+    if logits.dim() != 2 or logits.shape[1] < 1:
+        raise ArgumentError(f"logits: expected [rows][n_actions], got shape {tuple(logits.shape)}")
+    code = _dtype_code(logits, "logits")
+    n, a = logits.shape
+    sl = _rows(logits, logits.dtype, (n, a), "logits")
+    sm = _rows(mask, (torch.bool, torch.uint8), (n, a), "mask")
+    sd = _rows(dlogits, logits.dtype, (n, a), "dlogits")
+    _check_buf(weight, torch.float32, n, False, "weight")
+    return n, a, code, sl, sd, sm
+
+
+def _loss_work(code, n, a, work, device, stream):
+    import torch
+    need = C.c_int64()
+    _check(lib().malib_loss_work(code, n, a, C.byref(need)))
+    if work is None and need.value:
+        work = _empty(need.value, torch.uint8, device, stream)
+    if work is not None:
+        _dbytes(work, need.value, "work")
+    return work, 0 if work is None else work.numel() * work.element_size()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
+                ref_logp=None, ref_logits=None, mask=None, weight=None, grad: bool = True,
+                total=None, stats=None, dlogits=None, work=None, stream=None):
+    """malib_policy_loss: the clipped policy loss with a divergence term over
+    logits [rows][n_actions] (float32 or bfloat16) and its gradient.  actions:
+    uint8, int32 or int64 [rows] (out of range: no action); mask: bool or uint8
+    [rows][n_actions], legal entries.  Returns (total [1], stats [4][rows] =
+    loss, log probability of the action, divergence and entropy of each row,
+    dlogits or None without `grad`)."""
+    import torch
+    n, a, code, sl, sd, sm = _loss_args(logits, mask, weight, dlogits)
+    f32 = torch.float32
+    if actions.dtype not in (torch.uint8, torch.int32, torch.int64):
+        raise ArgumentError(f"actions: expected dtype uint8, int32 or int64, got {actions.dtype}")
+    sr = _rows(ref_logits, logits.dtype, (n, a), "ref_logits")
+    for t, dt, what in ((actions, actions.dtype, "actions"), (old_logp, f32, "old_logp"),
+                        (advantage, f32, "advantage"), (ref_logp, f32, "ref_logp")):
+        _check_buf(t, dt, n, False, what)
+    _check_buf(total, f32, 1, False, "total")
+    _check_buf(stats, f32, 4 * n, False, "stats")
+    _on_device((logits, "logits"), (actions, "actions"), (old_logp, "old_logp"),
+               (advantage, "advantage"), (ref_logp, "ref_logp"), (ref_logits, "ref_logits"),
+               (mask, "mask"), (weight, "weight"), (total, "total"), (stats, "stats"),
+               (dlogits, "dlogits"), (work, "work"))
+    dev = logits.device
+    if total is None:
+        total = _empty(1, f32, dev, stream)
+    if stats is None:
+        stats = _empty((4, n), f32, dev, stream)
+    if not grad:
+        dlogits = None
+    elif dlogits is None:
+        dlogits, sd = _empty((n, a), logits.dtype, dev, stream), a
+    work, nbytes = _loss_work(code, n, a, work, dev, stream)
+    d = PolicyLossDesc(code, actions.element_size(), n, a, sl, sr, sd, sm, clip_low, clip_high,
+                       kl_coef, entropy_coef)
+    _check(lib().malib_policy_loss(
+        C.byref(d), _ptr(logits), _ptr(actions), _ptr(old_logp), _ptr(advantage), _ptr(ref_logp),
+        _ptr(ref_logits), _ptr(mask), _ptr(weight), _ptr(total), _ptr(stats), _ptr(dlogits),
+        _ptr(work), nbytes, _stream(stream)))
+    return total, stats, dlogits
+
+
+def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.0, mask=None,
+                 weight=None, grad: bool = True, total=None, loss=None, dlogits=None, work=None,
+                 stream=None):
+    """malib_distill_loss: distillation of teachers' top logits (teacher_idx
+    int32 and teacher_logits float32 [rows][top], index -1 pads a list) into
+    logits [rows][n_actions], and its gradient.  Returns (total [1], loss
+    [rows], dlogits or None without `grad`)."""
+    import torch
+    n, a, code, sl, sd, sm = _loss_args(logits, mask, weight, dlogits)
+    f32 = torch.float32
+    if teacher_idx.dim() != 2:
+        raise ArgumentError(f"teacher_idx: expected [rows][top], got shape "
+                            f"{tuple(teacher_idx.shape)}")
+    top = teacher_idx.shape[1]
+    _check_buf(teacher_idx, torch.int32, n * top, False, "teacher_idx")
+    _check_buf(teacher_logits, f32, n * top, False, "teacher_logits")
+    _check_buf(total, f32, 1, False, "total")
+    _check_buf(loss, f32, n, False, "loss")
+    _on_device((logits, "logits"), (teacher_idx, "teacher_idx"),
+               (teacher_logits, "teacher_logits"), (mask, "mask"), (weight, "weight"),
+               (total, "total"), (loss, "loss"), (dlogits, "dlogits"), (work, "work"))
+    dev = logits.device
+    if total is None:
+        total = _empty(1, f32, dev, stream)
+    if loss is None:
+        loss = _empty(n, f32, dev, stream)
+    if not grad:
+        dlogits = None
+    elif dlogits is None:
+        dlogits, sd = _empty((n, a), logits.dtype, dev, stream), a
+    work, nbytes = _loss_work(code, n, a, work, dev, stream)
+    d = DistillDesc(code, top, n, a, sl, sd, sm, temperature)
+    _check(lib().malib_distill_loss(
+        C.byref(d), _ptr(logits), _ptr(teacher_idx), _ptr(teacher_logits), _ptr(mask),
+        _ptr(weight), _ptr(total), _ptr(loss), _ptr(dlogits), _ptr(work), nbytes,
+        _stream(stream)))
+    return total, loss, dlogits
 
 
 def debug_tanh_ref(x, y=None, stream=None):

@@ -2,6 +2,8 @@
 // launch sequences.
 #include "internal.hpp"
 
+#include <cmath>
+
 using namespace malib;
 
 namespace {
@@ -234,6 +236,154 @@ malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* 
         a.K = (int)d->rows;
         HIP_TRY(launch_gemm(kGemmDw, d->dtype, a, p.dw, part, s));
     }
+    return MALIB_OK;
+}
+
+static malib_status check_loss(int dtype, int64_t rows, int64_t A)
+{
+    if (dtype != MALIB_DT_F32 && dtype != MALIB_DT_BF16)
+        return set_error(MALIB_E_INVAL, "unknown dtype %d", dtype);
+    if (rows < 0 || rows > kMaxRows)
+        return set_error(MALIB_E_INVAL, "rows must be in [0, 2^31)");
+    if (A < 1 || A > kMaxWidth)
+        return set_error(MALIB_E_INVAL, "n_actions must be in [1, 2^24]");
+    return MALIB_OK;
+}
+
+// A [rows][A] buffer of the losses.
+static malib_status check_rows(const void* p, int64_t stride, const char* what, int64_t rows,
+                               int64_t A, int size, bool output)
+{
+    if ((uintptr_t)p % size)
+        return set_error(MALIB_E_INVAL, "%s is not aligned to its elements", what);
+    if (rows > 1 && (stride < (output ? A : 0) || stride > ((int64_t)1 << 40)))
+        return set_error(MALIB_E_INVAL, "%s: bad row stride %lld for %lld entries", what,
+                         (long long)stride, (long long)A);
+    return MALIB_OK;
+}
+
+malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t A, int64_t* work_bytes)
+{
+    TRY(check_loss(dtype, rows, A));
+    if (!work_bytes)
+        return set_error(MALIB_E_INVAL, "work_bytes is NULL");
+    *work_bytes = loss_plan(rows, A, type_size(dtype)).work_bytes;
+    return MALIB_OK;
+}
+
+malib_status malib_policy_loss(const malib_policy_loss_desc* d, const void* logits,
+                               const void* actions, const float* old_logp,
+                               const float* advantage, const float* ref_logp,
+                               const void* ref_logits, const uint8_t* mask, const float* weight,
+                               float* total, float* stats, void* dlogits, void* work,
+                               int64_t work_bytes, void* stream)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    TRY(check_loss(d->dtype, d->rows, d->n_actions));
+    if (d->action_bytes != 1 && d->action_bytes != 4 && d->action_bytes != 8)
+        return set_error(MALIB_E_INVAL, "action_bytes must be 1, 4 or 8");
+    if (!(d->clip_low >= 0.0f) || !(d->clip_high >= 0.0f))
+        return set_error(MALIB_E_INVAL, "clip_low and clip_high must be >= 0");
+    if (!std::isfinite(d->kl_coef) || !std::isfinite(d->entropy_coef))
+        return set_error(MALIB_E_INVAL, "kl_coef and entropy_coef must be finite");
+    if (ref_logp && ref_logits)
+        return set_error(MALIB_E_INVAL, "ref_logp and ref_logits exclude each other");
+    if (d->kl_coef != 0.0f && !ref_logp && !ref_logits)
+        return set_error(MALIB_E_INVAL, "kl_coef needs ref_logp or ref_logits");
+    const int size = type_size(d->dtype);
+    const LossPlan p = loss_plan(d->rows, d->n_actions, size);
+    if (d->rows > 0) {
+        if (!logits || !actions || !old_logp || !advantage)
+            return set_error(MALIB_E_INVAL,
+                             "logits, actions, old_logp and advantage must not be NULL");
+        if ((uintptr_t)actions % d->action_bytes)
+            return set_error(MALIB_E_INVAL, "actions is not aligned to its elements");
+        TRY(check_rows(logits, d->logits_stride, "logits", d->rows, d->n_actions, size, false));
+        if (ref_logits)
+            TRY(check_rows(ref_logits, d->ref_stride, "ref_logits", d->rows, d->n_actions, size,
+                           false));
+        if (mask)
+            TRY(check_rows(mask, d->mask_stride, "mask", d->rows, d->n_actions, 1, false));
+        if (dlogits)
+            TRY(check_rows(dlogits, d->dlogits_stride, "dlogits", d->rows, d->n_actions, size,
+                           true));
+        TRY(check_work(work, work_bytes, p.work_bytes));
+    }
+    LossArgs a{};
+    a.logits = logits;
+    a.ref_logits = ref_logits;
+    a.mask = mask;
+    a.weight = weight;
+    a.actions = actions;
+    a.old_logp = old_logp;
+    a.advantage = advantage;
+    a.ref_logp = ref_logp;
+    a.dlogits = dlogits;
+    a.stats = stats;
+    a.total = total;
+    a.rows = d->rows;
+    a.logits_ld = d->logits_stride;
+    a.ref_ld = d->ref_stride;
+    a.mask_ld = d->mask_stride;
+    a.dlogits_ld = d->dlogits_stride;
+    a.A = (int)d->n_actions;
+    a.action_bytes = d->action_bytes;
+    a.row_weight = d->rows > 0 ? (float)(1.0 / (double)d->rows) : 0.0f;
+    a.clip_low = d->clip_low;
+    a.clip_high = d->clip_high;
+    a.kl_coef = d->kl_coef;
+    a.entropy_coef = d->entropy_coef;
+    a.temperature = 1.0f;
+    HIP_TRY(launch_loss(a, d->dtype, false, p, work, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_distill_loss(const malib_distill_desc* d, const void* logits,
+                                const int32_t* teacher_idx, const float* teacher_logits,
+                                const uint8_t* mask, const float* weight, float* total,
+                                float* loss, void* dlogits, void* work, int64_t work_bytes,
+                                void* stream)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    TRY(check_loss(d->dtype, d->rows, d->n_actions));
+    if (d->top < 1 || d->top > 256)
+        return set_error(MALIB_E_INVAL, "top must be in [1, 256]");
+    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature))
+        return set_error(MALIB_E_INVAL, "temperature must be positive and finite");
+    const int size = type_size(d->dtype);
+    const LossPlan p = loss_plan(d->rows, d->n_actions, size);
+    if (d->rows > 0) {
+        if (!logits || !teacher_idx || !teacher_logits)
+            return set_error(MALIB_E_INVAL,
+                             "logits, teacher_idx and teacher_logits must not be NULL");
+        TRY(check_rows(logits, d->logits_stride, "logits", d->rows, d->n_actions, size, false));
+        if (mask)
+            TRY(check_rows(mask, d->mask_stride, "mask", d->rows, d->n_actions, 1, false));
+        if (dlogits)
+            TRY(check_rows(dlogits, d->dlogits_stride, "dlogits", d->rows, d->n_actions, size,
+                           true));
+        TRY(check_work(work, work_bytes, p.work_bytes));
+    }
+    LossArgs a{};
+    a.logits = logits;
+    a.mask = mask;
+    a.weight = weight;
+    a.idx = teacher_idx;
+    a.val = teacher_logits;
+    a.dlogits = dlogits;
+    a.stats = loss;
+    a.total = total;
+    a.rows = d->rows;
+    a.logits_ld = d->logits_stride;
+    a.mask_ld = d->mask_stride;
+    a.dlogits_ld = d->dlogits_stride;
+    a.A = (int)d->n_actions;
+    a.top = d->top;
+    a.row_weight = d->rows > 0 ? (float)(1.0 / (double)d->rows) : 0.0f;
+    a.temperature = d->temperature;
+    HIP_TRY(launch_loss(a, d->dtype, true, p, work, (hipStream_t)stream));
     return MALIB_OK;
 }
 

@@ -395,6 +395,35 @@ hipError_t launch_dz(int dtype, const DzPlan& p, const MatArg& dy, const MatArg&
                      const MatArg& dz, int act, int groups, int M, int N, float* sums, float* db,
                      hipStream_t s);
 
+// The learner's losses (k_loss.hip).
+struct LossArgs {
+    const void* logits;        // [rows][A], rows logits_ld apart
+    const void* ref_logits;    // policy loss: reference's logits, or null
+    const uint8_t* mask;       // legal entries, or null
+    const float* weight;       // [rows], or null: row_weight each
+    const void* actions;       // policy loss: action_bytes each
+    const float *old_logp, *advantage, *ref_logp;
+    const int32_t* idx;        // distillation: [rows][top]
+    const float* val;
+    void* dlogits;
+    float *stats, *total;
+    int64_t rows, logits_ld, ref_ld, mask_ld, dlogits_ld;
+    int A, top, action_bytes;
+    float row_weight, clip_low, clip_high, kl_coef, entropy_coef, temperature;
+    // set by launch_loss
+    int splits, part_chunks;
+    void* part;
+    double* part_total;
+};
+enum { kLossLane, kLossRow16, kLossRow64, kLossRow256, kLossRow1024, kLossLong, kLossSplit };
+struct LossPlan {
+    int variant, splits, part_chunks;
+    int64_t blocks, part_bytes, work_bytes;
+};
+LossPlan loss_plan(int64_t rows, int64_t A, int size);
+hipError_t launch_loss(LossArgs a, int dtype, bool distill, const LossPlan& p, void* work,
+                       hipStream_t s);
+
 // The message of malib_last_error and its status (api.hip).
 malib_status set_error(malib_status code, const char* fmt, ...);
 

@@ -8,6 +8,7 @@
 // of dx) or with its row index contiguous ("RC": W of dx, dz and x of dW).
 #include "internal.hpp"
 
+#include "chunk.hpp"
 #include "device.hpp"
 
 namespace malib {
@@ -18,104 +19,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-// 16 bytes at any element's address (global memory takes unaligned vectors)
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-struct bf16_t {
-    uint16_t b;
-};
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(bf16_t x) { return __uint_as_float((uint32_t)x.b << 16); }
-template <typename E>
-__device__ __forceinline__ E from_f32(float x);
-template <>
-__device__ __forceinline__ float from_f32<float>(float x)
-{
-    return x;
-}
-template <>
-__device__ __forceinline__ bf16_t from_f32<bf16_t>(float x)
-{
-    return bf16_t{__builtin_bit_cast(uint16_t, (__bf16)x)};
-}
-
-// A chunk: 16 bytes of consecutive elements, the unit of every load.
-template <typename E>
-constexpr int kChunk = 16 / (int)sizeof(E);
 // k per tile: 128 bytes
 template <typename E>
 constexpr int kBK = 128 / (int)sizeof(E);
-
-template <typename E>
-__device__ __forceinline__ void unpack(u32x4 v, float (&f)[kChunk<E>])
-{
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f[i] = __uint_as_float(v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(v[i] << 16);
-            f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-        }
-    }
-}
-
-template <typename E>
-__device__ __forceinline__ u32x4 pack(const float (&f)[kChunk<E>])
-{
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        v[i] = sizeof(E) == 4 ? __float_as_uint(f[i]) : pack_bf16x2(f[2 * i], f[2 * i + 1]);
-    return v;
-}
-
-// The first `n` elements of the chunk at p (zeros behind them; nothing behind
-// them is read).
-template <typename E>
-__device__ __forceinline__ u32x4 load_chunk(const E* p, int n)
-{
-    if (n >= kChunk<E>)
-        return *(const u32x4_any*)p;
-    u32x4 v = {0, 0, 0, 0};
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n)
-                v[i] = __float_as_uint(p[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n)
-                v[i >> 1] |= (uint32_t)p[i].b << (16 * (i & 1));
-    }
-    return v;
-}
-
-template <typename E>
-__device__ __forceinline__ void store_chunk(E* p, int n, u32x4 v)
-{
-    if (n >= kChunk<E>) {
-        *(u32x4_any*)p = v;
-        return;
-    }
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n)
-                p[i] = __uint_as_float(v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n)
-                p[i].b = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
-    }
-}
 
 // The activation and its derivative at z, in fp32.  relu passes a NaN on, as the
 // policies' hidden layers do; its derivative at 0 is 0.

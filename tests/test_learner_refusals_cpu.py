@@ -110,3 +110,104 @@ def test_linear_binding_checks():
         M.linear_backward(torch.zeros(4, 5), x, w)
     with pytest.raises(M.ArgumentError, match="x: expected shape"):
         M.linear_backward(dy, torch.zeros(5, 8), w)
+
+
+def _policy(L, *, ptrs=(), work=P, nbytes=1 << 20, **kw):
+    f = dict(dtype=B.DT_F32, action_bytes=4, rows=600, n_actions=5, logits_stride=5,
+             ref_stride=5, dlogits_stride=5, mask_stride=5, clip_low=0.2, clip_high=0.2,
+             kl_coef=0.0, entropy_coef=0.0)
+    f.update(kw)
+    a = dict(logits=P, actions=P, old=P, adv=P, ref_logp=None, ref_logits=None, mask=None,
+             weight=None, total=P, stats=P, dlogits=P)
+    a.update(ptrs)
+    return L.malib_policy_loss(C.byref(B.PolicyLossDesc(*f.values())), *a.values(), work, nbytes,
+                               None)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=3), b"dtype"), (dict(action_bytes=2), b"action_bytes"), (dict(rows=-1), b"rows"),
+    (dict(rows=1 << 31), b"rows"), (dict(n_actions=0), b"n_actions"),
+    (dict(n_actions=(1 << 24) + 1), b"n_actions"), (dict(clip_low=-0.1), b"clip"),
+    (dict(clip_high=float("nan")), b"clip"), (dict(kl_coef=float("inf")), b"finite"),
+    (dict(entropy_coef=float("nan")), b"finite"), (dict(kl_coef=0.1), b"kl_coef needs"),
+    (dict(ptrs=dict(ref_logp=P, ref_logits=P)), b"exclude"),
+    (dict(ptrs=dict(logits=None)), b"NULL"), (dict(ptrs=dict(actions=None)), b"NULL"),
+    (dict(ptrs=dict(old=None)), b"NULL"), (dict(ptrs=dict(adv=None)), b"NULL"),
+    (dict(ptrs=dict(logits=P + 2)), b"logits"), (dict(ptrs=dict(actions=P + 2)), b"actions"),
+    (dict(logits_stride=-5), b"logits"), (dict(dlogits_stride=4), b"dlogits"),
+    (dict(ref_stride=1 << 41, ptrs=dict(ref_logits=P)), b"ref_logits"),
+    (dict(mask_stride=-1, ptrs=dict(mask=P)), b"mask"), (dict(work=None), b"workspace"),
+    (dict(nbytes=4), b"workspace"), (dict(work=P + 4), b"16 bytes"),
+])
+def test_policy_loss_refuses(kw, word):
+    L = M.lib()
+    assert _policy(L, **kw) == B.E_INVAL
+    assert word in L.malib_last_error()
+
+
+def _distill(L, *, ptrs=(), work=P, nbytes=1 << 20, **kw):
+    f = dict(dtype=B.DT_F32, top=3, rows=600, n_actions=5, logits_stride=5, dlogits_stride=5,
+             mask_stride=5, temperature=1.0)
+    f.update(kw)
+    a = dict(logits=P, idx=P, val=P, mask=None, weight=None, total=P, loss=P, dlogits=P)
+    a.update(ptrs)
+    return L.malib_distill_loss(C.byref(B.DistillDesc(*f.values())), *a.values(), work, nbytes,
+                                None)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=3), b"dtype"), (dict(top=0), b"top"), (dict(top=257), b"top"),
+    (dict(temperature=0.0), b"temperature"), (dict(temperature=float("inf")), b"temperature"),
+    (dict(temperature=float("nan")), b"temperature"), (dict(rows=-1), b"rows"),
+    (dict(n_actions=0), b"n_actions"), (dict(ptrs=dict(logits=None)), b"NULL"),
+    (dict(ptrs=dict(idx=None)), b"NULL"), (dict(ptrs=dict(val=None)), b"NULL"),
+    (dict(dlogits_stride=4), b"dlogits"), (dict(work=None), b"workspace"),
+])
+def test_distill_loss_refuses(kw, word):
+    L = M.lib()
+    assert _distill(L, **kw) == B.E_INVAL
+    assert word in L.malib_last_error()
+
+
+def test_loss_work_and_null_descriptions():
+    L = M.lib()
+    n = C.c_int64(-1)
+    assert L.malib_loss_work(B.DT_F32, 100, 5, None) == B.E_INVAL
+    assert L.malib_loss_work(9, 100, 5, C.byref(n)) == B.E_INVAL
+    assert L.malib_loss_work(B.DT_F32, 100, 5, C.byref(n)) == B.MALIB_OK and n.value >= 0
+    assert L.malib_policy_loss(None, *[None] * 12, 0, None) == B.E_INVAL
+    assert L.malib_distill_loss(None, *[None] * 9, 0, None) == B.E_INVAL
+
+
+def test_loss_binding_checks():
+    n, a = 6, 9
+    ok = dict(logits=torch.zeros(n, a), actions=torch.zeros(n, dtype=torch.int32),
+              old_logp=torch.zeros(n), advantage=torch.zeros(n))
+    with pytest.raises(M.ArgumentError, match="device tensor"):
+        M.policy_loss(**ok)
+    for bad, match in ((dict(logits=torch.zeros(n, a).half()), "dtype"),
+                       (dict(logits=torch.zeros(n)), "logits: expected"),
+                       (dict(logits=torch.zeros(a, n).t()), "contiguous rows"),
+                       (dict(actions=torch.zeros(n, dtype=torch.int16)), "actions"),
+                       (dict(actions=torch.zeros(n - 1, dtype=torch.int32)), "actions"),
+                       (dict(old_logp=torch.zeros(n).double()), "old_logp"),
+                       (dict(advantage=torch.zeros(n + 1)), "advantage"),
+                       (dict(ref_logp=torch.zeros(n - 1)), "ref_logp"),
+                       (dict(ref_logits=torch.zeros(n, a).bfloat16()), "ref_logits"),
+                       (dict(mask=torch.zeros(n, a)), "mask"),
+                       (dict(mask=torch.zeros((n, a + 1), dtype=torch.bool)), "mask"),
+                       (dict(weight=torch.zeros(1)), "weight"),
+                       (dict(stats=torch.zeros(n)), "stats"),
+                       (dict(dlogits=torch.zeros(n, a + 1)), "dlogits")):
+        with pytest.raises(M.ArgumentError, match=match):
+            M.policy_loss(**{**ok, **bad})
+    ok = dict(logits=torch.zeros(n, a), teacher_idx=torch.zeros((n, 2), dtype=torch.int32),
+              teacher_logits=torch.zeros(n, 2))
+    with pytest.raises(M.ArgumentError, match="device tensor"):
+        M.distill_loss(**ok)
+    for bad, match in ((dict(teacher_idx=torch.zeros((n, 2), dtype=torch.int64)), "teacher_idx"),
+                       (dict(teacher_idx=torch.zeros(n, dtype=torch.int32)), "teacher_idx"),
+                       (dict(teacher_logits=torch.zeros(n, 3)), "teacher_logits"),
+                       (dict(loss=torch.zeros(2)), "loss"), (dict(total=torch.zeros(2)), "total")):
+        with pytest.raises(M.ArgumentError, match=match):
+            M.distill_loss(**{**ok, **bad})
