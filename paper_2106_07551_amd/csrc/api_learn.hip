@@ -25,6 +25,7 @@ namespace {
 
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;
+constexpr int64_t kFusedMost = (int64_t)1 << 20;   // values of dz
 
 int type_size(int dtype) { return dtype == MALIB_DT_BF16 ? 2 : 4; }
 
@@ -94,28 +95,37 @@ malib_status check_grid(const malib_linear_desc* d, const GemmPlan& p, int64_t M
     return MALIB_OK;
 }
 
-// The backward pass's launches and the layout of its workspace: dz (rows padded to
-// 16 bytes), the column sums' parts, the parts of the products' splits (dx and dW
-// in turn use the same).
+// The backward pass's launches and the layout of its workspace.  dz = dy act'(z) is
+// either formed while the products load it (`fused`: one launch, but every
+// tile that needs a value forms it again) or once into the workspace (rows padded to
+// 16 bytes).  dbias comes with dW's product (sums of what it multiplies), except
+// where that is rounded or the product's tile has no room for it: then from the
+// kernel that forms dz.
 struct BackwardPlan {
     GemmPlan dx, dw;
     DzPlan dz;
-    int64_t dz_ld, dz_at, sum_at, part_at, bytes;
+    bool fused, own_sums;   // own_sums: dbias from dz's kernel
+    int64_t dz_ld, dz_at, sum_at, dw_at, dx_at, bytes;
 };
 
 BackwardPlan backward_plan(const malib_linear_desc* d)
 {
     const int size = type_size(d->dtype), ch = 16 / size;
+    const bool act = d->act != MALIB_ACT_NONE;
+    const bool rounded = size == 2 && (d->act == MALIB_ACT_GELU || d->act == MALIB_ACT_SILU);
     BackwardPlan p;
     p.dx = gemm_plan(d->groups, d->rows, d->in, d->out, size);
     p.dw = gemm_plan(d->groups, d->out, d->in, d->rows, size);
     p.dz = dz_plan(d->groups, d->rows, d->out, size);
+    p.fused = act && !rounded && d->groups * d->rows * d->out <= kFusedMost &&
+              p.dx.tile < 256 && p.dw.tile < 256;
+    p.own_sums = (act && !p.fused) || p.dw.tile == 256;
     p.dz_ld = (d->out + ch - 1) / ch * ch;
     p.dz_at = 0;
-    p.sum_at =
-        d->act != MALIB_ACT_NONE ? align256(d->groups * d->rows * p.dz_ld * (int64_t)size) : 0;
-    p.part_at = p.sum_at + align256(p.dz.sum_bytes);
-    p.bytes = p.part_at + align256(std::max(p.dx.part_bytes, p.dw.part_bytes));
+    p.sum_at = act && !p.fused ? align256(d->groups * d->rows * p.dz_ld * (int64_t)size) : 0;
+    p.dw_at = p.sum_at + align256(std::max(p.dz.sum_bytes, p.dw.sum_bytes));
+    p.dx_at = p.dw_at + align256(p.dw.part_bytes);
+    p.bytes = p.dx_at + align256(p.dx.part_bytes);
     return p;
 }
 
@@ -166,7 +176,7 @@ malib_status malib_linear(const malib_linear_desc* d, const malib_mat* x, const 
     a.K = (int)d->in;
     a.groups = (int)d->groups;
     a.act = d->act;
-    HIP_TRY(launch_gemm(kGemmForward, d->dtype, a, p, (float*)work, (hipStream_t)stream));
+    HIP_TRY(launch_linear(d->dtype, a, p, (float*)work, (hipStream_t)stream));
     return MALIB_OK;
 }
 
@@ -201,41 +211,47 @@ malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* 
     TRY(check_work(work, work_bytes, p.bytes));
     hipStream_t s = (hipStream_t)stream;
     char* ws = (char*)work;
-    MatArg dz = arg(dy);
-    if (d->rows == 0)
-        dz = MatArg{nullptr, d->out, 0};
-    const bool need_dz = act && (dx || dw) && d->rows > 0;
-    if (need_dz || dbias) {
+    const bool rows = d->rows > 0;
+    MatArg dz = rows ? arg(dy) : MatArg{nullptr, d->out, 0};
+    const bool products = dw || (dx && rows);
+    const bool make_dz = act && !p.fused && products && rows;
+    const bool own_sums = dbias && (p.own_sums || !dw);
+    if (make_dz || own_sums) {
         MatArg to{nullptr, 0, 0};
-        if (need_dz)
+        if (make_dz)
             to = MatArg{ws + p.dz_at, p.dz_ld, d->rows * p.dz_ld};
         HIP_TRY(launch_dz(d->dtype, p.dz, arg(dy), arg(pre), to, d->act, (int)d->groups,
-                          (int)d->rows, (int)d->out, dbias ? (float*)(ws + p.sum_at) : nullptr,
-                          dbias, s));
-        if (need_dz)
+                          (int)d->rows, (int)d->out, (float*)(ws + p.sum_at),
+                          own_sums ? dbias : nullptr, s));
+        if (make_dz)
             dz = to;
     }
-    float* part = (float*)(ws + p.part_at);
-    GemmArgs a{};
-    a.groups = (int)d->groups;
-    if (dx && d->rows > 0) {
-        a.a = dz;
-        a.b = arg(w);
-        a.c = arg(dx);
-        a.M = (int)d->rows;
-        a.N = (int)d->in;
-        a.K = (int)d->out;
-        HIP_TRY(launch_gemm(kGemmDx, d->dtype, a, p.dx, part, s));
+    if (!products)
+        return MALIB_OK;
+    GemmArgs ax{}, aw{};
+    ax.groups = aw.groups = (int)d->groups;
+    ax.a = aw.a = dz;
+    if (act && p.fused && rows) {
+        ax.a_pre = aw.a_pre = arg(pre);
+        ax.a_act = aw.a_act = d->act;
+    }
+    if (dx && rows) {
+        ax.b = arg(w);
+        ax.c = arg(dx);
+        ax.M = (int)d->rows;
+        ax.N = (int)d->in;
+        ax.K = (int)d->out;
     }
     if (dw) {
-        a.a = dz;
-        a.b = d->rows > 0 ? arg(x) : MatArg{nullptr, d->in, 0};
-        a.c = arg(dw);
-        a.M = (int)d->out;
-        a.N = (int)d->in;
-        a.K = (int)d->rows;
-        HIP_TRY(launch_gemm(kGemmDw, d->dtype, a, p.dw, part, s));
+        aw.b = rows ? arg(x) : MatArg{nullptr, d->in, 0};
+        aw.c = arg(dw);
+        aw.M = (int)d->out;
+        aw.N = (int)d->in;
+        aw.K = (int)d->rows;
+        aw.sum_out = dbias && !own_sums ? dbias : nullptr;
     }
+    HIP_TRY(launch_linear_backward(d->dtype, aw, p.dw, (float*)(ws + p.dw_at),
+                                   (float*)(ws + p.sum_at), ax, p.dx, (float*)(ws + p.dx_at), s));
     return MALIB_OK;
 }
 

@@ -369,23 +369,29 @@ struct MatArg {
 // (bias, activation, residual, the values before the activation) where given.
 struct GemmArgs {
     MatArg a, b, c, res, pre;
+    MatArg a_pre;        // backward: A is a act'(a_pre) where a_act is an activation
+    int a_act;
     const float* bias;   // [groups][N] or null
+    float* sum_out;      // dW: [groups][M], sums of A over k, or null
     int M, N, K, groups, act;
-    // set by launch_gemm
+    // set by the launchers
     int mt, nt, splits;
-    int64_t k_split;
-    float* part;
+    int64_t k_split, blocks;
+    float *part, *sum;   // the splits' parts
 };
-// Tile side, number of splits of k (each k_split long) and the bytes of their parts.
+// Tile side, number of splits of k (each k_split long), the bytes of their parts and
+// of the parts of the column sums.
 struct GemmPlan {
     int tile, splits;
-    int64_t k_split, part_bytes;
+    int64_t k_split, part_bytes, sum_bytes;
 };
-// Which index is contiguous in memory: forward k and k, dx k and n, dW m and n.
-enum { kGemmForward, kGemmDx, kGemmDw };
 GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
-hipError_t launch_gemm(int form, int dtype, GemmArgs a, const GemmPlan& p, float* part,
-                       hipStream_t s);
+hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s);
+// dW and dx (either left out where its c.p is null), in one launch where both use
+// the same tile
+hipError_t launch_linear_backward(int dtype, GemmArgs dw, const GemmPlan& pw, float* dw_part,
+                                  float* sum_part, GemmArgs dx, const GemmPlan& px, float* dx_part,
+                                  hipStream_t s);
 struct DzPlan {
     int rows_per_block, parts, col_blocks;
     int64_t sum_bytes;

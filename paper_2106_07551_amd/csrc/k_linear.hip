@@ -8,6 +8,8 @@
 // of dx) or with its row index contiguous ("RC": W of dx, dz and x of dW).
 #include "internal.hpp"
 
+#include <type_traits>
+
 #include "chunk.hpp"
 #include "device.hpp"
 
@@ -16,10 +18,8 @@ namespace malib {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // k per tile: 128 bytes
 template <typename E>
@@ -118,40 +118,119 @@ __device__ __forceinline__ void slot_chunk(int s, int& row, int& c)
     c = chunk_slot<E, KC, BR>(row, s % CPR) - row * CPR;
 }
 
-// Operand fragment of step kk (0 .. 3) of a tile for the 32 rows from rb: 8
+// Transposing LDS reads: 16 lanes read a block of 4 rows of k by 16, each lane 8
+// bytes of it, and get a column each.  Written as assembly because the compiler
+// puts a wait for all loads from memory to LDS in front of the builtin, which
+// would end the overlap of the next tile's loads with this tile's products; the
+// wait for the reads themselves is in the same block.
+constexpr int kHalfRows = 4;   // rows of k between a fragment's two reads
+
+template <int OFF, int STEP>
+__device__ __forceinline__ void read_transposed(const uint32_t (&p)[1], u32x4 (&v)[1])
+{
+    uint64_t a, b;
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\t"
+                 "ds_read_b64_tr_b16 %1, %2 offset:%4\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b)
+                 : "v"(p[0]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    v[0] = u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
+
+template <int OFF, int STEP>
+__device__ __forceinline__ void read_transposed(const uint32_t (&p)[2], u32x4 (&v)[2])
+{
+    uint64_t a, b, c, d;
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                 "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+                 : "v"(p[0]), "v"(p[1]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    v[0] = u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    v[1] = u32x4{(uint32_t)c, (uint32_t)(c >> 32), (uint32_t)d, (uint32_t)(d >> 32)};
+}
+
+template <int OFF, int STEP>
+__device__ __forceinline__ void read_transposed(const uint32_t (&p)[4], u32x4 (&v)[4])
+{
+    uint64_t a, b, c, d, e, f, g, h;
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(e), "=&v"(f), "=&v"(g), "=&v"(h)
+                 : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(OFF), "n"(OFF + STEP)
+                 : "memory");
+    v[0] = u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    v[1] = u32x4{(uint32_t)c, (uint32_t)(c >> 32), (uint32_t)d, (uint32_t)(d >> 32)};
+    v[2] = u32x4{(uint32_t)e, (uint32_t)(e >> 32), (uint32_t)f, (uint32_t)(f >> 32)};
+    v[3] = u32x4{(uint32_t)g, (uint32_t)(g >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
+// Operand fragments of step kk (0 .. 3) of a tile for N times 32 rows from rb: 8
 // values of k per lane in bf16 (one 32x32x16 product), 4 in f32 (four 32x32x2
 // products); lanes 0-31 hold the first half of the step's k, lanes 32-63 the
 // second, the same for both operands.
-template <typename E, bool KC, int BR>
-__device__ __forceinline__ u32x4 fragment(const char* tile, int rb, int kk, int lane)
-{
-    const int r = lane & 31, h = lane >> 5;
-    if constexpr (KC) {
-        return *(const u32x4*)(tile + 16 * chunk_slot<E, true, BR>(rb + r, 2 * kk + h));
-    } else if constexpr (sizeof(E) == 2) {
-        // 16 lanes read a 4 x 16 block (4 of k) and get its transpose
-        const int row = rb + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        const int k = 16 * kk + 8 * h + ((lane >> 2) & 3);
-        u32x4 v;
+template <typename E, bool KC, int BR, int N>
+struct Fragments {
+    uint32_t at[N];   // RC in bf16: LDS address of this lane's part at kk = 0 of the first stage
+    const char* tile0;
+    int rb, lane;
+
+    __device__ __forceinline__ Fragments(const char* tile, int rb_, int lane_)
+        : tile0(tile), rb(rb_), lane(lane_)
+    {
+        if constexpr (!KC && sizeof(E) == 2) {
+            const int k = 8 * (lane >> 5) + ((lane >> 2) & 3);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const char* p = tile + 16 * chunk_slot<E, false, BR>(k + 4 * i, row >> 3) + 2 * (row & 7);
-            const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-            const uint64_t u = __builtin_bit_cast(uint64_t, t);
-            v[2 * i] = (uint32_t)u;
-            v[2 * i + 1] = (uint32_t)(u >> 32);
+            for (int i = 0; i < N; ++i) {
+                const int row = rb + 32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                at[i] = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)tile +
+                        16 * chunk_slot<E, false, BR>(k, row >> 3) + 2 * (row & 7);
+            }
         }
-        return v;
-    } else {
-        u32x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = *(const uint32_t*)(tile + 16 * chunk_slot<E, false, BR>(8 * kk + 4 * h + j,
-                                                                           (rb + r) >> 2) +
-                                      4 * (r & 3));
-        return v;
     }
-}
+
+    // of the stage `stage` bytes behind the first
+    template <int KK>
+    __device__ __forceinline__ void read(int stage, u32x4 (&v)[N]) const
+    {
+        const int r = lane & 31, h = lane >> 5;
+        if constexpr (KC) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = *(const u32x4*)(tile0 + stage +
+                                       16 * chunk_slot<E, true, BR>(rb + 32 * i + r, 2 * KK + h));
+        } else if constexpr (sizeof(E) == 2) {
+            // (the chunk index is xor-ed with bits of k mod 4 only: rows 4 and 16 further
+            // are at fixed distances)
+            constexpr int kRow = BR * 2;
+            uint32_t p[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                p[i] = at[i] + (uint32_t)stage;
+            read_transposed<16 * KK * kRow, kHalfRows * kRow>(p, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    v[i][j] = *(const uint32_t*)(
+                        tile0 + stage +
+                        16 * chunk_slot<E, false, BR>(8 * KK + 4 * h + j, (rb + 32 * i + r) >> 2) +
+                        4 * (r & 3));
+        }
+    }
+};
 
 template <typename E>
 __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c)
@@ -170,24 +249,34 @@ __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c)
 
 // -------------------------------------------------------------- tile loading
 
+// How operand tiles get to LDS: straight from memory (rows on 16-byte boundaries
+// that end with whole chunks), or through registers (any alignment, any extent),
+// or through registers with A = dy act'(pre) formed on the way (backward pass).
+enum { kDirect, kStaged, kFused };
+
 constexpr uint32_t kNoOffset = 0xF0000000u;   // beyond every buffer: reads as zero
 
 // One operand's share of a thread: NI chunks of every tile.
-template <typename E, bool KC, int BR, int THREADS, bool FAST>
+template <typename E, bool KC, int BR, int THREADS, int LOAD>
 struct TileLoader {
     static constexpr int NI = BR * 8 / THREADS;
     static constexpr int CH = kChunk<E>;
     const E* base;       // the tile's first row (KC) or column (RC) at k = 0
-    int64_t ld;
-    uint32_t off[NI];    // FAST: byte offset from the tile's start, or kNoOffset
-    int row[NI], k[NI];  // !FAST: row and first k (KC) / first row and k (RC) in the tile
-    int n_rows;          // rows of the operand from the tile's first on
-    u32x4 reg[FAST ? 1 : NI];
+    const E* pre;        // kFused: the same place in the values before the activation
+    int64_t ld, pre_ld;
+    uint32_t off[NI];    // kDirect: byte offset from the tile's start, or kNoOffset
+    int row[NI], k[NI];  // first row and first k of the chunk in the tile
+    int n_rows, act;     // rows of the operand from the tile's first on
+    u32x4 reg[LOAD == kDirect ? 1 : NI];
 
-    __device__ __forceinline__ TileLoader(const MatArg& m, int g, int64_t r0, int R, int tid)
+    __device__ __forceinline__ TileLoader(const MatArg& m, const MatArg& z, int act_, int g,
+                                          int64_t r0, int R, int tid)
     {
         ld = m.ld;
         base = (const E*)m.p + g * m.gs + (KC ? r0 * m.ld : r0);
+        pre_ld = z.ld;
+        pre = (const E*)z.p + g * z.gs + (KC ? r0 * z.ld : r0);
+        act = act_;
         n_rows = (int)(R - r0);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -195,15 +284,15 @@ struct TileLoader {
             slot_chunk<E, KC, BR>(tid + i * THREADS, rr, c);
             row[i] = KC ? rr : c * CH;
             k[i] = KC ? c * CH : rr;
-            if constexpr (FAST)
+            if constexpr (LOAD == kDirect)
                 off[i] = row[i] < n_rows
                              ? (uint32_t)(((int64_t)rr * ld + c * CH) * (int64_t)sizeof(E))
                              : kNoOffset;
         }
     }
 
-    // FAST: chunks of the tile at k0 straight into LDS; a wavefront's 64 chunks
-    // are consecutive slots.  Chunks at or behind k1 read as zeros.
+    // kDirect: the chunks of the tile at k0; a wavefront's 64 chunks are
+    // consecutive slots.  Chunks at or behind k1 read as zeros.
     __device__ __forceinline__ void issue(char* tile, int64_t k0, int64_t k1, int tid)
     {
         const E* p = base + (KC ? k0 : k0 * ld);
@@ -219,7 +308,7 @@ struct TileLoader {
         }
     }
 
-    // !FAST: the same through registers, any alignment, any extent
+    // kStaged, kFused
     __device__ __forceinline__ void load(int64_t k0, int64_t k1)
     {
 #pragma unroll
@@ -231,8 +320,19 @@ struct TileLoader {
                 n = rl > 0 ? (int)(left < CH ? left : CH) : 0;
             else
                 n = left > 0 ? rl : 0;
-            const E* p = base + (KC ? row[i] * ld + k0 + k[i] : (k0 + k[i]) * ld + row[i]);
-            reg[i] = n > 0 ? load_chunk(p, n) : u32x4{0, 0, 0, 0};
+            const int64_t r = KC ? row[i] : k0 + k[i], c = KC ? k0 + k[i] : row[i];
+            reg[i] = n > 0 ? load_chunk(base + r * ld + c, n) : u32x4{0, 0, 0, 0};
+            if constexpr (LOAD == kFused) {
+                if (n > 0) {
+                    float v[CH], z[CH];
+                    unpack<E>(reg[i], v);
+                    unpack<E>(load_chunk(pre + r * pre_ld + c, n), z);
+#pragma unroll
+                    for (int e = 0; e < CH; ++e)
+                        v[e] *= act_slope_f32(act, z[e]);
+                    reg[i] = pack<E>(v);
+                }
+            }
         }
     }
     __device__ __forceinline__ void store(char* tile, int tid)
@@ -245,33 +345,44 @@ struct TileLoader {
 
 // --------------------------------------------------------------------- kernel
 
-template <int BM, int BN, int WM, int WN>
+template <int TILE>
 struct GemmShape {
-    static constexpr int kThreads = WM * WN * 64;
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32x32 tiles per wavefront
-    static constexpr int kStage = (BM + BN) * 128;               // bytes of one stage
-    static constexpr int kOutLd = TN * 32 + 4;                   // floats per staged output row
-    static constexpr int kLds = 2 * kStage > WM * WN * 32 * kOutLd * 4 ? 2 * kStage
-                                                                      : WM * WN * 32 * kOutLd * 4;
+    static constexpr int kWm = 2, kWn = TILE == 256 ? 4 : 2;     // wavefronts
+    static constexpr int kThreads = kWm * kWn * 64;
+    static constexpr int kTm = TILE / kWm / 32, kTn = TILE / kWn / 32;   // 32x32 tiles of each
+    static constexpr int kStage = 2 * TILE * 128;                // bytes of one stage
+    // kDirect: tiles in flight and in use.  Four small ones hide the latency of short
+    // products that leave few workgroups per CU; larger tiles take two.
+    static constexpr int kStages = TILE == 64 ? 4 : 2;
+    static constexpr int kOutLd = kTn * 32 + 4;                  // floats per staged output row
+    static constexpr int kOut = kWm * kWn * 32 * kOutLd * 4;
+    static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
 };
 
-template <typename E, bool AKC, bool BKC, int BM, int BN, int WM, int WN, bool FAST>
-__global__ __launch_bounds__(WM* WN * 64) void gemm_kernel(GemmArgs a)
+// s_waitcnt: at most `vm` vector loads outstanding, no LDS operation
+constexpr int wait_code(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4); }
+
+// One workgroup's tile of C, number `block` of `n_blocks` of this product.
+template <typename E, bool AKC, bool BKC, int TILE, int LOAD>
+__device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uint32_t n_blocks,
+                                          char* lds)
 {
-    using S = GemmShape<BM, BN, WM, WN>;
-    constexpr int CH = kChunk<E>;
-    __shared__ __attribute__((aligned(16))) char lds[S::kLds];
+    using S = GemmShape<TILE>;
+    constexpr int CH = kChunk<E>, TM = S::kTm, TN = S::kTn;
+    constexpr int STAGES = LOAD == kDirect ? S::kStages : 2;
+    // column sums of A beside dW; the largest tile has no registers for them
+    constexpr bool kSums = !AKC && TILE < 256;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / WN, wn = wave % WN;
+    const int wm = wave / S::kWn, wn = wave % S::kWn;
 
     // Workgroup -> tile: consecutive workgroups go to the 8 XCDs in turn, so each
     // XCD gets one run of the tile order; within it, bands of 8 tile rows are
     // walked column by column, which keeps both operands' tiles in its L2.
     uint32_t id;
     {
-        const uint32_t nb = gridDim.x, q = nb / 8, r = nb % 8, x = blockIdx.x % 8;
-        id = x * q + (x < r ? x : r) + blockIdx.x / 8;
+        const uint32_t q = n_blocks / 8, r = n_blocks % 8, x = block % 8;
+        id = x * q + (x < r ? x : r) + block / 8;
     }
     const uint32_t tiles = (uint32_t)a.mt * (uint32_t)a.nt;   // below 2^31, as the grid
     const uint32_t sg = id / tiles, t0 = id % tiles;
@@ -284,65 +395,110 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_kernel(GemmArgs a)
         mt = (int)(band * 8 + u % rows);
         nt = (int)(u / rows);
     }
-    const int64_t m0 = (int64_t)mt * BM, n0 = (int64_t)nt * BN;
+    const int64_t m0 = (int64_t)mt * TILE, n0 = (int64_t)nt * TILE;
     const int64_t kb = (int64_t)split * a.k_split;
     const int64_t ke = kb + a.k_split < a.K ? kb + a.k_split : a.K;
     const int n_k = (int)((ke - kb + kBK<E> - 1) / kBK<E>);
 
-    TileLoader<E, AKC, BM, S::kThreads, FAST> la(a.a, g, m0, a.M, tid);
-    TileLoader<E, BKC, BN, S::kThreads, FAST> lb(a.b, g, n0, a.N, tid);
+    TileLoader<E, AKC, TILE, S::kThreads, LOAD> la(a.a, a.a_pre, a.a_act, g, m0, a.M, tid);
+    TileLoader<E, BKC, TILE, S::kThreads, LOAD == kFused ? kStaged : LOAD> lb(a.b, a.b, 0, g, n0,
+                                                                              a.N, tid);
 
-    f32x16 acc[S::TM][S::TN];
+    f32x16 acc[TM][TN], sum[kSums ? TM : 1];
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i)
+    for (int r = 0; r < 16; ++r) {
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
+            for (int j = 0; j < TN; ++j)
                 acc[i][j][r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < (kSums ? TM : 1); ++i)
+            sum[i][r] = 0.0f;
+    }
+    const Fragments<E, AKC, TILE, TM> fa(lds, wm * TM * 32, lane);
+    const Fragments<E, BKC, TILE, TN> fb(lds + TILE * 128, wn * TN * 32, lane);
+    const bool sums = kSums && a.sum && nt == 0 && wn == 0;
+    const uint32_t one = sizeof(E) == 2 ? 0x3F803F80u : 0x3F800000u;
 
-    if (n_k > 0) {
-        if constexpr (FAST) {
-            la.issue(lds, kb, ke, tid);
-            lb.issue(lds + BM * 128, kb, ke, tid);
-        } else {
-            la.load(kb, ke);
-            lb.load(kb, ke);
+    if constexpr (LOAD == kDirect) {
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t) {
+            const int64_t k = kb + (int64_t)t * kBK<E>;
+            la.issue(lds + t * S::kStage, k, ke, tid);
+            lb.issue(lds + t * S::kStage + TILE * 128, k, ke, tid);
         }
+    } else if (n_k > 0) {
+        la.load(kb, ke);
+        lb.load(kb, ke);
     }
     for (int t = 0; t < n_k; ++t) {
-        char* cur = lds + (t & 1) * S::kStage;
-        char* nxt = lds + ((t + 1) & 1) * S::kStage;
-        const int64_t k_next = kb + (int64_t)(t + 1) * kBK<E>;
-        if constexpr (!FAST) {
+        char* cur = lds + (t & (STAGES - 1)) * S::kStage;
+        const int next = LOAD == kDirect ? t + STAGES - 1 : t + 1;
+        const int64_t k_next = kb + (int64_t)next * kBK<E>;
+        if constexpr (LOAD == kDirect) {
+            // this tile has arrived (later ones may be on the way: the loads of each
+            // tile are issued in every round, behind the end as reads of nothing, so
+            // that the count holds), and every wavefront is done with the stage that is
+            // filled next
+            constexpr int kLater = (STAGES - 2) * (decltype(la)::NI + decltype(lb)::NI);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(wait_code(kLater));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            char* to = lds + (next & (STAGES - 1)) * S::kStage;
+            if (STAGES > 2 || next < n_k) {
+                la.issue(to, k_next, ke, tid);
+                lb.issue(to + TILE * 128, k_next, ke, tid);
+            }
+        } else {
             la.store(cur, tid);
-            lb.store(cur + BM * 128, tid);
-        }
-        // this tile has arrived; every wavefront is done with the other stage
-        __syncthreads();
-        if (t + 1 < n_k) {
-            if constexpr (FAST) {
-                la.issue(nxt, k_next, ke, tid);
-                lb.issue(nxt + BM * 128, k_next, ke, tid);
-            } else {
+            lb.store(cur + TILE * 128, tid);
+            __syncthreads();
+            if (next < n_k) {
                 la.load(k_next, ke);
                 lb.load(k_next, ke);
             }
         }
+        const int stage = (t & (STAGES - 1)) * S::kStage;
+        auto step = [&](auto kk) {
+            u32x4 va[TM], vb[TN];
+            fa.template read<decltype(kk)::value>(stage, va);
+            fb.template read<decltype(kk)::value>(stage, vb);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            u32x4 fa[S::TM], fb[S::TN];
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
-                fa[i] = fragment<E, AKC, BM>(cur, (wm * S::TM + i) * 32, kk, lane);
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = multiply<E>(va[i], vb[j], acc[i][j]);
+            if constexpr (kSums) {
+                if (sums) {
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j)
-                fb[j] = fragment<E, BKC, BN>(cur + BM * 128, (wn * S::TN + j) * 32, kk, lane);
+                    for (int i = 0; i < TM; ++i)
+                        sum[i] = multiply<E>(va[i], u32x4{one, one, one, one}, sum[i]);
+                }
+            }
+        };
+        step(std::integral_constant<int, 0>{});
+        step(std::integral_constant<int, 1>{});
+        step(std::integral_constant<int, 2>{});
+        step(std::integral_constant<int, 3>{});
+    }
+
+    // nothing may still land in LDS
+    if constexpr (LOAD == kDirect)
+        __builtin_amdgcn_s_waitcnt(wait_code(0));
+    const int h = lane >> 5;
+    if constexpr (kSums) {
+        if (sums && (lane & 31) == 0) {
+            float* o = a.sum + ((int64_t)split * a.groups + g) * a.M;
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j)
-                    acc[i][j] = multiply<E>(fa[i], fb[j], acc[i][j]);
+                for (int r = 0; r < 16; ++r) {
+                    const int64_t m = m0 + (wm * TM + i) * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+                    if (m < a.M)
+                        o[m] = sum[i][r];
+                }
         }
     }
 
@@ -350,22 +506,21 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_kernel(GemmArgs a)
     // a lane holds 16 bytes of a row and a row's lanes are neighbours.
     __syncthreads();
     float* buf = (float*)lds + wave * 32 * S::kOutLd;
-    const int h = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j)
+        for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 buf[(8 * (r >> 2) + 4 * h + (r & 3)) * S::kOutLd + j * 32 + (lane & 31)] =
                     acc[i][j][r];
         wave_lds_sync();
-        constexpr int LPR = S::TN * 32 / CH;   // lanes per row
+        constexpr int LPR = TN * 32 / CH;   // lanes per row
 #pragma unroll 1
         for (int p = 0; p < 32; p += 64 / LPR) {
             const int r = p + lane / LPR, c = (lane % LPR) * CH;
-            const int64_t m = m0 + (wm * S::TM + i) * 32 + r;
-            const int64_t n = n0 + wn * S::TN * 32 + c;
+            const int64_t m = m0 + (wm * TM + i) * 32 + r;
+            const int64_t n = n0 + wn * TN * 32 + c;
             if (m < a.M && n < a.N) {
                 const int cnt = (int)(a.N - n < CH ? a.N - n : CH);
                 float v[CH];
@@ -392,31 +547,102 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_kernel(GemmArgs a)
     }
 }
 
-// Sum of the splits' parts in split order, then the epilogue.
+template <typename E, int TILE, int LOAD>
+__global__ __launch_bounds__(GemmShape<TILE>::kThreads) void forward_kernel(GemmArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::kLds];
+    gemm_tile<E, true, true, TILE, LOAD>(a, blockIdx.x, gridDim.x, lds);
+}
+
+// dW's tiles, then dx's, in one launch: neither waits for the other's last tiles.
+template <typename E, int TILE, int LOAD>
+__global__ __launch_bounds__(GemmShape<TILE>::kThreads) void backward_kernel(GemmArgs dw,
+                                                                             uint32_t n_dw,
+                                                                             GemmArgs dx)
+{
+    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::kLds];
+    if (blockIdx.x < n_dw)
+        gemm_tile<E, false, false, TILE, LOAD>(dw, blockIdx.x, n_dw, lds);
+    else
+        gemm_tile<E, true, false, TILE, LOAD>(dx, blockIdx.x - n_dw, gridDim.x - n_dw, lds);
+}
+
+// Sums of the splits' parts, then the epilogue, of up to two products: 32 chunks of
+// output per workgroup, each thread a share of the splits, the shares added in
+// order.  Column sums are further items behind the first product's chunks.
+constexpr int kSumItems = 32, kSumShares = 8;
+
 template <typename E>
-__global__ __launch_bounds__(256) void split_sum_kernel(GemmArgs a)
+__device__ __forceinline__ void split_sum_block(const GemmArgs& a, int64_t block, float* red)
 {
     constexpr int CH = kChunk<E>;
+    const int item = threadIdx.x % kSumItems, share = threadIdx.x / kSumItems;
     const int64_t per_row = (a.N + CH - 1) / CH;
     const int64_t n_chunks = (int64_t)a.groups * a.M * per_row;
-    const int64_t plane = (int64_t)a.groups * a.M * a.N;
-    for (int64_t q = blockIdx.x * 256ll + threadIdx.x; q < n_chunks; q += gridDim.x * 256ll) {
-        const int64_t gm = q / per_row;
-        const int n = (int)(q % per_row) * CH;
-        const int cnt = a.N - n < CH ? a.N - n : CH;
-        float v[CH];
+    const int64_t n_sums = a.sum_out ? (int64_t)a.groups * a.M : 0;
+    const int64_t q = block * kSumItems + item;
+    const int64_t gm = q < n_chunks ? q / per_row : q - n_chunks;
+    const int n = q < n_chunks ? (int)(q - gm * per_row) * CH : 0;
+    const int cnt = q < n_chunks ? (a.N - n < CH ? a.N - n : CH) : q < n_chunks + n_sums ? 1 : 0;
+    const int64_t plane = (int64_t)a.groups * a.M * (q < n_chunks ? a.N : 1);
+    const float* p = q < n_chunks ? a.part + gm * a.N + n : a.sum + gm;
+    float v[CH];
 #pragma unroll
-        for (int e = 0; e < CH; ++e)
-            v[e] = 0.0f;
-        const float* p = a.part + gm * a.N + n;
-        for (int s = 0; s < a.splits; ++s, p += plane) {
+    for (int e = 0; e < CH; ++e)
+        v[e] = 0.0f;
+    if (cnt == CH && plane % 4 == 0 && a.N % 4 == 0) {
+#pragma unroll 4
+        for (int s = share; s < a.splits; s += kSumShares) {
+#pragma unroll
+            for (int e = 0; e < CH; e += 4) {
+                const f32x4 t = *(const f32x4*)(p + s * plane + e);
+                v[e] += t[0];
+                v[e + 1] += t[1];
+                v[e + 2] += t[2];
+                v[e + 3] += t[3];
+            }
+        }
+    } else if (cnt > 0) {
+#pragma unroll 4
+        for (int s = share; s < a.splits; s += kSumShares)
 #pragma unroll
             for (int e = 0; e < CH; ++e)
                 if (e < cnt)
-                    v[e] += p[e];
-        }
-        epilogue_chunk<E>(a, (int)(gm / a.M), gm % a.M, n, cnt, v);
+                    v[e] += p[s * plane + e];
     }
+#pragma unroll
+    for (int e = 0; e < CH; ++e)
+        red[(share * CH + e) * kSumItems + item] = v[e];
+    __syncthreads();
+    if (share != 0 || cnt == 0)
+        return;
+#pragma unroll
+    for (int e = 0; e < CH; ++e)
+        for (int t = 1; t < kSumShares; ++t)
+            v[e] += red[(t * CH + e) * kSumItems + item];
+    if (q < n_chunks)
+        epilogue_chunk<E>(a, (int)(gm / a.M), gm % a.M, n, cnt, v);
+    else
+        a.sum_out[gm] = v[0];
+}
+
+template <typename E>
+__global__ __launch_bounds__(kSumItems* kSumShares) void split_sum_kernel(GemmArgs a,
+                                                                          uint32_t n_a, GemmArgs b)
+{
+    __shared__ float red[kSumShares * kChunk<E> * kSumItems];
+    if (blockIdx.x < n_a)
+        split_sum_block<E>(a, blockIdx.x, red);
+    else
+        split_sum_block<E>(b, blockIdx.x - n_a, red);
+}
+
+template <typename E>
+int64_t split_sum_blocks(const GemmArgs& a)
+{
+    const int64_t per_row = (a.N + kChunk<E> - 1) / kChunk<E>;
+    const int64_t items = (int64_t)a.groups * a.M * (per_row + (a.sum_out ? 1 : 0));
+    return (items + kSumItems - 1) / kSumItems;
 }
 
 // dz = dy act'(z) rounded to the layer's type (where there is an activation), and
@@ -476,38 +702,78 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
     }
 }
 
-// db[i] = sum over the row ranges, in order.
-__global__ __launch_bounds__(256) void db_kernel(const float* sums, int64_t n, int parts, float* db)
+// db[i] = sum over the row ranges: shares of the ranges by thread, added in order.
+__global__ __launch_bounds__(kSumItems* kSumShares) void db_kernel(const float* sums, int64_t n,
+                                                                   int parts, float* db)
 {
-    const int64_t i = blockIdx.x * 256ll + threadIdx.x;
-    if (i >= n)
-        return;
+    __shared__ float red[kSumShares][kSumItems];
+    const int item = threadIdx.x % kSumItems, share = threadIdx.x / kSumItems;
+    const int64_t i = (int64_t)blockIdx.x * kSumItems + item;
     float t = 0.0f;
-    for (int p = 0; p < parts; ++p)
-        t += sums[p * n + i];
-    db[i] = t;
+    if (i < n) {
+#pragma unroll 4
+        for (int p = share; p < parts; p += kSumShares)
+            t += sums[p * n + i];
+    }
+    red[share][item] = t;
+    __syncthreads();
+    if (share == 0 && i < n) {
+        for (int k = 1; k < kSumShares; ++k)
+            t += red[k][item];
+        db[i] = t;
+    }
 }
 
-template <typename E, bool AKC, bool BKC, int BM, int BN, int WM, int WN>
-hipError_t launch_shape(const GemmArgs& a, bool fast, int64_t blocks, hipStream_t s)
+template <typename E>
+hipError_t launch_forward_as(const GemmArgs& a, int tile, bool direct, hipStream_t s)
 {
-    if (fast)
-        gemm_kernel<E, AKC, BKC, BM, BN, WM, WN, true>
-            <<<(unsigned)blocks, WM * WN * 64, 0, s>>>(a);
+    const unsigned nb = (unsigned)a.blocks;
+    if (tile == 256 && direct)
+        forward_kernel<E, 256, kDirect><<<nb, 512, 0, s>>>(a);
+    else if (tile == 128 && direct)
+        forward_kernel<E, 128, kDirect><<<nb, 256, 0, s>>>(a);
+    else if (tile == 128)
+        forward_kernel<E, 128, kStaged><<<nb, 256, 0, s>>>(a);
+    else if (direct)
+        forward_kernel<E, 64, kDirect><<<nb, 256, 0, s>>>(a);
     else
-        gemm_kernel<E, AKC, BKC, BM, BN, WM, WN, false>
-            <<<(unsigned)blocks, WM * WN * 64, 0, s>>>(a);
+        forward_kernel<E, 64, kStaged><<<nb, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename E, bool AKC, bool BKC>
-hipError_t launch_form(const GemmArgs& a, int tile, bool fast, int64_t blocks, hipStream_t s)
+template <typename E>
+hipError_t launch_backward_as(const GemmArgs& dw, const GemmArgs& dx, int tile, int load,
+                              hipStream_t s)
 {
-    if (tile == 256)
-        return launch_shape<E, AKC, BKC, 256, 256, 2, 4>(a, fast, blocks, s);
-    if (tile == 128)
-        return launch_shape<E, AKC, BKC, 128, 128, 2, 2>(a, fast, blocks, s);
-    return launch_shape<E, AKC, BKC, 64, 64, 2, 2>(a, fast, blocks, s);
+    const uint32_t n_dw = (uint32_t)dw.blocks, nb = n_dw + (uint32_t)dx.blocks;
+    if (nb == 0)
+        return hipSuccess;
+    if (tile == 256 && load == kDirect)
+        backward_kernel<E, 256, kDirect><<<nb, 512, 0, s>>>(dw, n_dw, dx);
+    else if (tile == 128 && load == kDirect)
+        backward_kernel<E, 128, kDirect><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (tile == 128 && load == kStaged)
+        backward_kernel<E, 128, kStaged><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (tile == 128)
+        backward_kernel<E, 128, kFused><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (load == kDirect)
+        backward_kernel<E, 64, kDirect><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (load == kStaged)
+        backward_kernel<E, 64, kStaged><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else
+        backward_kernel<E, 64, kFused><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_split_sums(const GemmArgs& a, const GemmArgs& b, hipStream_t s)
+{
+    const int64_t na = a.blocks && a.part ? split_sum_blocks<E>(a) : 0;
+    const int64_t nb = b.blocks && b.part ? split_sum_blocks<E>(b) : 0;
+    if (na + nb == 0)
+        return hipSuccess;
+    split_sum_kernel<E><<<(unsigned)(na + nb), kSumItems * kSumShares, 0, s>>>(a, (uint32_t)na, b);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -542,48 +808,75 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
     p.splits = (int)((k_tiles + per - 1) / per);
     p.k_split = per * bk;
     p.part_bytes = p.splits > 1 ? p.splits * groups * M * N * 4 : 0;
+    p.sum_bytes = p.splits > 1 ? p.splits * groups * M * 4 : 0;
     return p;
 }
 
-hipError_t launch_gemm(int form, int dtype, GemmArgs a, const GemmPlan& p, float* part,
-                       hipStream_t s)
+// The plan's part of a product's arguments
+static void apply(GemmArgs& a, const GemmPlan& p, float* part)
 {
-    const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
-    const int64_t t = p.tile;
-    a.mt = (int)((a.M + t - 1) / t);
-    a.nt = (int)((a.N + t - 1) / t);
+    a.mt = (a.M + p.tile - 1) / p.tile;
+    a.nt = (a.N + p.tile - 1) / p.tile;
     a.splits = p.splits;
     a.k_split = p.k_split;
     a.part = p.splits > 1 ? part : nullptr;
-    const bool fast = chunked(a.a, size, form == kGemmDw ? a.M : a.K, a.groups) &&
-                      chunked(a.b, size, form == kGemmForward ? a.K : a.N, a.groups);
-    const int64_t blocks = (int64_t)a.mt * a.nt * a.groups * a.splits;
-    if (blocks == 0)
-        return hipSuccess;
+    a.blocks = (int64_t)a.mt * a.nt * a.groups * a.splits;
+}
+
+hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s)
+{
+    const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
+    const bool direct = chunked(a.a, size, a.K, a.groups) && chunked(a.b, size, a.K, a.groups);
+    apply(a, p, part);
+    const GemmArgs none{};
     hipError_t e;
-    const bool bf = dtype == MALIB_DT_BF16;
-    switch (form) {
-    case kGemmForward:
-        e = bf ? launch_form<bf16_t, true, true>(a, p.tile, fast, blocks, s)
-               : launch_form<float, true, true>(a, p.tile, fast, blocks, s);
-        break;
-    case kGemmDx:
-        e = bf ? launch_form<bf16_t, true, false>(a, p.tile, fast, blocks, s)
-               : launch_form<float, true, false>(a, p.tile, fast, blocks, s);
-        break;
-    default:
-        e = bf ? launch_form<bf16_t, false, false>(a, p.tile, fast, blocks, s)
-               : launch_form<float, false, false>(a, p.tile, fast, blocks, s);
+    if (dtype == MALIB_DT_BF16) {
+        e = launch_forward_as<bf16_t>(a, p.tile, direct, s);
+        return e != hipSuccess ? e : launch_split_sums<bf16_t>(a, none, s);
     }
-    if (e != hipSuccess || !a.part)
-        return e;
-    const int64_t chunks = (int64_t)a.groups * a.M * ((a.N + 16 / size - 1) / (16 / size));
-    const unsigned nb = (unsigned)std::min<int64_t>((chunks + 255) / 256, 8192);
-    if (bf)
-        split_sum_kernel<bf16_t><<<nb, 256, 0, s>>>(a);
-    else
-        split_sum_kernel<float><<<nb, 256, 0, s>>>(a);
-    return hipGetLastError();
+    e = launch_forward_as<float>(a, p.tile, direct, s);
+    return e != hipSuccess ? e : launch_split_sums<float>(a, none, s);
+}
+
+template <typename E>
+static hipError_t backward_as(const GemmArgs& dw, int dw_tile, const GemmArgs& dx, int dx_tile,
+                              int load, hipStream_t s)
+{
+    const GemmArgs none{};
+    hipError_t e;
+    if (dw_tile == dx_tile) {
+        e = launch_backward_as<E>(dw, dx, dw_tile, load, s);
+    } else {
+        e = launch_backward_as<E>(dw, none, dw_tile, load, s);
+        if (e == hipSuccess)
+            e = launch_backward_as<E>(none, dx, dx_tile, load, s);
+    }
+    return e != hipSuccess ? e : launch_split_sums<E>(dw, dx, s);
+}
+
+hipError_t launch_linear_backward(int dtype, GemmArgs dw, const GemmPlan& pw, float* dw_part,
+                                  float* sum_part, GemmArgs dx, const GemmPlan& px, float* dx_part,
+                                  hipStream_t s)
+{
+    const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
+    bool direct = true, fused = false;
+    if (dw.c.p) {
+        apply(dw, pw, dw_part);
+        if (dw.sum_out)
+            dw.sum = pw.splits > 1 ? sum_part : dw.sum_out;
+        direct = chunked(dw.a, size, dw.M, dw.groups) && chunked(dw.b, size, dw.N, dw.groups);
+        fused = dw.a_act != MALIB_ACT_NONE;
+    }
+    if (dx.c.p) {
+        apply(dx, px, dx_part);
+        direct = direct && chunked(dx.a, size, dx.K, dx.groups) &&
+                 chunked(dx.b, size, dx.N, dx.groups);
+        fused = fused || dx.a_act != MALIB_ACT_NONE;
+    }
+    const int load = fused ? kFused : direct ? kDirect : kStaged;
+    return dtype == MALIB_DT_BF16
+               ? backward_as<bf16_t>(dw, pw.tile, dx, px.tile, load, s)
+               : backward_as<float>(dw, pw.tile, dx, px.tile, load, s);
 }
 
 DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size)
@@ -595,7 +888,7 @@ DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size)
     p.rows_per_block = (int)std::max<int64_t>(1, (M + parts - 1) / parts);
     p.parts = (int)std::max<int64_t>(1, (M + p.rows_per_block - 1) / p.rows_per_block);
     p.col_blocks = (int)cols;
-    p.sum_bytes = (int64_t)p.parts * groups * N * 4;
+    p.sum_bytes = p.parts > 1 ? (int64_t)p.parts * groups * N * 4 : 0;
     return p;
 }
 
@@ -604,17 +897,19 @@ hipError_t launch_dz(int dtype, const DzPlan& p, const MatArg& dy, const MatArg&
                      hipStream_t s)
 {
     const dim3 grid(p.col_blocks, p.parts, groups);
+    float* to = !db ? nullptr : p.parts > 1 ? sums : db;
     if (dtype == MALIB_DT_BF16)
         dz_kernel<bf16_t><<<grid, kDzCols * kDzRows, 0, s>>>(dy, pre, dz, act, M, N,
-                                                             p.rows_per_block, sums);
+                                                             p.rows_per_block, to);
     else
         dz_kernel<float><<<grid, kDzCols * kDzRows, 0, s>>>(dy, pre, dz, act, M, N,
-                                                            p.rows_per_block, sums);
+                                                            p.rows_per_block, to);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !db)
+    if (e != hipSuccess || to == db)
         return e;
     const int64_t n = (int64_t)groups * N;
-    db_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sums, n, p.parts, db);
+    db_kernel<<<(unsigned)((n + kSumItems - 1) / kSumItems), kSumItems * kSumShares, 0, s>>>(
+        sums, n, p.parts, db);
     return hipGetLastError();
 }
 
