@@ -283,7 +283,9 @@ malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t A, int64_t* wo
     TRY(check_loss(dtype, rows, A));
     if (!work_bytes)
         return set_error(MALIB_E_INVAL, "work_bytes is NULL");
-    *work_bytes = loss_plan(rows, A, type_size(dtype)).work_bytes;
+    // (the longest list takes the most workgroups)
+    *work_bytes = std::max(loss_plan(rows, A, 0, type_size(dtype)).work_bytes,
+                           loss_plan(rows, A, 256, type_size(dtype)).work_bytes);
     return MALIB_OK;
 }
 
@@ -308,7 +310,7 @@ malib_status malib_policy_loss(const malib_policy_loss_desc* d, const void* logi
     if (d->kl_coef != 0.0f && !ref_logp && !ref_logits)
         return set_error(MALIB_E_INVAL, "kl_coef needs ref_logp or ref_logits");
     const int size = type_size(d->dtype);
-    const LossPlan p = loss_plan(d->rows, d->n_actions, size);
+    const LossPlan p = loss_plan(d->rows, d->n_actions, 0, size);
     if (d->rows > 0) {
         if (!logits || !actions || !old_logp || !advantage)
             return set_error(MALIB_E_INVAL,
@@ -369,7 +371,7 @@ malib_status malib_distill_loss(const malib_distill_desc* d, const void* logits,
     if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature))
         return set_error(MALIB_E_INVAL, "temperature must be positive and finite");
     const int size = type_size(d->dtype);
-    const LossPlan p = loss_plan(d->rows, d->n_actions, size);
+    const LossPlan p = loss_plan(d->rows, d->n_actions, d->top, size);
     if (d->rows > 0) {
         if (!logits || !teacher_idx || !teacher_logits)
             return set_error(MALIB_E_INVAL,

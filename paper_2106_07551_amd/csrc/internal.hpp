@@ -421,12 +421,12 @@ struct LossArgs {
     void* part;
     double* part_total;
 };
-enum { kLossLane, kLossRow16, kLossRow64, kLossRow256, kLossRow1024, kLossLong, kLossSplit };
+enum { kLossLane, kLossRow, kLossLong, kLossSplit };
 struct LossPlan {
-    int variant, splits, part_chunks;
+    int variant, group, splits, part_chunks;
     int64_t blocks, part_bytes, work_bytes;
 };
-LossPlan loss_plan(int64_t rows, int64_t A, int size);
+LossPlan loss_plan(int64_t rows, int64_t A, int top, int size);   // top: 0 for the policy loss
 hipError_t launch_loss(LossArgs a, int dtype, bool distill, const LossPlan& p, void* work,
                        hipStream_t s);
 

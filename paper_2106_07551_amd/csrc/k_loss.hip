@@ -217,136 +217,291 @@ __device__ __forceinline__ void store_total(const LossArgs& a, double t)
         a.part_total[blockIdx.x] = t;
 }
 
+constexpr uint32_t kNegInfBits = 0xFF800000u;
+
+// v with -inf as entry i
+template <typename E>
+__device__ __forceinline__ void exclude(u32x4& v, int i, bool out)
+{
+    if constexpr (sizeof(E) == 4) {
+        v[i] = out ? kNegInfBits : v[i];
+    } else {
+        const uint32_t w = v[i >> 1];
+        v[i >> 1] = out ? ((i & 1) ? (w & 0xFFFFu) | kNegInfBits
+                                   : (w & 0xFFFF0000u) | (kNegInfBits >> 16))
+                        : w;
+    }
+}
+
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
+// Raw chunk of a row with n entries left, with -inf in the entries behind the row's
+// end and those that are not legal.
+template <typename E>
+__device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* mask)
+{
+    constexpr int CH = kChunk<E>;
+    if (n >= CH) {
+        u32x4 v = *(const u32x4_any*)p;
+        if (mask) {
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                const uint32_t b = *(const u32_any*)(mask + i);
+                exclude<E>(v, i, (b & 0xFFu) == 0);
+                exclude<E>(v, i + 1, (b & 0xFF00u) == 0);
+                exclude<E>(v, i + 2, (b & 0xFF0000u) == 0);
+                exclude<E>(v, i + 3, (b & 0xFF000000u) == 0);
+            }
+        }
+        return v;
+    }
+    u32x4 v = n > 0 ? load_chunk(p, n) : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        exclude<E>(v, i, i >= n || (mask && i < n && mask[i] == 0));
+    return v;
+}
+
 // ------------------------------------------------- few actions: a lane per row
 
-// 64 rows per wavefront: their logits go through LDS (row stride odd, so that lanes
-// that read the same column of neighbouring rows fall into different banks), so
-// that memory is read and written in its own order while each lane works on a row
-// alone: no reductions, and a row's scalar work is not repeated by other lanes.
-constexpr int kLaneThreads = 256, kLaneRows = 64;
+// 64 rows per wavefront, up to kLaneMost entries each: rows go through LDS (row
+// stride odd, so that lanes that read the same column of neighbouring rows fall
+// into different banks), so that memory is read and written in its own order,
+// 16 bytes per lane where rows follow each other without gaps, while each lane
+// works on a row alone in registers: no reductions, and a row's scalar work is
+// not repeated by other lanes.
+constexpr int kLaneThreads = 256, kLaneRows = 64, kLaneMost = 31;
+
+// i / w for i < 2048, w <= 32
+struct SmallDiv {
+    uint32_t magic;
+    __device__ __forceinline__ explicit SmallDiv(int w) : magic((1u << 20) / (uint32_t)w + 1u) {}
+    __device__ __forceinline__ int operator()(int i) const
+    {
+        return (int)(((uint32_t)i * magic) >> 20);
+    }
+};
+
+// n rows of w values (rows ld apart) into LDS rows of w | 1; -inf where the mask
+// excludes an entry.
+template <typename E>
+__device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const uint8_t* mask,
+                                            int64_t mask_ld, int n, int w, float* to, int lane)
+{
+    constexpr int CH = kChunk<E>;
+    const int ldw = w | 1, count = n * w;
+    const SmallDiv div(w);
+    if (ld == w && (!mask || mask_ld == w)) {
+        for (int i = lane * CH; i < count; i += 64 * CH) {
+            float v[CH];
+            unpack<E>(load_masked(p + i, count - i, mask ? mask + i : nullptr), v);
+            int r = div(i), j = i - r * w;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                if (i + e < count)
+                    to[r * ldw + j] = v[e];
+                const bool wrap = j + 1 == w;
+                r += wrap;
+                j = wrap ? 0 : j + 1;
+            }
+        }
+        return;
+    }
+    for (int i = lane; i < count; i += 64) {
+        const int r = div(i), j = i - r * w;
+        const bool legal = !mask || mask[r * mask_ld + j] != 0;
+        const float v = to_f32(p[r * ld + j]);
+        to[r * ldw + j] = legal ? v : kNegInf;
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ void rows_from_lds(const float* from, E* p, int64_t ld, int n, int w,
+                                              int lane)
+{
+    constexpr int CH = kChunk<E>;
+    const int ldw = w | 1, count = n * w;
+    const SmallDiv div(w);
+    if (ld == w) {
+        for (int i = lane * CH; i < count; i += 64 * CH) {
+            float v[CH];
+            int r = div(i), j = i - r * w;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                v[e] = i + e < count ? from[r * ldw + j] : 0.0f;
+                const bool wrap = j + 1 == w;
+                r += wrap;
+                j = wrap ? 0 : j + 1;
+            }
+            store_chunk(p + i, count - i, pack<E>(v));
+        }
+        return;
+    }
+    for (int i = lane; i < count; i += 64) {
+        const int r = div(i), j = i - r * w;
+        p[r * ld + j] = from_f32<E>(from[r * ldw + j]);
+    }
+}
+
+// Floats of LDS per row: logits, the reference's or the teacher's dense
+// probabilities, the teacher's list.
+__host__ __device__ constexpr int lane_floats(int kind, int A, int top)
+{
+    return (A | 1) * (kind == kPolicy ? 1 : 2) + (kind == kDistill ? 2 * (top | 1) : 0);
+}
 
 template <typename E, int KIND>
 __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
 {
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int A = a.A, ldw = A | 1;
-    constexpr int kBufs = KIND == kPolicyRef ? 2 : 1;
-    float* bx = lds + wave * kLaneRows * ldw * kBufs;
+    const int A = a.A, ldw = A | 1, top = KIND == kDistill ? a.top : 0, ldt = top | 1;
+    float* bx = lds + wave * kLaneRows * lane_floats(KIND, A, top);
     float* by = bx + kLaneRows * ldw;
-    float* xr = bx + lane * ldw;
-    float* yr = by + lane * ldw;
+    float* bv = by + kLaneRows * ldw;                  // distillation: the list's logits
+    float* bi = bv + kLaneRows * ldt;                  // and indices (as floats' bits)
     const float c = kLog2e / a.temperature;
     double total = 0.0;
     const int64_t tiles = (a.rows + kLaneThreads - 1) / kLaneThreads;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t r0 = tile * kLaneThreads + wave * kLaneRows;
-        const int n = (int)(a.rows - r0 < kLaneRows ? a.rows - r0 : kLaneRows);   // may be <= 0
-        const int count = n > 0 ? n * A : 0;
+        const int64_t left = a.rows - r0;
+        const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
+        const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
         wave_lds_sync();
-        for (int i = lane; i < count; i += 64) {
-            const int r = i / A, j = i - r * A;
-            float x = to_f32(((const E*)a.logits)[(r0 + r) * a.logits_ld + j]);
-            const bool legal = !a.mask || a.mask[(r0 + r) * a.mask_ld + j] != 0;
-            bx[r * ldw + j] = legal ? x : kNegInf;
-            if (KIND == kPolicyRef) {
-                const float y = to_f32(((const E*)a.ref_logits)[(r0 + r) * a.ref_ld + j]);
-                by[r * ldw + j] = legal ? y : kNegInf;
-            }
+        rows_to_lds((const E*)a.logits + r0 * a.logits_ld, a.logits_ld, mask, a.mask_ld, n, A, bx,
+                    lane);
+        if (KIND == kPolicyRef)
+            rows_to_lds((const E*)a.ref_logits + r0 * a.ref_ld, a.ref_ld, mask, a.mask_ld, n, A,
+                        by, lane);
+        if (KIND == kDistill) {
+            rows_to_lds(a.val + r0 * top, top, nullptr, 0, n, top, bv, lane);
+            rows_to_lds((const float*)a.idx + r0 * top, top, nullptr, 0, n, top, bi, lane);
         }
         wave_lds_sync();
         const int64_t row = r0 + lane;
         if (lane < n) {
-            PolicyRow pr{};
-            bool counts;
-            float w;
-            if (KIND == kDistill) {
-                w = a.weight ? a.weight[row] : a.row_weight;
-                counts = w != 0.0f;
-            } else {
-                pr = policy_row(a, row);
-                w = pr.w;
-                counts = pr.counts;
+            float* xr = bx + lane * ldw;
+            float* yr = by + lane * ldw;
+            float x[kLaneMost + 1], y[KIND == kPolicyRef ? kLaneMost + 1 : 1];
+            float m = kNegInf, my = kNegInf;
+#pragma unroll
+            for (int j = 0; j <= kLaneMost; ++j) {
+                x[j] = kNegInf;
+                if (KIND == kPolicyRef)
+                    y[j] = kNegInf;
+            }
+            // (four entries per uniform branch)
+#pragma unroll
+            for (int q = 0; q <= kLaneMost; q += 4) {
+                if (q >= A)
+                    break;
+#pragma unroll
+                for (int j = q; j < q + 4; ++j) {
+                    if (j < A) {
+                        x[j] = xr[j];
+                        m = fmaxf(m, x[j]);
+                        if (KIND == kPolicyRef) {
+                            y[j] = yr[j];
+                            my = fmaxf(my, y[j]);
+                        }
+                    }
+                }
             }
             Stats st = empty_stats();
-            float m = kNegInf, my = kNegInf;
-            for (int j = 0; j < A; ++j) {
-                m = fmaxf(m, xr[j]);
-                if (KIND == kPolicyRef)
-                    my = fmaxf(my, yr[j]);
-            }
             st.m = m;
             st.my = my;
             m = m == kNegInf ? 0.0f : m;
             my = my == kNegInf ? 0.0f : my;
-            for (int j = 0; j < A; ++j)
-                add_entry<KIND>(st, xr[j], KIND == kPolicyRef ? yr[j] : 0.0f, m, my, c);
-            counts = counts && st.s != 0.0f;
+#pragma unroll
+            for (int q = 0; q <= kLaneMost; q += 4) {
+                if (q >= A)
+                    break;
+#pragma unroll
+                for (int j = q; j < q + 4; ++j)
+                    add_entry<KIND>(st, x[j], KIND == kPolicyRef ? y[j] : 0.0f, m, my, c);
+            }
             RowGrad g{};
+            PolicyRow pr{0, 0.0f, false};
+            bool counts;
+            float ts = 0.0f;   // distillation: sum of the teacher's exponentials
             if (KIND != kDistill) {
+                pr = policy_row(a, row);
+                counts = pr.counts && st.s != 0.0f;
                 PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
                 if (counts) {
-                    o = policy_finish<KIND>(a, row, w, st, xr[pr.action], g);
-                    total += (double)w * o.loss;
+                    o = policy_finish<KIND>(a, row, pr.w, st, xr[pr.action], g);
+                    total += (double)pr.w * o.loss;
                 }
                 store_policy(a, row, o);
             } else {
-                // the teacher's softmax over the entries that count
                 const float T = a.temperature;
-                float tm = kNegInf, ts = 0.0f, loss = 0.0f;
-                for (int k = 0; k < a.top; ++k)
-                    if (list_index(a, row, k) >= 0)
-                        tm = fmaxf(tm, a.val[row * a.top + k]);
-                const float tm0 = tm == kNegInf ? 0.0f : tm;
-                for (int k = 0; k < a.top; ++k)
-                    if (list_index(a, row, k) >= 0)
-                        ts += exp2_hw((a.val[row * a.top + k] - tm0) * c);
-                counts = counts && ts != 0.0f;
-                if (counts) {
-                    const float ln_ts = logf(ts), ln_s = logf(st.s);
-                    for (int k = 0; k < a.top; ++k) {
-                        const int i = list_index(a, row, k);
-                        if (i < 0)
-                            continue;
-                        const float b = (a.val[row * a.top + k] - tm0) / T;
-                        const float p = exp2_hw((a.val[row * a.top + k] - tm0) * c) / ts;
-                        if (p != 0.0f)
-                            loss += p * ((b - ln_ts) - ((xr[i] - m) / T - ln_s));
+                pr.w = a.weight ? a.weight[row] : a.row_weight;
+                const float* v = bv + lane * ldt;
+                const float* ix = bi + lane * ldt;
+                float tm = kNegInf;
+                for (int j = 0; j < A; ++j)
+                    yr[j] = 0.0f;
+                // an entry counts if the mask left its logit's place (-inf logits that are
+                // legal count: the loss is then infinite)
+                auto index = [&](int k) {
+                    const int i = (int)__float_as_uint(ix[k]);
+                    const bool ok = i >= 0 && i < A && (!mask || mask[lane * a.mask_ld + i] != 0);
+                    return ok ? i : -1;
+                };
+                for (int k = 0; k < top; ++k)
+                    if (index(k) >= 0)
+                        tm = fmaxf(tm, v[k]);
+                tm = tm == kNegInf ? 0.0f : tm;
+                float own = 0.0f, ce = 0.0f;   // sums of e b and e (x - m) over the list
+                for (int k = 0; k < top; ++k) {
+                    const int i = index(k);
+                    if (i < 0)
+                        continue;
+                    const float b = v[k] - tm, e = exp2_hw(b * c);
+                    ts += e;
+                    yr[i] += e;
+                    if (e != 0.0f) {
+                        own = __builtin_fmaf(e, b, own);
+                        ce = __builtin_fmaf(e, xr[i] - m, ce);
                     }
-                    loss *= T * T;
-                    total += (double)w * loss;
+                }
+                counts = pr.w != 0.0f && st.s != 0.0f && ts != 0.0f;
+                float loss = 0.0f;
+                if (counts) {
+                    loss = T * T * ((own - ce) / (T * ts) + (logf(st.s) - logf(ts)));
+                    total += (double)pr.w * loss;
                     g.m = m;
-                    g.c0 = w * T / st.s;
+                    g.c0 = pr.w * T / st.s;
                 }
                 if (a.stats)
                     a.stats[row] = loss;
-                if (a.dlogits) {
-                    for (int j = 0; j < A; ++j)
-                        xr[j] = counts ? grad_entry<KIND>(g, xr[j], 0.0f, c) : 0.0f;
-                    if (counts)
-                        for (int k = 0; k < a.top; ++k) {
-                            const int i = list_index(a, row, k);
-                            if (i >= 0)
-                                xr[i] -= w * T *
-                                         (exp2_hw((a.val[row * a.top + k] - tm0) * c) / ts);
-                        }
-                }
             }
-            if (KIND != kDistill && a.dlogits) {
-                for (int j = 0; j < A; ++j)
-                    xr[j] = counts ? grad_entry<KIND>(g, xr[j], KIND == kPolicyRef ? yr[j] : 0.0f,
-                                                      c)
-                                   : 0.0f;
-                if (counts)
+            if (a.dlogits) {
+                const float wt = KIND == kDistill && counts ? pr.w * a.temperature / ts : 0.0f;
+#pragma unroll
+                for (int q = 0; q <= kLaneMost; q += 4) {
+                    if (q >= A)
+                        break;
+#pragma unroll
+                    for (int j = q; j < q + 4; ++j) {
+                        if (j < A) {
+                            float d = counts ? grad_entry<KIND>(
+                                                   g, x[j], KIND == kPolicyRef ? y[j] : 0.0f, c)
+                                             : 0.0f;
+                            if (KIND == kDistill && counts)
+                                d = __builtin_fmaf(-wt, yr[j], d);
+                            xr[j] = d;
+                        }
+                    }
+                }
+                if (KIND != kDistill && counts)
                     xr[pr.action] += g.at_action;
             }
         }
         wave_lds_sync();
         if (a.dlogits)
-            for (int i = lane; i < count; i += 64) {
-                const int r = i / A, j = i - r * A;
-                ((E*)a.dlogits)[(r0 + r) * a.dlogits_ld + j] = from_f32<E>(bx[r * ldw + j]);
-            }
+            rows_from_lds(bx, (E*)a.dlogits + r0 * a.dlogits_ld, a.dlogits_ld, n, A, lane);
     }
     if (a.total)
         store_total(a, block_sum<kLaneThreads>(total));
@@ -354,7 +509,7 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
 
 // ------------------------------------------------------- a group of lanes per row
 
-// T threads per row: lanes of one wavefront (T <= 64) or a workgroup.
+// T threads per row: neighbouring lanes of one wavefront (T <= 64) or a workgroup.
 template <int T>
 __device__ __forceinline__ void group_sync()
 {
@@ -364,123 +519,123 @@ __device__ __forceinline__ void group_sync()
         __syncthreads();
 }
 
-// Merge over the group; every thread gets the result.  `scratch`: LDS, T > 64 only.
+struct MaxOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct SumOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __uint_as_float(
+        __builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+
+// v combined over groups of N lanes (N a power of two up to 64), in every lane:
+// neighbours, pairs, then mirrored halves of 8 and 16 lanes (whose lanes are equal by
+// then), which need no LDS; the last two steps cross rows of 16 lanes.
+template <int N, typename Op>
+__device__ __forceinline__ float lanes_combine(float v, Op op)
+{
+    if constexpr (N >= 2)
+        v = op(v, dpp<0xB1>(v));     // quad_perm 1 0 3 2
+    if constexpr (N >= 4)
+        v = op(v, dpp<0x4E>(v));     // quad_perm 2 3 0 1
+    if constexpr (N >= 8)
+        v = op(v, dpp<0x141>(v));    // row_half_mirror
+    if constexpr (N >= 16)
+        v = op(v, dpp<0x140>(v));    // row_mirror
+    if constexpr (N >= 32)
+        v = op(v, __shfl_xor(v, 16));
+    if constexpr (N >= 64)
+        v = op(v, __shfl_xor(v, 32));
+    return v;
+}
+
+// n values combined over the group, in every thread, always in the same order.
+// T > 64: through half HALF (0 or 1) of `scratch`, with one barrier.  Calls use the
+// halves in turn: a thread writes a half again only after the barrier of the call
+// on the other half, by when all have read it.
+constexpr int kScratch = 16 * 4;   // floats of a half
+
+template <int T, int HALF, int NV, typename Op>
+__device__ __forceinline__ void group_combine(float (&v)[NV], Op op, float* scratch)
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        v[i] = lanes_combine<(T < 64 ? T : 64)>(v[i], op);
+    if constexpr (T > 64) {
+        constexpr int W = T / 64;
+        float* half = scratch + HALF * kScratch;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                half[(threadIdx.x >> 6) * NV + i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            v[i] = lanes_combine<W>(half[(threadIdx.x & (W - 1)) * NV + i], op);
+    }
+}
+
+// The group's parts of a row as one, in every thread: the common maxima first, then
+// each thread's sums rescaled to them.  `flag` (in LDS, set before the call) clears
+// `counts` where it is 0.
 template <int T, int KIND>
-__device__ __forceinline__ Stats group_merge(Stats st, float c, float* scratch)
+__device__ __forceinline__ Stats group_merge(const Stats& st, float c, float* scratch,
+                                             const int* flag, bool& counts)
 {
-#pragma unroll
-    for (int o = (T < 64 ? T : 64) / 2; o; o >>= 1) {
-        Stats b;
-        b.m = __shfl_xor(st.m, o);
-        b.s = __shfl_xor(st.s, o);
-        b.t = KIND != kDistill ? __shfl_xor(st.t, o) : 0.0f;
-        if (KIND == kPolicyRef) {
-            b.my = __shfl_xor(st.my, o);
-            b.sy = __shfl_xor(st.sy, o);
-            b.v = __shfl_xor(st.v, o);
-        }
-        st = merge<KIND>(st, b, c);
+    Stats r = empty_stats();
+    if constexpr (KIND == kPolicyRef) {
+        float mx[2] = {st.m, st.my};
+        group_combine<T, 0>(mx, MaxOp(), scratch);
+        r.m = mx[0];
+        r.my = mx[1];
+    } else {
+        float mx[1] = {st.m};
+        group_combine<T, 0>(mx, MaxOp(), scratch);
+        r.m = mx[0];
     }
-    if constexpr (T > 64) {
-        Stats* w = (Stats*)scratch;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0)
-            w[threadIdx.x >> 6] = st;
-        __syncthreads();
-        st = w[0];
-#pragma unroll
-        for (int i = 1; i < T / 64; ++i)
-            st = merge<KIND>(st, w[i], c);
+    if (flag)
+        counts = counts && *flag != 0;
+    const float d = st.s == 0.0f ? 0.0f : fmaxf((st.m - r.m) * c, kLeast);
+    const float k = exp2_hw(d);   // 0 at kLeast
+    if constexpr (KIND == kPolicyRef) {
+        const float f = st.my == kNegInf ? kNegInf : (st.my - r.my) * kLog2e;
+        float sum[4] = {st.s * k, k * (st.t + st.s * d), st.sy * exp2_hw(f),
+                        st.s == 0.0f || k == 0.0f ? 0.0f : k * (st.v + st.s * f)};
+        group_combine<T, 1>(sum, SumOp(), scratch);
+        r.s = sum[0];
+        r.t = sum[1];
+        r.sy = sum[2];
+        r.v = sum[3];
+    } else if constexpr (KIND == kPolicy) {
+        float sum[2] = {st.s * k, k * (st.t + st.s * d)};
+        group_combine<T, 1>(sum, SumOp(), scratch);
+        r.s = sum[0];
+        r.t = sum[1];
+    } else {
+        float sum[1] = {st.s * k};
+        group_combine<T, 1>(sum, SumOp(), scratch);
+        r.s = sum[0];
     }
-    return st;
+    return r;
 }
 
-template <int T>
-__device__ __forceinline__ float group_max(float v, float* scratch)
-{
-#pragma unroll
-    for (int o = (T < 64 ? T : 64) / 2; o; o >>= 1)
-        v = fmaxf(v, __shfl_xor(v, o));
-    if constexpr (T > 64) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0)
-            scratch[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = scratch[0];
-        for (int i = 1; i < T / 64; ++i)
-            v = fmaxf(v, scratch[i]);
-    }
-    return v;
-}
-
-template <int T>
-__device__ __forceinline__ float group_sum(float v, float* scratch)
-{
-#pragma unroll
-    for (int o = (T < 64 ? T : 64) / 2; o; o >>= 1)
-        v += __shfl_xor(v, o);
-    if constexpr (T > 64) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0)
-            scratch[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = scratch[0];
-        for (int i = 1; i < T / 64; ++i)
-            v += scratch[i];
-    }
-    return v;
-}
-
-constexpr uint32_t kNegInfBits = 0xFF800000u;
-
-// Raw chunk with -inf in the entries that do not exist or are not legal.
-template <typename E>
-__device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* mask)
-{
-    constexpr int CH = kChunk<E>;
-    u32x4 v = n > 0 ? load_chunk(p, n) : u32x4{0, 0, 0, 0};
-    uint32_t out = 0;   // bit i: entry i does not count
-    if (n < CH)
-        out = n > 0 ? (0xFFu << n) & 0xFFu : 0xFFu;
-    if (mask && n > 0) {
-        if (n >= CH) {
-            typedef uint32_t u32_any __attribute__((aligned(1)));
-            uint32_t b[CH / 4];
-#pragma unroll
-            for (int i = 0; i < CH / 4; ++i)
-                b[i] = ((const u32_any*)mask)[i];
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-                out |= ((b[i / 4] >> (8 * (i % 4))) & 0xFFu) == 0 ? 1u << i : 0u;
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-                if (i < n)
-                    out |= mask[i] == 0 ? 1u << i : 0u;
-        }
-    }
-    if (out) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-            if ((out >> i) & 1u) {
-                if constexpr (sizeof(E) == 4)
-                    v[i] = kNegInfBits;
-                else
-                    v[i >> 1] = (i & 1) ? (v[i >> 1] & 0xFFFFu) | kNegInfBits
-                                        : (v[i >> 1] & 0xFFFF0000u) | (kNegInfBits >> 16);
-            }
-    }
-    return v;
-}
-
-// The sums over C chunks that a thread holds.
+// The sums over the first `used` of C chunks that a thread holds.
 template <typename E, int KIND, int C>
-__device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y, float c)
+__device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y, int used,
+                                             float c)
 {
     constexpr int CH = kChunk<E>;
     Stats st = empty_stats();
 #pragma unroll
     for (int i = 0; i < C; ++i) {
+        if (i >= used)
+            break;
         float f[CH];
         unpack<E>(x[i], f);
 #pragma unroll
@@ -496,6 +651,8 @@ __device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y
     const float m = st.m == kNegInf ? 0.0f : st.m, my = st.my == kNegInf ? 0.0f : st.my;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
+        if (i >= used)
+            break;
         float f[CH], r[CH];
         unpack<E>(x[i], f);
         if (KIND == kPolicyRef)
@@ -538,78 +695,98 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const RowGrad& g, 
     store_chunk((E*)a.dlogits + row * a.dlogits_ld + j0, n, pack<E>(f));
 }
 
-// The teacher's list of a row: softmax over the entries that count into LDS (index
-// and probability; probability 0 and index -1 elsewhere).  Returns whether any
-// entry counts.
-template <int T>
-__device__ __forceinline__ bool load_list(const LossArgs& a, int64_t row, int lane, bool live_row,
-                                          int* li, float* lp, float* scratch, float c,
-                                          float& tm0, float& ts)
-{
-    float tm = kNegInf;
-    for (int k = lane; k < a.top; k += T) {
-        const int i = live_row ? list_index(a, row, k) : -1;
-        const float v = live_row ? a.val[row * a.top + k] : 0.0f;
-        li[k] = i;
-        lp[k] = v;
-        if (i >= 0)
-            tm = fmaxf(tm, v);
-    }
-    tm = group_max<T>(tm, scratch);
-    tm0 = tm == kNegInf ? 0.0f : tm;
-    float s = 0.0f;
-    for (int k = lane; k < a.top; k += T)
-        if (li[k] >= 0)
-            s += exp2_hw((lp[k] - tm0) * c);
-    ts = group_sum<T>(s, scratch);
-    return ts != 0.0f;
-}
+// The teacher's list of a row, handled by TL lanes (the row's own, or its first
+// wavefront): index (-1 where an entry does not count), probability and the
+// student's logit of each entry, in LDS.
+struct List {
+    int* i;
+    float *p, *x;
+    int top, padded;   // padded: top rounded up to 4
 
-// This lane's share of the list's part of the loss (before the factor T^2): sum of
-// t (ln t - ln q) over entries with t > 0.
-template <typename E, int T>
-__device__ __forceinline__ float list_loss(const LossArgs& a, int64_t row, int lane,
-                                           const int* li, const float* lp, float c, float tm0,
-                                           float ts, float m, float ln_s)
+    __device__ __forceinline__ List(void* lds, int slot, int top_)
+        : top(top_), padded((top_ + 3) & ~3)
+    {
+        i = (int*)lds + slot * padded * 3;
+        p = (float*)(i + padded);
+        x = p + padded;
+    }
+};
+constexpr int list_bytes(int top) { return ((top + 3) & ~3) * 12; }
+
+// Loads the list and forms the probabilities.  Returns whether any entry counts (in
+// the TL lanes).  `part`: this lane's sum of t ln t.
+template <typename E, int TL>
+__device__ __forceinline__ bool load_list(const LossArgs& a, const List& l, int64_t row, int lane,
+                                          bool live_row, float c, float& part)
 {
     const E* x = (const E*)a.logits + row * a.logits_ld;
-    const float ln_ts = logf(ts);
-    float loss = 0.0f;
-    for (int k = lane; k < a.top; k += T) {
-        const int i = li[k];
-        if (i < 0)
-            continue;
-        const float b = lp[k] - tm0;
-        const float p = exp2_hw(b * c) / ts;
-        if (p != 0.0f)
-            loss += p * ((b / a.temperature - ln_ts) - ((to_f32(x[i]) - m) / a.temperature - ln_s));
+    float tm = kNegInf;
+    for (int k = lane; k < l.padded; k += TL) {
+        const int i = live_row && k < l.top ? list_index(a, row, k) : -1;
+        const float v = i >= 0 ? a.val[row * a.top + k] : kNegInf;
+        l.i[k] = i;
+        l.p[k] = v;
+        l.x[k] = i >= 0 ? to_f32(x[i]) : 0.0f;
+        tm = i >= 0 ? fmaxf(tm, v) : tm;
     }
-    return loss;
+    tm = lanes_combine<TL>(tm, MaxOp());
+    tm = tm == kNegInf ? 0.0f : tm;
+    float s = 0.0f;
+    for (int k = lane; k < l.padded; k += TL)
+        if (l.i[k] >= 0)
+            s += exp2_hw((l.p[k] - tm) * c);
+    s = lanes_combine<TL>(s, SumOp());
+    const float inv = 1.0f / s, ln_s = logf(s);
+    part = 0.0f;
+    for (int k = lane; k < l.padded; k += TL) {
+        const float b = l.p[k] - tm;
+        const float p = l.i[k] >= 0 ? exp2_hw(b * c) * inv : 0.0f;
+        l.p[k] = p;
+        if (p != 0.0f)
+            part = __builtin_fmaf(p, b / a.temperature - ln_s, part);
+    }
+    return s != 0.0f;
+}
+
+// The row's loss in the TL lanes, from load_list's part.
+template <int TL>
+__device__ __forceinline__ float list_loss(const LossArgs& a, const List& l, int lane, float part,
+                                           float m, float ln_s)
+{
+    for (int k = lane; k < l.padded; k += TL)
+        if (l.p[k] != 0.0f)
+            part -= l.p[k] * ((l.x[k] - m) / a.temperature - ln_s);
+    return lanes_combine<TL>(part, SumOp()) * a.temperature * a.temperature;
 }
 
 // The entries' part of the gradient, over what write_grad left there: an index that
 // the list holds more than once is written by its first entry with the sum of all.
-template <typename E, int T>
-__device__ __forceinline__ void write_list(const LossArgs& a, const RowGrad& g, int64_t row,
-                                           int lane, const int* li, const float* lp, float c,
-                                           float tm0, float ts, float w, int j_lo, int j_hi)
+template <typename E, int TL>
+__device__ __forceinline__ void write_list(const LossArgs& a, const List& l, const RowGrad& g,
+                                           int64_t row, int lane, float c, float w, int j_lo,
+                                           int j_hi)
 {
-    const E* x = (const E*)a.logits + row * a.logits_ld;
     E* o = (E*)a.dlogits + row * a.dlogits_ld;
-    for (int k = lane; k < a.top; k += T) {
-        const int i = li[k];
+    for (int k = lane; k < l.top; k += TL) {
+        const int i = l.i[k];
         if (i < j_lo || i >= j_hi)
             continue;
-        bool first = true;
-        float p = 0.0f;
-        for (int q = 0; q < a.top; ++q)
-            if (li[q] == i) {
-                first = first && q >= k;
-                p += exp2_hw((lp[q] - tm0) * c) / ts;
-            }
-        if (first)
-            o[i] = from_f32<E>(grad_entry<kDistill>(g, to_f32(x[i]), 0.0f, c) -
-                               w * a.temperature * p);
+        int before = 0, after = 0;   // entries of the same index
+        for (int q = 0; q < l.padded; q += 4) {
+            const int4 e = *(const int4*)(l.i + q);
+            const int n0 = e.x == i, n1 = e.y == i, n2 = e.z == i, n3 = e.w == i;
+            before += (n0 & (q < k)) + (n1 & (q + 1 < k)) + (n2 & (q + 2 < k)) + (n3 & (q + 3 < k));
+            after += n0 + n1 + n2 + n3;
+        }
+        if (before)
+            continue;
+        float p = l.p[k];
+        if (after > 1) {
+            for (int q = k + 1; q < l.top; ++q)
+                if (l.i[q] == i)
+                    p += l.p[q];
+        }
+        o[i] = from_f32<E>(grad_entry<kDistill>(g, l.x[k], 0.0f, c) - w * a.temperature * p);
     }
 }
 
@@ -620,10 +797,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
     constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T;
     constexpr int CH = kChunk<E>;
     extern __shared__ float lds[];
-    __shared__ Stats scratch[T > 64 ? T / 64 : 1];
+    __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
-    int* li = (int*)lds + slot * a.top * 2;
-    float* lp = (float*)(li + a.top);
+    constexpr int TL = T < 64 ? T : 64;
+    const List list(lds, slot, KIND == kDistill ? a.top : 0);
+    __shared__ int any_entry;
+    const bool lists = KIND == kDistill && lane < TL;
     const float c = kLog2e / a.temperature;
     double total = 0.0;
     const int64_t tiles = (a.rows + ROWS - 1) / ROWS;
@@ -652,13 +831,23 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
             if (KIND == kPolicyRef)
                 y[i] = load_masked(py + j, n, pm ? pm + j : nullptr);
         }
-        float tm0 = 0.0f, ts = 1.0f;
-        if (KIND == kDistill) {
-            group_sync<T>();
-            const bool any = load_list<T>(a, row, lane, counts, li, lp, (float*)scratch, c, tm0, ts);
-            counts = counts && any;
+        const int used = (a.A + T * CH - 1) / (T * CH);   // chunks that any thread holds
+        float part = 0.0f;
+        if (lists) {
+            // (the group's other wavefronts learn from LDS whether the list counts: written
+            // before the barriers of the merge, read between them)
+            wave_lds_sync();
+            const bool any = load_list<E, TL>(a, list, row, lane, counts, c, part);
+            if (T > 64) {
+                if (lane == 0)
+                    any_entry = any;
+            } else {
+                counts = counts && any;
+            }
+            wave_lds_sync();
         }
-        Stats st = group_merge<T, KIND>(chunk_stats<E, KIND, C>(x, y, c), c, (float*)scratch);
+        Stats st = group_merge<T, KIND>(chunk_stats<E, KIND, C>(x, y, used, c), c, scratch,
+                                        KIND == kDistill && T > 64 ? &any_entry : nullptr, counts);
         counts = counts && st.s != 0.0f;
         RowGrad g{};
         if (KIND != kDistill) {
@@ -671,14 +860,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
                 store_policy(a, row, o);
             }
         } else {
-            float loss = 0.0f;
-            const float m = st.m == kNegInf ? 0.0f : st.m;
-            group_sync<T>();   // the list is whole
-            if (counts)
-                loss = list_loss<E, T>(a, row, lane, li, lp, c, tm0, ts, m, logf(st.s));
-            loss = group_sum<T>(loss, (float*)scratch) * a.temperature * a.temperature;
-            g.m = m;
+            g.m = st.m == kNegInf ? 0.0f : st.m;
             g.c0 = pr.w * a.temperature / st.s;
+            float loss = 0.0f;
+            if (lists)
+                loss = list_loss<TL>(a, list, lane, part, g.m, logf(st.s));
             if (live && lane == 0) {
                 if (counts)
                     total += (double)pr.w * loss;
@@ -687,6 +873,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
             }
         }
         if (a.dlogits && live) {
+            // (the raw chunks are what stays in registers, not their unpacked values)
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                asm volatile("" : "+v"(x[i]));
+                if (KIND == kPolicyRef)
+                    asm volatile("" : "+v"(y[i]));
+            }
 #pragma unroll
             for (int i = 0; i < C; ++i)
                 write_grad<E, KIND>(a, g, counts, row, pr.action, lane + i * T, x[i],
@@ -694,8 +887,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         }
         if (KIND == kDistill && a.dlogits) {
             group_sync<T>();
-            if (counts)
-                write_list<E, T>(a, g, row, lane, li, lp, c, tm0, ts, pr.w, 0, a.A);
+            if (counts && lists)
+                write_list<E, TL>(a, list, g, row, lane, c, pr.w, 0, a.A);
         }
     }
     if (a.total)
@@ -715,10 +908,11 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
 {
     constexpr int T = kLongThreads, U = kLongUnroll, CH = kChunk<E>;
     extern __shared__ float lds[];
-    __shared__ Stats scratch[T / 64];
+    __shared__ float scratch[2 * kScratch];
     const int tid = threadIdx.x;
-    int* li = (int*)lds;
-    float* lp = (float*)(li + a.top);
+    const List list(lds, 0, KIND == kDistill ? a.top : 0);
+    __shared__ int any_entry;
+    const bool lists = KIND == kDistill && tid < 64;
     const float c = kLog2e / a.temperature;
     double total = 0.0;
     const int64_t items = PHASE == 0 ? a.rows : a.rows * a.splits;
@@ -752,10 +946,10 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
                         if (KIND == kPolicyRef)
                             y[u] = load_masked(py + j, n, pm ? pm + j : nullptr);
                     }
-                    st = merge<KIND>(st, chunk_stats<E, KIND, U>(x, y, c), c);
+                    st = merge<KIND>(st, chunk_stats<E, KIND, U>(x, y, U, c), c);
                 }
             }
-            st = group_merge<T, KIND>(st, c, (float*)scratch);
+            st = group_merge<T, KIND>(st, c, scratch, nullptr, counts);
             if (PHASE == 1) {
                 if (tid == 0)
                     ((Stats*)a.part)[row * a.splits + part] = st;
@@ -765,11 +959,17 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
             for (int i = 0; i < a.splits; ++i)
                 st = merge<KIND>(st, ((const Stats*)a.part)[row * a.splits + i], c);
         }
-        float tm0 = 0.0f, ts = 1.0f;
+        float from_list = 0.0f;
         if (KIND == kDistill) {
+            __syncthreads();   // (the last row's flag has been read)
+            if (lists) {
+                const bool any = load_list<E, 64>(a, list, row, tid, counts, c, from_list);
+                if (tid == 0)
+                    any_entry = any;
+                wave_lds_sync();
+            }
             __syncthreads();
-            const bool any = load_list<T>(a, row, tid, counts, li, lp, (float*)scratch, c, tm0, ts);
-            counts = counts && any;
+            counts = counts && any_entry != 0;
         }
         counts = counts && st.s != 0.0f;
         RowGrad g{};
@@ -783,14 +983,11 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
                 store_policy(a, row, o);
             }
         } else {
-            float loss = 0.0f;
-            const float m = st.m == kNegInf ? 0.0f : st.m;
-            __syncthreads();
-            if (counts)
-                loss = list_loss<E, T>(a, row, tid, li, lp, c, tm0, ts, m, logf(st.s));
-            loss = group_sum<T>(loss, (float*)scratch) * a.temperature * a.temperature;
-            g.m = m;
+            g.m = st.m == kNegInf ? 0.0f : st.m;
             g.c0 = pr.w * a.temperature / st.s;
+            float loss = 0.0f;
+            if (lists)
+                loss = list_loss<64>(a, list, tid, from_list, g.m, logf(st.s));
             if (tid == 0 && part == 0) {
                 if (counts)
                     total += (double)pr.w * loss;
@@ -817,8 +1014,8 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
             }
             if (KIND == kDistill) {
                 __syncthreads();
-                if (counts)
-                    write_list<E, T>(a, g, row, tid, li, lp, c, tm0, ts, pr.w, q0 * CH, q1 * CH);
+                if (counts && lists)
+                    write_list<E, 64>(a, list, g, row, tid, c, pr.w, q0 * CH, q1 * CH);
             }
         }
     }
@@ -839,25 +1036,40 @@ __global__ __launch_bounds__(256) void loss_total_kernel(const double* part, int
 template <typename E, int KIND>
 hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
 {
-    const size_t list = KIND == kDistill ? (size_t)a.top * 8 : 0;
+    const size_t list = KIND == kDistill ? (size_t)list_bytes(a.top) : 0;
     const unsigned nb = (unsigned)p.blocks;
     switch (p.variant) {
     case kLossLane: {
-        const size_t lds = (size_t)kLaneThreads * (a.A | 1) * 4 * (KIND == kPolicyRef ? 2 : 1);
+        const size_t lds = (size_t)kLaneThreads * 4 * lane_floats(KIND, a.A, a.top);
         loss_lane_kernel<E, KIND><<<nb, kLaneThreads, lds, s>>>(a);
         break;
     }
-    case kLossRow16:
-        loss_row_kernel<E, KIND, 16, 2><<<nb, 256, list * 16, s>>>(a);
-        break;
-    case kLossRow64:
-        loss_row_kernel<E, KIND, 64, 4><<<nb, 256, list * 4, s>>>(a);
-        break;
-    case kLossRow256:
-        loss_row_kernel<E, KIND, 256, 4><<<nb, 256, list, s>>>(a);
-        break;
-    case kLossRow1024:
-        loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list, s>>>(a);
+    case kLossRow:
+        switch (p.group) {
+        case 4:
+            loss_row_kernel<E, KIND, 4, 4><<<nb, 256, list * 64, s>>>(a);
+            break;
+        case 8:
+            loss_row_kernel<E, KIND, 8, 4><<<nb, 256, list * 32, s>>>(a);
+            break;
+        case 16:
+            loss_row_kernel<E, KIND, 16, 4><<<nb, 256, list * 16, s>>>(a);
+            break;
+        case 32:
+            loss_row_kernel<E, KIND, 32, 4><<<nb, 256, list * 8, s>>>(a);
+            break;
+        case 64:
+            loss_row_kernel<E, KIND, 64, 4><<<nb, 256, list * 4, s>>>(a);
+            break;
+        case 256:
+            loss_row_kernel<E, KIND, 256, 4><<<nb, 256, list, s>>>(a);
+            break;
+        case 512:
+            loss_row_kernel<E, KIND, 512, 4><<<nb, 512, list, s>>>(a);
+            break;
+        default:
+            loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list, s>>>(a);
+        }
         break;
     case kLossLong:
         loss_long_kernel<E, KIND, 0><<<nb, kLongThreads, list, s>>>(a);
@@ -877,7 +1089,7 @@ __global__ void zero_total_kernel(float* total) { *total = 0.0f; }
 
 }  // namespace
 
-LossPlan loss_plan(int64_t rows, int64_t A, int size)
+LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
 {
     constexpr int64_t kCus = 256;
     LossPlan p{};
@@ -885,19 +1097,17 @@ LossPlan loss_plan(int64_t rows, int64_t A, int size)
     p.splits = 1;
     int64_t per = 1;   // rows per workgroup
     int64_t most = 2048;
-    if (A < 32) {   // two buffers of 256 rows of 31 fit 64 KB of LDS
+    // (the rows of a workgroup fit 64 KB of LDS)
+    if (A <= kLaneMost && (top == 0 || (top <= 32 && lane_floats(kDistill, (int)A, top) <= 64))) {
         p.variant = kLossLane;
         per = kLaneThreads;
-    } else if (A <= 16 * 2 * ch) {
-        p.variant = kLossRow16;
-        per = 16;
-    } else if (A <= 64 * 4 * ch) {
-        p.variant = kLossRow64;
-        per = 4;
-    } else if (A <= 256 * 4 * ch) {
-        p.variant = kLossRow256;
-    } else if (A <= 1024 * 4 * ch && rows >= kCus / 2) {
-        p.variant = kLossRow1024;
+    } else if (A <= 256 * 4 * ch || (A <= 1024 * 4 * ch && rows >= kCus / 2)) {
+        p.variant = kLossRow;
+        p.group = 4;
+        // at most 8 entries of a teacher's list per lane
+        while (p.group * 4 * ch < A || (p.group < 64 && p.group * 8 < top))
+            p.group *= p.group == 64 ? 4 : 2;
+        per = std::max(1, 256 / p.group);
     } else {
         p.variant = kLossLong;
         const int64_t chunks = (A + ch - 1) / ch;
