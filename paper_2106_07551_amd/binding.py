@@ -6,6 +6,8 @@ call goes straight to the C ABI of ``include/malib.h``; names follow it.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import struct
 import sys
 import os
 from typing import Optional, Sequence
@@ -166,16 +168,16 @@ def lib():
         L.malib_pop_set_graph.restype = i32
         L.malib_pop_policy_ids.argtypes = [vp, vp, i32, C.POINTER(i32)]
         L.malib_pop_policy_ids.restype = i32
-        mp, lp = C.POINTER(Mat), C.POINTER(LinearDesc)
-        L.malib_linear.argtypes = [lp, mp, mp, vp, mp, mp, mp, vp, i64, vp]
+        # (descriptions as packed bytes or by reference)
+        L.malib_linear.argtypes = [vp] * 8 + [i64, vp]
         L.malib_linear.restype = i32
-        L.malib_linear_backward.argtypes = [lp, mp, mp, mp, mp, mp, mp, vp, vp, i64, vp]
+        L.malib_linear_backward.argtypes = [vp] * 9 + [i64, vp]
         L.malib_linear_backward.restype = i32
-        L.malib_linear_work.argtypes = [lp, i32, C.POINTER(i64)]
+        L.malib_linear_work.argtypes = [vp, i32, C.POINTER(i64)]
         L.malib_linear_work.restype = i32
-        L.malib_policy_loss.argtypes = [C.POINTER(PolicyLossDesc)] + [vp] * 12 + [i64, vp]
+        L.malib_policy_loss.argtypes = [vp] * 13 + [i64, vp]
         L.malib_policy_loss.restype = i32
-        L.malib_distill_loss.argtypes = [C.POINTER(DistillDesc)] + [vp] * 9 + [i64, vp]
+        L.malib_distill_loss.argtypes = [vp] * 10 + [i64, vp]
         L.malib_distill_loss.restype = i32
         L.malib_loss_work.argtypes = [i32, i64, i64, C.POINTER(i64)]
         L.malib_loss_work.restype = i32
@@ -680,6 +682,16 @@ def meta_sample_device(sigma, n_policies: int, n_envs: int, n_agents: int, seed:
 
 
 # ------------------------------------------------------------ learner operators
+#
+# These are called once per layer and step, often on small batches where the host's
+# share is the time: descriptions are packed into bytes (a tenth of a ctypes
+# structure's time), and checks name what they found only once one has failed.
+
+_MAT = struct.Struct("@Pqq")                  # malib_mat
+_LINEAR = struct.Struct("@iiqqqq")            # malib_linear_desc
+_POLICY_LOSS = struct.Struct("@iiqqqqqqffff")  # malib_policy_loss_desc
+_DISTILL = struct.Struct("@iiqqqqqf4x")        # malib_distill_desc
+
 
 def _empty(shape, dtype, device, stream):
     """A tensor from the memory pool of the stream the call runs on (the caching
@@ -693,67 +705,85 @@ def _empty(shape, dtype, device, stream):
 
 def _dtype_code(t, what):
     import torch
-    if t.dtype == torch.float32:
-        return DT_F32
-    if t.dtype == torch.bfloat16:
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return DT_BF16
-    raise ArgumentError(f"{what}: expected dtype float32 or bfloat16, got {t.dtype}")
+    if dt is torch.float32:
+        return DT_F32
+    raise ArgumentError(f"{what}: expected dtype float32 or bfloat16, got {dt}")
 
 
-def _mat(t, dtype, shape, what, out: bool = False):
-    """A malib_mat over a tensor [rows][cols] or [groups][rows][cols] whose rows
-    are contiguous; `shape` is (groups, rows, cols), groups None for one group.
-    An input without the group dimension is shared by the groups."""
+def _mat(t, dtype, G, rows, cols, what, out: bool = False):
+    """A malib_mat (packed) over a tensor [rows][cols] or [groups][rows][cols]
+    whose rows are contiguous; G is None without the group dimension.  An input
+    without it is shared by the groups."""
     if t is None:
         return None
-    G, rows, cols = shape
-    want = (rows, cols) if G is None else (G, rows, cols)
-    shared = not out and G is not None and t.dim() == 2
-    if tuple(t.shape) != ((rows, cols) if shared else want):
-        raise ArgumentError(f"{what}: expected shape {want}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
+    shape = t.shape
+    shared = G is not None and not out and len(shape) == 2
+    want = (rows, cols) if G is None or shared else (G, rows, cols)
+    if shape != want:
+        raise ArgumentError(f"{what}: expected shape {want}, got {tuple(shape)}")
+    if t.dtype is not dtype:
         raise ArgumentError(f"{what}: expected dtype {dtype}, got {t.dtype}")
-    if cols > 1 and t.stride(-1) != 1:
-        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {t.stride(-1)}")
-    row = t.stride(-2) if rows > 1 else cols
-    group = 0 if G is None or shared else t.stride(0) if G > 1 else rows * row
-    return Mat(t.data_ptr(), row, group)
+    st = t.stride()
+    if st[-1] != 1 and cols > 1:
+        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {st[-1]}")
+    row = st[-2] if rows > 1 else cols
+    group = 0 if G is None or shared else st[0] if G > 1 else rows * row
+    return _MAT.pack(t.data_ptr(), row, group)
 
 
-def _on_device(*named):
-    for t, what in named:
-        if t is not None and not t.is_cuda:
-            raise ArgumentError(f"{what}: expected a device tensor, got one on {t.device}")
+def _on_device(names, *tensors):
+    for t, what in zip(names.split(), tensors):
+        if what is not None and not what.is_cuda:
+            raise ArgumentError(f"{t}: expected a device tensor, got one on {what.device}")
 
 
-def _layer(x_like, w, act):
+def _layer(x, w, act):
     """(groups or None, out, in) of a layer from its weight, and its checks."""
-    if w.dim() not in (2, 3):
+    shape, nx = w.shape, x.dim()
+    n = len(shape)
+    if n != 2 and n != 3:
         raise ArgumentError(f"w: expected [out][in] or [groups][out][in], got shape "
-                            f"{tuple(w.shape)}")
-    if x_like.dim() not in (2, 3) or x_like.dim() > w.dim():
+                            f"{tuple(shape)}")
+    if nx != n and (nx != 2 or n != 3):
         raise ArgumentError(f"x: expected [rows][in] or, with weights per group, "
-                            f"[groups][rows][in], got shape {tuple(x_like.shape)}")
+                            f"[groups][rows][in], got shape {tuple(x.shape)}")
     if act not in (ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU):
         raise ArgumentError(f"act: unknown activation {act!r}")
-    G = w.shape[0] if w.dim() == 3 else None
-    return G, w.shape[-2], w.shape[-1]
+    return shape[0] if n == 3 else None, shape[-2], shape[-1]
 
 
-def _work(desc, backward, work, device, stream):
-    """The workspace a call needs (allocated unless the caller's is given)."""
-    import torch
+@functools.lru_cache(maxsize=4096)
+def _linear_work(desc, backward):
     need = C.c_int64()
-    _check(lib().malib_linear_work(C.byref(desc), backward, C.byref(need)))
-    if work is None and need.value:
-        work = _empty(need.value, torch.uint8, device, stream)
+    _check(lib().malib_linear_work(desc, backward, C.byref(need)))
+    return need.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _loss_work(code, n, a):
+    need = C.c_int64()
+    _check(lib().malib_loss_work(code, n, a, C.byref(need)))
+    return need.value
+
+
+def _workspace(need, work, device, stream):
+    """(address, bytes, tensor) of a call's workspace, allocated unless the
+    caller's is given."""
+    import torch
     if work is not None:
-        _dbytes(work, need.value, "work")
-    return work, 0 if work is None else work.numel() * work.element_size()
+        _dbytes(work, need, "work")
+        return work.data_ptr(), work.numel() * work.element_size(), work
+    if not need:
+        return None, 0, None
+    work = _empty(need, torch.uint8, device, stream)
+    return work.data_ptr(), need, work
 
 
-def _ref(m):
-    return None if m is None else C.byref(m)
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def linear(x, w, bias=None, *, act: int = ACT_NONE, residual=None, pre=None, out=None, work=None,
@@ -763,25 +793,22 @@ def linear(x, w, bias=None, *, act: int = ACT_NONE, residual=None, pre=None, out
     group dimension is shared by the groups); float32 or bfloat16, bias
     float32.  `pre` receives the values before the activation, which
     linear_backward needs.  Returns [..][rows][out]."""
-    import torch
     code = _dtype_code(x, "x")
     G, n_out, n_in = _layer(x, w, act)
     rows, dt = x.shape[-2], x.dtype
-    full = (rows, n_out) if G is None else (G, rows, n_out)
-    mx = _mat(x, dt, (G, rows, n_in), "x")
-    mw = _mat(w, dt, (G, n_out, n_in), "w")
-    mr = _mat(residual, dt, (G, rows, n_out), "residual")
-    mp = _mat(pre, dt, (G, rows, n_out), "pre", True)
-    _check_buf(bias, torch.float32, n_out * (G or 1), False, "bias")
-    _on_device((x, "x"), (w, "w"), (bias, "bias"), (residual, "residual"), (pre, "pre"),
-               (out, "out"))
+    mx = _mat(x, dt, G, rows, n_in, "x")
+    mw = _mat(w, dt, G, n_out, n_in, "w")
+    mr = _mat(residual, dt, G, rows, n_out, "residual")
+    mp = _mat(pre, dt, G, rows, n_out, "pre", True)
+    if bias is not None:
+        _check_buf(bias, _f32(), n_out * (G or 1), False, "bias")
+    _on_device("x w bias residual pre out", x, w, bias, residual, pre, out)
     if out is None:
-        out = _empty(full, dt, x.device, stream)
-    my = _mat(out, dt, (G, rows, n_out), "out", True)
-    d = LinearDesc(code, act, G or 1, rows, n_in, n_out)
-    work, nbytes = _work(d, 0, work, x.device, stream)
-    _check(lib().malib_linear(C.byref(d), C.byref(mx), C.byref(mw), _dptr(bias), _ref(mr),
-                              _ref(mp), C.byref(my), _dptr(work), nbytes, _stream(stream)))
+        out = _empty((rows, n_out) if G is None else (G, rows, n_out), dt, x.device, stream)
+    my = _mat(out, dt, G, rows, n_out, "out", True)
+    d = _LINEAR.pack(code, act, G or 1, rows, n_in, n_out)
+    wp, nbytes, work = _workspace(_linear_work(d, 0), work, x.device, stream)
+    _check(lib().malib_linear(d, mx, mw, _ptr(bias), mr, mp, my, wp, nbytes, _stream(stream)))
     return out
 
 
@@ -791,78 +818,74 @@ def linear_backward(dy, x, w, *, act: int = ACT_NONE, pre=None, want=(True, True
     its output; `pre` is what linear wrote there (needed with an activation).
     `want` leaves outputs out (None is returned for them).  The residual's
     gradient is dy."""
-    import torch
     code = _dtype_code(dy, "dy")
     G, n_out, n_in = _layer(dy, w, act)
-    rows, dt = dy.shape[-2], dy.dtype
+    rows, dt, dev = dy.shape[-2], dy.dtype, dy.device
     lead = () if G is None else (G,)
-    mdy = _mat(dy, dt, (G, rows, n_out), "dy")
-    mx = _mat(x, dt, (G, rows, n_in), "x")
-    mw = _mat(w, dt, (G, n_out, n_in), "w")
-    mp = _mat(pre, dt, (G, rows, n_out), "pre") if act != ACT_NONE else None
-    if act != ACT_NONE and pre is None:
+    mdy = _mat(dy, dt, G, rows, n_out, "dy")
+    mx = _mat(x, dt, G, rows, n_in, "x")
+    mw = _mat(w, dt, G, n_out, n_in, "w")
+    if act == ACT_NONE:
+        mp = None
+    elif pre is None:
         raise ArgumentError("pre: the backward pass of an activation needs the values before it")
-    _on_device((dy, "dy"), (x, "x"), (w, "w"), (pre, "pre"), (dx, "dx"), (dw, "dw"),
-               (dbias, "dbias"))
-    if want[0] and dx is None:
-        dx = _empty(lead + (rows, n_in), dt, dy.device, stream)
-    if want[1] and dw is None:
-        dw = _empty(lead + (n_out, n_in), dt, dy.device, stream)
-    if want[2] and dbias is None:
-        dbias = _empty(lead + (n_out,), torch.float32, dy.device, stream)
-    dx, dw, dbias = (t if ok else None for t, ok in zip((dx, dw, dbias), want))
-    mdx = _mat(dx, dt, (G, rows, n_in), "dx", True)
-    mdw = _mat(dw, dt, (G, n_out, n_in), "dw", True)
-    _check_buf(dbias, torch.float32, n_out * (G or 1), False, "dbias")
-    d = LinearDesc(code, act, G or 1, rows, n_in, n_out)
-    work, nbytes = _work(d, 1, work, dy.device, stream)
-    _check(lib().malib_linear_backward(
-        C.byref(d), C.byref(mdy), _ref(mx), C.byref(mw), _ref(mp), _ref(mdx), _ref(mdw),
-        _dptr(dbias), _dptr(work), nbytes, _stream(stream)))
+    else:
+        mp = _mat(pre, dt, G, rows, n_out, "pre")
+    _on_device("dy x w pre dx dw dbias", dy, x, w, pre, dx, dw, dbias)
+    if not want[0]:
+        dx = None
+    elif dx is None:
+        dx = _empty(lead + (rows, n_in), dt, dev, stream)
+    if not want[1]:
+        dw = None
+    elif dw is None:
+        dw = _empty(lead + (n_out, n_in), dt, dev, stream)
+    if not want[2]:
+        dbias = None
+    elif dbias is None:
+        dbias = _empty(lead + (n_out,), _f32(), dev, stream)
+    else:
+        _check_buf(dbias, _f32(), n_out * (G or 1), False, "dbias")
+    mdx = _mat(dx, dt, G, rows, n_in, "dx", True)
+    mdw = _mat(dw, dt, G, n_out, n_in, "dw", True)
+    d = _LINEAR.pack(code, act, G or 1, rows, n_in, n_out)
+    wp, nbytes, work = _workspace(_linear_work(d, 1), work, dev, stream)
+    _check(lib().malib_linear_backward(d, mdy, mx, mw, mp, mdx, mdw, _ptr(dbias), wp, nbytes,
+                                       _stream(stream)))
     return dx, dw, dbias
 
 
-def _rows(t, dtype, shape, what) -> int:
-    """Row stride of a tensor [rows][n] whose rows are contiguous, checked."""
+def _rows(t, dtypes, n, a, what) -> int:
+    """Row stride of a tensor [n][a] whose rows are contiguous, checked."""
     if t is None:
         return 0
-    if tuple(t.shape) != tuple(shape):
-        raise ArgumentError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
-        raise ArgumentError(f"{what}: expected dtype {dtype}, got {t.dtype}")
-    if shape[1] > 1 and t.stride(1) != 1:
-        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {t.stride(1)}")
-    return t.stride(0) if shape[0] > 1 else shape[1]
+    if t.shape != (n, a):
+        raise ArgumentError(f"{what}: expected shape {(n, a)}, got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise ArgumentError(f"{what}: expected dtype {' or '.join(map(str, dtypes))}, got "
+                            f"{t.dtype}")
+    st = t.stride()
+    if st[1] != 1 and a > 1:
+        raise ArgumentError(f"{what}: expected contiguous rows, got column stride {st[1]}")
+    return st[0] if n > 1 else a
 
 
 def _loss_args(logits, mask, weight, dlogits):
     """What both losses check: (rows, n_actions, dtype code, strides of logits,
     dlogits and mask)."""
     import torch
-    if logits.dim() != 2 or logits.shape[1] < 1:
-        raise ArgumentError(f"logits: expected [rows][n_actions], got shape {tuple(logits.shape)}")
+    shape = logits.shape
+    if len(shape) != 2 or shape[1] < 1:
+        raise ArgumentError(f"logits: expected [rows][n_actions], got shape {tuple(shape)}")
     code = _dtype_code(logits, "logits")
-    n, a = logits.shape
-    sl = _rows(logits, logits.dtype, (n, a), "logits")
-    sm = _rows(mask, (torch.bool, torch.uint8), (n, a), "mask")
-    sd = _rows(dlogits, logits.dtype, (n, a), "dlogits")
-    _check_buf(weight, torch.float32, n, False, "weight")
+    n, a = shape
+    dts = (logits.dtype,)
+    sl = _rows(logits, dts, n, a, "logits")
+    sm = _rows(mask, (torch.bool, torch.uint8), n, a, "mask")
+    sd = _rows(dlogits, dts, n, a, "dlogits")
+    if weight is not None:
+        _check_buf(weight, torch.float32, n, False, "weight")
     return n, a, code, sl, sd, sm
-
-
-def _loss_work(code, n, a, work, device, stream):
-    import torch
-    need = C.c_int64()
-    _check(lib().malib_loss_work(code, n, a, C.byref(need)))
-    if work is None and need.value:
-        work = _empty(need.value, torch.uint8, device, stream)
-    if work is not None:
-        _dbytes(work, need.value, "work")
-    return work, 0 if work is None else work.numel() * work.element_size()
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
 
 
 def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
@@ -880,16 +903,16 @@ def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
     f32 = torch.float32
     if actions.dtype not in (torch.uint8, torch.int32, torch.int64):
         raise ArgumentError(f"actions: expected dtype uint8, int32 or int64, got {actions.dtype}")
-    sr = _rows(ref_logits, logits.dtype, (n, a), "ref_logits")
-    for t, dt, what in ((actions, actions.dtype, "actions"), (old_logp, f32, "old_logp"),
-                        (advantage, f32, "advantage"), (ref_logp, f32, "ref_logp")):
-        _check_buf(t, dt, n, False, what)
+    sr = _rows(ref_logits, (logits.dtype,), n, a, "ref_logits")
+    _check_buf(actions, None, n, False, "actions")
+    _check_buf(old_logp, f32, n, False, "old_logp")
+    _check_buf(advantage, f32, n, False, "advantage")
+    _check_buf(ref_logp, f32, n, False, "ref_logp")
     _check_buf(total, f32, 1, False, "total")
     _check_buf(stats, f32, 4 * n, False, "stats")
-    _on_device((logits, "logits"), (actions, "actions"), (old_logp, "old_logp"),
-               (advantage, "advantage"), (ref_logp, "ref_logp"), (ref_logits, "ref_logits"),
-               (mask, "mask"), (weight, "weight"), (total, "total"), (stats, "stats"),
-               (dlogits, "dlogits"), (work, "work"))
+    _on_device("logits actions old_logp advantage ref_logp ref_logits mask weight total stats "
+               "dlogits", logits, actions, old_logp, advantage, ref_logp, ref_logits, mask, weight,
+               total, stats, dlogits)
     dev = logits.device
     if total is None:
         total = _empty(1, f32, dev, stream)
@@ -899,13 +922,13 @@ def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
         dlogits = None
     elif dlogits is None:
         dlogits, sd = _empty((n, a), logits.dtype, dev, stream), a
-    work, nbytes = _loss_work(code, n, a, work, dev, stream)
-    d = PolicyLossDesc(code, actions.element_size(), n, a, sl, sr, sd, sm, clip_low, clip_high,
-                       kl_coef, entropy_coef)
+    wp, nbytes, work = _workspace(_loss_work(code, n, a), work, dev, stream)
+    d = _POLICY_LOSS.pack(code, actions.element_size(), n, a, sl, sr, sd, sm, clip_low, clip_high,
+                          kl_coef, entropy_coef)
     _check(lib().malib_policy_loss(
-        C.byref(d), _ptr(logits), _ptr(actions), _ptr(old_logp), _ptr(advantage), _ptr(ref_logp),
-        _ptr(ref_logits), _ptr(mask), _ptr(weight), _ptr(total), _ptr(stats), _ptr(dlogits),
-        _ptr(work), nbytes, _stream(stream)))
+        d, logits.data_ptr(), actions.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(),
+        _ptr(ref_logp), _ptr(ref_logits), _ptr(mask), _ptr(weight), total.data_ptr(),
+        stats.data_ptr(), _ptr(dlogits), wp, nbytes, _stream(stream)))
     return total, stats, dlogits
 
 
@@ -927,9 +950,8 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
     _check_buf(teacher_logits, f32, n * top, False, "teacher_logits")
     _check_buf(total, f32, 1, False, "total")
     _check_buf(loss, f32, n, False, "loss")
-    _on_device((logits, "logits"), (teacher_idx, "teacher_idx"),
-               (teacher_logits, "teacher_logits"), (mask, "mask"), (weight, "weight"),
-               (total, "total"), (loss, "loss"), (dlogits, "dlogits"), (work, "work"))
+    _on_device("logits teacher_idx teacher_logits mask weight total loss dlogits", logits,
+               teacher_idx, teacher_logits, mask, weight, total, loss, dlogits)
     dev = logits.device
     if total is None:
         total = _empty(1, f32, dev, stream)
@@ -939,11 +961,11 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
         dlogits = None
     elif dlogits is None:
         dlogits, sd = _empty((n, a), logits.dtype, dev, stream), a
-    work, nbytes = _loss_work(code, n, a, work, dev, stream)
-    d = DistillDesc(code, top, n, a, sl, sd, sm, temperature)
+    wp, nbytes, work = _workspace(_loss_work(code, n, a), work, dev, stream)
+    d = _DISTILL.pack(code, top, n, a, sl, sd, sm, temperature)
     _check(lib().malib_distill_loss(
-        C.byref(d), _ptr(logits), _ptr(teacher_idx), _ptr(teacher_logits), _ptr(mask),
-        _ptr(weight), _ptr(total), _ptr(loss), _ptr(dlogits), _ptr(work), nbytes,
+        d, logits.data_ptr(), teacher_idx.data_ptr(), teacher_logits.data_ptr(), _ptr(mask),
+        _ptr(weight), total.data_ptr(), loss.data_ptr(), _ptr(dlogits), wp, nbytes,
         _stream(stream)))
     return total, loss, dlogits
 

@@ -22,6 +22,8 @@ namespace malib {
 
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 enum { kPolicy, kPolicyRef, kDistill };   // template KIND
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -264,12 +266,15 @@ __device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* m
 
 // ------------------------------------------------- few actions: a lane per row
 
-// 64 rows per wavefront, up to kLaneMost entries each: rows go through LDS (row
-// stride odd, so that lanes that read the same column of neighbouring rows fall
-// into different banks), so that memory is read and written in its own order,
-// 16 bytes per lane where rows follow each other without gaps, while each lane
-// works on a row alone in registers: no reductions, and a row's scalar work is
-// not repeated by other lanes.
+// 64 rows per wavefront, up to kLaneMost entries each: rows go through LDS as one run
+// of values, so that memory is read and written in its own order, 16 bytes per
+// lane where rows follow each other without gaps, while each lane works on a row
+// alone in registers: no reductions, and a row's scalar work is not repeated by
+// other lanes.  A lane moves its row in the widest pieces that rows are aligned
+// to: pieces of neighbouring rows then fall into different banks unless A is a
+// multiple of 8 (up to 4 lanes per bank at 16).  (Rows padded to an odd stride
+// instead, their places found element by element: 105 us against 94 us for 2^21
+// rows of 18.)
 constexpr int kLaneThreads = 256, kLaneRows = 64, kLaneMost = 31;
 
 // i / w for i < 2048, w <= 32
@@ -282,27 +287,28 @@ struct SmallDiv {
     }
 };
 
-// n rows of w values (rows ld apart) into LDS rows of w | 1; -inf where the mask
-// excludes an entry.
-template <typename E>
+// n rows of w values (rows ld apart) into LDS, value j of row r at r * w + j, or at
+// r * (w + 1) + j with PAD; -inf where the mask excludes an entry.
+template <bool PAD, typename E>
 __device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const uint8_t* mask,
                                             int64_t mask_ld, int n, int w, float* to, int lane)
 {
     constexpr int CH = kChunk<E>;
-    const int ldw = w | 1, count = n * w;
+    const int count = n * w;
     const SmallDiv div(w);
     if (ld == w && (!mask || mask_ld == w)) {
         for (int i = lane * CH; i < count; i += 64 * CH) {
             float v[CH];
             unpack<E>(load_masked(p + i, count - i, mask ? mask + i : nullptr), v);
-            int r = div(i), j = i - r * w;
+            if (!PAD && i + CH <= count) {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                if (i + e < count)
-                    to[r * ldw + j] = v[e];
-                const bool wrap = j + 1 == w;
-                r += wrap;
-                j = wrap ? 0 : j + 1;
+                for (int e = 0; e < CH; e += 4)
+                    *(f32x4*)(to + i + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    if (i + e < count)
+                        to[i + e + (PAD ? div(i + e) : 0)] = v[e];
             }
         }
         return;
@@ -311,7 +317,7 @@ __device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const uint8_
         const int r = div(i), j = i - r * w;
         const bool legal = !mask || mask[r * mask_ld + j] != 0;
         const float v = to_f32(p[r * ld + j]);
-        to[r * ldw + j] = legal ? v : kNegInf;
+        to[i + (PAD ? r : 0)] = legal ? v : kNegInf;
     }
 }
 
@@ -320,26 +326,96 @@ __device__ __forceinline__ void rows_from_lds(const float* from, E* p, int64_t l
                                               int lane)
 {
     constexpr int CH = kChunk<E>;
-    const int ldw = w | 1, count = n * w;
-    const SmallDiv div(w);
+    const int count = n * w;
     if (ld == w) {
         for (int i = lane * CH; i < count; i += 64 * CH) {
             float v[CH];
-            int r = div(i), j = i - r * w;
+            if (i + CH <= count) {
 #pragma unroll
-            for (int e = 0; e < CH; ++e) {
-                v[e] = i + e < count ? from[r * ldw + j] : 0.0f;
-                const bool wrap = j + 1 == w;
-                r += wrap;
-                j = wrap ? 0 : j + 1;
+                for (int e = 0; e < CH; e += 4) {
+                    const f32x4 q = *(const f32x4*)(from + i + e);
+                    v[e] = q[0];
+                    v[e + 1] = q[1];
+                    v[e + 2] = q[2];
+                    v[e + 3] = q[3];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    v[e] = i + e < count ? from[i + e] : 0.0f;
             }
             store_chunk(p + i, count - i, pack<E>(v));
         }
         return;
     }
+    const SmallDiv div(w);
     for (int i = lane; i < count; i += 64) {
         const int r = div(i), j = i - r * w;
-        p[r * ld + j] = from_f32<E>(from[r * ldw + j]);
+        p[r * ld + j] = from_f32<E>(from[i]);
+    }
+}
+
+// A lane's row of A <= NA values between LDS and registers, in pieces of W values
+// (A a multiple of W).
+template <int NA, int W>
+__device__ __forceinline__ void row_read(const float* p, int A, float (&x)[NA])
+{
+    typedef float piece __attribute__((ext_vector_type(W)));
+#pragma unroll
+    for (int j = 0; j < NA; j += W) {
+        if (j >= A)
+            break;
+        const piece q = *(const piece*)(p + j);
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            x[j + e] = q[e];
+    }
+}
+template <int NA, int W>
+__device__ __forceinline__ void row_write(float* p, int A, const float (&x)[NA])
+{
+    typedef float piece __attribute__((ext_vector_type(W)));
+#pragma unroll
+    for (int j = 0; j < NA; j += W) {
+        if (j >= A)
+            break;
+        piece q;
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            q[e] = x[j + e];
+        *(piece*)(p + j) = q;
+    }
+}
+template <int NA>
+__device__ __forceinline__ void row_read(const float* p, int A, float (&x)[NA])
+{
+    if (A % 4 == 0)
+        row_read<NA, 4>(p, A, x);
+    else if (A % 2 == 0)
+        row_read<NA, 2>(p, A, x);
+    else {
+#pragma unroll
+        for (int j = 0; j < NA; ++j) {
+            if (j >= A)
+                break;
+            x[j] = p[j];
+        }
+    }
+}
+template <int NA>
+__device__ __forceinline__ void row_write(float* p, int A, const float (&x)[NA])
+{
+    if (A % 4 == 0)
+        row_write<NA, 4>(p, A, x);
+    else if (A % 2 == 0)
+        row_write<NA, 2>(p, A, x);
+    else {
+#pragma unroll
+        for (int j = 0; j < NA; ++j) {
+            if (j >= A)
+                break;
+            p[j] = x[j];
+        }
     }
 }
 
@@ -347,18 +423,19 @@ __device__ __forceinline__ void rows_from_lds(const float* from, E* p, int64_t l
 // probabilities, the teacher's list.
 __host__ __device__ constexpr int lane_floats(int kind, int A, int top)
 {
-    return (A | 1) * (kind == kPolicy ? 1 : 2) + (kind == kDistill ? 2 * (top | 1) : 0);
+    return A * (kind == kPolicy ? 1 : 2) + (kind == kDistill ? 2 * (top + 1) : 0);
 }
 
-template <typename E, int KIND>
+// NA: entries in registers, A rounded up to 8
+template <typename E, int KIND, int NA>
 __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
 {
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int A = a.A, ldw = A | 1, top = KIND == kDistill ? a.top : 0, ldt = top | 1;
+    const int A = a.A, top = KIND == kDistill ? a.top : 0, ldt = top + 1;
     float* bx = lds + wave * kLaneRows * lane_floats(KIND, A, top);
-    float* by = bx + kLaneRows * ldw;
-    float* bv = by + kLaneRows * ldw;                  // distillation: the list's logits
+    float* by = bx + kLaneRows * A;
+    float* bv = by + kLaneRows * A;                  // distillation: the list's logits
     float* bi = bv + kLaneRows * ldt;                  // and indices (as floats' bits)
     const float c = kLog2e / a.temperature;
     double total = 0.0;
@@ -369,43 +446,41 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
         const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
         const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
         wave_lds_sync();
-        rows_to_lds((const E*)a.logits + r0 * a.logits_ld, a.logits_ld, mask, a.mask_ld, n, A, bx,
+        rows_to_lds<false>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld, mask, a.mask_ld, n, A, bx,
                     lane);
         if (KIND == kPolicyRef)
-            rows_to_lds((const E*)a.ref_logits + r0 * a.ref_ld, a.ref_ld, mask, a.mask_ld, n, A,
+            rows_to_lds<false>((const E*)a.ref_logits + r0 * a.ref_ld, a.ref_ld, mask, a.mask_ld, n, A,
                         by, lane);
         if (KIND == kDistill) {
-            rows_to_lds(a.val + r0 * top, top, nullptr, 0, n, top, bv, lane);
-            rows_to_lds((const float*)a.idx + r0 * top, top, nullptr, 0, n, top, bi, lane);
+            rows_to_lds<true>(a.val + r0 * top, top, nullptr, 0, n, top, bv, lane);
+            rows_to_lds<true>((const float*)a.idx + r0 * top, top, nullptr, 0, n, top, bi, lane);
         }
         wave_lds_sync();
         const int64_t row = r0 + lane;
         if (lane < n) {
-            float* xr = bx + lane * ldw;
-            float* yr = by + lane * ldw;
-            float x[kLaneMost + 1], y[KIND == kPolicyRef ? kLaneMost + 1 : 1];
+            float* xr = bx + lane * A;
+            float* yr = by + lane * A;
+            float x[NA], y[KIND == kPolicy ? 1 : NA];
             float m = kNegInf, my = kNegInf;
 #pragma unroll
-            for (int j = 0; j <= kLaneMost; ++j) {
+            for (int j = 0; j < NA; ++j) {
                 x[j] = kNegInf;
                 if (KIND == kPolicyRef)
                     y[j] = kNegInf;
             }
+            row_read(xr, A, x);
+            if constexpr (KIND == kPolicyRef)
+                row_read(yr, A, y);
             // (four entries per uniform branch)
 #pragma unroll
-            for (int q = 0; q <= kLaneMost; q += 4) {
+            for (int q = 0; q < NA; q += 4) {
                 if (q >= A)
                     break;
 #pragma unroll
                 for (int j = q; j < q + 4; ++j) {
-                    if (j < A) {
-                        x[j] = xr[j];
-                        m = fmaxf(m, x[j]);
-                        if (KIND == kPolicyRef) {
-                            y[j] = yr[j];
-                            my = fmaxf(my, y[j]);
-                        }
-                    }
+                    m = fmaxf(m, x[j]);
+                    if (KIND == kPolicyRef)
+                        my = fmaxf(my, y[j]);
                 }
             }
             Stats st = empty_stats();
@@ -414,7 +489,7 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
             m = m == kNegInf ? 0.0f : m;
             my = my == kNegInf ? 0.0f : my;
 #pragma unroll
-            for (int q = 0; q <= kLaneMost; q += 4) {
+            for (int q = 0; q < NA; q += 4) {
                 if (q >= A)
                     break;
 #pragma unroll
@@ -440,8 +515,10 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
                 const float* v = bv + lane * ldt;
                 const float* ix = bi + lane * ldt;
                 float tm = kNegInf;
-                for (int j = 0; j < A; ++j)
-                    yr[j] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NA; ++j)
+                    y[j] = 0.0f;
+                row_write(yr, A, y);
                 // an entry counts if the mask left its logit's place (-inf logits that are
                 // legal count: the loss is then infinite)
                 auto index = [&](int k) {
@@ -479,22 +556,21 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
             }
             if (a.dlogits) {
                 const float wt = KIND == kDistill && counts ? pr.w * a.temperature / ts : 0.0f;
+                if constexpr (KIND == kDistill)
+                    row_read(yr, A, y);
 #pragma unroll
-                for (int q = 0; q <= kLaneMost; q += 4) {
+                for (int q = 0; q < NA; q += 4) {
                     if (q >= A)
                         break;
 #pragma unroll
                     for (int j = q; j < q + 4; ++j) {
-                        if (j < A) {
-                            float d = counts ? grad_entry<KIND>(
-                                                   g, x[j], KIND == kPolicyRef ? y[j] : 0.0f, c)
-                                             : 0.0f;
-                            if (KIND == kDistill && counts)
-                                d = __builtin_fmaf(-wt, yr[j], d);
-                            xr[j] = d;
-                        }
+                        float d = grad_entry<KIND>(g, x[j], KIND == kPolicyRef ? y[j] : 0.0f, c);
+                        if (KIND == kDistill)
+                            d = __builtin_fmaf(-wt, y[j], d);
+                        x[j] = counts ? d : 0.0f;
                     }
                 }
+                row_write(xr, A, x);
                 if (KIND != kDistill && counts)
                     xr[pr.action] += g.at_action;
             }
@@ -1041,7 +1117,14 @@ hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
     switch (p.variant) {
     case kLossLane: {
         const size_t lds = (size_t)kLaneThreads * 4 * lane_floats(KIND, a.A, a.top);
-        loss_lane_kernel<E, KIND><<<nb, kLaneThreads, lds, s>>>(a);
+        if (a.A <= 8)
+            loss_lane_kernel<E, KIND, 8><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 16)
+            loss_lane_kernel<E, KIND, 16><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 24)
+            loss_lane_kernel<E, KIND, 24><<<nb, kLaneThreads, lds, s>>>(a);
+        else
+            loss_lane_kernel<E, KIND, 32><<<nb, kLaneThreads, lds, s>>>(a);
         break;
     }
     case kLossRow:

@@ -48,8 +48,9 @@ def test_linear_desc_and_work_refused():
     L = M.lib()
     n = C.c_int64()
     assert L.malib_linear_work(None, 0, C.byref(n)) == B.E_INVAL
-    d = B.LinearDesc(B.DT_F32, B.ACT_RELU, 1, 8, 16, 24)
+    d = B.LinearDesc(B.DT_F32, B.ACT_RELU, 1, 100000, 16, 24)
     assert L.malib_linear_work(C.byref(d), 0, None) == B.E_INVAL
+    # (dW sums over 100000 rows: split over workgroups)
     assert L.malib_linear_work(C.byref(d), 1, C.byref(n)) == B.MALIB_OK and n.value > 0
     # more tiles than one launch takes
     d = B.LinearDesc(B.DT_F32, B.ACT_NONE, 65535, (1 << 31) - 1, 8, 1 << 24)
@@ -72,14 +73,14 @@ def test_linear_without_rows_does_nothing():
     (dict(dy=None), b"dy is NULL"), (dict(x=None), b"x is NULL"), (dict(w=None), b"w is NULL"),
     (dict(act=B.ACT_GELU), b"pre is NULL"), (dict(dw=B.Mat(P, 15, 0)), b"dw"),
     (dict(dx=B.Mat(P, 15, 0)), b"dx"), (dict(dbias=P + 1), b"dbias"),
-    (dict(nbytes=0), b"workspace"), (dict(work=None), b"workspace"),
+    (dict(rows=100000, nbytes=0), b"workspace"), (dict(rows=100000, work=None), b"workspace"),
 ])
 def test_linear_backward_refuses(kw, word):
     L = M.lib()
-    a = dict(act=B.ACT_NONE, dy=B.Mat(P, 24, 0), x=B.Mat(P, 16, 0), w=B.Mat(P, 16, 0), pre=None,
+    a = dict(rows=8, act=B.ACT_NONE, dy=B.Mat(P, 24, 0), x=B.Mat(P, 16, 0), w=B.Mat(P, 16, 0), pre=None,
              dx=B.Mat(P, 16, 0), dw=B.Mat(P, 16, 0), dbias=P, work=P, nbytes=1 << 30)
     a.update(kw)
-    d = B.LinearDesc(B.DT_F32, a["act"], 1, 8, 16, 24)
+    d = B.LinearDesc(B.DT_F32, a["act"], 1, a["rows"], 16, 24)
     ref = [None if a[k] is None else C.byref(a[k]) for k in ("dy", "x", "w", "pre", "dx", "dw")]
     assert L.malib_linear_backward(C.byref(d), *ref, a["dbias"], a["work"], a["nbytes"],
                                    None) == B.E_INVAL
