@@ -86,10 +86,13 @@ malib_status check_work(void* work, int64_t have, int64_t need)
     return MALIB_OK;
 }
 
-// Workgroups of one product fit a launch
+// Workgroups of one product fit a launch (the largest tile may become 128)
 malib_status check_grid(const malib_linear_desc* d, const GemmPlan& p, int64_t M, int64_t N)
 {
-    const int64_t mt = (M + p.tile - 1) / p.tile, nt = (N + p.tile - 1) / p.tile;
+    if (p.tile == 0)
+        return MALIB_OK;
+    const int64_t tile = std::min(p.tile, 128);
+    const int64_t mt = (M + tile - 1) / tile, nt = (N + tile - 1) / tile;
     if (mt * nt > kMaxRows / ((int64_t)d->groups * p.splits))
         return set_error(MALIB_E_UNSUPPORTED, "the layer has more tiles than one launch takes");
     return MALIB_OK;
@@ -117,8 +120,7 @@ BackwardPlan backward_plan(const malib_linear_desc* d)
     p.dx = gemm_plan(d->groups, d->rows, d->in, d->out, size);
     p.dw = gemm_plan(d->groups, d->out, d->in, d->rows, size);
     p.dz = dz_plan(d->groups, d->rows, d->out, size);
-    p.fused = act && !rounded && d->groups * d->rows * d->out <= kFusedMost &&
-              p.dx.tile < 256 && p.dw.tile < 256;
+    p.fused = act && !rounded && d->groups * d->rows * d->out <= kFusedMost;
     p.own_sums = (act && !p.fused) || p.dw.tile == 256;
     p.dz_ld = (d->out + ch - 1) / ch * ch;
     p.dz_at = 0;
@@ -139,7 +141,7 @@ malib_status malib_linear_work(const malib_linear_desc* d, int32_t backward, int
     if (!work_bytes)
         return set_error(MALIB_E_INVAL, "work_bytes is NULL");
     *work_bytes = backward ? backward_plan(d).bytes
-                           : gemm_plan(d->groups, d->rows, d->out, d->in, type_size(d->dtype))
+                           : linear_plan(d->groups, d->rows, d->out, d->in, type_size(d->dtype))
                                  .part_bytes;
     return MALIB_OK;
 }
@@ -161,7 +163,7 @@ malib_status malib_linear(const malib_linear_desc* d, const malib_mat* x, const 
         TRY(check_mat(pre, "pre", d->rows, d->out, d->groups, size, true));
     if (bias && (uintptr_t)bias % 4)
         return set_error(MALIB_E_INVAL, "bias is not aligned to its elements");
-    const GemmPlan p = gemm_plan(d->groups, d->rows, d->out, d->in, size);
+    const GemmPlan p = linear_plan(d->groups, d->rows, d->out, d->in, size);
     TRY(check_grid(d, p, d->rows, d->out));
     TRY(check_work(work, work_bytes, p.part_bytes));
     GemmArgs a{};

@@ -386,11 +386,14 @@ struct GemmPlan {
     int64_t k_split, part_bytes, sum_bytes;
 };
 GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
+// the forward's plan: up to kFewRows rows a kernel of its own (tile 0)
+constexpr int kFewRows = 16;
+GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
 hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s);
 // dW and dx (either left out where its c.p is null), in one launch where both use
 // the same tile
-hipError_t launch_linear_backward(int dtype, GemmArgs dw, const GemmPlan& pw, float* dw_part,
-                                  float* sum_part, GemmArgs dx, const GemmPlan& px, float* dx_part,
+hipError_t launch_linear_backward(int dtype, GemmArgs dw, GemmPlan pw, float* dw_part,
+                                  float* sum_part, GemmArgs dx, GemmPlan px, float* dx_part,
                                   hipStream_t s);
 struct DzPlan {
     int rows_per_block, parts, col_blocks;

@@ -8,6 +8,7 @@
 // of dx) or with its row index contiguous ("RC": W of dx, dz and x of dW).
 #include "internal.hpp"
 
+#include <cmath>
 #include <type_traits>
 
 #include "chunk.hpp"
@@ -25,63 +26,125 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <typename E>
 constexpr int kBK = 128 / (int)sizeof(E);
 
-// The activation and its derivative at z, in fp32.  relu passes a NaN on, as the
+// The activations and their derivatives at z, in fp32.  relu passes a NaN on, as the
 // policies' hidden layers do; its derivative at 0 is 0.
-__device__ __forceinline__ float act_f32(int act, float z)
+__device__ __forceinline__ float relu_f32(float z) { return z != z ? z : (z > 0.0f ? z : 0.0f); }
+
+// e^-x^2 / 2 (`e`) and Phi(x), the normal distribution function, by Hastings' rational
+// approximation of erf (Abramowitz and Stegun 7.1.26, absolute error below 1.5e-7, a
+// quarter of what 1 + erf loses in fp32 to the left of -3 anyway).
+__device__ __forceinline__ float normal_cdf(float x, float& e)
+{
+    const float ax = __builtin_fabsf(x) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, ax, 1.0f));
+    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+    p = __builtin_fmaf(p, t, 1.421413741f);
+    p = __builtin_fmaf(p, t, -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.254829592f);
+    e = __builtin_amdgcn_exp2f(-0.72134752044448170f * (x * x));
+    const float tail = 0.5f * (p * t) * e;   // 1 - Phi(|x|)
+    return x > 0.0f ? 1.0f - tail : tail;
+}
+
+__device__ __forceinline__ float sigmoid_f32(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * z));
+}
+
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N])
 {
     switch (act) {
     case MALIB_ACT_RELU:
-        return z != z ? z : (z > 0.0f ? z : 0.0f);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] = relu_f32(v[i]);
+        break;
     case MALIB_ACT_GELU:
-        return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float e;
+            v[i] *= normal_cdf(v[i], e);
+        }
+        break;
     case MALIB_ACT_SILU:
-        return z / (1.0f + expf(-z));
-    default:
-        return z;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] *= sigmoid_f32(v[i]);
+        break;
     }
 }
 
-__device__ __forceinline__ float act_slope_f32(int act, float z)
+// v[i] *= act'(z[i])
+template <int N>
+__device__ __forceinline__ void times_slope(int act, const float (&z)[N], float (&v)[N])
 {
     switch (act) {
     case MALIB_ACT_RELU:
-        return z > 0.0f ? 1.0f : 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] *= z[i] > 0.0f ? 1.0f : 0.0f;
+        break;
     case MALIB_ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) +
-               z * (0.39894228040143268f * expf(-0.5f * z * z));
-    case MALIB_ACT_SILU: {
-        const float s = 1.0f / (1.0f + expf(-z));
-        return s * (1.0f + z * (1.0f - s));
-    }
-    default:
-        return 1.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float e;
+            const float p = normal_cdf(z[i], e);
+            v[i] *= __builtin_fmaf(z[i] * 0.39894228040143268f, e, p);
+        }
+        break;
+    case MALIB_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float s = sigmoid_f32(z[i]);
+            v[i] *= s * __builtin_fmaf(z[i], 1.0f - s, 1.0f);
+        }
+        break;
     }
 }
 
 // ------------------------------------------------------------------- epilogue
 
+// Bias of columns n .. n + cnt - 1 (zeros without one, and behind cnt)
+template <int N>
+__device__ __forceinline__ void load_bias(const GemmArgs& a, int g, int64_t n, int cnt,
+                                          float (&b)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const u32x4 t = a.bias && cnt > i
+                            ? load_chunk(a.bias + (int64_t)g * a.N + n + i, cnt - i)
+                            : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            b[i + e] = __uint_as_float(t[e]);
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ u32x4 load_residual(const GemmArgs& a, int g, int64_t m, int64_t n,
+                                               int cnt)
+{
+    return load_chunk((const E*)a.res.p + g * a.res.gs + m * a.res.ld + n, cnt);
+}
+
 // One chunk of an output row: columns n .. n + cnt - 1 of row m of group g.
 template <typename E>
-__device__ __forceinline__ void epilogue_chunk(const GemmArgs& a, int g, int64_t m, int n, int cnt,
-                                               float (&v)[kChunk<E>])
+__device__ __forceinline__ void finish_chunk(const GemmArgs& a, int g, int64_t m, int64_t n,
+                                             int cnt, const float (&bias)[kChunk<E>], u32x4 res,
+                                             float (&v)[kChunk<E>])
 {
     if (a.bias) {
-        const float* b = a.bias + (int64_t)g * a.N + n;
 #pragma unroll
         for (int i = 0; i < kChunk<E>; ++i)
-            if (i < cnt)
-                v[i] += b[i];
+            v[i] += bias[i];
     }
     if (a.pre.p)
         store_chunk((E*)a.pre.p + g * a.pre.gs + m * a.pre.ld + n, cnt, pack<E>(v));
-    if (a.act != MALIB_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < kChunk<E>; ++i)
-            v[i] = act_f32(a.act, v[i]);
-    }
+    activate(a.act, v);
     if (a.res.p) {
         float r[kChunk<E>];
-        unpack<E>(load_chunk((const E*)a.res.p + g * a.res.gs + m * a.res.ld + n, cnt), r);
+        unpack<E>(res, r);
 #pragma unroll
         for (int i = 0; i < kChunk<E>; ++i)
             v[i] += r[i];
@@ -261,33 +324,46 @@ template <typename E, bool KC, int BR, int THREADS, int LOAD>
 struct TileLoader {
     static constexpr int NI = BR * 8 / THREADS;
     static constexpr int CH = kChunk<E>;
-    const E* base;       // the tile's first row (KC) or column (RC) at k = 0
-    const E* pre;        // kFused: the same place in the values before the activation
-    int64_t ld, pre_ld;
+    const E* base;       // kDirect: the tile's first row (KC) or column (RC) at k = 0
+    int64_t ld;
     uint32_t off[NI];    // kDirect: byte offset from the tile's start, or kNoOffset
-    int row[NI], k[NI];  // first row and first k of the chunk in the tile
-    int n_rows, act;     // rows of the operand from the tile's first on
-    u32x4 reg[LOAD == kDirect ? 1 : NI];
+    // else: this thread's chunks of the next tile, in the operand and in the values
+    // before the activation, and how many of their elements are rows of the operand
+    const E *at[NI], *pre[NI];
+    int valid[NI];
+    int k[NI];           // first k of the chunk in the tile
+    int64_t step, pre_step;
+    int act;
+    u32x4 reg[LOAD == kDirect ? 1 : NI], reg_z[LOAD == kFused ? NI : 1];
 
+    // the first tile starts at k0
     __device__ __forceinline__ TileLoader(const MatArg& m, const MatArg& z, int act_, int g,
-                                          int64_t r0, int R, int tid)
+                                          int64_t r0, int R, int64_t k0, int tid)
     {
         ld = m.ld;
         base = (const E*)m.p + g * m.gs + (KC ? r0 * m.ld : r0);
-        pre_ld = z.ld;
-        pre = (const E*)z.p + g * z.gs + (KC ? r0 * z.ld : r0);
         act = act_;
-        n_rows = (int)(R - r0);
+        step = KC ? kBK<E> : kBK<E> * m.ld;
+        pre_step = KC ? kBK<E> : kBK<E> * z.ld;
+        const int n_rows = (int)(R - r0);   // rows of the operand from the tile's first on
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             int rr, c;
             slot_chunk<E, KC, BR>(tid + i * THREADS, rr, c);
-            row[i] = KC ? rr : c * CH;
+            const int row = KC ? rr : c * CH;
             k[i] = KC ? c * CH : rr;
-            if constexpr (LOAD == kDirect)
-                off[i] = row[i] < n_rows
+            if constexpr (LOAD == kDirect) {
+                off[i] = row < n_rows
                              ? (uint32_t)(((int64_t)rr * ld + c * CH) * (int64_t)sizeof(E))
                              : kNoOffset;
+            } else {
+                const int64_t r = KC ? row : k0 + k[i], col = KC ? k0 + k[i] : row;
+                at[i] = base + r * ld + col;
+                if (LOAD == kFused)
+                    pre[i] = (const E*)z.p + g * z.gs + (KC ? r0 * z.ld : r0) + r * z.ld + col;
+                const int left = n_rows - row;
+                valid[i] = KC ? (left > 0 ? CH : 0) : left < 0 ? 0 : left > CH ? CH : left;
+            }
         }
     }
 
@@ -308,38 +384,41 @@ struct TileLoader {
         }
     }
 
-    // kStaged, kFused
-    __device__ __forceinline__ void load(int64_t k0, int64_t k1)
+    // kStaged, kFused: the next tile's chunks into registers; `left`: k from its first on
+    __device__ __forceinline__ void load(int64_t left)
     {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int64_t left = k1 - k0 - k[i];
-            const int rl = n_rows - row[i];
-            int n;
-            if constexpr (KC)
-                n = rl > 0 ? (int)(left < CH ? left : CH) : 0;
-            else
-                n = left > 0 ? rl : 0;
-            const int64_t r = KC ? row[i] : k0 + k[i], c = KC ? k0 + k[i] : row[i];
-            reg[i] = n > 0 ? load_chunk(base + r * ld + c, n) : u32x4{0, 0, 0, 0};
+            int n = valid[i];
+            if (left < kBK<E>) {
+                const int kl = (int)left - k[i];
+                n = KC ? (n == 0 || kl < 0 ? 0 : kl < CH ? kl : CH) : kl > 0 ? n : 0;
+            }
+            reg[i] = u32x4{0, 0, 0, 0};
+            if (n > 0)
+                reg[i] = load_chunk(at[i], n);
+            at[i] += step;
             if constexpr (LOAD == kFused) {
-                if (n > 0) {
-                    float v[CH], z[CH];
-                    unpack<E>(reg[i], v);
-                    unpack<E>(load_chunk(pre + r * pre_ld + c, n), z);
-#pragma unroll
-                    for (int e = 0; e < CH; ++e)
-                        v[e] *= act_slope_f32(act, z[e]);
-                    reg[i] = pack<E>(v);
-                }
+                reg_z[i] = u32x4{0, 0, 0, 0};
+                if (n > 0)
+                    reg_z[i] = load_chunk(pre[i], n);
+                pre[i] += pre_step;
             }
         }
     }
     __device__ __forceinline__ void store(char* tile, int tid)
     {
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < NI; ++i) {
+            if constexpr (LOAD == kFused) {
+                float v[CH], z[CH];
+                unpack<E>(reg[i], v);
+                unpack<E>(reg_z[i], z);
+                times_slope(act, z, v);
+                reg[i] = pack<E>(v);
+            }
             *(u32x4*)(tile + (tid + i * THREADS) * 16) = reg[i];
+        }
     }
 };
 
@@ -351,25 +430,27 @@ struct GemmShape {
     static constexpr int kThreads = kWm * kWn * 64;
     static constexpr int kTm = TILE / kWm / 32, kTn = TILE / kWn / 32;   // 32x32 tiles of each
     static constexpr int kStage = 2 * TILE * 128;                // bytes of one stage
-    // kDirect: tiles in flight and in use.  Four small ones hide the latency of short
-    // products that leave few workgroups per CU; larger tiles take two.
-    static constexpr int kStages = TILE == 64 ? 4 : 2;
     static constexpr int kOutLd = kTn * 32 + 4;                  // floats per staged output row
     static constexpr int kOut = kWm * kWn * 32 * kOutLd * 4;
-    static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
+    static constexpr int lds(int stages)
+    {
+        return stages * kStage > kOut ? stages * kStage : kOut;
+    }
 };
 
 // s_waitcnt: at most `vm` vector loads outstanding, no LDS operation
 constexpr int wait_code(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4); }
 
 // One workgroup's tile of C, number `block` of `n_blocks` of this product.
-template <typename E, bool AKC, bool BKC, int TILE, int LOAD>
+// STAGES (kDirect): tiles in LDS, in use and on the way.  Four small ones hide the
+// latency of products that leave few workgroups per CU; where there are many, two
+// leave LDS for more of them.
+template <typename E, bool AKC, bool BKC, int TILE, int LOAD, int STAGES>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uint32_t n_blocks,
                                           char* lds)
 {
     using S = GemmShape<TILE>;
     constexpr int CH = kChunk<E>, TM = S::kTm, TN = S::kTn;
-    constexpr int STAGES = LOAD == kDirect ? S::kStages : 2;
     // column sums of A beside dW; the largest tile has no registers for them
     constexpr bool kSums = !AKC && TILE < 256;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -400,9 +481,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
     const int64_t ke = kb + a.k_split < a.K ? kb + a.k_split : a.K;
     const int n_k = (int)((ke - kb + kBK<E> - 1) / kBK<E>);
 
-    TileLoader<E, AKC, TILE, S::kThreads, LOAD> la(a.a, a.a_pre, a.a_act, g, m0, a.M, tid);
+    TileLoader<E, AKC, TILE, S::kThreads, LOAD> la(a.a, a.a_pre, a.a_act, g, m0, a.M, kb, tid);
     TileLoader<E, BKC, TILE, S::kThreads, LOAD == kFused ? kStaged : LOAD> lb(a.b, a.b, 0, g, n0,
-                                                                              a.N, tid);
+                                                                              a.N, kb, tid);
 
     f32x16 acc[TM][TN], sum[kSums ? TM : 1];
 #pragma unroll
@@ -429,8 +510,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
             lb.issue(lds + t * S::kStage + TILE * 128, k, ke, tid);
         }
     } else if (n_k > 0) {
-        la.load(kb, ke);
-        lb.load(kb, ke);
+        la.load(ke - kb);
+        lb.load(ke - kb);
     }
     for (int t = 0; t < n_k; ++t) {
         char* cur = lds + (t & (STAGES - 1)) * S::kStage;
@@ -456,8 +537,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
             lb.store(cur + TILE * 128, tid);
             __syncthreads();
             if (next < n_k) {
-                la.load(k_next, ke);
-                lb.load(k_next, ke);
+                la.load(ke - k_next);
+                lb.load(ke - k_next);
             }
         }
         const int stage = (t & (STAGES - 1)) * S::kStage;
@@ -506,8 +587,20 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
     // a lane holds 16 bytes of a row and a row's lanes are neighbours.
     __syncthreads();
     float* buf = (float*)lds + wave * 32 * S::kOutLd;
+    constexpr int LPR = TN * 32 / CH, RPP = 64 / LPR;   // lanes per row, rows per pass
+    const int64_t n = n0 + wn * TN * 32 + lane % LPR * CH;
+    const int cnt = n < a.N ? (int)(a.N - n < CH ? a.N - n : CH) : 0;
+    float bias[CH];
+    load_bias(a, g, n, a.part ? 0 : cnt, bias);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
+        const int64_t mi = m0 + (wm * TM + i) * 32 + lane / LPR;
+        u32x4 res[32 / RPP];
+#pragma unroll
+        for (int p = 0; p < 32 / RPP; ++p)
+            res[p] = a.res.p && !a.part && cnt > 0 && mi + p * RPP < a.M
+                         ? load_residual<E>(a, g, mi + p * RPP, n, cnt)
+                         : u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -515,18 +608,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
                 buf[(8 * (r >> 2) + 4 * h + (r & 3)) * S::kOutLd + j * 32 + (lane & 31)] =
                     acc[i][j][r];
         wave_lds_sync();
-        constexpr int LPR = TN * 32 / CH;   // lanes per row
-#pragma unroll 1
-        for (int p = 0; p < 32; p += 64 / LPR) {
-            const int r = p + lane / LPR, c = (lane % LPR) * CH;
-            const int64_t m = m0 + (wm * TM + i) * 32 + r;
-            const int64_t n = n0 + wn * TN * 32 + c;
-            if (m < a.M && n < a.N) {
-                const int cnt = (int)(a.N - n < CH ? a.N - n : CH);
+        float* row = buf + lane / LPR * S::kOutLd + lane % LPR * CH;
+#pragma unroll
+        for (int p = 0; p < 32 / RPP; ++p) {
+            const int64_t m = mi + p * RPP;
+            if (m < a.M && cnt > 0) {
                 float v[CH];
 #pragma unroll
                 for (int e = 0; e < CH; e += 4) {
-                    const f32x4 q = *(const f32x4*)(buf + r * S::kOutLd + c + e);
+                    const f32x4 q = *(const f32x4*)(row + p * RPP * S::kOutLd + e);
                     v[e] = q[0];
                     v[e + 1] = q[1];
                     v[e + 2] = q[2];
@@ -535,11 +625,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
                 if (a.part) {
                     float* o = a.part + (((int64_t)split * a.groups + g) * a.M + m) * a.N + n;
 #pragma unroll
-                    for (int e = 0; e < CH; ++e)
-                        if (e < cnt)
-                            o[e] = v[e];
+                    for (int e = 0; e < CH; e += 4)
+                        store_chunk(o + e, cnt - e,
+                                    u32x4{__float_as_uint(v[e]), __float_as_uint(v[e + 1]),
+                                          __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])});
                 } else {
-                    epilogue_chunk<E>(a, g, m, (int)n, cnt, v);
+                    finish_chunk<E>(a, g, m, n, cnt, bias, res[p], v);
                 }
             }
         }
@@ -547,40 +638,140 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
     }
 }
 
-template <typename E, int TILE, int LOAD>
+template <typename E, int TILE, int LOAD, int STAGES>
 __global__ __launch_bounds__(GemmShape<TILE>::kThreads) void forward_kernel(GemmArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::kLds];
-    gemm_tile<E, true, true, TILE, LOAD>(a, blockIdx.x, gridDim.x, lds);
+    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::lds(STAGES)];
+    gemm_tile<E, true, true, TILE, LOAD, STAGES>(a, blockIdx.x, gridDim.x, lds);
 }
 
 // dW's tiles, then dx's, in one launch: neither waits for the other's last tiles.
-template <typename E, int TILE, int LOAD>
+template <typename E, int TILE, int LOAD, int STAGES>
 __global__ __launch_bounds__(GemmShape<TILE>::kThreads) void backward_kernel(GemmArgs dw,
                                                                              uint32_t n_dw,
                                                                              GemmArgs dx)
 {
-    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::lds(STAGES)];
     if (blockIdx.x < n_dw)
-        gemm_tile<E, false, false, TILE, LOAD>(dw, blockIdx.x, n_dw, lds);
+        gemm_tile<E, false, false, TILE, LOAD, STAGES>(dw, blockIdx.x, n_dw, lds);
     else
-        gemm_tile<E, true, false, TILE, LOAD>(dx, blockIdx.x - n_dw, gridDim.x - n_dw, lds);
+        gemm_tile<E, true, false, TILE, LOAD, STAGES>(dx, blockIdx.x - n_dw, gridDim.x - n_dw, lds);
 }
 
-// Sums of the splits' parts, then the epilogue, of up to two products: 32 chunks of
-// output per workgroup, each thread a share of the splits, the shares added in
-// order.  Column sums are further items behind the first product's chunks.
-constexpr int kSumItems = 32, kSumShares = 8;
+// -------------------------------------------------------------- few rows, forward
 
-template <typename E>
+// At most 16 rows of x: the product reads W once and does little else.  A workgroup
+// takes 16 output units, each of its wavefronts a share of k in pieces of 256 bytes
+// per unit (64 bytes per lane, so that whole lines are asked for at once), straight
+// from memory to registers, W as the first operand of 16x16 products and x as the
+// second; the shares are added through LDS.  The order of k within a piece is the
+// same for both operands and otherwise free: a lane's 64 bytes are its part of four
+// products.
+template <typename E, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(GemmArgs a)
+{
+    constexpr int CH = kChunk<E>, PIECE = 16 * CH;   // k of a piece
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = blockIdx.y;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int r = lane & 15, h = lane >> 4;
+    const E* w = (const E*)a.b.p + g * a.b.gs + (n0 + r) * a.b.ld + h * 4 * CH;
+    const E* x = (const E*)a.a.p + g * a.a.gs + r * a.a.ld + h * 4 * CH;
+    const bool has_w = n0 + r < a.N, has_x = r < a.M;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t whole = a.K / PIECE;
+    auto product = [&](const u32x4 (&vw)[4], const u32x4 (&vx)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(E) == 2) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vw[i]),
+                                                              __builtin_bit_cast(bf16x8, vx[i]),
+                                                              acc, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[i][j]),
+                                                               __uint_as_float(vx[i][j]), acc, 0,
+                                                               0, 0);
+            }
+        }
+    };
+    const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll 2
+    for (int64_t p = wave; p < whole; p += WAVES) {
+        u32x4 vw[4], vx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vw[i] = vx[i] = zero;
+            if (has_w)
+                vw[i] = *(const u32x4_any*)(w + p * PIECE + i * CH);
+            if (has_x)
+                vx[i] = *(const u32x4_any*)(x + p * PIECE + i * CH);
+        }
+        product(vw, vx);
+    }
+    if (whole * PIECE < a.K && wave == (int)(whole % WAVES)) {
+        u32x4 vw[4], vx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t left = a.K - whole * PIECE - (h * 4 + i) * CH;
+            const int n = left > 0 ? (int)(left < CH ? left : CH) : 0;
+            vw[i] = has_w && n > 0 ? load_chunk(w + whole * PIECE + i * CH, n) : zero;
+            vx[i] = has_x && n > 0 ? load_chunk(x + whole * PIECE + i * CH, n) : zero;
+        }
+        product(vw, vx);
+    }
+    // lane: row r of x, output units 4 h .. 4 h + 3
+    __shared__ f32x4 part[WAVES][64];
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave != 0 || !has_x)
+        return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+        const f32x4 t = part[i][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] += t[e];
+    }
+    const int64_t n = n0 + 4 * h;
+    const int cnt = n < a.N ? (int)(a.N - n < 4 ? a.N - n : 4) : 0;
+    float bias[4];
+    load_bias(a, g, n, cnt, bias);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] += a.bias ? bias[e] : 0.0f;
+    if (a.pre.p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < cnt)
+                ((E*)a.pre.p)[g * a.pre.gs + r * a.pre.ld + n + e] = from_f32<E>(v[e]);
+    activate(a.act, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < cnt) {
+            if (a.res.p)
+                v[e] += to_f32(((const E*)a.res.p)[g * a.res.gs + r * a.res.ld + n + e]);
+            ((E*)a.c.p)[g * a.c.gs + r * a.c.ld + n + e] = from_f32<E>(v[e]);
+        }
+}
+
+// Sums of the splits' parts, then the epilogue, of up to two products: a workgroup
+// takes 256 / SHARES chunks of output, each thread a share of the splits, the shares
+// added in order.  Column sums are further items behind a product's chunks.
+constexpr int kSumThreads = 256;
+
+template <typename E, int SHARES>
 __device__ __forceinline__ void split_sum_block(const GemmArgs& a, int64_t block, float* red)
 {
-    constexpr int CH = kChunk<E>;
-    const int item = threadIdx.x % kSumItems, share = threadIdx.x / kSumItems;
+    constexpr int CH = kChunk<E>, ITEMS = kSumThreads / SHARES;
+    const int item = threadIdx.x % ITEMS, share = threadIdx.x / ITEMS;
     const int64_t per_row = (a.N + CH - 1) / CH;
     const int64_t n_chunks = (int64_t)a.groups * a.M * per_row;
     const int64_t n_sums = a.sum_out ? (int64_t)a.groups * a.M : 0;
-    const int64_t q = block * kSumItems + item;
+    const int64_t q = block * ITEMS + item;
     const int64_t gm = q < n_chunks ? q / per_row : q - n_chunks;
     const int n = q < n_chunks ? (int)(q - gm * per_row) * CH : 0;
     const int cnt = q < n_chunks ? (a.N - n < CH ? a.N - n : CH) : q < n_chunks + n_sums ? 1 : 0;
@@ -590,59 +781,73 @@ __device__ __forceinline__ void split_sum_block(const GemmArgs& a, int64_t block
 #pragma unroll
     for (int e = 0; e < CH; ++e)
         v[e] = 0.0f;
-    if (cnt == CH && plane % 4 == 0 && a.N % 4 == 0) {
+    if (cnt == CH) {
 #pragma unroll 4
-        for (int s = share; s < a.splits; s += kSumShares) {
+        for (int s = share; s < a.splits; s += SHARES) {
 #pragma unroll
             for (int e = 0; e < CH; e += 4) {
-                const f32x4 t = *(const f32x4*)(p + s * plane + e);
-                v[e] += t[0];
-                v[e + 1] += t[1];
-                v[e + 2] += t[2];
-                v[e + 3] += t[3];
+                const u32x4 t = *(const u32x4_any*)(p + s * plane + e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[e + i] += __uint_as_float(t[i]);
             }
         }
     } else if (cnt > 0) {
 #pragma unroll 4
-        for (int s = share; s < a.splits; s += kSumShares)
+        for (int s = share; s < a.splits; s += SHARES)
 #pragma unroll
             for (int e = 0; e < CH; ++e)
                 if (e < cnt)
                     v[e] += p[s * plane + e];
     }
+    if constexpr (SHARES > 1) {
 #pragma unroll
-    for (int e = 0; e < CH; ++e)
-        red[(share * CH + e) * kSumItems + item] = v[e];
-    __syncthreads();
-    if (share != 0 || cnt == 0)
+        for (int e = 0; e < CH; ++e)
+            red[(share * CH + e) * ITEMS + item] = v[e];
+        __syncthreads();
+        if (share != 0)
+            return;
+#pragma unroll
+        for (int e = 0; e < CH; ++e)
+            for (int t = 1; t < SHARES; ++t)
+                v[e] += red[(t * CH + e) * ITEMS + item];
+    }
+    if (cnt == 0)
         return;
-#pragma unroll
-    for (int e = 0; e < CH; ++e)
-        for (int t = 1; t < kSumShares; ++t)
-            v[e] += red[(t * CH + e) * kSumItems + item];
-    if (q < n_chunks)
-        epilogue_chunk<E>(a, (int)(gm / a.M), gm % a.M, n, cnt, v);
-    else
+    if (q >= n_chunks) {
         a.sum_out[gm] = v[0];
+        return;
+    }
+    const int g = (int)(gm / a.M);
+    float bias[CH];
+    load_bias(a, g, n, cnt, bias);
+    const u32x4 res = a.res.p ? load_residual<E>(a, g, gm % a.M, n, cnt) : u32x4{0, 0, 0, 0};
+    finish_chunk<E>(a, g, gm % a.M, n, cnt, bias, res, v);
 }
 
-template <typename E>
-__global__ __launch_bounds__(kSumItems* kSumShares) void split_sum_kernel(GemmArgs a,
-                                                                          uint32_t n_a, GemmArgs b)
+template <typename E, int SHARES>
+__global__ __launch_bounds__(kSumThreads) void split_sum_kernel(GemmArgs a, uint32_t n_a,
+                                                                GemmArgs b)
 {
-    __shared__ float red[kSumShares * kChunk<E> * kSumItems];
+    __shared__ float red[SHARES > 1 ? kSumThreads * kChunk<E> : 1];
     if (blockIdx.x < n_a)
-        split_sum_block<E>(a, blockIdx.x, red);
+        split_sum_block<E, SHARES>(a, blockIdx.x, red);
     else
-        split_sum_block<E>(b, blockIdx.x - n_a, red);
+        split_sum_block<E, SHARES>(b, blockIdx.x - n_a, red);
+}
+
+// Threads per chunk: as many as bring about four loads each
+static int sum_shares(const GemmArgs& a)
+{
+    return a.splits >= 24 ? 8 : a.splits >= 6 ? 2 : 1;
 }
 
 template <typename E>
-int64_t split_sum_blocks(const GemmArgs& a)
+int64_t split_sum_blocks(const GemmArgs& a, int shares)
 {
     const int64_t per_row = (a.N + kChunk<E> - 1) / kChunk<E>;
     const int64_t items = (int64_t)a.groups * a.M * (per_row + (a.sum_out ? 1 : 0));
-    return (items + kSumItems - 1) / kSumItems;
+    return (items * shares + kSumThreads - 1) / kSumThreads;
 }
 
 // dz = dy act'(z) rounded to the layer's type (where there is an activation), and
@@ -672,9 +877,7 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
             if (act != MALIB_ACT_NONE) {
                 float z[CH];
                 unpack<E>(load_chunk((const E*)pre.p + g * pre.gs + m * pre.ld + n, cnt), z);
-#pragma unroll
-                for (int e = 0; e < CH; ++e)
-                    v[e] *= act_slope_f32(act, z[e]);
+                times_slope(act, z, v);
                 if (dz.p)
                     store_chunk((E*)dz.p + g * dz.gs + m * dz.ld + n, cnt, pack<E>(v));
             }
@@ -703,6 +906,8 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
 }
 
 // db[i] = sum over the row ranges: shares of the ranges by thread, added in order.
+constexpr int kSumItems = 8, kSumShares = 32;
+
 __global__ __launch_bounds__(kSumItems* kSumShares) void db_kernel(const float* sums, int64_t n,
                                                                    int parts, float* db)
 {
@@ -724,20 +929,45 @@ __global__ __launch_bounds__(kSumItems* kSumShares) void db_kernel(const float* 
     }
 }
 
+// Stages of 64-wide tiles: see gemm_tile.  (16 groups of 8192 x 24 -> 64 fp32: 28 us
+// with four, 20 us with two; 1024 x 1024 -> 1024 bf16: 11 us and 13 us.)
+int small_stages(int64_t blocks, int64_t k_split, int bk)
+{
+    return blocks >= 1024 || k_split <= 2 * bk ? 2 : 4;
+}
+
 template <typename E>
 hipError_t launch_forward_as(const GemmArgs& a, int tile, bool direct, hipStream_t s)
 {
     const unsigned nb = (unsigned)a.blocks;
-    if (tile == 256 && direct)
-        forward_kernel<E, 256, kDirect><<<nb, 512, 0, s>>>(a);
-    else if (tile == 128 && direct)
-        forward_kernel<E, 128, kDirect><<<nb, 256, 0, s>>>(a);
+    if constexpr (sizeof(E) == 2) {   // (fp32 plans take no larger tile than 128)
+        if (tile == 256) {
+            forward_kernel<E, 256, kDirect, 2><<<nb, 512, 0, s>>>(a);
+            return hipGetLastError();
+        }
+    }
+    if (tile == 128 && direct)
+        forward_kernel<E, 128, kDirect, 2><<<nb, 256, 0, s>>>(a);
     else if (tile == 128)
-        forward_kernel<E, 128, kStaged><<<nb, 256, 0, s>>>(a);
-    else if (direct)
-        forward_kernel<E, 64, kDirect><<<nb, 256, 0, s>>>(a);
+        forward_kernel<E, 128, kStaged, 2><<<nb, 256, 0, s>>>(a);
+    else if (!direct)
+        forward_kernel<E, 64, kStaged, 2><<<nb, 256, 0, s>>>(a);
+    else if (small_stages(a.blocks, a.k_split, kBK<E>) == 2)
+        forward_kernel<E, 64, kDirect, 2><<<nb, 256, 0, s>>>(a);
     else
-        forward_kernel<E, 64, kStaged><<<nb, 256, 0, s>>>(a);
+        forward_kernel<E, 64, kDirect, 4><<<nb, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_few_rows_as(const GemmArgs& a, hipStream_t s)
+{
+    // (16 wavefronts where few workgroups share the work)
+    const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)a.groups);
+    if ((int64_t)grid.x * grid.y < 512 && a.K >= 1024)
+        few_rows_kernel<E, 16><<<grid, 1024, 0, s>>>(a);
+    else
+        few_rows_kernel<E, 4><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -748,31 +978,45 @@ hipError_t launch_backward_as(const GemmArgs& dw, const GemmArgs& dx, int tile, 
     const uint32_t n_dw = (uint32_t)dw.blocks, nb = n_dw + (uint32_t)dx.blocks;
     if (nb == 0)
         return hipSuccess;
-    if (tile == 256 && load == kDirect)
-        backward_kernel<E, 256, kDirect><<<nb, 512, 0, s>>>(dw, n_dw, dx);
-    else if (tile == 128 && load == kDirect)
-        backward_kernel<E, 128, kDirect><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    const int64_t k = std::max(dw.blocks ? dw.k_split : 0, dx.blocks ? dx.k_split : 0);
+    if constexpr (sizeof(E) == 2) {
+        if (tile == 256) {
+            backward_kernel<E, 256, kDirect, 2><<<nb, 512, 0, s>>>(dw, n_dw, dx);
+            return hipGetLastError();
+        }
+    }
+    if (tile == 128 && load == kDirect)
+        backward_kernel<E, 128, kDirect, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
     else if (tile == 128 && load == kStaged)
-        backward_kernel<E, 128, kStaged><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+        backward_kernel<E, 128, kStaged, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
     else if (tile == 128)
-        backward_kernel<E, 128, kFused><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (load == kDirect)
-        backward_kernel<E, 64, kDirect><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+        backward_kernel<E, 128, kFused, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
     else if (load == kStaged)
-        backward_kernel<E, 64, kStaged><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+        backward_kernel<E, 64, kStaged, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (load == kFused)
+        backward_kernel<E, 64, kFused, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+    else if (small_stages(nb, k, kBK<E>) == 2)
+        backward_kernel<E, 64, kDirect, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
     else
-        backward_kernel<E, 64, kFused><<<nb, 256, 0, s>>>(dw, n_dw, dx);
+        backward_kernel<E, 64, kDirect, 4><<<nb, 256, 0, s>>>(dw, n_dw, dx);
     return hipGetLastError();
 }
 
 template <typename E>
 hipError_t launch_split_sums(const GemmArgs& a, const GemmArgs& b, hipStream_t s)
 {
-    const int64_t na = a.blocks && a.part ? split_sum_blocks<E>(a) : 0;
-    const int64_t nb = b.blocks && b.part ? split_sum_blocks<E>(b) : 0;
-    if (na + nb == 0)
+    const bool pa = a.blocks && a.part, pb = b.blocks && b.part;
+    if (!pa && !pb)
         return hipSuccess;
-    split_sum_kernel<E><<<(unsigned)(na + nb), kSumItems * kSumShares, 0, s>>>(a, (uint32_t)na, b);
+    const int shares = std::max(pa ? sum_shares(a) : 1, pb ? sum_shares(b) : 1);
+    const uint32_t na = pa ? (uint32_t)split_sum_blocks<E>(a, shares) : 0;
+    const uint32_t nb = na + (pb ? (uint32_t)split_sum_blocks<E>(b, shares) : 0);
+    if (shares == 8)
+        split_sum_kernel<E, 8><<<nb, kSumThreads, 0, s>>>(a, na, b);
+    else if (shares == 2)
+        split_sum_kernel<E, 2><<<nb, kSumThreads, 0, s>>>(a, na, b);
+    else
+        split_sum_kernel<E, 1><<<nb, kSumThreads, 0, s>>>(a, na, b);
     return hipGetLastError();
 }
 
@@ -787,29 +1031,51 @@ static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups)
            contiguous % ch == 0 && m.ld * size <= (int64_t)(0x70000000 / 256);
 }
 
+// Tile and splits by estimated time on 256 CUs, from measured constants (us; bf16,
+// fp32): a CU's time per 128 bytes of k of a tile with several workgroups on it
+// (`busy`) and with one (`alone`), and the time of a tile's output (`out`).  The
+// sum of the splits' parts is a launch and their bytes at about 3.5 TB/s.
+//   8192 x 4096 -> 4096 bf16: 64 480 us, 128 279 us, 256 238 us; 2048^3: 64 33 us,
+//   128 28 us, 256 53 us, 128 with two splits 64 us; 4096 x 2048 -> 2048 fp32: 64
+//   307 us, 128 267 us; 20000 x 256 -> 256 fp32: 64 32 us, 128 40 us.
 GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
 {
-    GemmPlan p;
+    struct Cost {
+        int tile;
+        double busy, alone, out;
+    };
+    static constexpr Cost kCosts[2][3] = {{{64, 0.23, 0.30, 1.3}, {128, 0.55, 0.75, 3.1}, {256, 1.75, 1.75, 10.0}},
+                                          {{64, 0.60, 0.70, 1.4}, {128, 2.08, 2.1, 2.7}, {0, 0, 0, 0}}};
+    constexpr double kCus = 256, kSumLaunch = 5.0, kSumBytes = 3.5e6;
     const int bk = 128 / size;
-    auto blocks = [&](int t) { return groups * ((M + t - 1) / t) * ((N + t - 1) / t); };
     const int64_t k_tiles = std::max<int64_t>(1, (K + bk - 1) / bk);
-    p.tile = 64;
-    if (blocks(128) * k_tiles >= 1024 && std::min(M, N) > 64)
-        p.tile = 128;
-    if (size == 2 && blocks(256) * k_tiles >= 8192 && std::min(M, N) > 128)
-        p.tile = 256;
-    const int64_t b = std::max<int64_t>(1, blocks(p.tile));
-    const int64_t want = p.tile == 256 ? 256 : p.tile == 128 ? 512 : 1024;
-    int64_t splits = 1;
-    if (b < want && k_tiles > 4)
-        splits = std::min(std::min(want / b, k_tiles / 4), (int64_t)128);
-    splits = std::max<int64_t>(1, splits);
-    const int64_t per = (k_tiles + splits - 1) / splits;
-    p.splits = (int)((k_tiles + per - 1) / per);
-    p.k_split = per * bk;
-    p.part_bytes = p.splits > 1 ? p.splits * groups * M * N * 4 : 0;
-    p.sum_bytes = p.splits > 1 ? p.splits * groups * M * 4 : 0;
-    return p;
+    GemmPlan best{};
+    double least = 1e30;
+    for (const Cost& c : kCosts[size == 4]) {
+        if (c.tile == 0 || (c.tile > 64 && std::max(M, N) <= c.tile / 2))
+            continue;
+        const double blocks = (double)groups * (double)((M + c.tile - 1) / c.tile) *
+                              (double)((N + c.tile - 1) / c.tile);
+        for (int64_t s = 1; s <= 512; s *= 2) {
+            if (s > 1 && (k_tiles < 2 * s || blocks * (double)(s / 2) >= 2 * kCus))
+                break;
+            const int64_t per = (k_tiles + s - 1) / s;
+            const int64_t splits = (k_tiles + per - 1) / per;
+            const double n = std::max(1.0, std::ceil(blocks * (double)splits / kCus));
+            double t = (double)per * std::max(c.alone, n * c.busy) + n * c.out;
+            if (splits > 1)
+                t += kSumLaunch + (double)splits * (double)groups * (double)M * (double)N * 4.0 / kSumBytes;
+            if (t < least) {
+                least = t;
+                best.tile = c.tile;
+                best.splits = (int)splits;
+                best.k_split = per * bk;
+            }
+        }
+    }
+    best.part_bytes = best.splits > 1 ? best.splits * groups * M * N * 4 : 0;
+    best.sum_bytes = best.splits > 1 ? best.splits * groups * M * 4 : 0;
+    return best;
 }
 
 // The plan's part of a product's arguments
@@ -823,19 +1089,33 @@ static void apply(GemmArgs& a, const GemmPlan& p, float* part)
     a.blocks = (int64_t)a.mt * a.nt * a.groups * a.splits;
 }
 
+GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
+{
+    if (M <= kFewRows) {
+        GemmPlan p{};
+        p.splits = 1;
+        p.k_split = K;
+        return p;
+    }
+    return gemm_plan(groups, M, N, K, size);
+}
+
 hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s)
 {
-    const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
+    const bool bf = dtype == MALIB_DT_BF16;
+    if (p.tile == 0)
+        return bf ? launch_few_rows_as<bf16_t>(a, s) : launch_few_rows_as<float>(a, s);
+    const int size = bf ? 2 : 4;
     const bool direct = chunked(a.a, size, a.K, a.groups) && chunked(a.b, size, a.K, a.groups);
+    if (p.tile == 256 && !direct)
+        p.tile = 128;   // the largest tile takes aligned rows only
     apply(a, p, part);
     const GemmArgs none{};
-    hipError_t e;
-    if (dtype == MALIB_DT_BF16) {
-        e = launch_forward_as<bf16_t>(a, p.tile, direct, s);
-        return e != hipSuccess ? e : launch_split_sums<bf16_t>(a, none, s);
-    }
-    e = launch_forward_as<float>(a, p.tile, direct, s);
-    return e != hipSuccess ? e : launch_split_sums<float>(a, none, s);
+    const hipError_t e = bf ? launch_forward_as<bf16_t>(a, p.tile, direct, s)
+                            : launch_forward_as<float>(a, p.tile, direct, s);
+    if (e != hipSuccess)
+        return e;
+    return bf ? launch_split_sums<bf16_t>(a, none, s) : launch_split_sums<float>(a, none, s);
 }
 
 template <typename E>
@@ -854,26 +1134,33 @@ static hipError_t backward_as(const GemmArgs& dw, int dw_tile, const GemmArgs& d
     return e != hipSuccess ? e : launch_split_sums<E>(dw, dx, s);
 }
 
-hipError_t launch_linear_backward(int dtype, GemmArgs dw, const GemmPlan& pw, float* dw_part,
-                                  float* sum_part, GemmArgs dx, const GemmPlan& px, float* dx_part,
+hipError_t launch_linear_backward(int dtype, GemmArgs dw, GemmPlan pw, float* dw_part,
+                                  float* sum_part, GemmArgs dx, GemmPlan px, float* dx_part,
                                   hipStream_t s)
 {
     const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
     bool direct = true, fused = false;
     if (dw.c.p) {
-        apply(dw, pw, dw_part);
-        if (dw.sum_out)
-            dw.sum = pw.splits > 1 ? sum_part : dw.sum_out;
         direct = chunked(dw.a, size, dw.M, dw.groups) && chunked(dw.b, size, dw.N, dw.groups);
         fused = dw.a_act != MALIB_ACT_NONE;
     }
     if (dx.c.p) {
-        apply(dx, px, dx_part);
         direct = direct && chunked(dx.a, size, dx.K, dx.groups) &&
                  chunked(dx.b, size, dx.N, dx.groups);
         fused = fused || dx.a_act != MALIB_ACT_NONE;
     }
     const int load = fused ? kFused : direct ? kDirect : kStaged;
+    if (load != kDirect) {   // the largest tile takes aligned rows only
+        pw.tile = std::min(pw.tile, 128);
+        px.tile = std::min(px.tile, 128);
+    }
+    if (dw.c.p) {
+        apply(dw, pw, dw_part);
+        if (dw.sum_out)
+            dw.sum = pw.splits > 1 ? sum_part : dw.sum_out;
+    }
+    if (dx.c.p)
+        apply(dx, px, dx_part);
     return dtype == MALIB_DT_BF16
                ? backward_as<bf16_t>(dw, pw.tile, dx, px.tile, load, s)
                : backward_as<float>(dw, pw.tile, dx, px.tile, load, s);

@@ -154,6 +154,24 @@ def test_large_tiles(dtype, M, K, N):
     check_layer(dtype, None, M, K, N, "relu")
 
 
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M, K, N", [(2050, 1024, 1032), (4096, 520, 1304), (700, 2049, 3001)])
+def test_large_sizes_unaligned(dtype, M, K, N, act):
+    """Sizes that get the largest tiles, with rows that do not start on 16-byte
+    boundaries."""
+    check_layer(dtype, None, M, K, N, act, pad=1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 3, 7, 16, 17])
+@pytest.mark.parametrize("K, N, G", [(8192, 136, None), (1024, 1000, 3), (130, 17, 2), (4100, 33, None),
+                                     (96, 2000, None)])
+def test_few_rows(dtype, M, K, N, G):
+    check_layer(dtype, G, M, K, N, "silu")
+    check_layer(dtype, G, M, K, N, "relu", pad=3, shift=1, bias=False)
+
+
 @pytest.mark.parametrize("pad, shift", [(1, 0), (8, 0), (8, 1), (3, 5), (0, 2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_strides_and_alignment(dtype, pad, shift):
