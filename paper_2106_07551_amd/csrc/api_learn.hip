@@ -25,7 +25,7 @@ namespace {
 
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;
-constexpr int64_t kFusedMost = (int64_t)1 << 20;   // values of dz
+constexpr int64_t kFusedMost = (int64_t)1 << 20, kFusedWidth = 128;   // see BackwardPlan
 
 int type_size(int dtype) { return dtype == MALIB_DT_BF16 ? 2 : 4; }
 
@@ -120,7 +120,8 @@ BackwardPlan backward_plan(const malib_linear_desc* d)
     p.dx = gemm_plan(d->groups, d->rows, d->in, d->out, size);
     p.dw = gemm_plan(d->groups, d->out, d->in, d->rows, size);
     p.dz = dz_plan(d->groups, d->rows, d->out, size);
-    p.fused = act && !rounded && d->groups * d->rows * d->out <= kFusedMost;
+    p.fused = act && !rounded &&
+              (d->groups * d->rows * d->out <= kFusedMost || d->in <= kFusedWidth);
     p.own_sums = (act && !p.fused) || p.dw.tile == 256;
     p.dz_ld = (d->out + ch - 1) / ch * ch;
     p.dz_at = 0;

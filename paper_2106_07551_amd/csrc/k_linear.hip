@@ -662,25 +662,26 @@ __global__ __launch_bounds__(GemmShape<TILE>::kThreads) void backward_kernel(Gem
 
 // At most 16 rows of x: the product reads W once and does little else.  A workgroup
 // takes 16 output units, each of its wavefronts a share of k in pieces of 256 bytes
-// per unit (64 bytes per lane, so that whole lines are asked for at once), straight
-// from memory to registers, W as the first operand of 16x16 products and x as the
-// second; the shares are added through LDS.  The order of k within a piece is the
-// same for both operands and otherwise free: a lane's 64 bytes are its part of four
-// products.
-template <typename E, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(GemmArgs a)
+// per unit, straight from memory to registers, W as the first operand of 16x16
+// products and x as the second; the shares are added through LDS.  Units and rows
+// that do not exist repeat the last one: their results are not written.  Bound by
+// the read of W: 3 rows x 8192 -> 8192 bf16 32 us, 4.3 TB/s (with 4 wavefronts 35 us,
+// 16 32 us; as 64-wide tiles with split sums 33 us and more, in two launches).
+template <typename E>
+__global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a)
 {
+    constexpr int WAVES = 8;
     constexpr int CH = kChunk<E>, PIECE = 16 * CH;   // k of a piece
+    constexpr int AHEAD = 4;                         // pieces on the way
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.y;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const int r = lane & 15, h = lane >> 4;
-    const E* w = (const E*)a.b.p + g * a.b.gs + (n0 + r) * a.b.ld + h * 4 * CH;
-    const E* x = (const E*)a.a.p + g * a.a.gs + r * a.a.ld + h * 4 * CH;
-    const bool has_w = n0 + r < a.N, has_x = r < a.M;
+    const int64_t unit = n0 + r < a.N ? n0 + r : a.N - 1, row = r < a.M ? r : a.M - 1;
+    const E* w = (const E*)a.b.p + g * a.b.gs + unit * a.b.ld + h * CH;
+    const E* x = (const E*)a.a.p + g * a.a.gs + row * a.a.ld + h * CH;
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t whole = a.K / PIECE;
     auto product = [&](const u32x4 (&vw)[4], const u32x4 (&vx)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -697,28 +698,35 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(GemmArgs a)
             }
         }
     };
-    const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll 2
-    for (int64_t p = wave; p < whole; p += WAVES) {
-        u32x4 vw[4], vx[4];
+    const int64_t whole = a.K / PIECE;
+    int64_t p = wave;
+    for (; p + (AHEAD - 1) * WAVES < whole; p += AHEAD * WAVES) {
+        u32x4 vw[AHEAD][4], vx[AHEAD][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            vw[i] = vx[i] = zero;
-            if (has_w)
-                vw[i] = *(const u32x4_any*)(w + p * PIECE + i * CH);
-            if (has_x)
-                vx[i] = *(const u32x4_any*)(x + p * PIECE + i * CH);
-        }
-        product(vw, vx);
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                vw[u][i] = *(const u32x4_any*)(w + (p + u * WAVES) * PIECE + i * 4 * CH);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                vx[u][i] = *(const u32x4_any*)(x + (p + u * WAVES) * PIECE + i * 4 * CH);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            product(vw[u], vx[u]);
     }
-    if (whole * PIECE < a.K && wave == (int)(whole % WAVES)) {
+    for (; p * PIECE < a.K; p += WAVES) {   // single pieces, the last one short
         u32x4 vw[4], vx[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t left = a.K - whole * PIECE - (h * 4 + i) * CH;
+            const int64_t left = a.K - p * PIECE - (i * 4 + h) * CH;
             const int n = left > 0 ? (int)(left < CH ? left : CH) : 0;
-            vw[i] = has_w && n > 0 ? load_chunk(w + whole * PIECE + i * CH, n) : zero;
-            vx[i] = has_x && n > 0 ? load_chunk(x + whole * PIECE + i * CH, n) : zero;
+            vw[i] = vx[i] = u32x4{0, 0, 0, 0};
+            if (n > 0) {
+                vw[i] = load_chunk(w + p * PIECE + i * 4 * CH, n);
+                vx[i] = load_chunk(x + p * PIECE + i * 4 * CH, n);
+            }
         }
         product(vw, vx);
     }
@@ -726,7 +734,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(GemmArgs a)
     __shared__ f32x4 part[WAVES][64];
     part[wave][lane] = acc;
     __syncthreads();
-    if (wave != 0 || !has_x)
+    if (wave != 0 || r >= a.M)
         return;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -962,12 +970,8 @@ hipError_t launch_forward_as(const GemmArgs& a, int tile, bool direct, hipStream
 template <typename E>
 hipError_t launch_few_rows_as(const GemmArgs& a, hipStream_t s)
 {
-    // (16 wavefronts where few workgroups share the work)
     const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)a.groups);
-    if ((int64_t)grid.x * grid.y < 512 && a.K >= 1024)
-        few_rows_kernel<E, 16><<<grid, 1024, 0, s>>>(a);
-    else
-        few_rows_kernel<E, 4><<<grid, 256, 0, s>>>(a);
+    few_rows_kernel<E><<<grid, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 

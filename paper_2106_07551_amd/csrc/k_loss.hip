@@ -107,10 +107,11 @@ __device__ __forceinline__ float grad_entry(const RowGrad& g, float x, float y, 
 // A row's scalar inputs of the policy loss.
 struct PolicyRow {
     int64_t action;
-    float w;
+    float w, old_logp, advantage, ref_logp;
     bool counts;
 };
 
+template <int KIND>
 __device__ __forceinline__ PolicyRow policy_row(const LossArgs& a, int64_t row)
 {
     PolicyRow r;
@@ -118,6 +119,9 @@ __device__ __forceinline__ PolicyRow policy_row(const LossArgs& a, int64_t row)
                : a.action_bytes == 4 ? (int64_t)((const int32_t*)a.actions)[row]
                                      : ((const int64_t*)a.actions)[row];
     r.w = a.weight ? a.weight[row] : a.row_weight;
+    r.old_logp = a.old_logp[row];
+    r.advantage = a.advantage[row];
+    r.ref_logp = KIND == kPolicy && a.ref_logp ? a.ref_logp[row] : 0.0f;
     r.counts = r.action >= 0 && r.action < a.A && r.w != 0.0f;
     if (r.counts && a.mask)
         r.counts = a.mask[row * a.mask_ld + r.action] != 0;
@@ -131,7 +135,7 @@ struct PolicyOut {
 // The loss of a row that counts and its gradient's coefficients; x_a: the action's
 // logit.
 template <int KIND>
-__device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, int64_t row, float w,
+__device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, const PolicyRow& row,
                                                    const Stats& st, float x_a, RowGrad& g)
 {
     PolicyOut o;
@@ -139,8 +143,8 @@ __device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, int64_t ro
     const float ln_s = logf(st.s), inv = 1.0f / st.s;
     o.logp = (x_a - m) - ln_s;
     o.entropy = ln_s - kLn2 * st.t * inv;
-    const float adv = a.advantage[row];
-    const float ratio = expf(o.logp - a.old_logp[row]);
+    const float adv = row.advantage, w = row.w;
+    const float ratio = expf(o.logp - row.old_logp);
     const float lo = 1.0f - a.clip_low, hi = 1.0f + a.clip_high;
     const float s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
     float slope = s1 <= s2 ? -s1 : s1 != s1 ? s1 : 0.0f;   // d loss / d log p[action]
@@ -152,7 +156,7 @@ __device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, int64_t ro
         o.kl = kLn2 * (st.t - st.v) * inv - ln_s + ln_sy;
         pull = a.kl_coef * (ln_sy - ln_s - o.kl);
     } else if (a.ref_logp) {
-        const float d = a.ref_logp[row] - o.logp;
+        const float d = row.ref_logp - o.logp;
         const float em = expm1f(d);
         o.kl = em - d;
         slope -= a.kl_coef * em;
@@ -288,36 +292,82 @@ struct SmallDiv {
 };
 
 // n rows of w values (rows ld apart) into LDS, value j of row r at r * w + j, or at
-// r * (w + 1) + j with PAD; -inf where the mask excludes an entry.
-template <bool PAD, typename E>
-__device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const uint8_t* mask,
-                                            int64_t mask_ld, int n, int w, float* to, int lane)
+// r * (w + 1) + j with PAD; -inf where the mask excludes an entry.  With BOTH a
+// second array of the same shape under the same mask goes along: a round of the
+// loop asks for everything it needs before it waits.
+template <bool PAD, bool BOTH, typename E>
+__device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const E* p2, int64_t ld2,
+                                            const uint8_t* mask, int64_t mask_ld, int n, int w,
+                                            float* to, float* to2, int lane)
 {
     constexpr int CH = kChunk<E>;
     const int count = n * w;
     const SmallDiv div(w);
-    if (ld == w && (!mask || mask_ld == w)) {
-        for (int i = lane * CH; i < count; i += 64 * CH) {
-            float v[CH];
-            unpack<E>(load_masked(p + i, count - i, mask ? mask + i : nullptr), v);
-            if (!PAD && i + CH <= count) {
+    auto put = [&](float* t, int i, u32x4 raw) {
+        float v[CH];
+        unpack<E>(raw, v);
+        if (!PAD && i + CH <= count) {
 #pragma unroll
-                for (int e = 0; e < CH; e += 4)
-                    *(f32x4*)(to + i + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-            } else {
+            for (int e = 0; e < CH; e += 4)
+                *(f32x4*)(t + i + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+        } else {
 #pragma unroll
-                for (int e = 0; e < CH; ++e)
-                    if (i + e < count)
-                        to[i + e + (PAD ? div(i + e) : 0)] = v[e];
+            for (int e = 0; e < CH; ++e)
+                if (i + e < count)
+                    t[i + e + (PAD ? div(i + e) : 0)] = v[e];
+        }
+    };
+    if (ld == w && (!BOTH || ld2 == w) && (!mask || mask_ld == w)) {
+        constexpr int U = 2;
+        for (int i0 = lane * CH; i0 < count; i0 += U * 64 * CH) {
+            u32x4 v[U], v2[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * 64 * CH;
+                v[u] = load_masked(p + i, count - i, mask ? mask + i : nullptr);
+                if (BOTH)
+                    v2[u] = load_masked(p2 + i, count - i, mask ? mask + i : nullptr);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * 64 * CH;
+                if (i < count) {
+                    put(to, i, v[u]);
+                    if (BOTH)
+                        put(to2, i, v2[u]);
+                }
             }
         }
         return;
     }
-    for (int i = lane; i < count; i += 64) {
-        const int r = div(i), j = i - r * w;
-        const bool legal = !mask || mask[r * mask_ld + j] != 0;
-        const float v = to_f32(p[r * ld + j]);
-        to[i + (PAD ? r : 0)] = legal ? v : kNegInf;
+    constexpr int U = 4;
+    for (int i0 = lane; i0 < count; i0 += U * 64) {
+        float v[U], v2[U];
+        int at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * 64;
+            v[u] = v2[u] = kNegInf;
+            at[u] = -1;
+            if (i < count) {
+                const int r = div(i), j = i - r * w;
+                const bool legal = !mask || mask[r * mask_ld + j] != 0;
+                const float x = to_f32(p[r * ld + j]);
+                v[u] = legal ? x : kNegInf;
+                if (BOTH) {
+                    const float y = to_f32(p2[r * ld2 + j]);
+                    v2[u] = legal ? y : kNegInf;
+                }
+                at[u] = i + (PAD ? r : 0);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (at[u] >= 0) {
+                to[at[u]] = v[u];
+                if (BOTH)
+                    to2[at[u]] = v2[u];
+            }
     }
 }
 
@@ -445,18 +495,22 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
         const int64_t left = a.rows - r0;
         const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
         const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
-        wave_lds_sync();
-        rows_to_lds<false>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld, mask, a.mask_ld, n, A, bx,
-                    lane);
-        if (KIND == kPolicyRef)
-            rows_to_lds<false>((const E*)a.ref_logits + r0 * a.ref_ld, a.ref_ld, mask, a.mask_ld, n, A,
-                        by, lane);
-        if (KIND == kDistill) {
-            rows_to_lds<true>(a.val + r0 * top, top, nullptr, 0, n, top, bv, lane);
-            rows_to_lds<true>((const float*)a.idx + r0 * top, top, nullptr, 0, n, top, bi, lane);
+        const int64_t row = r0 + lane;
+        PolicyRow pr{};
+        if (lane < n) {
+            if (KIND != kDistill)
+                pr = policy_row<KIND>(a, row);
+            else
+                pr.w = a.weight ? a.weight[row] : a.row_weight;
         }
         wave_lds_sync();
-        const int64_t row = r0 + lane;
+        rows_to_lds<false, KIND == kPolicyRef>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld,
+                                               (const E*)a.ref_logits + r0 * a.ref_ld, a.ref_ld,
+                                               mask, a.mask_ld, n, A, bx, by, lane);
+        if (KIND == kDistill)
+            rows_to_lds<true, true>(a.val + r0 * top, top, (const float*)a.idx + r0 * top, top,
+                                    nullptr, 0, n, top, bv, bi, lane);
+        wave_lds_sync();
         if (lane < n) {
             float* xr = bx + lane * A;
             float* yr = by + lane * A;
@@ -497,42 +551,39 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
                     add_entry<KIND>(st, x[j], KIND == kPolicyRef ? y[j] : 0.0f, m, my, c);
             }
             RowGrad g{};
-            PolicyRow pr{0, 0.0f, false};
             bool counts;
             float ts = 0.0f;   // distillation: sum of the teacher's exponentials
             if (KIND != kDistill) {
-                pr = policy_row(a, row);
                 counts = pr.counts && st.s != 0.0f;
                 PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
                 if (counts) {
-                    o = policy_finish<KIND>(a, row, pr.w, st, xr[pr.action], g);
+                    o = policy_finish<KIND>(a, pr, st, xr[pr.action], g);
                     total += (double)pr.w * o.loss;
                 }
                 store_policy(a, row, o);
             } else {
                 const float T = a.temperature;
-                pr.w = a.weight ? a.weight[row] : a.row_weight;
                 const float* v = bv + lane * ldt;
-                const float* ix = bi + lane * ldt;
+                float* ix = bi + lane * ldt;
                 float tm = kNegInf;
 #pragma unroll
                 for (int j = 0; j < NA; ++j)
                     y[j] = 0.0f;
                 row_write(yr, A, y);
-                // an entry counts if the mask left its logit's place (-inf logits that are
-                // legal count: the loss is then infinite)
-                auto index = [&](int k) {
+                // an entry counts if its index is a legal entry (-inf logits that are legal
+                // count: the loss is then infinite); the others' index becomes -1
+#pragma unroll 4
+                for (int k = 0; k < top; ++k) {
                     const int i = (int)__float_as_uint(ix[k]);
-                    const bool ok = i >= 0 && i < A && (!mask || mask[lane * a.mask_ld + i] != 0);
-                    return ok ? i : -1;
-                };
-                for (int k = 0; k < top; ++k)
-                    if (index(k) >= 0)
+                    if (i < 0 || i >= A || (mask && mask[lane * a.mask_ld + i] == 0))
+                        ix[k] = __uint_as_float(0xFFFFFFFFu);
+                    else
                         tm = fmaxf(tm, v[k]);
+                }
                 tm = tm == kNegInf ? 0.0f : tm;
                 float own = 0.0f, ce = 0.0f;   // sums of e b and e (x - m) over the list
                 for (int k = 0; k < top; ++k) {
-                    const int i = index(k);
+                    const int i = (int)__float_as_uint(ix[k]);
                     if (i < 0)
                         continue;
                     const float b = v[k] - tm, e = exp2_hw(b * c);
@@ -885,10 +936,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t row = tile * ROWS + slot;
         const bool live = row < a.rows;
-        PolicyRow pr{0, 0.0f, false};
+        PolicyRow pr{};
         if (live) {
             if (KIND != kDistill) {
-                pr = policy_row(a, row);
+                pr = policy_row<KIND>(a, row);
             } else {
                 pr.w = a.weight ? a.weight[row] : a.row_weight;
                 pr.counts = pr.w != 0.0f;
@@ -929,7 +980,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         if (KIND != kDistill) {
             PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
             if (counts)
-                o = policy_finish<KIND>(a, row, pr.w, st, to_f32(px[pr.action]), g);
+                o = policy_finish<KIND>(a, pr, st, to_f32(px[pr.action]), g);
             if (live && lane == 0) {
                 if (counts)
                     total += (double)pr.w * o.loss;
@@ -998,9 +1049,9 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
         const int q0 = PHASE == 0 ? 0 : part * a.part_chunks;
         const int chunks = (a.A + CH - 1) / CH;
         const int q1 = PHASE == 0 || q0 + a.part_chunks > chunks ? chunks : q0 + a.part_chunks;
-        PolicyRow pr{0, 0.0f, false};
+        PolicyRow pr{};
         if (KIND != kDistill) {
-            pr = policy_row(a, row);
+            pr = policy_row<KIND>(a, row);
         } else {
             pr.w = a.weight ? a.weight[row] : a.row_weight;
             pr.counts = pr.w != 0.0f;
@@ -1052,7 +1103,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
         if (KIND != kDistill) {
             PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
             if (counts)
-                o = policy_finish<KIND>(a, row, pr.w, st, to_f32(px[pr.action]), g);
+                o = policy_finish<KIND>(a, pr, st, to_f32(px[pr.action]), g);
             if (tid == 0 && part == 0) {
                 if (counts)
                     total += (double)pr.w * o.loss;
