@@ -329,8 +329,10 @@ struct TileLoader {
     uint32_t off[NI];    // kDirect: byte offset from the tile's start, or kNoOffset
     // else: this thread's chunks of the next tile, in the operand and in the values
     // before the activation, and how many of their elements are rows of the operand
+    // (KC: rows behind the last repeat it; what they give is not written)
     const E *at[NI], *pre[NI];
     int valid[NI];
+    bool whole;          // every chunk of the tile's rows is
     int k[NI];           // first k of the chunk in the tile
     int64_t step, pre_step;
     int act;
@@ -357,14 +359,16 @@ struct TileLoader {
                              ? (uint32_t)(((int64_t)rr * ld + c * CH) * (int64_t)sizeof(E))
                              : kNoOffset;
             } else {
-                const int64_t r = KC ? row : k0 + k[i], col = KC ? k0 + k[i] : row;
+                const int64_t r = KC ? (row < n_rows ? row : n_rows - 1) : k0 + k[i];
+                const int64_t col = KC ? k0 + k[i] : row;
                 at[i] = base + r * ld + col;
                 if (LOAD == kFused)
                     pre[i] = (const E*)z.p + g * z.gs + (KC ? r0 * z.ld : r0) + r * z.ld + col;
                 const int left = n_rows - row;
-                valid[i] = KC ? (left > 0 ? CH : 0) : left < 0 ? 0 : left > CH ? CH : left;
+                valid[i] = KC || left > CH ? CH : left < 0 ? 0 : left;
             }
         }
+        whole = KC || n_rows >= BR;
     }
 
     // kDirect: the chunks of the tile at k0; a wavefront's 64 chunks are
@@ -387,23 +391,32 @@ struct TileLoader {
     // kStaged, kFused: the next tile's chunks into registers; `left`: k from its first on
     __device__ __forceinline__ void load(int64_t left)
     {
+        if (whole && left >= kBK<E>) {   // (the same for the whole workgroup)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                reg[i] = *(const u32x4_any*)at[i];
+                if (LOAD == kFused)
+                    reg_z[i] = *(const u32x4_any*)pre[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                int n = valid[i];
+                const int kl = (int)(left < kBK<E> ? left : kBK<E>) - k[i];
+                if (KC)
+                    n = kl < 0 ? 0 : kl < CH ? kl : CH;
+                else if (kl <= 0)
+                    n = 0;
+                reg[i] = n > 0 ? load_chunk(at[i], n) : u32x4{0, 0, 0, 0};
+                if (LOAD == kFused)
+                    reg_z[i] = n > 0 ? load_chunk(pre[i], n) : u32x4{0, 0, 0, 0};
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            int n = valid[i];
-            if (left < kBK<E>) {
-                const int kl = (int)left - k[i];
-                n = KC ? (n == 0 || kl < 0 ? 0 : kl < CH ? kl : CH) : kl > 0 ? n : 0;
-            }
-            reg[i] = u32x4{0, 0, 0, 0};
-            if (n > 0)
-                reg[i] = load_chunk(at[i], n);
             at[i] += step;
-            if constexpr (LOAD == kFused) {
-                reg_z[i] = u32x4{0, 0, 0, 0};
-                if (n > 0)
-                    reg_z[i] = load_chunk(pre[i], n);
+            if (LOAD == kFused)
                 pre[i] += pre_step;
-            }
         }
     }
     __device__ __forceinline__ void store(char* tile, int tid)
