@@ -698,9 +698,9 @@ def _empty(shape, dtype, device, stream):
     allocator hands memory out again in the order of one stream only)."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 def _dtype_code(t, what):
@@ -735,9 +735,10 @@ def _mat(t, dtype, G, rows, cols, what, out: bool = False):
 
 
 def _on_device(names, *tensors):
-    for t, what in zip(names.split(), tensors):
-        if what is not None and not what.is_cuda:
-            raise ArgumentError(f"{t}: expected a device tensor, got one on {what.device}")
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            what = next(n for n, u in zip(names.split(), tensors) if u is t)
+            raise ArgumentError(f"{what}: expected a device tensor, got one on {t.device}")
 
 
 def _layer(x, w, act):
@@ -778,7 +779,7 @@ def _workspace(need, work, device, stream):
         return work.data_ptr(), work.numel() * work.element_size(), work
     if not need:
         return None, 0, None
-    work = _empty(need, torch.uint8, device, stream)
+    work = _empty((need,), torch.uint8, device, stream)
     return work.data_ptr(), need, work
 
 
@@ -915,7 +916,7 @@ def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
                total, stats, dlogits)
     dev = logits.device
     if total is None:
-        total = _empty(1, f32, dev, stream)
+        total = _empty((1,), f32, dev, stream)
     if stats is None:
         stats = _empty((4, n), f32, dev, stream)
     if not grad:
@@ -954,9 +955,9 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
                teacher_idx, teacher_logits, mask, weight, total, loss, dlogits)
     dev = logits.device
     if total is None:
-        total = _empty(1, f32, dev, stream)
+        total = _empty((1,), f32, dev, stream)
     if loss is None:
-        loss = _empty(n, f32, dev, stream)
+        loss = _empty((n,), f32, dev, stream)
     if not grad:
         dlogits = None
     elif dlogits is None:

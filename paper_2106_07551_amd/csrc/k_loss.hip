@@ -1026,8 +1026,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
 
 // PHASE 0: a workgroup takes a row whole, once for its sums and once for its
 // gradient (the second time from the caches).  PHASE 1: the sums of one of
-// `splits` parts of a row, into a.part; PHASE 2: the parts merged (in order, by every
-// workgroup alike) and the gradient of one part.
+// `splits` parts of a row, into a.part; PHASE 2: the parts merged (by every workgroup
+// alike) and the gradient of one part.
 constexpr int kLongThreads = 512, kLongUnroll = 4;
 
 template <typename E, int KIND, int PHASE>
@@ -1083,8 +1083,10 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
                 continue;
             }
         } else {
-            for (int i = 0; i < a.splits; ++i)
+            // (each thread takes every T-th part, then as within a row)
+            for (int i = tid; i < a.splits; i += T)
                 st = merge<KIND>(st, ((const Stats*)a.part)[row * a.splits + i], c);
+            st = group_merge<T, KIND>(st, c, scratch, nullptr, counts);
         }
         float from_list = 0.0f;
         if (KIND == kDistill) {

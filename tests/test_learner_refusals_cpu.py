@@ -35,8 +35,9 @@ def _linear(L, *, dtype=B.DT_BF16, act=B.ACT_NONE, groups=1, rows=8, n_in=16, n_
     (dict(groups=2, y=B.Mat(P, 24, 24)), b"overlap"),
     (dict(groups=2, pre=B.Mat(P, 24, 100)), b"overlap"),
     (dict(bias=P + 2), b"bias"), (dict(residual=B.Mat(P + 1, 24, 0)), b"residual"),
-    (dict(n_in=4096), b"workspace"), (dict(n_in=4096, work=P, nbytes=16), b"workspace"),
-    (dict(n_in=4096, work=P + 8, nbytes=1 << 30), b"16 bytes"),
+    (dict(rows=64, n_in=65536), b"workspace"),
+    (dict(rows=64, n_in=65536, work=P, nbytes=16), b"workspace"),
+    (dict(rows=64, n_in=65536, work=P + 8, nbytes=1 << 30), b"16 bytes"),
 ])
 def test_linear_refuses(kw, word):
     L = M.lib()
