@@ -61,13 +61,35 @@ __device__ __forceinline__ u32x4 pack(const float (&f)[kChunk<E>])
     return v;
 }
 
-// The first `n` elements of the chunk at p (zeros behind them; nothing behind
-// them is read).
+// v without its first `s` elements (0 <= s <= a chunk's), zeros behind the rest.
 template <typename E>
-__device__ __forceinline__ u32x4 load_chunk(const E* p, int n)
+__device__ __forceinline__ u32x4 drop_front(u32x4 v, int s)
 {
-    if (n >= kChunk<E>)
-        return *(const u32x4_any*)p;
+    const int bits = s * 8 * (int)sizeof(E);
+    uint64_t lo = (uint64_t)v[0] | (uint64_t)v[1] << 32, hi = (uint64_t)v[2] | (uint64_t)v[3] << 32;
+    if (bits >= 64) {
+        lo = bits >= 128 ? 0 : hi >> (bits - 64);
+        hi = 0;
+    } else if (bits > 0) {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// The first n (>= 1) elements of the chunk at p, zeros behind them.  Nothing behind
+// them is read: a short chunk is the end of the 16 bytes before its own end, where
+// `before` elements in front of p make that possible, and is read element by element
+// only in arrays shorter than a chunk.  (Element by element everywhere, a row's short
+// end cost its wavefront up to eight loads one after the other.)
+template <typename E>
+__device__ __forceinline__ u32x4 load_chunk(const E* p, int n, int64_t before)
+{
+    const int short_by = n < kChunk<E> ? kChunk<E> - n : 0;
+    if (short_by <= before) {
+        const u32x4 v = *(const u32x4_any*)(p - short_by);
+        return short_by ? drop_front<E>(v, short_by) : v;
+    }
     u32x4 v = {0, 0, 0, 0};
     if constexpr (sizeof(E) == 4) {
 #pragma unroll

@@ -113,7 +113,7 @@ __device__ __forceinline__ void load_bias(const GemmArgs& a, int g, int64_t n, i
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
         const u32x4 t = a.bias && cnt > i
-                            ? load_chunk(a.bias + (int64_t)g * a.N + n + i, cnt - i)
+                            ? load_chunk(a.bias + (int64_t)g * a.N + n + i, cnt - i, n + i)
                             : u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -125,7 +125,7 @@ template <typename E>
 __device__ __forceinline__ u32x4 load_residual(const GemmArgs& a, int g, int64_t m, int64_t n,
                                                int cnt)
 {
-    return load_chunk((const E*)a.res.p + g * a.res.gs + m * a.res.ld + n, cnt);
+    return load_chunk((const E*)a.res.p + g * a.res.gs + m * a.res.ld + n, cnt, n);
 }
 
 // One chunk of an output row: columns n .. n + cnt - 1 of row m of group g.
@@ -328,19 +328,24 @@ struct TileLoader {
     int64_t ld;
     uint32_t off[NI];    // kDirect: byte offset from the tile's start, or kNoOffset
     // else: this thread's chunks of the next tile, in the operand and in the values
-    // before the activation, and how many of their elements are rows of the operand
-    // (KC: rows behind the last repeat it; what they give is not written)
+    // before the activation.  What lies behind the operand's end is not read: rows
+    // (KC) behind the last repeat it, as what they give is not written; a chunk that
+    // crosses the end is read from the last 16 bytes before it, and the first `drop`
+    // elements dropped (all of them: not read).  An operand narrower than a chunk goes
+    // element by element.
     const E *at[NI], *pre[NI];
-    int valid[NI];
-    bool whole;          // every chunk of the tile's rows is
+    int drop[NI];
+    bool narrow, trim;   // (the same for the whole workgroup)
     int k[NI];           // first k of the chunk in the tile
     int64_t step, pre_step;
     int act;
     u32x4 reg[LOAD == kDirect ? 1 : NI], reg_z[LOAD == kFused ? NI : 1];
+    int cut[LOAD == kDirect ? 1 : NI];   // elements to drop from what `reg` holds
+    bool cuts;
 
-    // the first tile starts at k0
+    // R rows by K; the first tile starts at k0
     __device__ __forceinline__ TileLoader(const MatArg& m, const MatArg& z, int act_, int g,
-                                          int64_t r0, int R, int64_t k0, int tid)
+                                          int64_t r0, int R, int K, int64_t k0, int tid)
     {
         ld = m.ld;
         base = (const E*)m.p + g * m.gs + (KC ? r0 * m.ld : r0);
@@ -348,6 +353,7 @@ struct TileLoader {
         step = KC ? kBK<E> : kBK<E> * m.ld;
         pre_step = KC ? kBK<E> : kBK<E> * z.ld;
         const int n_rows = (int)(R - r0);   // rows of the operand from the tile's first on
+        narrow = (KC ? K : (int64_t)R) < CH;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             int rr, c;
@@ -359,16 +365,19 @@ struct TileLoader {
                              ? (uint32_t)(((int64_t)rr * ld + c * CH) * (int64_t)sizeof(E))
                              : kNoOffset;
             } else {
+                const int last = n_rows - CH;   // (RC; below 0 also where the operand is wider)
                 const int64_t r = KC ? (row < n_rows ? row : n_rows - 1) : k0 + k[i];
-                const int64_t col = KC ? k0 + k[i] : row;
+                const int64_t col = KC ? k0 + k[i] : narrow ? row : row < last ? row : last;
                 at[i] = base + r * ld + col;
                 if (LOAD == kFused)
                     pre[i] = (const E*)z.p + g * z.gs + (KC ? r0 * z.ld : r0) + r * z.ld + col;
-                const int left = n_rows - row;
-                valid[i] = KC || left > CH ? CH : left < 0 ? 0 : left;
+                const int behind = KC || narrow || row <= last ? 0 : row - last;
+                drop[i] = behind < CH ? behind : CH;
+                if (narrow && !KC)   // elements that are there
+                    drop[i] = n_rows - row;
             }
         }
-        whole = KC || n_rows >= BR;
+        trim = !KC && n_rows < BR;
     }
 
     // kDirect: the chunks of the tile at k0; a wavefront's 64 chunks are
@@ -388,10 +397,23 @@ struct TileLoader {
         }
     }
 
-    // kStaged, kFused: the next tile's chunks into registers; `left`: k from its first on
+    // kStaged, kFused: the next tile's chunks into registers; `left` (> 0): k from its
+    // first on
     __device__ __forceinline__ void load(int64_t left)
     {
-        if (whole && left >= kBK<E>) {   // (the same for the whole workgroup)
+        const bool end = left < kBK<E>;   // the tile ends with k
+        cuts = trim || end;
+        if (narrow) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int kl = (int)(end ? left : kBK<E>) - k[i];
+                const int n = KC ? kl : kl > 0 ? drop[i] : 0;
+                reg[i] = n > 0 ? load_chunk(at[i], n, 0) : u32x4{0, 0, 0, 0};
+                if (LOAD == kFused)
+                    reg_z[i] = n > 0 ? load_chunk(pre[i], n, 0) : u32x4{0, 0, 0, 0};
+                cut[i] = 0;
+            }
+        } else if (!cuts) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 reg[i] = *(const u32x4_any*)at[i];
@@ -401,15 +423,26 @@ struct TileLoader {
         } else {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                int n = valid[i];
-                const int kl = (int)(left < kBK<E> ? left : kBK<E>) - k[i];
-                if (KC)
-                    n = kl < 0 ? 0 : kl < CH ? kl : CH;
-                else if (kl <= 0)
-                    n = 0;
-                reg[i] = n > 0 ? load_chunk(at[i], n) : u32x4{0, 0, 0, 0};
+                int over = 0;   // KC: elements of the chunk behind the end of k
+                cut[i] = KC ? 0 : drop[i];
+                if (end) {
+                    const int rest = (int)left;
+                    if (KC) {
+                        over = k[i] + CH - rest;
+                        over = over < 0 ? 0 : over;
+                        cut[i] = over < CH ? over : CH;
+                    } else if (k[i] >= rest) {
+                        cut[i] = CH;
+                    }
+                }
+                reg[i] = u32x4{0, 0, 0, 0};
                 if (LOAD == kFused)
-                    reg_z[i] = n > 0 ? load_chunk(pre[i], n) : u32x4{0, 0, 0, 0};
+                    reg_z[i] = u32x4{0, 0, 0, 0};
+                if (cut[i] < CH) {
+                    reg[i] = *(const u32x4_any*)(at[i] - over);
+                    if (LOAD == kFused)
+                        reg_z[i] = *(const u32x4_any*)(pre[i] - over);
+                }
             }
         }
 #pragma unroll
@@ -430,6 +463,8 @@ struct TileLoader {
                 times_slope(act, z, v);
                 reg[i] = pack<E>(v);
             }
+            if (cuts)
+                reg[i] = drop_front<E>(reg[i], cut[i]);
             *(u32x4*)(tile + (tid + i * THREADS) * 16) = reg[i];
         }
     }
@@ -494,9 +529,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
     const int64_t ke = kb + a.k_split < a.K ? kb + a.k_split : a.K;
     const int n_k = (int)((ke - kb + kBK<E> - 1) / kBK<E>);
 
-    TileLoader<E, AKC, TILE, S::kThreads, LOAD> la(a.a, a.a_pre, a.a_act, g, m0, a.M, kb, tid);
+    TileLoader<E, AKC, TILE, S::kThreads, LOAD> la(a.a, a.a_pre, a.a_act, g, m0, a.M, a.K, kb,
+                                                        tid);
     TileLoader<E, BKC, TILE, S::kThreads, LOAD == kFused ? kStaged : LOAD> lb(a.b, a.b, 0, g, n0,
-                                                                              a.N, kb, tid);
+                                                                              a.N, a.K, kb, tid);
 
     f32x16 acc[TM][TN], sum[kSums ? TM : 1];
 #pragma unroll
@@ -737,8 +773,9 @@ __global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a)
             const int n = left > 0 ? (int)(left < CH ? left : CH) : 0;
             vw[i] = vx[i] = u32x4{0, 0, 0, 0};
             if (n > 0) {
-                vw[i] = load_chunk(w + p * PIECE + i * 4 * CH, n);
-                vx[i] = load_chunk(x + p * PIECE + i * 4 * CH, n);
+                const int64_t k = p * PIECE + i * 4 * CH;
+                vw[i] = load_chunk(w + k, n, k + h * CH);
+                vx[i] = load_chunk(x + k, n, k + h * CH);
             }
         }
         product(vw, vx);
@@ -894,10 +931,10 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
     if (cnt > 0) {
         for (int64_t m = r0 + ry; m < r1; m += kDzRows) {
             float v[CH];
-            unpack<E>(load_chunk((const E*)dy.p + g * dy.gs + m * dy.ld + n, cnt), v);
+            unpack<E>(load_chunk((const E*)dy.p + g * dy.gs + m * dy.ld + n, cnt, n), v);
             if (act != MALIB_ACT_NONE) {
                 float z[CH];
-                unpack<E>(load_chunk((const E*)pre.p + g * pre.gs + m * pre.ld + n, cnt), z);
+                unpack<E>(load_chunk((const E*)pre.p + g * pre.gs + m * pre.ld + n, cnt, n), z);
                 times_slope(act, z, v);
                 if (dz.p)
                     store_chunk((E*)dz.p + g * dz.gs + m * dz.ld + n, cnt, pack<E>(v));

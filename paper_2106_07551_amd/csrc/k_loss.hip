@@ -240,11 +240,12 @@ __device__ __forceinline__ void exclude(u32x4& v, int i, bool out)
 }
 
 typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint64_t u64_any __attribute__((aligned(1)));
 
-// Raw chunk of a row with n entries left, with -inf in the entries behind the row's
-// end and those that are not legal.
+// Chunk at p of a row of which n entries are left and `before` lie in front, with -inf
+// in the entries behind the row's end and those that are not legal.
 template <typename E>
-__device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* mask)
+__device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* mask, int64_t before)
 {
     constexpr int CH = kChunk<E>;
     if (n >= CH) {
@@ -261,10 +262,24 @@ __device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* m
         }
         return v;
     }
-    u32x4 v = n > 0 ? load_chunk(p, n) : u32x4{0, 0, 0, 0};
+    u32x4 v = {0, 0, 0, 0};
+    uint64_t m = 0;   // bit 8 i up: entry i is legal
+    if (n > 0) {
+        v = load_chunk(p, n, before);
+        m = ~0ull >> (64 - 8 * n);
+        if (mask) {
+            if (before + n >= 8) {   // the 8 bytes before the row's end
+                m = *(const u64_any*)(mask + n - 8) >> (64 - 8 * n);
+            } else {
+                m = 0;
+                for (int i = 0; i < n; ++i)
+                    m |= (uint64_t)mask[i] << (8 * i);
+            }
+        }
+    }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        exclude<E>(v, i, i >= n || (mask && i < n && mask[i] == 0));
+        exclude<E>(v, i, ((uint32_t)(m >> (32 * (i / 4))) >> (8 * (i % 4)) & 0xFFu) == 0);
     return v;
 }
 
@@ -324,9 +339,9 @@ __device__ __forceinline__ void rows_to_lds(const E* p, int64_t ld, const E* p2,
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * 64 * CH;
-                v[u] = load_masked(p + i, count - i, mask ? mask + i : nullptr);
+                v[u] = load_masked(p + i, count - i, mask ? mask + i : nullptr, i);
                 if (BOTH)
-                    v2[u] = load_masked(p2 + i, count - i, mask ? mask + i : nullptr);
+                    v2[u] = load_masked(p2 + i, count - i, mask ? mask + i : nullptr, i);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -954,9 +969,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         for (int i = 0; i < C; ++i) {
             const int j = (lane + i * T) * CH;
             const int n = counts ? a.A - j : 0;
-            x[i] = load_masked(px + j, n, pm ? pm + j : nullptr);
+            x[i] = load_masked(px + j, n, pm ? pm + j : nullptr, j);
             if (KIND == kPolicyRef)
-                y[i] = load_masked(py + j, n, pm ? pm + j : nullptr);
+                y[i] = load_masked(py + j, n, pm ? pm + j : nullptr, j);
         }
         const int used = (a.A + T * CH - 1) / (T * CH);   // chunks that any thread holds
         float part = 0.0f;
@@ -1069,9 +1084,9 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
                     for (int u = 0; u < U; ++u) {
                         const int j = (q + u * T) * CH;
                         const int n = q + u * T < q1 ? a.A - j : 0;
-                        x[u] = load_masked(px + j, n, pm ? pm + j : nullptr);
+                        x[u] = load_masked(px + j, n, pm ? pm + j : nullptr, j);
                         if (KIND == kPolicyRef)
-                            y[u] = load_masked(py + j, n, pm ? pm + j : nullptr);
+                            y[u] = load_masked(py + j, n, pm ? pm + j : nullptr, j);
                     }
                     st = merge<KIND>(st, chunk_stats<E, KIND, U>(x, y, U, c), c);
                 }
@@ -1131,9 +1146,9 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
                 for (int u = 0; u < U; ++u) {
                     const int j = (q + u * T) * CH;
                     const int n = counts && q + u * T < q1 ? a.A - j : 0;
-                    x[u] = load_masked(px + j, n, pm ? pm + j : nullptr);
+                    x[u] = load_masked(px + j, n, pm ? pm + j : nullptr, j);
                     if (KIND == kPolicyRef)
-                        y[u] = load_masked(py + j, n, pm ? pm + j : nullptr);
+                        y[u] = load_masked(py + j, n, pm ? pm + j : nullptr, j);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
