@@ -185,15 +185,6 @@ __device__ __forceinline__ void store_policy(const LossArgs& a, int64_t row, con
     a.stats[3 * a.rows + row] = o.entropy;
 }
 
-// Whether entry k of a row's list counts: its index (or -1).
-__device__ __forceinline__ int list_index(const LossArgs& a, int64_t row, int k)
-{
-    const int i = a.idx[row * a.top + k];
-    if (i < 0 || i >= a.A || (a.mask && a.mask[row * a.mask_ld + i] == 0))
-        return -1;
-    return i;
-}
-
 // Sum of one value per thread over the workgroup (in a fixed order), in thread 0.
 template <int THREADS>
 __device__ __forceinline__ double block_sum(double v)
@@ -839,10 +830,17 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const RowGrad& g, 
 
 // The teacher's list of a row, handled by TL lanes (the row's own, or its first
 // wavefront): index (-1 where an entry does not count), probability and the
-// student's logit of each entry, in LDS.
+// student's logit of each entry, in LDS, and two bitmaps over the indices, `seen` and
+// `twice`: bits that an entry, or more than one, falls on.  Rows in registers have a
+// bit for each of their entries; longer ones share bits, so that a bit in `twice` says
+// only that the list has to be searched.
+template <int T>
 struct List {
+    static constexpr int kWords = T <= 64 ? T : 256;
+    static constexpr int kRows = T < 256 ? 256 / T : 1;   // per workgroup
     int* i;
     float *p, *x;
+    uint32_t *seen, *twice;
     int top, padded;   // padded: top rounded up to 4
 
     __device__ __forceinline__ List(void* lds, int slot, int top_)
@@ -851,25 +849,67 @@ struct List {
         i = (int*)lds + slot * padded * 3;
         p = (float*)(i + padded);
         x = p + padded;
+        seen = (uint32_t*)lds + kRows * padded * 3 + slot * 2 * kWords;
+        twice = seen + kWords;
     }
+    __device__ __forceinline__ static uint32_t word(int i)
+    {
+        return (uint32_t)i / 32 % (uint32_t)kWords;
+    }
+    __device__ __forceinline__ static uint32_t bit(int i) { return 1u << (i & 31); }
 };
-constexpr int list_bytes(int top) { return ((top + 3) & ~3) * 12; }
+// of a workgroup's lists
+constexpr int list_bytes(int top, int rows) { return (((top + 3) & ~3) * 12) * rows + 2 * 256 * 4; }
 
 // Loads the list and forms the probabilities.  Returns whether any entry counts (in
-// the TL lanes).  `part`: this lane's sum of t ln t.
-template <typename E, int TL>
-__device__ __forceinline__ bool load_list(const LossArgs& a, const List& l, int64_t row, int lane,
-                                          bool live_row, float c, float& part)
+// the TL lanes): its index is a legal entry.  `part`: this lane's sum of t ln t.
+template <typename E, int T>
+__device__ __forceinline__ bool load_list(const LossArgs& a, const List<T>& l, int64_t row,
+                                          int lane, bool live_row, float c, float& part)
 {
+    constexpr int TL = T < 64 ? T : 64, U = 4;
+    for (int w = lane; w < List<T>::kWords; w += TL)
+        l.seen[w] = l.twice[w] = 0;
+    wave_lds_sync();
     const E* x = (const E*)a.logits + row * a.logits_ld;
+    const uint8_t* mask = a.mask ? a.mask + row * a.mask_ld : nullptr;
     float tm = kNegInf;
-    for (int k = lane; k < l.padded; k += TL) {
-        const int i = live_row && k < l.top ? list_index(a, row, k) : -1;
-        const float v = i >= 0 ? a.val[row * a.top + k] : kNegInf;
-        l.i[k] = i;
-        l.p[k] = v;
-        l.x[k] = i >= 0 ? to_f32(x[i]) : 0.0f;
-        tm = i >= 0 ? fmaxf(tm, v) : tm;
+    for (int k0 = lane; k0 < l.padded; k0 += U * TL) {
+        int i[U];
+        float v[U], f[U];
+        bool in[U];
+        if (live_row) {   // (entries behind the list's end read its last)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + u * TL < l.top ? k0 + u * TL : l.top - 1;
+                i[u] = a.idx[row * a.top + k];
+                v[u] = a.val[row * a.top + k];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                in[u] = k0 + u * TL < l.top && i[u] >= 0 && i[u] < a.A;
+                const int j = in[u] ? i[u] : 0;
+                f[u] = to_f32(x[j]);
+                if (mask)
+                    in[u] = in[u] && mask[j] != 0;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u * TL;
+            if (k >= l.padded)
+                break;
+            const bool ok = live_row && in[u];
+            l.i[k] = ok ? i[u] : -1;
+            l.p[k] = ok ? v[u] : kNegInf;
+            l.x[k] = ok ? f[u] : 0.0f;
+            if (ok) {
+                tm = fmaxf(tm, v[u]);
+                const uint32_t w = l.word(i[u]), b = l.bit(i[u]);
+                if (a.dlogits && (atomicOr(l.seen + w, b) & b))
+                    atomicOr(l.twice + w, b);
+            }
+        }
     }
     tm = lanes_combine<TL>(tm, MaxOp());
     tm = tm == kNegInf ? 0.0f : tm;
@@ -891,10 +931,11 @@ __device__ __forceinline__ bool load_list(const LossArgs& a, const List& l, int6
 }
 
 // The row's loss in the TL lanes, from load_list's part.
-template <int TL>
-__device__ __forceinline__ float list_loss(const LossArgs& a, const List& l, int lane, float part,
-                                           float m, float ln_s)
+template <int T>
+__device__ __forceinline__ float list_loss(const LossArgs& a, const List<T>& l, int lane,
+                                           float part, float m, float ln_s)
 {
+    constexpr int TL = T < 64 ? T : 64;
     for (int k = lane; k < l.padded; k += TL)
         if (l.p[k] != 0.0f)
             part -= l.p[k] * ((l.x[k] - m) / a.temperature - ln_s);
@@ -902,31 +943,30 @@ __device__ __forceinline__ float list_loss(const LossArgs& a, const List& l, int
 }
 
 // The entries' part of the gradient, over what write_grad left there: an index that
-// the list holds more than once is written by its first entry with the sum of all.
-template <typename E, int TL>
-__device__ __forceinline__ void write_list(const LossArgs& a, const List& l, const RowGrad& g,
+// the list holds more than once is written by its first entry with the sum of all, in
+// their order.
+template <typename E, int T>
+__device__ __forceinline__ void write_list(const LossArgs& a, const List<T>& l, const RowGrad& g,
                                            int64_t row, int lane, float c, float w, int j_lo,
                                            int j_hi)
 {
+    constexpr int TL = T < 64 ? T : 64;
     E* o = (E*)a.dlogits + row * a.dlogits_ld;
     for (int k = lane; k < l.top; k += TL) {
         const int i = l.i[k];
         if (i < j_lo || i >= j_hi)
             continue;
-        int before = 0, after = 0;   // entries of the same index
-        for (int q = 0; q < l.padded; q += 4) {
-            const int4 e = *(const int4*)(l.i + q);
-            const int n0 = e.x == i, n1 = e.y == i, n2 = e.z == i, n3 = e.w == i;
-            before += (n0 & (q < k)) + (n1 & (q + 1 < k)) + (n2 & (q + 2 < k)) + (n3 & (q + 3 < k));
-            after += n0 + n1 + n2 + n3;
-        }
-        if (before)
-            continue;
         float p = l.p[k];
-        if (after > 1) {
-            for (int q = k + 1; q < l.top; ++q)
-                if (l.i[q] == i)
-                    p += l.p[q];
+        if (l.twice[l.word(i)] & l.bit(i)) {
+            bool first = true;
+            for (int q = 0; q < l.top; ++q) {
+                if (q == k || l.i[q] != i)
+                    continue;
+                first = first && q > k;
+                p += l.p[q];
+            }
+            if (!first)
+                continue;
         }
         o[i] = from_f32<E>(grad_entry<kDistill>(g, l.x[k], 0.0f, c) - w * a.temperature * p);
     }
@@ -942,7 +982,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
     __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
     constexpr int TL = T < 64 ? T : 64;
-    const List list(lds, slot, KIND == kDistill ? a.top : 0);
+    const List<T> list(lds, slot, KIND == kDistill ? a.top : 0);
     __shared__ int any_entry;
     const bool lists = KIND == kDistill && lane < TL;
     const float c = kLog2e / a.temperature;
@@ -979,7 +1019,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
             // (the group's other wavefronts learn from LDS whether the list counts: written
             // before the barriers of the merge, read between them)
             wave_lds_sync();
-            const bool any = load_list<E, TL>(a, list, row, lane, counts, c, part);
+            const bool any = load_list<E>(a, list, row, lane, counts, c, part);
             if (T > 64) {
                 if (lane == 0)
                     any_entry = any;
@@ -1006,7 +1046,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
             g.c0 = pr.w * a.temperature / st.s;
             float loss = 0.0f;
             if (lists)
-                loss = list_loss<TL>(a, list, lane, part, g.m, logf(st.s));
+                loss = list_loss(a, list, lane, part, g.m, logf(st.s));
             if (live && lane == 0) {
                 if (counts)
                     total += (double)pr.w * loss;
@@ -1030,7 +1070,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         if (KIND == kDistill && a.dlogits) {
             group_sync<T>();
             if (counts && lists)
-                write_list<E, TL>(a, list, g, row, lane, c, pr.w, 0, a.A);
+                write_list<E>(a, list, g, row, lane, c, pr.w, 0, a.A);
         }
     }
     if (a.total)
@@ -1052,7 +1092,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
     extern __shared__ float lds[];
     __shared__ float scratch[2 * kScratch];
     const int tid = threadIdx.x;
-    const List list(lds, 0, KIND == kDistill ? a.top : 0);
+    const List<T> list(lds, 0, KIND == kDistill ? a.top : 0);
     __shared__ int any_entry;
     const bool lists = KIND == kDistill && tid < 64;
     const float c = kLog2e / a.temperature;
@@ -1107,7 +1147,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
         if (KIND == kDistill) {
             __syncthreads();   // (the last row's flag has been read)
             if (lists) {
-                const bool any = load_list<E, 64>(a, list, row, tid, counts, c, from_list);
+                const bool any = load_list<E>(a, list, row, tid, counts, c, from_list);
                 if (tid == 0)
                     any_entry = any;
                 wave_lds_sync();
@@ -1131,7 +1171,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
             g.c0 = pr.w * a.temperature / st.s;
             float loss = 0.0f;
             if (lists)
-                loss = list_loss<64>(a, list, tid, from_list, g.m, logf(st.s));
+                loss = list_loss(a, list, tid, from_list, g.m, logf(st.s));
             if (tid == 0 && part == 0) {
                 if (counts)
                     total += (double)pr.w * loss;
@@ -1159,7 +1199,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
             if (KIND == kDistill) {
                 __syncthreads();
                 if (counts && lists)
-                    write_list<E, 64>(a, list, g, row, tid, c, pr.w, q0 * CH, q1 * CH);
+                    write_list<E>(a, list, g, row, tid, c, pr.w, q0 * CH, q1 * CH);
             }
         }
     }
@@ -1180,7 +1220,8 @@ __global__ __launch_bounds__(256) void loss_total_kernel(const double* part, int
 template <typename E, int KIND>
 hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
 {
-    const size_t list = KIND == kDistill ? (size_t)list_bytes(a.top) : 0;
+    const int top = a.top;
+    auto list = [top](int rows) { return KIND == kDistill ? (size_t)list_bytes(top, rows) : 0; };
     const unsigned nb = (unsigned)p.blocks;
     switch (p.variant) {
     case kLossLane: {
@@ -1198,36 +1239,36 @@ hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
     case kLossRow:
         switch (p.group) {
         case 4:
-            loss_row_kernel<E, KIND, 4, 4><<<nb, 256, list * 64, s>>>(a);
+            loss_row_kernel<E, KIND, 4, 4><<<nb, 256, list(64), s>>>(a);
             break;
         case 8:
-            loss_row_kernel<E, KIND, 8, 4><<<nb, 256, list * 32, s>>>(a);
+            loss_row_kernel<E, KIND, 8, 4><<<nb, 256, list(32), s>>>(a);
             break;
         case 16:
-            loss_row_kernel<E, KIND, 16, 4><<<nb, 256, list * 16, s>>>(a);
+            loss_row_kernel<E, KIND, 16, 4><<<nb, 256, list(16), s>>>(a);
             break;
         case 32:
-            loss_row_kernel<E, KIND, 32, 4><<<nb, 256, list * 8, s>>>(a);
+            loss_row_kernel<E, KIND, 32, 4><<<nb, 256, list(8), s>>>(a);
             break;
         case 64:
-            loss_row_kernel<E, KIND, 64, 4><<<nb, 256, list * 4, s>>>(a);
+            loss_row_kernel<E, KIND, 64, 4><<<nb, 256, list(4), s>>>(a);
             break;
         case 256:
-            loss_row_kernel<E, KIND, 256, 4><<<nb, 256, list, s>>>(a);
+            loss_row_kernel<E, KIND, 256, 4><<<nb, 256, list(1), s>>>(a);
             break;
         case 512:
-            loss_row_kernel<E, KIND, 512, 4><<<nb, 512, list, s>>>(a);
+            loss_row_kernel<E, KIND, 512, 4><<<nb, 512, list(1), s>>>(a);
             break;
         default:
-            loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list, s>>>(a);
+            loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list(1), s>>>(a);
         }
         break;
     case kLossLong:
-        loss_long_kernel<E, KIND, 0><<<nb, kLongThreads, list, s>>>(a);
+        loss_long_kernel<E, KIND, 0><<<nb, kLongThreads, list(1), s>>>(a);
         break;
     default:
-        loss_long_kernel<E, KIND, 1><<<nb, kLongThreads, list, s>>>(a);
-        loss_long_kernel<E, KIND, 2><<<nb, kLongThreads, list, s>>>(a);
+        loss_long_kernel<E, KIND, 1><<<nb, kLongThreads, list(1), s>>>(a);
+        loss_long_kernel<E, KIND, 2><<<nb, kLongThreads, list(1), s>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.total || p.blocks == 1)
