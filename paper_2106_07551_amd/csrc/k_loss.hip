@@ -758,10 +758,22 @@ __device__ __forceinline__ Stats group_merge(const Stats& st, float c, float* sc
     return r;
 }
 
+// Between two uses of a thread's chunks: the raw chunks are what stays in registers,
+// not their unpacked values (twice as many in bf16).
+template <int KIND, int C>
+__device__ __forceinline__ void keep_raw(u32x4 (&x)[C], u32x4* y)
+{
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        asm volatile("" : "+v"(x[i]));
+        if (KIND == kPolicyRef)
+            asm volatile("" : "+v"(y[i]));
+    }
+}
+
 // The sums over the first `used` of C chunks that a thread holds.
 template <typename E, int KIND, int C>
-__device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y, int used,
-                                             float c)
+__device__ __forceinline__ Stats chunk_stats(u32x4 (&x)[C], u32x4* y, int used, float c)
 {
     constexpr int CH = kChunk<E>;
     Stats st = empty_stats();
@@ -782,6 +794,7 @@ __device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y
         }
     }
     const float m = st.m == kNegInf ? 0.0f : st.m, my = st.my == kNegInf ? 0.0f : st.my;
+    keep_raw<KIND>(x, y);
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         if (i >= used)
@@ -793,17 +806,18 @@ __device__ __forceinline__ Stats chunk_stats(const u32x4 (&x)[C], const u32x4* y
 #pragma unroll
         for (int e = 0; e < CH; ++e)
             add_entry<KIND>(st, f[e], KIND == kPolicyRef ? r[e] : 0.0f, m, my, c);
+        __builtin_amdgcn_sched_barrier(0);
     }
     return st;
 }
 
-template <typename E, int KIND>
+// WHOLE: the chunk does not cross the row's end.
+template <typename E, int KIND, bool WHOLE>
 __device__ __forceinline__ void write_grad(const LossArgs& a, const RowGrad& g, bool counts,
-                                           int64_t row, int64_t action, int q, u32x4 x, u32x4 y,
-                                           float c)
+                                           int64_t row, int q, u32x4 x, u32x4 y, float c)
 {
     constexpr int CH = kChunk<E>;
-    const int j0 = q * CH, n = a.A - j0 < CH ? a.A - j0 : CH;
+    const int j0 = q * CH, n = WHOLE || a.A - j0 > CH ? CH : a.A - j0;
     if (n <= 0)
         return;
     float f[CH], r[CH];
@@ -814,18 +828,21 @@ __device__ __forceinline__ void write_grad(const LossArgs& a, const RowGrad& g, 
 #pragma unroll
         for (int e = 0; e < CH; ++e)
             f[e] = grad_entry<KIND>(g, f[e], KIND == kPolicyRef ? r[e] : 0.0f, c);
-        if (KIND != kDistill && action >= j0 && action < j0 + CH) {
-#pragma unroll
-            for (int e = 0; e < CH; ++e)
-                if (action == j0 + e)
-                    f[e] += g.at_action;
-        }
     } else {
 #pragma unroll
         for (int e = 0; e < CH; ++e)
             f[e] = 0.0f;
     }
     store_chunk((E*)a.dlogits + row * a.dlogits_ld + j0, n, pack<E>(f));
+}
+
+// The action's entry, over what write_grad left there, by the thread that wrote it (a
+// thread's stores to one place stay in order).
+template <typename E, int KIND>
+__device__ __forceinline__ void write_action(const LossArgs& a, const RowGrad& g, int64_t row,
+                                             int j, float x, float y, float c)
+{
+    ((E*)a.dlogits)[row * a.dlogits_ld + j] = from_f32<E>(grad_entry<KIND>(g, x, y, c) + g.at_action);
 }
 
 // The teacher's list of a row, handled by TL lanes (the row's own, or its first
@@ -972,6 +989,82 @@ __device__ __forceinline__ void write_list(const LossArgs& a, const List<T>& l, 
     }
 }
 
+// A row's chunks into registers, -inf in the entries that are not legal or not there,
+// and everywhere in a row that does not count.  Within a wavefront (T <= 64) every
+// chunk has its own conditions, so that all are asked for together; in workgroups the
+// chunks that all threads hold whole take none, and the one round that the row's end
+// falls into comes first, which leaves registers for more wavefronts (fp32, 2048 x
+// 32000 with reference logits: 173 us, with conditions on every chunk 290 us, with that
+// round last 196 us; 559269 x 91: 120, as workgroups' rows 139 us).
+template <typename E, int KIND, int T, int C>
+__device__ __forceinline__ void load_row(const LossArgs& a, bool counts, const E* px, const E* py,
+                                         const uint8_t* pm, int lane, u32x4 (&x)[C], u32x4* y)
+{
+    constexpr int CH = kChunk<E>;
+    if constexpr (T <= 64) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int j = (lane + i * T) * CH, n = counts ? a.A - j : 0;
+            x[i] = load_masked(px + j, n, pm ? pm + j : nullptr, j);
+            if (KIND == kPolicyRef)
+                y[i] = load_masked(py + j, n, pm ? pm + j : nullptr, j);
+        }
+        return;
+    }
+    const int whole = a.A / (T * CH);
+    const int jt = (lane + whole * T) * CH, nt = counts ? a.A - jt : 0;
+    const u32x4 tx = load_masked(px + jt, nt, pm ? pm + jt : nullptr, jt);
+    u32x4 ty = tx;
+    if (KIND == kPolicyRef)
+        ty = load_masked(py + jt, nt, pm ? pm + jt : nullptr, jt);
+    const u32x4 none = load_masked((const E*)nullptr, 0, nullptr, 0);
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        x[i] = i == whole ? tx : none;
+        if (KIND == kPolicyRef)
+            y[i] = i == whole ? ty : none;
+    }
+    if (!counts)
+        return;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        if (i < whole) {
+            const int j = (lane + i * T) * CH;
+            x[i] = *(const u32x4_any*)(px + j);
+            if (KIND == kPolicyRef)
+                y[i] = *(const u32x4_any*)(py + j);
+        }
+    }
+    if (!pm)
+        return;
+    uint32_t legal[C][CH / 4];
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int e = 0; e < CH / 4; ++e)
+            legal[i][e] = 0x01010101u;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        if (i < whole) {
+            const int j = (lane + i * T) * CH;
+#pragma unroll
+            for (int e = 0; e < CH / 4; ++e)
+                legal[i][e] = *(const u32_any*)(pm + j + 4 * e);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+            const bool out = (legal[i][e / 4] >> (8 * (e % 4)) & 0xFFu) == 0;
+            exclude<E>(x[i], e, out);
+            if (KIND == kPolicyRef)
+                exclude<E>(y[i], e, out);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // Rows that fit the registers of T threads, C chunks each: read once, written once.
 template <typename E, int KIND, int T, int C>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
@@ -1005,14 +1098,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         const E* py = (const E*)a.ref_logits + row * a.ref_ld;
         const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld : nullptr;
         u32x4 x[C], y[KIND == kPolicyRef ? C : 1];
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int j = (lane + i * T) * CH;
-            const int n = counts ? a.A - j : 0;
-            x[i] = load_masked(px + j, n, pm ? pm + j : nullptr, j);
-            if (KIND == kPolicyRef)
-                y[i] = load_masked(py + j, n, pm ? pm + j : nullptr, j);
-        }
+        load_row<E, KIND, T, C>(a, counts, px, py, pm, lane, x, y);
         const int used = (a.A + T * CH - 1) / (T * CH);   // chunks that any thread holds
         float part = 0.0f;
         if (lists) {
@@ -1032,10 +1118,15 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
                                         KIND == kDistill && T > 64 ? &any_entry : nullptr, counts);
         counts = counts && st.s != 0.0f;
         RowGrad g{};
+        float x_a = 0.0f, y_a = 0.0f;   // the action's logits
         if (KIND != kDistill) {
             PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
-            if (counts)
-                o = policy_finish<KIND>(a, pr, st, to_f32(px[pr.action]), g);
+            if (counts) {
+                x_a = to_f32(px[pr.action]);
+                if (KIND == kPolicyRef)
+                    y_a = to_f32(py[pr.action]);
+                o = policy_finish<KIND>(a, pr, st, x_a, g);
+            }
             if (live && lane == 0) {
                 if (counts)
                     total += (double)pr.w * o.loss;
@@ -1055,17 +1146,29 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
             }
         }
         if (a.dlogits && live) {
-            // (the raw chunks are what stays in registers, not their unpacked values)
+            keep_raw<KIND>(x, y);
+            if constexpr (T <= 64) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                asm volatile("" : "+v"(x[i]));
-                if (KIND == kPolicyRef)
-                    asm volatile("" : "+v"(y[i]));
+                for (int i = 0; i < C; ++i)
+                    write_grad<E, KIND, false>(a, g, counts, row, lane + i * T, x[i],
+                                               KIND == kPolicyRef ? y[i] : x[i], c);
+            } else {
+                const int whole = a.A / (T * CH);
+                u32x4 tx = x[0], ty = KIND == kPolicyRef ? y[0] : x[0];
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    if (i < whole)
+                        write_grad<E, KIND, true>(a, g, counts, row, lane + i * T, x[i],
+                                                  KIND == kPolicyRef ? y[i] : x[i], c);
+                    tx = i == whole ? x[i] : tx;
+                    if (KIND == kPolicyRef)
+                        ty = i == whole ? y[i] : ty;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                write_grad<E, KIND, false>(a, g, counts, row, lane + whole * T, tx, ty, c);
             }
-#pragma unroll
-            for (int i = 0; i < C; ++i)
-                write_grad<E, KIND>(a, g, counts, row, pr.action, lane + i * T, x[i],
-                                    KIND == kPolicyRef ? y[i] : x[i], c);
+            if (KIND != kDistill && counts && (int)pr.action / CH % T == lane)
+                write_action<E, KIND>(a, g, row, (int)pr.action, x_a, y_a, c);
         }
         if (KIND == kDistill && a.dlogits) {
             group_sync<T>();
@@ -1157,10 +1260,15 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
         }
         counts = counts && st.s != 0.0f;
         RowGrad g{};
+        float x_a = 0.0f, y_a = 0.0f;   // the action's logits
         if (KIND != kDistill) {
             PolicyOut o{0.0f, 0.0f, 0.0f, 0.0f};
-            if (counts)
-                o = policy_finish<KIND>(a, pr, st, to_f32(px[pr.action]), g);
+            if (counts) {
+                x_a = to_f32(px[pr.action]);
+                if (KIND == kPolicyRef)
+                    y_a = to_f32(py[pr.action]);
+                o = policy_finish<KIND>(a, pr, st, x_a, g);
+            }
             if (tid == 0 && part == 0) {
                 if (counts)
                     total += (double)pr.w * o.loss;
@@ -1193,8 +1301,13 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (q + u * T < q1)
-                        write_grad<E, KIND>(a, g, counts, row, pr.action, q + u * T, x[u],
-                                            KIND == kPolicyRef ? y[u] : x[u], c);
+                        write_grad<E, KIND, false>(a, g, counts, row, q + u * T, x[u],
+                                                   KIND == kPolicyRef ? y[u] : x[u], c);
+            }
+            if (KIND != kDistill && counts) {
+                const int q = (int)pr.action / CH;
+                if (q >= q0 && q < q1 && (q - q0) % T == tid)
+                    write_action<E, KIND>(a, g, row, (int)pr.action, x_a, y_a, c);
             }
             if (KIND == kDistill) {
                 __syncthreads();
@@ -1259,8 +1372,11 @@ hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
         case 512:
             loss_row_kernel<E, KIND, 512, 4><<<nb, 512, list(1), s>>>(a);
             break;
-        default:
+        case 1024:
             loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list(1), s>>>(a);
+            break;
+        default:
+            loss_row_kernel<E, KIND, 1024, 8><<<nb, 1024, list(1), s>>>(a);
         }
         break;
     case kLossLong:
@@ -1281,6 +1397,13 @@ __global__ void zero_total_kernel(float* total) { *total = 0.0f; }
 
 }  // namespace
 
+// Up to 31 actions a lane per row; up to 8 chunks of 16 bytes for each of 1024 threads
+// (65536 bf16 or 32768 fp32 entries) a row stays in the registers of as few threads as
+// hold it; above, and where a workgroup per row would leave half of the CUs idle, rows
+// are read twice, in parts where there are few.  Rows in registers against rows read
+// twice: 4096 x 65536 bf16 with reference logits 394 and 411 us, 2048 x 32000 fp32 with
+// them 172 and 227 us, 2047 x 50001 bf16 distilled 122 and 129 us, 4096 x 50000 bf16 207
+// and 205 us.
 LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
 {
     constexpr int64_t kCus = 256;
@@ -1293,7 +1416,7 @@ LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
     if (A <= kLaneMost && (top == 0 || (top <= 32 && lane_floats(kDistill, (int)A, top) <= 64))) {
         p.variant = kLossLane;
         per = kLaneThreads;
-    } else if (A <= 256 * 4 * ch || (A <= 1024 * 4 * ch && rows >= kCus / 2)) {
+    } else if (A <= 256 * 4 * ch || (A <= 1024 * 8 * ch && rows >= kCus / 2)) {
         p.variant = kLossRow;
         p.group = 4;
         // at most 8 entries of a teacher's list per lane

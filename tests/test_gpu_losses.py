@@ -188,6 +188,22 @@ def test_policy_masks_and_strides(dtype, n, a, how):
         check_policy(d, how=how, tag=f"{dtype} {n}x{a} mask pad={pad}")
 
 
+# rows of up to 8 chunks of 16 bytes per thread of a workgroup, whole rounds of chunks or
+# not, and one entry more than registers take
+LONG_ROWS = [(130, 16384), (129, 24577), (140, 32767), (131, 32768), (128, 49152), (133, 65535),
+             (129, 65536), (128, 65537)]
+
+
+@DTYPES
+@pytest.mark.parametrize("n, a", LONG_ROWS)
+def test_policy_long_rows(dtype, n, a):
+    how = ("none", "sampled", "full")
+    d = policy_inputs(dtype, n, a, seed=n + a, weight=True)
+    check_policy(d, how=how[a % 3], tag=f"{dtype} {n}x{a}")
+    d = policy_inputs(dtype, n, a, seed=n + a + 1, mask=True, pad=3, shift=1)
+    check_policy(d, how=how[(a + 1) % 3], tag=f"{dtype} {n}x{a} mask")
+
+
 @DTYPES
 @pytest.mark.parametrize("a", [4, 40, 900, 6000, 20000, 70000])
 def test_policy_infinite_logits(dtype, a):
@@ -332,6 +348,19 @@ def check_distill(dtype, n, a, top, T, *, mask=False, weight=False, pad=0, shift
 def test_distill_sizes(dtype, n, a):
     check_distill(dtype, n, a, min(a, (1, 6, 64, 256)[n % 4]), (1.0, 2.0, 0.7)[a % 3],
                   weight=n % 2 == 1)
+
+
+@DTYPES
+@pytest.mark.parametrize("n, a", LONG_ROWS)
+def test_distill_long_rows(dtype, n, a):
+    check_distill(dtype, n, a, 40, 2.0, weight=True)
+    check_distill(dtype, n, a, 70, 1.0, mask=True, repeat=True, pad=3, shift=1)
+
+
+@DTYPES
+@pytest.mark.parametrize("n, a, top", [(300, 16, 15), (300, 16, 16), (257, 31, 1), (70, 20, 11)])
+def test_distill_few_actions_long_lists(dtype, n, a, top):
+    check_distill(dtype, n, a, top, 1.0, weight=True)
 
 
 @DTYPES
