@@ -310,7 +310,7 @@ malib_status malib_policy_loss(const malib_policy_loss_desc* d, const void* logi
         return set_error(MALIB_E_INVAL, "kl_coef and entropy_coef must be finite");
     if (ref_logp && ref_logits)
         return set_error(MALIB_E_INVAL, "ref_logp and ref_logits exclude each other");
-    if (d->kl_coef != 0.0f && !ref_logp && !ref_logits)
+    if (d->kl_coef != 0.0f && d->rows > 0 && !ref_logp && !ref_logits)   // (of no rows: NULL)
         return set_error(MALIB_E_INVAL, "kl_coef needs ref_logp or ref_logits");
     const int size = type_size(d->dtype);
     const LossPlan p = loss_plan(d->rows, d->n_actions, 0, size);

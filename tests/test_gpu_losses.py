@@ -371,6 +371,15 @@ def test_distill_masks_repeats_and_strides(dtype, n, a):
     check_distill(dtype, n, a, min(a, 30), 1.0, mask=True, weight=True)
 
 
+def test_policy_no_rows_with_a_reference():
+    import paper_2106_07551_amd as MA
+    none = torch.empty(0, device="cuda")
+    for kw in (dict(ref_logp=none), dict(ref_logits=torch.empty((0, 7), device="cuda"))):
+        total, stats, grad = MA.policy_loss(
+            torch.empty((0, 7), device="cuda"), none.int(), none, none, kl_coef=0.5, **kw)
+        assert float(total) == 0.0 and stats.shape == (4, 0) and grad.shape == (0, 7)
+
+
 def test_distill_no_rows():
     import paper_2106_07551_amd as MA
     total, loss, grad = MA.distill_loss(
