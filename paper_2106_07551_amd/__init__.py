@@ -2,7 +2,8 @@
 
 The compute path is ``libmalib.so`` (hand-written HIP kernels behind the C ABI
 in ``include/malib.h``); this package only marshals arguments to it with
-ctypes and uses torch for device memory and streams.  There is no CPU
+ctypes (the learner operators, whose small calls are bound by the host, with a
+C++ extension module) and uses torch for device memory and streams.  There is no CPU
 fallback: importing the binding without the built library raises.
 """
 from .binding import (  # noqa: F401

@@ -191,11 +191,9 @@ def _check(st: int):
 
 
 def _stream(stream):
-    import torch
     if stream is not None:
         return C.c_void_p(stream.cuda_stream)
-    # (torch.cuda.current_stream() takes 8 us to make the object this is read from)
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    return C.c_void_p(_current_stream())
 
 
 def _dptr(t, dtype=None, numel: Optional[int] = None, *, at_least: bool = False,
@@ -693,6 +691,33 @@ _POLICY_LOSS = struct.Struct("@iiqqqqqqffff")  # malib_policy_loss_desc
 _DISTILL = struct.Struct("@iiqqqqqf4x")        # malib_distill_desc
 
 
+_calls = None
+
+
+def _native():
+    """The learner operators' calls in C++ (csrc/learner_calls.cpp): each takes the
+    arguments of the function below that has its name, checks them, allocates and calls the
+    library, or returns None where it does not take them.  Raises if they have not been
+    built."""
+    global _calls
+    if _calls is None:
+        lib()
+        import torch  # noqa: F401  (the module's symbols)
+        try:
+            from . import _learner_calls as m
+        except ImportError as e:
+            raise ImportError(f"{e}: build it with __graft_entry__.build()") from e
+        m.load(LIB_PATH)
+        _calls = m
+    return _calls
+
+
+def _current_stream():
+    import torch
+    # (torch.cuda.current_stream() takes 8 us to make the object this is read from)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _empty(shape, dtype, device, stream):
     """A tensor from the memory pool of the stream the call runs on (the caching
     allocator hands memory out again in the order of one stream only)."""
@@ -794,6 +819,11 @@ def linear(x, w, bias=None, *, act: int = ACT_NONE, residual=None, pre=None, out
     group dimension is shared by the groups); float32 or bfloat16, bias
     float32.  `pre` receives the values before the activation, which
     linear_backward needs.  Returns [..][rows][out]."""
+    if stream is None and x.is_cuda:
+        y = (_calls or _native()).linear(x, w, bias, act, residual, pre, out, work,
+                                         _current_stream())
+        if y is not None:
+            return y
     code = _dtype_code(x, "x")
     G, n_out, n_in = _layer(x, w, act)
     rows, dt = x.shape[-2], x.dtype
@@ -819,6 +849,11 @@ def linear_backward(dy, x, w, *, act: int = ACT_NONE, pre=None, want=(True, True
     its output; `pre` is what linear wrote there (needed with an activation).
     `want` leaves outputs out (None is returned for them).  The residual's
     gradient is dy."""
+    if stream is None and dy.is_cuda:
+        out = (_calls or _native()).linear_backward(dy, x, w, act, pre, want, dx, dw, dbias, work,
+                                                    _current_stream())
+        if out is not None:
+            return out
     code = _dtype_code(dy, "dy")
     G, n_out, n_in = _layer(dy, w, act)
     rows, dt, dev = dy.shape[-2], dy.dtype, dy.device
@@ -899,6 +934,13 @@ def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
     [rows][n_actions], legal entries.  Returns (total [1], stats [4][rows] =
     loss, log probability of the action, divergence and entropy of each row,
     dlogits or None without `grad`)."""
+    if stream is None and logits.is_cuda:
+        out = (_calls or _native()).policy_loss(
+            logits, actions, old_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef,
+            ref_logp, ref_logits, mask, weight, grad, total, stats, dlogits, work,
+            _current_stream())
+        if out is not None:
+            return out
     import torch
     n, a, code, sl, sd, sm = _loss_args(logits, mask, weight, dlogits)
     f32 = torch.float32
@@ -940,6 +982,12 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
     int32 and teacher_logits float32 [rows][top], index -1 pads a list) into
     logits [rows][n_actions], and its gradient.  Returns (total [1], loss
     [rows], dlogits or None without `grad`)."""
+    if stream is None and logits.is_cuda:
+        out = (_calls or _native()).distill_loss(
+            logits, teacher_idx, teacher_logits, temperature, mask, weight, grad, total, loss,
+            dlogits, work, _current_stream())
+        if out is not None:
+            return out
     import torch
     n, a, code, sl, sd, sm = _loss_args(logits, mask, weight, dlogits)
     f32 = torch.float32

@@ -1,4 +1,5 @@
-"""Build libmalib.so (HIP, gfx950) in-tree with hipcc.
+"""Build libmalib.so (HIP, gfx950) in-tree with hipcc, and the native calls of the
+learner operators' binding (_learner_calls.so) with the host's C++ compiler.
 
 Every .hip source under csrc/ is compiled to an object in parallel, then
 linked into paper_2106_07551_amd/libmalib.so.  Flags: no fast-math, no fp
@@ -12,12 +13,14 @@ import glob
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libmalib.so")
+CALLS = os.path.join(HERE, "_learner_calls.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # gfx950 with XNACK off (the device runs without page-fault replay; code built
 # for it measured ~0.5% faster on the largest kernels than the XNACK-any default)
@@ -39,11 +42,31 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_calls() -> None:
+    import torch
+    home = os.path.dirname(torch.__file__)
+    inc = os.path.join(home, "include")
+    tmp = CALLS + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-isystem", inc,
+           "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "learner_calls.cpp"),
+           "-o", tmp, "-L", os.path.join(home, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python",
+           "-ldl"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for learner_calls.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        calls = ex.submit(_build_calls)
         objs = list(ex.map(_compile, srcs))
+        calls.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
