@@ -3,6 +3,7 @@
 #include "internal.hpp"
 
 #include <cmath>
+#include <cstring>
 
 using namespace malib;
 
@@ -111,14 +112,13 @@ struct BackwardPlan {
     int64_t dz_ld, dz_at, sum_at, dw_at, dx_at, bytes;
 };
 
-BackwardPlan backward_plan(const malib_linear_desc* d)
+BackwardPlan make_backward_plan(const malib_linear_desc* d)
 {
     const int size = type_size(d->dtype), ch = 16 / size;
     const bool act = d->act != MALIB_ACT_NONE;
     const bool rounded = size == 2 && (d->act == MALIB_ACT_GELU || d->act == MALIB_ACT_SILU);
     BackwardPlan p;
-    p.dx = gemm_plan(d->groups, d->rows, d->in, d->out, size);
-    p.dw = gemm_plan(d->groups, d->out, d->in, d->rows, size);
+    backward_plans(d->groups, d->rows, d->in, d->out, size, p.dw, p.dx);
     p.dz = dz_plan(d->groups, d->rows, d->out, size);
     p.fused = act && !rounded &&
               (d->groups * d->rows * d->out <= kFusedMost || d->in <= kFusedWidth);
@@ -130,6 +130,28 @@ BackwardPlan backward_plan(const malib_linear_desc* d)
     p.dx_at = p.dw_at + align256(p.dw.part_bytes);
     p.bytes = p.dx_at + align256(p.dx.part_bytes);
     return p;
+}
+
+// The plan of a description: a few microseconds of the host to make, so each thread
+// keeps the last ones (it depends on nothing else).
+const BackwardPlan& backward_plan(const malib_linear_desc* d)
+{
+    struct Kept {
+        malib_linear_desc d;
+        BackwardPlan p;
+    };
+    constexpr uint64_t kSlots = 32;
+    static thread_local Kept kept[kSlots];   // (no description has groups = 0)
+    const uint64_t h = (uint64_t)d->rows * 31 + (uint64_t)d->in * 17 + (uint64_t)d->out * 7 +
+                       (uint64_t)d->groups * 3 + (uint64_t)(d->act + 4 * d->dtype);
+    Kept& k = kept[h * 0x9E3779B97F4A7C15ull >> 59];
+    static_assert(kSlots == 1u << (64 - 59), "");
+    static_assert(sizeof(malib_linear_desc) == 40, "no padding: compared as bytes");
+    if (std::memcmp(&k.d, d, sizeof *d) != 0) {
+        k.p = make_backward_plan(d);
+        k.d = *d;
+    }
+    return k.p;
 }
 
 }  // namespace
@@ -206,7 +228,7 @@ malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* 
         TRY(check_mat(dw, "dw", d->out, d->in, d->groups, size, true));
     if (dbias && (uintptr_t)dbias % 4)
         return set_error(MALIB_E_INVAL, "dbias is not aligned to its elements");
-    const BackwardPlan p = backward_plan(d);
+    const BackwardPlan& p = backward_plan(d);
     if (dx)
         TRY(check_grid(d, p.dx, d->rows, d->in));
     if (dw)
@@ -219,21 +241,23 @@ malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* 
     const bool products = dw || (dx && rows);
     const bool make_dz = act && !p.fused && products && rows;
     const bool own_sums = dbias && (p.own_sums || !dw);
+    DbArgs db{};
     if (make_dz || own_sums) {
         MatArg to{nullptr, 0, 0};
         if (make_dz)
             to = MatArg{ws + p.dz_at, p.dz_ld, d->rows * p.dz_ld};
+        float* sums = !own_sums ? nullptr : p.dz.parts > 1 ? (float*)(ws + p.sum_at) : dbias;
         HIP_TRY(launch_dz(d->dtype, p.dz, arg(dy), arg(pre), to, d->act, (int)d->groups,
-                          (int)d->rows, (int)d->out, (float*)(ws + p.sum_at),
-                          own_sums ? dbias : nullptr, s));
+                          (int)d->rows, (int)d->out, sums, s));
+        if (sums && p.dz.parts > 1)
+            db = DbArgs{sums, d->groups * d->out, p.dz.parts, dbias};
         if (make_dz)
             dz = to;
     }
-    if (!products)
-        return MALIB_OK;
     GemmArgs ax{}, aw{};
     ax.groups = aw.groups = (int)d->groups;
     ax.a = aw.a = dz;
+    ax.a_padded = aw.a_padded = make_dz;
     if (act && p.fused && rows) {
         ax.a_pre = aw.a_pre = arg(pre);
         ax.a_act = aw.a_act = d->act;
@@ -254,7 +278,8 @@ malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* 
         aw.sum_out = dbias && !own_sums ? dbias : nullptr;
     }
     HIP_TRY(launch_linear_backward(d->dtype, aw, p.dw, (float*)(ws + p.dw_at),
-                                   (float*)(ws + p.sum_at), ax, p.dx, (float*)(ws + p.dx_at), s));
+                                   (float*)(ws + p.sum_at), ax, p.dx, (float*)(ws + p.dx_at), db,
+                                   s));
     return MALIB_OK;
 }
 

@@ -371,6 +371,7 @@ struct GemmArgs {
     MatArg a, b, c, res, pre;
     MatArg a_pre;        // backward: A is a act'(a_pre) where a_act is an activation
     int a_act;
+    bool a_padded;       // A's rows are padded with zeros to a multiple of 16 bytes
     const float* bias;   // [groups][N] or null
     float* sum_out;      // dW: [groups][M], sums of A over k, or null
     int M, N, K, groups, act;
@@ -384,24 +385,38 @@ struct GemmArgs {
 struct GemmPlan {
     int tile, splits;
     int64_t k_split, part_bytes, sum_bytes;
+    double us;   // estimated
 };
-GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
+// `tile`: only that one (0: the best)
+GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int tile = 0);
+// dW's and dx's plans of a backward pass, on the same tile where one launch is cheaper
+void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, GemmPlan& dw,
+                    GemmPlan& dx);
 // the forward's plan: up to kFewRows rows a kernel of its own (tile 0)
 constexpr int kFewRows = 16;
 GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
 hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s);
 // dW and dx (either left out where its c.p is null), in one launch where both use
 // the same tile
+// then the sums of their splits and of db's row ranges.
+struct DbArgs {
+    const float* parts;   // [count][n], or null
+    int64_t n;
+    int count;
+    float* out;
+};
 hipError_t launch_linear_backward(int dtype, GemmArgs dw, GemmPlan pw, float* dw_part,
                                   float* sum_part, GemmArgs dx, GemmPlan px, float* dx_part,
-                                  hipStream_t s);
+                                  const DbArgs& db, hipStream_t s);
 struct DzPlan {
     int rows_per_block, parts, col_blocks;
     int64_t sum_bytes;
 };
 DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size);
+// dz (where dz.p) with zeros behind each row up to a multiple of 16 bytes, and its sums
+// over p.parts ranges of rows (where sums)
 hipError_t launch_dz(int dtype, const DzPlan& p, const MatArg& dy, const MatArg& pre,
-                     const MatArg& dz, int act, int groups, int M, int N, float* sums, float* db,
+                     const MatArg& dz, int act, int groups, int M, int N, float* sums,
                      hipStream_t s);
 
 // The learner's losses (k_loss.hip).

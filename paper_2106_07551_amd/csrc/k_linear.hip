@@ -883,15 +883,46 @@ __device__ __forceinline__ void split_sum_block(const GemmArgs& a, int64_t block
     finish_chunk<E>(a, g, gm % a.M, n, cnt, bias, res, v);
 }
 
+// db[i] = sum over the row ranges: shares of the ranges by thread, added in order.
+constexpr int kDbItems = 8, kDbShares = kSumThreads / kDbItems;
+
+__device__ __forceinline__ void db_block(const DbArgs& d, int64_t block, float* red)
+{
+    const int item = threadIdx.x % kDbItems, share = threadIdx.x / kDbItems;
+    const int64_t i = block * kDbItems + item;
+    float t = 0.0f;
+    if (i < d.n) {
+#pragma unroll 4
+        for (int p = share; p < d.count; p += kDbShares)
+            t += d.parts[p * d.n + i];
+    }
+    red[share * kDbItems + item] = t;
+    __syncthreads();
+    if (share == 0 && i < d.n) {
+        for (int k = 1; k < kDbShares; ++k)
+            t += red[k * kDbItems + item];
+        d.out[i] = t;
+    }
+}
+
+// The sums of dW's splits (n_a workgroups), of dx's (up to n_b) and of db's ranges
 template <typename E, int SHARES>
 __global__ __launch_bounds__(kSumThreads) void split_sum_kernel(GemmArgs a, uint32_t n_a,
-                                                                GemmArgs b)
+                                                                GemmArgs b, uint32_t n_b, DbArgs d)
 {
-    __shared__ float red[SHARES > 1 ? kSumThreads * kChunk<E> : 1];
+    __shared__ float red[SHARES > 1 ? kSumThreads * kChunk<E> : kSumThreads];
     if (blockIdx.x < n_a)
         split_sum_block<E, SHARES>(a, blockIdx.x, red);
-    else
+    else if (blockIdx.x < n_b)
         split_sum_block<E, SHARES>(b, blockIdx.x - n_a, red);
+    else
+        db_block(d, blockIdx.x - n_b, red);
+}
+
+__global__ __launch_bounds__(kSumThreads) void db_kernel(DbArgs d)
+{
+    __shared__ float red[kSumThreads];
+    db_block(d, blockIdx.x, red);
 }
 
 // Threads per chunk: as many as bring about four loads each
@@ -929,19 +960,37 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
     for (int e = 0; e < CH; ++e)
         s[e] = 0.0f;
     if (cnt > 0) {
-        for (int64_t m = r0 + ry; m < r1; m += kDzRows) {
-            float v[CH];
-            unpack<E>(load_chunk((const E*)dy.p + g * dy.gs + m * dy.ld + n, cnt, n), v);
-            if (act != MALIB_ACT_NONE) {
-                float z[CH];
-                unpack<E>(load_chunk((const E*)pre.p + g * pre.gs + m * pre.ld + n, cnt, n), z);
-                times_slope(act, z, v);
-                if (dz.p)
-                    store_chunk((E*)dz.p + g * dz.gs + m * dz.ld + n, cnt, pack<E>(v));
+        constexpr int U = 4;   // rows asked for together
+        for (int64_t m0 = r0 + ry; m0 < r1; m0 += U * kDzRows) {
+            u32x4 vy[U], vz[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t m = m0 + u * kDzRows;
+                vy[u] = vz[u] = u32x4{0, 0, 0, 0};
+                if (m < r1) {
+                    vy[u] = load_chunk((const E*)dy.p + g * dy.gs + m * dy.ld + n, cnt, n);
+                    if (act != MALIB_ACT_NONE)
+                        vz[u] = load_chunk((const E*)pre.p + g * pre.gs + m * pre.ld + n, cnt, n);
+                }
             }
 #pragma unroll
-            for (int e = 0; e < CH; ++e)
-                s[e] += v[e];
+            for (int u = 0; u < U; ++u) {
+                const int64_t m = m0 + u * kDzRows;
+                if (m >= r1)
+                    break;
+                float v[CH];
+                unpack<E>(vy[u], v);
+                if (act != MALIB_ACT_NONE) {
+                    float z[CH];
+                    unpack<E>(vz[u], z);
+                    times_slope(act, z, v);
+                    if (dz.p)
+                        store_chunk((E*)dz.p + g * dz.gs + m * dz.ld + n, CH, pack<E>(v));
+                }
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    s[e] += v[e];
+            }
         }
     }
     if (!sums)
@@ -960,30 +1009,6 @@ __global__ __launch_bounds__(kDzCols* kDzRows) void dz_kernel(MatArg dy, MatArg 
                 t += red[r][c];
             sums[((int64_t)blockIdx.y * gridDim.z + g) * N + col] = t;
         }
-    }
-}
-
-// db[i] = sum over the row ranges: shares of the ranges by thread, added in order.
-constexpr int kSumItems = 8, kSumShares = 32;
-
-__global__ __launch_bounds__(kSumItems* kSumShares) void db_kernel(const float* sums, int64_t n,
-                                                                   int parts, float* db)
-{
-    __shared__ float red[kSumShares][kSumItems];
-    const int item = threadIdx.x % kSumItems, share = threadIdx.x / kSumItems;
-    const int64_t i = (int64_t)blockIdx.x * kSumItems + item;
-    float t = 0.0f;
-    if (i < n) {
-#pragma unroll 4
-        for (int p = share; p < parts; p += kSumShares)
-            t += sums[p * n + i];
-    }
-    red[share][item] = t;
-    __syncthreads();
-    if (share == 0 && i < n) {
-        for (int k = 1; k < kSumShares; ++k)
-            t += red[k][item];
-        db[i] = t;
     }
 }
 
@@ -1057,20 +1082,23 @@ hipError_t launch_backward_as(const GemmArgs& dw, const GemmArgs& dx, int tile, 
 }
 
 template <typename E>
-hipError_t launch_split_sums(const GemmArgs& a, const GemmArgs& b, hipStream_t s)
+hipError_t launch_split_sums(const GemmArgs& a, const GemmArgs& b, const DbArgs& d, hipStream_t s)
 {
     const bool pa = a.blocks && a.part, pb = b.blocks && b.part;
-    if (!pa && !pb)
-        return hipSuccess;
     const int shares = std::max(pa ? sum_shares(a) : 1, pb ? sum_shares(b) : 1);
     const uint32_t na = pa ? (uint32_t)split_sum_blocks<E>(a, shares) : 0;
     const uint32_t nb = na + (pb ? (uint32_t)split_sum_blocks<E>(b, shares) : 0);
-    if (shares == 8)
-        split_sum_kernel<E, 8><<<nb, kSumThreads, 0, s>>>(a, na, b);
+    const uint32_t n = nb + (d.parts ? (uint32_t)((d.n + kDbItems - 1) / kDbItems) : 0);
+    if (n == 0)
+        return hipSuccess;
+    if (nb == 0)
+        db_kernel<<<n, kSumThreads, 0, s>>>(d);
+    else if (shares == 8)
+        split_sum_kernel<E, 8><<<n, kSumThreads, 0, s>>>(a, na, b, nb, d);
     else if (shares == 2)
-        split_sum_kernel<E, 2><<<nb, kSumThreads, 0, s>>>(a, na, b);
+        split_sum_kernel<E, 2><<<n, kSumThreads, 0, s>>>(a, na, b, nb, d);
     else
-        split_sum_kernel<E, 1><<<nb, kSumThreads, 0, s>>>(a, na, b);
+        split_sum_kernel<E, 1><<<n, kSumThreads, 0, s>>>(a, na, b, nb, d);
     return hipGetLastError();
 }
 
@@ -1078,9 +1106,12 @@ hipError_t launch_split_sums(const GemmArgs& a, const GemmArgs& b, hipStream_t s
 
 // Whether an operand's tiles can go straight to LDS: rows on 16-byte boundaries
 // that end with whole chunks, and a tile's bytes within 31 bits.
-static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups)
+static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups,
+                    bool padded = false)
 {
     const int64_t ch = 16 / size;
+    if (padded)
+        contiguous = 0;   // (a chunk that crosses the end holds zeros there)
     return (uintptr_t)m.p % 16 == 0 && m.ld % ch == 0 && (groups == 1 || m.gs % ch == 0) &&
            contiguous % ch == 0 && m.ld * size <= (int64_t)(0x70000000 / 256);
 }
@@ -1092,7 +1123,7 @@ static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups)
 //   8192 x 4096 -> 4096 bf16: 64 480 us, 128 279 us, 256 238 us; 2048^3: 64 33 us,
 //   128 28 us, 256 53 us, 128 with two splits 64 us; 4096 x 2048 -> 2048 fp32: 64
 //   307 us, 128 267 us; 20000 x 256 -> 256 fp32: 64 32 us, 128 40 us.
-GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
+GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int tile)
 {
     struct Cost {
         int tile;
@@ -1106,7 +1137,7 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
     GemmPlan best{};
     double least = 1e30;
     for (const Cost& c : kCosts[size == 4]) {
-        if (c.tile == 0 || (c.tile > 64 && std::max(M, N) <= c.tile / 2))
+        if (c.tile == 0 || (tile == 0 ? c.tile > 64 && std::max(M, N) <= c.tile / 2 : c.tile != tile))
             continue;
         const double blocks = (double)groups * (double)((M + c.tile - 1) / c.tile) *
                               (double)((N + c.tile - 1) / c.tile);
@@ -1127,9 +1158,29 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
             }
         }
     }
+    best.us = least;
     best.part_bytes = best.splits > 1 ? best.splits * groups * M * N * 4 : 0;
     best.sum_bytes = best.splits > 1 ? best.splits * groups * M * 4 : 0;
     return best;
+}
+
+// On different tiles the products are two launches, of which the second waits for the
+// first's last workgroups: 5 us and more (34998 x 225 -> 64 fp32).
+void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, GemmPlan& dw,
+                    GemmPlan& dx)
+{
+    constexpr double kLaunch = 5.0;
+    dw = gemm_plan(groups, out, in, rows, size);
+    dx = gemm_plan(groups, rows, in, out, size);
+    if (dw.tile == dx.tile)
+        return;
+    const GemmPlan w = gemm_plan(groups, out, in, rows, size, dx.tile);
+    const GemmPlan x = gemm_plan(groups, rows, in, out, size, dw.tile);
+    const double apart = dw.us + dx.us + kLaunch, as_dx = w.us + dx.us, as_dw = dw.us + x.us;
+    if (as_dx < apart && as_dx <= as_dw)
+        dw = w;
+    else if (as_dw < apart)
+        dx = x;
 }
 
 // The plan's part of a product's arguments
@@ -1169,12 +1220,14 @@ hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStre
                             : launch_forward_as<float>(a, p.tile, direct, s);
     if (e != hipSuccess)
         return e;
-    return bf ? launch_split_sums<bf16_t>(a, none, s) : launch_split_sums<float>(a, none, s);
+    const DbArgs no_db{};
+    return bf ? launch_split_sums<bf16_t>(a, none, no_db, s)
+              : launch_split_sums<float>(a, none, no_db, s);
 }
 
 template <typename E>
 static hipError_t backward_as(const GemmArgs& dw, int dw_tile, const GemmArgs& dx, int dx_tile,
-                              int load, hipStream_t s)
+                              int load, const DbArgs& db, hipStream_t s)
 {
     const GemmArgs none{};
     hipError_t e;
@@ -1185,21 +1238,21 @@ static hipError_t backward_as(const GemmArgs& dw, int dw_tile, const GemmArgs& d
         if (e == hipSuccess)
             e = launch_backward_as<E>(none, dx, dx_tile, load, s);
     }
-    return e != hipSuccess ? e : launch_split_sums<E>(dw, dx, s);
+    return e != hipSuccess ? e : launch_split_sums<E>(dw, dx, db, s);
 }
 
 hipError_t launch_linear_backward(int dtype, GemmArgs dw, GemmPlan pw, float* dw_part,
                                   float* sum_part, GemmArgs dx, GemmPlan px, float* dx_part,
-                                  hipStream_t s)
+                                  const DbArgs& db, hipStream_t s)
 {
     const int size = dtype == MALIB_DT_BF16 ? 2 : 4;
     bool direct = true, fused = false;
     if (dw.c.p) {
-        direct = chunked(dw.a, size, dw.M, dw.groups) && chunked(dw.b, size, dw.N, dw.groups);
+        direct = chunked(dw.a, size, dw.M, dw.groups, dw.a_padded) && chunked(dw.b, size, dw.N, dw.groups);
         fused = dw.a_act != MALIB_ACT_NONE;
     }
     if (dx.c.p) {
-        direct = direct && chunked(dx.a, size, dx.K, dx.groups) &&
+        direct = direct && chunked(dx.a, size, dx.K, dx.groups, dx.a_padded) &&
                  chunked(dx.b, size, dx.N, dx.groups);
         fused = fused || dx.a_act != MALIB_ACT_NONE;
     }
@@ -1216,8 +1269,8 @@ hipError_t launch_linear_backward(int dtype, GemmArgs dw, GemmPlan pw, float* dw
     if (dx.c.p)
         apply(dx, px, dx_part);
     return dtype == MALIB_DT_BF16
-               ? backward_as<bf16_t>(dw, pw.tile, dx, px.tile, load, s)
-               : backward_as<float>(dw, pw.tile, dx, px.tile, load, s);
+               ? backward_as<bf16_t>(dw, pw.tile, dx, px.tile, load, db, s)
+               : backward_as<float>(dw, pw.tile, dx, px.tile, load, db, s);
 }
 
 DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size)
@@ -1234,23 +1287,16 @@ DzPlan dz_plan(int64_t groups, int64_t M, int64_t N, int size)
 }
 
 hipError_t launch_dz(int dtype, const DzPlan& p, const MatArg& dy, const MatArg& pre,
-                     const MatArg& dz, int act, int groups, int M, int N, float* sums, float* db,
+                     const MatArg& dz, int act, int groups, int M, int N, float* sums,
                      hipStream_t s)
 {
     const dim3 grid(p.col_blocks, p.parts, groups);
-    float* to = !db ? nullptr : p.parts > 1 ? sums : db;
     if (dtype == MALIB_DT_BF16)
         dz_kernel<bf16_t><<<grid, kDzCols * kDzRows, 0, s>>>(dy, pre, dz, act, M, N,
-                                                             p.rows_per_block, to);
+                                                             p.rows_per_block, sums);
     else
         dz_kernel<float><<<grid, kDzCols * kDzRows, 0, s>>>(dy, pre, dz, act, M, N,
-                                                            p.rows_per_block, to);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || to == db)
-        return e;
-    const int64_t n = (int64_t)groups * N;
-    db_kernel<<<(unsigned)((n + kSumItems - 1) / kSumItems), kSumItems * kSumShares, 0, s>>>(
-        sums, n, p.parts, db);
+                                                            p.rows_per_block, sums);
     return hipGetLastError();
 }
 
