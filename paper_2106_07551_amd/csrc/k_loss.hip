@@ -285,6 +285,8 @@ __device__ __forceinline__ u32x4 load_masked(const E* p, int n, const uint8_t* m
 // multiple of 8 (up to 4 lanes per bank at 16).  (Rows padded to an odd stride
 // instead, their places found element by element: 105 us against 94 us for 2^21
 // rows of 18.)
+// Bound by memory for many rows: 2097152 x 18 fp32 86 us, 4.2 TB/s; 192 rows with masks and
+// reference logits 9 us, one chain of loads, LDS and stores.
 constexpr int kLaneThreads = 256, kLaneRows = 64, kLaneMost = 31;
 
 // i / w for i < 2048, w <= 32
@@ -1066,6 +1068,8 @@ __device__ __forceinline__ void load_row(const LossArgs& a, bool counts, const E
 }
 
 // Rows that fit the registers of T threads, C chunks each: read once, written once.
+// Bound by memory: 16384 x 8192 bf16 123 us, 4.4 TB/s; 4096 x 65536 bf16 with reference
+// logits 389 us, 4.1 TB/s; 2048 x 32000 fp32 distilled 123 us, 4.3 TB/s.
 template <typename E, int KIND, int T, int C>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
 {
@@ -1186,6 +1190,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
 // gradient (the second time from the caches).  PHASE 1: the sums of one of
 // `splits` parts of a row, into a.part; PHASE 2: the parts merged (by every workgroup
 // alike) and the gradient of one part.
+// 3 x 131071 bf16 in parts 13.5 us: three dependent launches.
 constexpr int kLongThreads = 512, kLongUnroll = 4;
 
 template <typename E, int KIND, int PHASE>
