@@ -311,9 +311,10 @@ malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t A, int64_t* wo
     TRY(check_loss(dtype, rows, A));
     if (!work_bytes)
         return set_error(MALIB_E_INVAL, "work_bytes is NULL");
-    // (the longest list takes the most workgroups)
-    *work_bytes = std::max(loss_plan(rows, A, 0, type_size(dtype)).work_bytes,
-                           loss_plan(rows, A, 256, type_size(dtype)).work_bytes);
+    // (of lists that as many threads take, the longest needs the most workgroups)
+    *work_bytes = 0;
+    for (const int top : {0, 32, 64, 128, 256})
+        *work_bytes = std::max(*work_bytes, loss_plan(rows, A, top, type_size(dtype)).work_bytes);
     return MALIB_OK;
 }
 

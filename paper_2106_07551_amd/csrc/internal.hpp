@@ -441,7 +441,7 @@ struct LossArgs {
 };
 enum { kLossLane, kLossRow, kLossLong, kLossSplit };
 struct LossPlan {
-    int variant, group, splits, part_chunks;
+    int variant, group, threads, splits, part_chunks;   // group: threads per row
     int64_t blocks, part_bytes, work_bytes;
 };
 LossPlan loss_plan(int64_t rows, int64_t A, int top, int size);   // top: 0 for the policy loss

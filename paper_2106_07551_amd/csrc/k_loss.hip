@@ -186,10 +186,9 @@ __device__ __forceinline__ void store_policy(const LossArgs& a, int64_t row, con
 }
 
 // Sum of one value per thread over the workgroup (in a fixed order), in thread 0.
-template <int THREADS>
 __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double part[THREADS / 64];
+    __shared__ double part[16];
 #pragma unroll
     for (int o = 32; o; o >>= 1)
         v += __shfl_xor(v, o);
@@ -199,7 +198,7 @@ __device__ __forceinline__ double block_sum(double v)
     __syncthreads();
     double t = 0.0;
     if (threadIdx.x == 0)
-        for (int i = 0; i < THREADS / 64; ++i)
+        for (int i = 0; i < (int)(blockDim.x >> 6); ++i)
             t += part[i];
     return t;
 }
@@ -639,7 +638,7 @@ __global__ __launch_bounds__(kLaneThreads) void loss_lane_kernel(LossArgs a)
             rows_from_lds(bx, (E*)a.dlogits + r0 * a.dlogits_ld, a.dlogits_ld, n, A, lane);
     }
     if (a.total)
-        store_total(a, block_sum<kLaneThreads>(total));
+        store_total(a, block_sum(total));
 }
 
 // ------------------------------------------------------- a group of lanes per row
@@ -856,19 +855,19 @@ __device__ __forceinline__ void write_action(const LossArgs& a, const RowGrad& g
 template <int T>
 struct List {
     static constexpr int kWords = T <= 64 ? T : 256;
-    static constexpr int kRows = T < 256 ? 256 / T : 1;   // per workgroup
     int* i;
     float *p, *x;
     uint32_t *seen, *twice;
     int top, padded;   // padded: top rounded up to 4
 
-    __device__ __forceinline__ List(void* lds, int slot, int top_)
+    // of row `slot` of the workgroup's `rows`
+    __device__ __forceinline__ List(void* lds, int slot, int rows, int top_)
         : top(top_), padded((top_ + 3) & ~3)
     {
         i = (int*)lds + slot * padded * 3;
         p = (float*)(i + padded);
         x = p + padded;
-        seen = (uint32_t*)lds + kRows * padded * 3 + slot * 2 * kWords;
+        seen = (uint32_t*)lds + rows * padded * 3 + slot * 2 * kWords;
         twice = seen + kWords;
     }
     __device__ __forceinline__ static uint32_t word(int i)
@@ -877,8 +876,12 @@ struct List {
     }
     __device__ __forceinline__ static uint32_t bit(int i) { return 1u << (i & 31); }
 };
-// of a workgroup's lists
-constexpr int list_bytes(int top, int rows) { return (((top + 3) & ~3) * 12) * rows + 2 * 256 * 4; }
+// of a workgroup's lists, with T threads per row
+constexpr int list_bytes(int top, int T, int threads)
+{
+    return T <= 64 ? ((top + 3) & ~3) * 12 * (threads / T) + 8 * threads
+                   : ((top + 3) & ~3) * 12 + 8 * 256;
+}
 
 // Loads the list and forms the probabilities.  Returns whether any entry counts (in
 // the TL lanes): its index is a legal entry.  `part`: this lane's sum of t ln t.
@@ -1071,15 +1074,15 @@ __device__ __forceinline__ void load_row(const LossArgs& a, bool counts, const E
 // Bound by memory: 16384 x 8192 bf16 123 us, 4.4 TB/s; 4096 x 65536 bf16 with reference
 // logits 389 us, 4.1 TB/s; 2048 x 32000 fp32 distilled 123 us, 4.3 TB/s.
 template <typename E, int KIND, int T, int C>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
+__global__ __launch_bounds__(T <= 64 ? 1024 : T) void loss_row_kernel(LossArgs a)
 {
-    constexpr int THREADS = T < 256 ? 256 : T, ROWS = THREADS / T;
+    const int ROWS = T <= 64 ? (int)blockDim.x / T : 1;
     constexpr int CH = kChunk<E>;
     extern __shared__ float lds[];
     __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
     constexpr int TL = T < 64 ? T : 64;
-    const List<T> list(lds, slot, KIND == kDistill ? a.top : 0);
+    const List<T> list(lds, slot, ROWS, KIND == kDistill ? a.top : 0);
     __shared__ int any_entry;
     const bool lists = KIND == kDistill && lane < TL;
     const float c = kLog2e / a.temperature;
@@ -1181,7 +1184,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void loss_row_kernel(LossArgs a)
         }
     }
     if (a.total)
-        store_total(a, block_sum<THREADS>(total));
+        store_total(a, block_sum(total));
 }
 
 // ------------------------------------------- long rows: a workgroup per part of a row
@@ -1200,7 +1203,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
     extern __shared__ float lds[];
     __shared__ float scratch[2 * kScratch];
     const int tid = threadIdx.x;
-    const List<T> list(lds, 0, KIND == kDistill ? a.top : 0);
+    const List<T> list(lds, 0, 1, KIND == kDistill ? a.top : 0);
     __shared__ int any_entry;
     const bool lists = KIND == kDistill && tid < 64;
     const float c = kLog2e / a.temperature;
@@ -1322,7 +1325,7 @@ __global__ __launch_bounds__(kLongThreads) void loss_long_kernel(LossArgs a)
         }
     }
     if (PHASE != 1 && a.total)
-        store_total(a, block_sum<T>(total));
+        store_total(a, block_sum(total));
 }
 
 __global__ __launch_bounds__(256) void loss_total_kernel(const double* part, int64_t n, float* total)
@@ -1330,7 +1333,7 @@ __global__ __launch_bounds__(256) void loss_total_kernel(const double* part, int
     double v = 0.0;
     for (int64_t i = threadIdx.x; i < n; i += 256)
         v += part[i];
-    v = block_sum<256>(v);
+    v = block_sum(v);
     if (threadIdx.x == 0)
         *total = (float)v;
 }
@@ -1338,58 +1341,57 @@ __global__ __launch_bounds__(256) void loss_total_kernel(const double* part, int
 template <typename E, int KIND>
 hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
 {
-    const int top = a.top;
-    auto list = [top](int rows) { return KIND == kDistill ? (size_t)list_bytes(top, rows) : 0; };
-    const unsigned nb = (unsigned)p.blocks;
+    const unsigned nb = (unsigned)p.blocks, nt = (unsigned)p.threads;
+    const size_t lds = p.variant == kLossLane
+                           ? (size_t)kLaneThreads * 4 * lane_floats(KIND, a.A, a.top)
+                       : KIND == kDistill ? (size_t)list_bytes(a.top, p.group, p.threads) : 0;
     switch (p.variant) {
-    case kLossLane: {
-        const size_t lds = (size_t)kLaneThreads * 4 * lane_floats(KIND, a.A, a.top);
+    case kLossLane:
         if (a.A <= 8)
-            loss_lane_kernel<E, KIND, 8><<<nb, kLaneThreads, lds, s>>>(a);
+            loss_lane_kernel<E, KIND, 8><<<nb, nt, lds, s>>>(a);
         else if (a.A <= 16)
-            loss_lane_kernel<E, KIND, 16><<<nb, kLaneThreads, lds, s>>>(a);
+            loss_lane_kernel<E, KIND, 16><<<nb, nt, lds, s>>>(a);
         else if (a.A <= 24)
-            loss_lane_kernel<E, KIND, 24><<<nb, kLaneThreads, lds, s>>>(a);
+            loss_lane_kernel<E, KIND, 24><<<nb, nt, lds, s>>>(a);
         else
-            loss_lane_kernel<E, KIND, 32><<<nb, kLaneThreads, lds, s>>>(a);
+            loss_lane_kernel<E, KIND, 32><<<nb, nt, lds, s>>>(a);
         break;
-    }
     case kLossRow:
         switch (p.group) {
         case 4:
-            loss_row_kernel<E, KIND, 4, 4><<<nb, 256, list(64), s>>>(a);
+            loss_row_kernel<E, KIND, 4, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 8:
-            loss_row_kernel<E, KIND, 8, 4><<<nb, 256, list(32), s>>>(a);
+            loss_row_kernel<E, KIND, 8, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 16:
-            loss_row_kernel<E, KIND, 16, 4><<<nb, 256, list(16), s>>>(a);
+            loss_row_kernel<E, KIND, 16, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 32:
-            loss_row_kernel<E, KIND, 32, 4><<<nb, 256, list(8), s>>>(a);
+            loss_row_kernel<E, KIND, 32, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 64:
-            loss_row_kernel<E, KIND, 64, 4><<<nb, 256, list(4), s>>>(a);
+            loss_row_kernel<E, KIND, 64, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 256:
-            loss_row_kernel<E, KIND, 256, 4><<<nb, 256, list(1), s>>>(a);
+            loss_row_kernel<E, KIND, 256, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 512:
-            loss_row_kernel<E, KIND, 512, 4><<<nb, 512, list(1), s>>>(a);
+            loss_row_kernel<E, KIND, 512, 4><<<nb, nt, lds, s>>>(a);
             break;
         case 1024:
-            loss_row_kernel<E, KIND, 1024, 4><<<nb, 1024, list(1), s>>>(a);
+            loss_row_kernel<E, KIND, 1024, 4><<<nb, nt, lds, s>>>(a);
             break;
         default:
-            loss_row_kernel<E, KIND, 1024, 8><<<nb, 1024, list(1), s>>>(a);
+            loss_row_kernel<E, KIND, 1024, 8><<<nb, nt, lds, s>>>(a);
         }
         break;
     case kLossLong:
-        loss_long_kernel<E, KIND, 0><<<nb, kLongThreads, list(1), s>>>(a);
+        loss_long_kernel<E, KIND, 0><<<nb, nt, lds, s>>>(a);
         break;
     default:
-        loss_long_kernel<E, KIND, 1><<<nb, kLongThreads, list(1), s>>>(a);
-        loss_long_kernel<E, KIND, 2><<<nb, kLongThreads, list(1), s>>>(a);
+        loss_long_kernel<E, KIND, 1><<<nb, nt, lds, s>>>(a);
+        loss_long_kernel<E, KIND, 2><<<nb, nt, lds, s>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.total || p.blocks == 1)
@@ -1420,16 +1422,26 @@ LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
     // (the rows of a workgroup fit 64 KB of LDS)
     if (A <= kLaneMost && (top == 0 || (top <= 32 && lane_floats(kDistill, (int)A, top) <= 64))) {
         p.variant = kLossLane;
-        per = kLaneThreads;
+        per = p.threads = kLaneThreads;
     } else if (A <= 256 * 4 * ch || (A <= 1024 * 8 * ch && rows >= kCus / 2)) {
         p.variant = kLossRow;
         p.group = 4;
         // at most 8 entries of a teacher's list per lane
         while (p.group * 4 * ch < A || (p.group < 64 && p.group * 8 < top))
             p.group *= p.group == 64 ? 4 : 2;
-        per = std::max(1, 256 / p.group);
+        // rows that 1024 threads hold at once are one workgroup's, which leaves no totals
+        // of others to add in a launch of its own: 10 x 266 fp32 distilled 7.7 us, in
+        // workgroups of 256 threads 11.4 us.  (Two rounds: 128 x 281 bf16 14.8 and 11.5 us.)
+        p.threads = p.group <= 64 ? 256 : std::min(p.group, 1024);
+        if (p.group <= 64 && rows > 0 && rows * p.group <= 1024) {
+            const int one = (int)((rows * p.group + 63) / 64 * 64);
+            if (list_bytes(top, p.group, one) <= 65536)
+                p.threads = one;
+        }
+        per = std::max(1, p.threads / p.group);
     } else {
         p.variant = kLossLong;
+        p.threads = p.group = kLongThreads;
         const int64_t chunks = (A + ch - 1) / ch;
         if (rows < 2 * kCus) {
             // parts of at least 512 chunks (8 KB)
