@@ -1130,7 +1130,8 @@ static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups,
 // sum of the splits' parts is a launch and their bytes at about 3.5 TB/s.
 //   8192 x 4096 -> 4096 bf16: 64 480 us, 128 279 us, 256 238 us; 2048^3: 64 33 us,
 //   128 28 us, 256 53 us, 128 with two splits 64 us; 4096 x 2048 -> 2048 fp32: 64
-//   307 us, 128 267 us; 20000 x 256 -> 256 fp32: 64 32 us, 128 40 us.
+//   307 us, 128 267 us; 20000 x 256 -> 256 fp32: 64 31 us, 128 43 us; 27815 x 61 -> 281
+//   fp32 with ReLU and residual: 64 26 us, 128 41 us.
 GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int tile)
 {
     struct Cost {
@@ -1138,7 +1139,7 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, in
         double busy, alone, out;
     };
     static constexpr Cost kCosts[2][3] = {{{64, 0.23, 0.30, 1.3}, {128, 0.55, 0.75, 3.1}, {256, 1.75, 1.75, 10.0}},
-                                          {{64, 0.60, 0.70, 1.4}, {128, 2.08, 2.1, 2.7}, {0, 0, 0, 0}}};
+                                          {{64, 0.60, 0.70, 1.4}, {128, 2.08, 2.1, 7.5}, {0, 0, 0, 0}}};
     constexpr double kCus = 256, kSumLaunch = 5.0, kSumBytes = 3.5e6;
     const int bk = 128 / size;
     const int64_t k_tiles = std::max<int64_t>(1, (K + bk - 1) / bk);
