@@ -172,6 +172,16 @@ def test_few_rows(dtype, M, K, N, G):
     check_layer(dtype, G, M, K, N, "relu", pad=3, shift=1, bias=False)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("G, M, K, N, act", [(1, 60001, 6, 24, "gelu"), (1, 40000, 40, 11, "relu"),
+                                             (3, 30000, 16, 5, "silu"), (1, 50000, 200, 72, "silu"),
+                                             (2, 9000, 320, 5, "gelu"), (1, 30000, 128, 64, "none")])
+def test_many_rows_of_narrow_layers(dtype, G, M, K, N, act):
+    """dW's sums in hundreds of parts, dbias from either kernel, dz's rows padded."""
+    check_layer(dtype, G, M, K, N, act, residual=False)
+    check_layer(dtype, G, M, K, N, act, residual=False, pad=3)
+
+
 @pytest.mark.parametrize("pad, shift", [(1, 0), (8, 0), (8, 1), (3, 5), (0, 2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_strides_and_alignment(dtype, pad, shift):
