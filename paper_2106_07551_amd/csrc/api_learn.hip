@@ -118,10 +118,16 @@ BackwardPlan make_backward_plan(const malib_linear_desc* d)
     const bool act = d->act != MALIB_ACT_NONE;
     const bool rounded = size == 2 && (d->act == MALIB_ACT_GELU || d->act == MALIB_ACT_SILU);
     BackwardPlan p;
-    backward_plans(d->groups, d->rows, d->in, d->out, size, p.dw, p.dx);
     p.dz = dz_plan(d->groups, d->rows, d->out, size);
     p.fused = act && !rounded &&
               (d->groups * d->rows * d->out <= kFusedMost || d->in <= kFusedWidth);
+    // (dz formed in the workspace has padded rows)
+    int loads = loads_of(d->in, size);
+    if (!act || p.fused)
+        loads = std::max(loads, loads_of(d->out, size));
+    if (p.fused)
+        loads = std::max<int>(loads, kLoadsStaged);
+    backward_plans(d->groups, d->rows, d->in, d->out, size, loads, p.dw, p.dx);
     p.own_sums = (act && !p.fused) || p.dw.tile == 256;
     p.dz_ld = (d->out + ch - 1) / ch * ch;
     p.dz_at = 0;

@@ -387,11 +387,20 @@ struct GemmPlan {
     int64_t k_split, part_bytes, sum_bytes;
     double us;   // estimated
 };
+// How operands load, as far as sizes tell: straight to LDS, through registers, or (a
+// contiguous extent below 16 bytes) element by element.
+enum { kLoadsDirect, kLoadsStaged, kLoadsNarrow };
+inline int loads_of(int64_t contiguous, int size)
+{
+    const int64_t ch = 16 / size;
+    return contiguous < ch ? kLoadsNarrow : contiguous % ch ? kLoadsStaged : kLoadsDirect;
+}
 // `tile`: only that one (0: the best)
-GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int tile = 0);
+GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int loads,
+                   int tile = 0);
 // dW's and dx's plans of a backward pass, on the same tile where one launch is cheaper
-void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, GemmPlan& dw,
-                    GemmPlan& dx);
+void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, int loads,
+                    GemmPlan& dw, GemmPlan& dx);
 // the forward's plan: up to kFewRows rows a kernel of its own (tile 0)
 constexpr int kFewRows = 16;
 GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);

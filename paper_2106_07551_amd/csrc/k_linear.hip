@@ -1129,13 +1129,15 @@ static bool chunked(const MatArg& m, int size, int64_t contiguous, int groups,
 
 // Tile and splits by estimated time on 256 CUs, from measured constants (us; bf16,
 // fp32): a CU's time per 128 bytes of k of a tile with several workgroups on it
-// (`busy`) and with one (`alone`), and the time of a tile's output (`out`).  The
+// (`busy`) and with one (`alone`; at least 1 us through registers, 2 us element by
+// element: 898 x 4 -> 1280 bf16 backward 43 us without splits), and the time of a
+// tile's output (`out`).  The
 // sum of the splits' parts is a launch and their bytes at about 3.5 TB/s.
 //   8192 x 4096 -> 4096 bf16: 64 480 us, 128 279 us, 256 238 us; 2048^3: 64 33 us,
 //   128 28 us, 256 53 us, 128 with two splits 64 us; 4096 x 2048 -> 2048 fp32: 64
 //   307 us, 128 267 us; 20000 x 256 -> 256 fp32: 64 31 us, 128 43 us; 27815 x 61 -> 281
 //   fp32 with ReLU and residual: 64 26 us, 128 41 us.
-GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int tile)
+GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, int loads, int tile)
 {
     struct Cost {
         int tile;
@@ -1151,6 +1153,8 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, in
     for (const Cost& c : kCosts[size == 4]) {
         if (c.tile == 0 || (tile == 0 ? c.tile > 64 && std::max(M, N) <= c.tile / 2 : c.tile != tile))
             continue;
+        const double alone = std::max(c.alone, loads == kLoadsNarrow   ? 2.0
+                                               : loads == kLoadsStaged ? 1.0 : 0.0);
         const double blocks = (double)groups * (double)((M + c.tile - 1) / c.tile) *
                               (double)((N + c.tile - 1) / c.tile);
         for (int64_t s = 1; s <= 512; s *= 2) {
@@ -1159,7 +1163,7 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, in
             const int64_t per = (k_tiles + s - 1) / s;
             const int64_t splits = (k_tiles + per - 1) / per;
             const double n = std::max(1.0, std::ceil(blocks * (double)splits / kCus));
-            double t = (double)per * std::max(c.alone, n * c.busy) + n * c.out;
+            double t = (double)per * std::max(alone, n * c.busy) + n * c.out;
             if (splits > 1)
                 t += kSumLaunch + (double)splits * (double)groups * (double)M * (double)N * 4.0 / kSumBytes;
             if (t < least) {
@@ -1178,16 +1182,16 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, in
 
 // On different tiles the products are two launches, of which the second waits for the
 // first's last workgroups: 5 us and more (34998 x 225 -> 64 fp32).
-void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, GemmPlan& dw,
-                    GemmPlan& dx)
+void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, int loads,
+                    GemmPlan& dw, GemmPlan& dx)
 {
     constexpr double kLaunch = 5.0;
-    dw = gemm_plan(groups, out, in, rows, size);
-    dx = gemm_plan(groups, rows, in, out, size);
+    dw = gemm_plan(groups, out, in, rows, size, loads);
+    dx = gemm_plan(groups, rows, in, out, size, loads);
     if (dw.tile == dx.tile)
         return;
-    const GemmPlan w = gemm_plan(groups, out, in, rows, size, dx.tile);
-    const GemmPlan x = gemm_plan(groups, rows, in, out, size, dw.tile);
+    const GemmPlan w = gemm_plan(groups, out, in, rows, size, loads, dx.tile);
+    const GemmPlan x = gemm_plan(groups, rows, in, out, size, loads, dw.tile);
     const double apart = dw.us + dx.us + kLaunch, as_dx = w.us + dx.us, as_dw = dw.us + x.us;
     if (as_dx < apart && as_dx <= as_dw)
         dw = w;
@@ -1214,7 +1218,7 @@ GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
         p.k_split = K;
         return p;
     }
-    return gemm_plan(groups, M, N, K, size);
+    return gemm_plan(groups, M, N, K, size, loads_of(K, size));
 }
 
 hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s)

@@ -1373,6 +1373,9 @@ hipError_t launch_kind(const LossArgs& a, const LossPlan& p, hipStream_t s)
         case 64:
             loss_row_kernel<E, KIND, 64, 4><<<nb, nt, lds, s>>>(a);
             break;
+        case 128:
+            loss_row_kernel<E, KIND, 128, 4><<<nb, nt, lds, s>>>(a);
+            break;
         case 256:
             loss_row_kernel<E, KIND, 256, 4><<<nb, nt, lds, s>>>(a);
             break;
@@ -1410,7 +1413,7 @@ __global__ void zero_total_kernel(float* total) { *total = 0.0f; }
 // are read twice, in parts where there are few.  Rows in registers against rows read
 // twice: 4096 x 65536 bf16 with reference logits 394 and 411 us, 2048 x 32000 fp32 with
 // them 172 and 227 us, 2047 x 50001 bf16 distilled 122 and 129 us, 4096 x 50000 bf16 207
-// and 205 us.
+// and 205 us.  128 threads against 256: 20888 x 3602 bf16 89 and 118 us.
 LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
 {
     constexpr int64_t kCus = 256;
@@ -1428,7 +1431,7 @@ LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
         p.group = 4;
         // at most 8 entries of a teacher's list per lane
         while (p.group * 4 * ch < A || (p.group < 64 && p.group * 8 < top))
-            p.group *= p.group == 64 ? 4 : 2;
+            p.group *= 2;
         // rows that 1024 threads hold at once are one workgroup's, which leaves no totals
         // of others to add in a launch of its own: 10 x 266 fp32 distilled 7.7 us, in
         // workgroups of 256 threads 11.4 us.  (Two rounds: 128 x 281 bf16 14.8 and 11.5 us.)
@@ -1439,6 +1442,8 @@ LossPlan loss_plan(int64_t rows, int64_t A, int top, int size)
                 p.threads = one;
         }
         per = std::max(1, p.threads / p.group);
+        if (p.threads == 128)
+            most = 4096;
     } else {
         p.variant = kLossLong;
         p.threads = p.group = kLongThreads;
