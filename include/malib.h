@@ -607,7 +607,8 @@ malib_status malib_linear_work(const malib_linear_desc* desc, int32_t backward,
  *   KL = sum_j p_j (log p_j - log q_j) where reference logits are given (q:
  *        their softmax over the same entries), else e^d - 1 - d with
  *        d = ref_logp - l where the reference's log probability of the action
- *        is given, else 0
+ *        is given, else 0 (with kl_coef 0 a statistic only: whatever it is, loss
+ *        and gradient are those without a reference)
  *   total = sum over rows of w loss
  *  logits, ref_logits, dlogits: [rows][actions] of `dtype`, rows the strides
  *       apart; ref_logits may be NULL.

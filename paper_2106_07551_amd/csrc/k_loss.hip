@@ -89,6 +89,7 @@ __device__ __forceinline__ void add_entry(Stats& r, float x, float y, float m, f
 // What a row's gradient needs.
 struct RowGrad {
     float m, my, c0, c1, c2;
+    float with_ref;       // the reference enters where e is above: 0, or inf (nowhere)
     float at_action;      // policy: added at the action
 };
 
@@ -100,7 +101,7 @@ __device__ __forceinline__ float grad_entry(const RowGrad& g, float x, float y, 
     if (KIND != kDistill)
         k = __builtin_fmaf(g.c1, fmaxf(d, kLeast), k);
     if (KIND == kPolicyRef)
-        k = __builtin_fmaf(g.c2, e > 0.0f ? (y - g.my) * kLog2e : 0.0f, k);
+        k = __builtin_fmaf(g.c2, e > g.with_ref ? (y - g.my) * kLog2e : 0.0f, k);
     return e * k;
 }
 
@@ -150,18 +151,23 @@ __device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, const Poli
     float slope = s1 <= s2 ? -s1 : s1 != s1 ? s1 : 0.0f;   // d loss / d log p[action]
     o.loss = -(s2 < s1 ? s2 : s1);
     o.kl = 0.0f;
+    // (a divergence with a coefficient of 0 is a statistic only: infinite or NaN, it
+    // leaves loss and gradient alone)
+    const bool with_kl = a.kl_coef != 0.0f;
     float pull = 0.0f;   // of the divergence, in every logit
     if (KIND == kPolicyRef) {
         const float ln_sy = logf(st.sy);
         o.kl = kLn2 * (st.t - st.v) * inv - ln_s + ln_sy;
-        pull = a.kl_coef * (ln_sy - ln_s - o.kl);
+        if (with_kl)
+            pull = a.kl_coef * (ln_sy - ln_s - o.kl);
     } else if (a.ref_logp) {
         const float d = row.ref_logp - o.logp;
         const float em = expm1f(d);
         o.kl = em - d;
-        slope -= a.kl_coef * em;
+        if (with_kl)
+            slope -= a.kl_coef * em;
     }
-    if (a.kl_coef != 0.0f)
+    if (with_kl)
         o.loss += a.kl_coef * o.kl;
     if (a.entropy_coef != 0.0f)
         o.loss -= a.entropy_coef * o.entropy;
@@ -171,6 +177,7 @@ __device__ __forceinline__ PolicyOut policy_finish(const LossArgs& a, const Poli
     g.c0 = k * (pull + a.entropy_coef * (o.entropy - ln_s) - slope);
     g.c1 = k * kLn2 * (a.entropy_coef + (KIND == kPolicyRef ? a.kl_coef : 0.0f));
     g.c2 = KIND == kPolicyRef ? -k * kLn2 * a.kl_coef : 0.0f;
+    g.with_ref = with_kl ? 0.0f : -kNegInf;
     g.at_action = w * slope;
     return o;
 }

@@ -254,6 +254,37 @@ def test_policy_infinite_logits(dtype, a):
     assert float(stats[2, 8]) == math.inf
 
 
+# rows by one lane, by lanes of a wavefront, by workgroups, read twice, in parts
+@DTYPES
+@pytest.mark.parametrize("n, a", [(70, 18), (40, 300), (20, 6000), (130, 12000), (520, 66000),
+                                  (3, 131071)])
+def test_policy_divergence_as_statistic(dtype, n, a):
+    """With a coefficient of 0 a divergence is only reported: loss and gradient are
+    those without a reference, where it is infinite or NaN too."""
+    import paper_2106_07551_amd as MA
+    d = policy_inputs(dtype, n, a, seed=n + a, weight=True)
+    x, old, adv = d["logits"], d["old_logp"], d["advantage"]
+    d["weight"][:2] = 0.5
+    act = torch.zeros(n, dtype=torch.int32, device="cuda")
+    y, ref_logp = d["ref_logits"], d["ref_logp"]
+    y[0, a - 1] = -math.inf           # excluded by the reference, not by the policy
+    y[1, :] = -math.inf
+    y[2, a // 2] = float("nan")
+    ref_logp[0], ref_logp[1], ref_logp[2] = 200.0, math.inf, float("nan")
+    x[0, 0] = -math.inf               # the action itself
+    T, S, G, scale, size, L, w, ok = policy64(x, act, old, adv, ent=0.02, weight=d["weight"])
+    eps = 2.0 ** -8 if dtype == torch.bfloat16 else U
+    for ref in (dict(ref_logits=y), dict(ref_logp=ref_logp)):
+        print("[statistic]", dtype, n, a, list(ref), flush=True)
+        total, stats, grad = MA.policy_loss(x, act, old, adv, clip_low=LO, clip_high=HI,
+                                            entropy_coef=0.02, weight=d["weight"], **ref)
+        assert not torch.isfinite(stats[2, :3][ok[:3]]).any()
+        bound = 400 * U * L * scale
+        close(stats[0], S[0], bound, "loss")
+        close(total[0], T, (w.abs() * bound)[ok].sum(), "total")
+        close(grad, G, 400 * U * L[:, None] * size, "gradient", eps)
+
+
 def test_policy_no_rows_and_one_action():
     import paper_2106_07551_amd as MA
     e = torch.empty(0, device="cuda")
