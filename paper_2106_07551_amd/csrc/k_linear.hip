@@ -30,19 +30,25 @@ constexpr int kBK = 128 / (int)sizeof(E);
 // policies' hidden layers do; its derivative at 0 is 0.
 __device__ __forceinline__ float relu_f32(float z) { return z != z ? z : (z > 0.0f ? z : 0.0f); }
 
-// e^-x^2 / 2 (`e`) and Phi(x), the normal distribution function, by Hastings' rational
-// approximation of erf (Abramowitz and Stegun 7.1.26, absolute error below 1.5e-7, a
-// quarter of what 1 + erf loses in fp32 to the left of -3 anyway).
+// e^-x^2 / 2 (`e`) and Phi(x), the normal distribution function.  With ax = |x|,
+// 1 - Phi(ax) = e^(-x^2 / 2) R(ax), where R is smooth and falls like 1 / ax: a polynomial
+// in t = 1 / (1 + 0.32 ax), fitted to R for the least relative error over all ax >= 0
+// (3.2e-8).  To the left the exponent's rounding is the larger part: Phi is within 4e-7 of
+// itself down to -2, 2e-6 at -6 (0.5 (1 + erf) in fp32: 1e-5 at -3, 5% at -5).
 __device__ __forceinline__ float normal_cdf(float x, float& e)
 {
-    const float ax = __builtin_fabsf(x) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, ax, 1.0f));
-    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-    p = __builtin_fmaf(p, t, 1.421413741f);
-    p = __builtin_fmaf(p, t, -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.254829592f);
+    constexpr int N = 10;
+    constexpr float kR[N] = {1.276615262e-01f, 1.276609451e-01f,  1.146223545e-01f,
+                             8.782909811e-02f, 5.865395442e-02f,  -9.377530776e-03f,
+                             6.532797217e-02f, -1.467074007e-01f, 9.540722519e-02f,
+                             -2.107816003e-02f};
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.32f, __builtin_fabsf(x), 1.0f));
+    float p = kR[N - 1];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i)
+        p = __builtin_fmaf(p, t, kR[i]);
     e = __builtin_amdgcn_exp2f(-0.72134752044448170f * (x * x));
-    const float tail = 0.5f * (p * t) * e;   // 1 - Phi(|x|)
+    const float tail = (p * t) * e;
     return x > 0.0f ? 1.0f - tail : tail;
 }
 

@@ -133,6 +133,48 @@ def test_activations(dtype, act):
     check_layer(dtype, None, 130, 96, 72, act)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_gelu_relative_to_itself(dtype):
+    """GELU and its slope z by z, far into the tail, through every kernel that
+    evaluates them.  Products of z with ones and zeros are exact, so each output is
+    the function's, rounded once.  Roundings in fp32, u = 2^-24 each: of 1 / (1 + q |z|)
+    3, which the fit in it magnifies by up to 2.5; of a sum of ten terms 3, the fit
+    itself 0.5; of the exponential 2 and, from its exponent, 1.5 z^2; of the
+    products 4: under (18 + 2 z^2) u of Phi and of z phi.  Then the output's rounding."""
+    import paper_2106_07551_amd as MA
+    u = 2.0 ** -24
+    z = torch.linspace(-12.0, 8.0, 20001, device="cuda").to(dtype)
+    zd = z.double()
+    phi, cdf = torch.exp(-zd * zd / 2) / math.sqrt(2 * math.pi), \
+        0.5 * torch.special.erfc(-zd / math.sqrt(2))
+    half = 1.01 * (2.0 ** -8 if dtype == torch.bfloat16 else u)
+    own = (18 + 2 * zd * zd) * u
+
+    def check(got, ref, bound, what):
+        err, tol = (got.double() - ref).abs(), bound + half * ref.abs()
+        assert (err <= tol).all(), (what, float((err / tol).max()), float(zd[(err / tol).argmax()]))
+
+    one = torch.ones((1, 1), dtype=dtype, device="cuda")
+    value, slope = zd * cdf, cdf + zd * phi
+    vb, sb = own * value.abs(), own * (cdf + (zd * phi).abs())
+    col = z[:, None].contiguous()
+    check(MA.linear(col, one, act=MA.ACT_GELU)[:, 0], value, vb, "tiles")
+    check(MA.linear(one, col, act=MA.ACT_GELU)[0], value, vb, "few rows")
+    dy = torch.ones_like(col)
+    dx, _, _ = MA.linear_backward(dy, col, one, act=MA.ACT_GELU, pre=col)
+    check(dx[:, 0], slope, sb, "slope, few values")
+    n, m = 64, 312 * 64                       # more than 2^20 values, more than 128 inputs
+    pre = col[:m].view(-1, n).repeat(64, 1)
+    w = torch.zeros((n, 136), dtype=dtype, device="cuda")
+    w[:, :n].fill_diagonal_(1.0)
+    x = torch.zeros((pre.shape[0], 136), dtype=dtype, device="cuda")
+    dx, _, _ = MA.linear_backward(torch.ones_like(pre), x, w, act=MA.ACT_GELU, pre=pre)
+    got = dx[:, :n].reshape(64, m)
+    assert (got == got[:1]).all()
+    check(torch.cat([got[0], dx.new_zeros(zd.numel() - m)]), torch.cat([slope[:m], 0 * zd[m:]]),
+          sb, "slope, many values")
+
+
 # one row, one unit, one input; both sides of chunks, tiles and stages; the
 # policies' own layers; long sums that are split over workgroups
 SIZES = [(1, 1, 1), (1, 24, 64), (3, 5, 7), (2, 8, 3), (64, 64, 64), (65, 63, 66), (127, 129, 31),
