@@ -87,7 +87,7 @@ malib_status check_work(void* work, int64_t have, int64_t need)
     return MALIB_OK;
 }
 
-// Workgroups of one product fit a launch (the largest tile may become 128)
+// Workgroups of one product are counted in 31 bits (the largest tile may become 128)
 malib_status check_grid(const malib_linear_desc* d, const GemmPlan& p, int64_t M, int64_t N)
 {
     if (p.tile == 0)
@@ -95,7 +95,7 @@ malib_status check_grid(const malib_linear_desc* d, const GemmPlan& p, int64_t M
     const int64_t tile = std::min(p.tile, 128);
     const int64_t mt = (M + tile - 1) / tile, nt = (N + tile - 1) / tile;
     if (mt * nt > kMaxRows / ((int64_t)d->groups * p.splits))
-        return set_error(MALIB_E_UNSUPPORTED, "the layer has more tiles than one launch takes");
+        return set_error(MALIB_E_UNSUPPORTED, "the layer has 2^31 tiles or more");
     return MALIB_OK;
 }
 

@@ -699,23 +699,25 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t block, uin
 }
 
 template <typename E, int TILE, int LOAD, int STAGES>
-__global__ __launch_bounds__(GemmShape<TILE>::kThreads) void forward_kernel(GemmArgs a)
+__global__ __launch_bounds__(GemmShape<TILE>::kThreads) void forward_kernel(GemmArgs a,
+                                                                            uint32_t first)
 {
     __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::lds(STAGES)];
-    gemm_tile<E, true, true, TILE, LOAD, STAGES>(a, blockIdx.x, gridDim.x, lds);
+    gemm_tile<E, true, true, TILE, LOAD, STAGES>(a, first + blockIdx.x, (uint32_t)a.blocks, lds);
 }
 
 // dW's tiles, then dx's, in one launch: neither waits for the other's last tiles.
 template <typename E, int TILE, int LOAD, int STAGES>
 __global__ __launch_bounds__(GemmShape<TILE>::kThreads) void backward_kernel(GemmArgs dw,
-                                                                             uint32_t n_dw,
-                                                                             GemmArgs dx)
+                                                                             GemmArgs dx,
+                                                                             uint32_t first)
 {
     __shared__ __attribute__((aligned(16))) char lds[GemmShape<TILE>::lds(STAGES)];
-    if (blockIdx.x < n_dw)
-        gemm_tile<E, false, false, TILE, LOAD, STAGES>(dw, blockIdx.x, n_dw, lds);
+    const uint32_t block = first + blockIdx.x, n_dw = (uint32_t)dw.blocks;
+    if (block < n_dw)
+        gemm_tile<E, false, false, TILE, LOAD, STAGES>(dw, block, n_dw, lds);
     else
-        gemm_tile<E, true, false, TILE, LOAD, STAGES>(dx, blockIdx.x - n_dw, gridDim.x - n_dw, lds);
+        gemm_tile<E, true, false, TILE, LOAD, STAGES>(dx, block - n_dw, (uint32_t)dx.blocks, lds);
 }
 
 // -------------------------------------------------------------- few rows, forward
@@ -1034,27 +1036,37 @@ int small_stages(int64_t blocks, int64_t k_split, int bk)
     return blocks >= 1024 || k_split <= 2 * bk ? 2 : 4;
 }
 
+// launch(first, count) for n workgroups: a launch takes fewer than 2^32 threads
+template <typename F>
+hipError_t in_launches(uint32_t n, F launch)
+{
+    constexpr uint64_t kMost = (uint64_t)1 << 22;   // (a multiple of the 8 XCDs)
+    for (uint64_t first = 0; first < n; first += kMost)
+        launch((uint32_t)first, (unsigned)std::min(kMost, n - first));
+    return hipGetLastError();
+}
+
 template <typename E>
 hipError_t launch_forward_as(const GemmArgs& a, int tile, bool direct, hipStream_t s)
 {
-    const unsigned nb = (unsigned)a.blocks;
+    auto run = [&](auto kernel, int threads) {
+        return in_launches((uint32_t)a.blocks, [&](uint32_t first, unsigned nb) {
+            kernel<<<nb, threads, 0, s>>>(a, first);
+        });
+    };
     if constexpr (sizeof(E) == 2) {   // (fp32 plans take no larger tile than 128)
-        if (tile == 256) {
-            forward_kernel<E, 256, kDirect, 2><<<nb, 512, 0, s>>>(a);
-            return hipGetLastError();
-        }
+        if (tile == 256)
+            return run(forward_kernel<E, 256, kDirect, 2>, 512);
     }
     if (tile == 128 && direct)
-        forward_kernel<E, 128, kDirect, 2><<<nb, 256, 0, s>>>(a);
-    else if (tile == 128)
-        forward_kernel<E, 128, kStaged, 2><<<nb, 256, 0, s>>>(a);
-    else if (!direct)
-        forward_kernel<E, 64, kStaged, 2><<<nb, 256, 0, s>>>(a);
-    else if (small_stages(a.blocks, a.k_split, kBK<E>) == 2)
-        forward_kernel<E, 64, kDirect, 2><<<nb, 256, 0, s>>>(a);
-    else
-        forward_kernel<E, 64, kDirect, 4><<<nb, 256, 0, s>>>(a);
-    return hipGetLastError();
+        return run(forward_kernel<E, 128, kDirect, 2>, 256);
+    if (tile == 128)
+        return run(forward_kernel<E, 128, kStaged, 2>, 256);
+    if (!direct)
+        return run(forward_kernel<E, 64, kStaged, 2>, 256);
+    if (small_stages(a.blocks, a.k_split, kBK<E>) == 2)
+        return run(forward_kernel<E, 64, kDirect, 2>, 256);
+    return run(forward_kernel<E, 64, kDirect, 4>, 256);
 }
 
 template <typename E>
@@ -1069,31 +1081,32 @@ template <typename E>
 hipError_t launch_backward_as(const GemmArgs& dw, const GemmArgs& dx, int tile, int load,
                               hipStream_t s)
 {
-    const uint32_t n_dw = (uint32_t)dw.blocks, nb = n_dw + (uint32_t)dx.blocks;
+    const uint32_t nb = (uint32_t)dw.blocks + (uint32_t)dx.blocks;   // (each below 2^31)
     if (nb == 0)
         return hipSuccess;
+    auto run = [&](auto kernel, int threads) {
+        return in_launches(nb, [&](uint32_t first, unsigned n) {
+            kernel<<<n, threads, 0, s>>>(dw, dx, first);
+        });
+    };
     const int64_t k = std::max(dw.blocks ? dw.k_split : 0, dx.blocks ? dx.k_split : 0);
     if constexpr (sizeof(E) == 2) {
-        if (tile == 256) {
-            backward_kernel<E, 256, kDirect, 2><<<nb, 512, 0, s>>>(dw, n_dw, dx);
-            return hipGetLastError();
-        }
+        if (tile == 256)
+            return run(backward_kernel<E, 256, kDirect, 2>, 512);
     }
     if (tile == 128 && load == kDirect)
-        backward_kernel<E, 128, kDirect, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (tile == 128 && load == kStaged)
-        backward_kernel<E, 128, kStaged, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (tile == 128)
-        backward_kernel<E, 128, kFused, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (load == kStaged)
-        backward_kernel<E, 64, kStaged, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (load == kFused)
-        backward_kernel<E, 64, kFused, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else if (small_stages(nb, k, kBK<E>) == 2)
-        backward_kernel<E, 64, kDirect, 2><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    else
-        backward_kernel<E, 64, kDirect, 4><<<nb, 256, 0, s>>>(dw, n_dw, dx);
-    return hipGetLastError();
+        return run(backward_kernel<E, 128, kDirect, 2>, 256);
+    if (tile == 128 && load == kStaged)
+        return run(backward_kernel<E, 128, kStaged, 2>, 256);
+    if (tile == 128)
+        return run(backward_kernel<E, 128, kFused, 2>, 256);
+    if (load == kStaged)
+        return run(backward_kernel<E, 64, kStaged, 2>, 256);
+    if (load == kFused)
+        return run(backward_kernel<E, 64, kFused, 2>, 256);
+    if (small_stages(nb, k, kBK<E>) == 2)
+        return run(backward_kernel<E, 64, kDirect, 2>, 256);
+    return run(backward_kernel<E, 64, kDirect, 4>, 256);
 }
 
 template <typename E>

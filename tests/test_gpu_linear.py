@@ -224,6 +224,25 @@ def test_many_rows_of_narrow_layers(dtype, G, M, K, N, act):
     check_layer(dtype, G, M, K, N, act, residual=False, pad=3)
 
 
+@pytest.mark.parametrize("rows", [(1 << 30) + 70])
+def test_most_rows(rows):
+    """More tiles than one launch has threads for.  Every number is exact: sums of
+    ones stay below 2^24 in each part, and the parts' sum is rounded once at most."""
+    import paper_2106_07551_amd as MA
+    base = torch.randn((1 << 20) + 7, device="cuda").bfloat16()
+    x = base.repeat(rows // base.numel() + 1)[:rows].view(rows, 1)
+    w = torch.full((1, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    print("[linear] most rows, forward", flush=True)
+    y = MA.linear(x, w)
+    assert torch.equal(y, x * 2)
+    dy = torch.ones_like(x)
+    print("[linear] most rows, backward", flush=True)
+    dx, dw, db = MA.linear_backward(dy, dy, w)
+    assert (dx == 2).all()
+    assert float(dw) == float(torch.tensor(float(rows)).bfloat16())
+    assert abs(float(db) - rows) <= 2.0 ** -23 * rows
+
+
 @pytest.mark.parametrize("pad, shift", [(1, 0), (8, 0), (8, 1), (3, 5), (0, 2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_strides_and_alignment(dtype, pad, shift):
