@@ -1221,7 +1221,7 @@ void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int s
 // The plan's part of a product's arguments
 static void apply(GemmArgs& a, const GemmPlan& p, float* part)
 {
-    a.mt = (a.M + p.tile - 1) / p.tile;
+    a.mt = (int)(((int64_t)a.M + p.tile - 1) / p.tile);   // (M may be 2^31 - 1)
     a.nt = (a.N + p.tile - 1) / p.tile;
     a.splits = p.splits;
     a.k_split = p.k_split;

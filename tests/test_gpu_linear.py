@@ -224,9 +224,10 @@ def test_many_rows_of_narrow_layers(dtype, G, M, K, N, act):
     check_layer(dtype, G, M, K, N, act, residual=False, pad=3)
 
 
-@pytest.mark.parametrize("rows", [(1 << 30) + 70])
+@pytest.mark.parametrize("rows", [(1 << 30) + 70, (1 << 31) - 1])
 def test_most_rows(rows):
-    """More tiles than one launch has threads for.  Every number is exact: sums of
+    """More tiles than one launch has threads for, and rows whose rounding up to
+    tiles passes 31 bits.  Every number is exact: sums of
     ones stay below 2^24 in each part, and the parts' sum is rounded once at most."""
     import paper_2106_07551_amd as MA
     base = torch.randn((1 << 20) + 7, device="cuda").bfloat16()
