@@ -546,7 +546,8 @@ typedef struct {
 
 /* A linear layer of `groups` policies side by side (each with weights of its
  * own), applied to `rows` inputs of each.
- * 1 <= groups <= 65535, 0 <= rows < 2^31, 1 <= in, out <= 2^24. */
+ * 1 <= groups <= 65535, 0 <= rows < 2^31, 1 <= in, out <= 2^24,
+ * groups * rows * out <= 2^46 (else MALIB_E_UNSUPPORTED). */
 typedef struct {
     int32_t dtype;       /* MALIB_DT_*: type of every matrix */
     int32_t act;         /* MALIB_ACT_* */

@@ -26,6 +26,7 @@ namespace {
 
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;
+constexpr int64_t kMaxValues = (int64_t)1 << 46;   // of y or dy: sizes in bytes fit 64 bits
 constexpr int64_t kFusedMost = (int64_t)1 << 20, kFusedWidth = 128;   // see BackwardPlan
 
 int type_size(int dtype) { return dtype == MALIB_DT_BF16 ? 2 : 4; }
@@ -46,6 +47,8 @@ malib_status check_linear(const malib_linear_desc* d)
         return set_error(MALIB_E_INVAL, "rows must be in [0, 2^31)");
     if (d->in < 1 || d->in > kMaxWidth || d->out < 1 || d->out > kMaxWidth)
         return set_error(MALIB_E_INVAL, "in and out must be in [1, 2^24]");
+    if (d->groups * d->rows > kMaxValues / d->out)
+        return set_error(MALIB_E_UNSUPPORTED, "groups * rows * out must be at most 2^46");
     return MALIB_OK;
 }
 

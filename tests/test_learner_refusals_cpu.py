@@ -63,6 +63,30 @@ def test_linear_desc_and_work_refused():
                                    None) == B.E_INVAL
 
 
+@pytest.mark.parametrize("act, groups, rows, n_in, n_out", [
+    (B.ACT_GELU, 65535, (1 << 31) - 1, 1 << 24, 1 << 24), (B.ACT_RELU, 1024, (1 << 31) - 1, 1, 1 << 24),
+    (B.ACT_GELU, 1, (1 << 31) - 1, 8, 1 << 16), (B.ACT_NONE, 65535, 1 << 31 >> 1, 8, 2)])
+def test_linear_sizes_beyond_64_bits(act, groups, rows, n_in, n_out):
+    """Bytes of matrices that no machine holds would not fit 64 bits: refused before
+    any size is computed from them."""
+    L = M.lib()
+    n = C.c_int64(-5)
+    for dtype in (B.DT_F32, B.DT_BF16):
+        d = B.LinearDesc(dtype, act, groups, rows, n_in, n_out)
+        for backward in (0, 1):
+            assert L.malib_linear_work(C.byref(d), backward, C.byref(n)) == B.E_UNSUPPORTED
+            assert b"2^46" in L.malib_last_error() and n.value == -5
+    m = B.Mat(P, 1 << 24, 0)
+    assert L.malib_linear(C.byref(d), C.byref(m), C.byref(m), None, None, None, C.byref(m), None,
+                          0, None) == B.E_UNSUPPORTED
+    assert L.malib_linear_backward(C.byref(d), C.byref(m), C.byref(m), C.byref(m), C.byref(m),
+                                   None, None, None, None, 0, None) == B.E_UNSUPPORTED
+    # the largest layer that is taken
+    d = B.LinearDesc(B.DT_BF16, B.ACT_GELU, 1 << 15, 1 << 30, 1 << 24, 2)
+    assert L.malib_linear_work(C.byref(d), 1, C.byref(n)) == B.MALIB_OK
+    assert n.value >= 2 << 45
+
+
 def test_linear_without_rows_does_nothing():
     L = M.lib()
     d = B.LinearDesc(B.DT_F32, B.ACT_NONE, 1, 0, 16, 24)
