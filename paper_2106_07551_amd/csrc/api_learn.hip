@@ -52,6 +52,24 @@ malib_status check_linear(const malib_linear_desc* d)
     return MALIB_OK;
 }
 
+// Whether any two rows of different groups share an element (rows of one group do not)
+bool groups_overlap(const malib_mat& m, int64_t rows, int64_t cols, int64_t groups)
+{
+    const __int128 row = rows > 1 ? m.row_stride : 0, group = m.group_stride;
+    if (groups == 1 || rows == 0 || group >= (rows - 1) * row + cols)   // one behind the other
+        return false;
+    if (rows == 1)
+        return true;
+    if (group >= cols && (groups - 1) * group + cols <= row)   // side by side within a stride
+        return false;
+    for (int64_t g = 1; g < groups; ++g) {   // the rows of a group around row 0 of one g further
+        const __int128 at = g * group, r = std::min<__int128>(at / row, rows - 1);
+        if (at - r * row < cols || (r + 1 < rows && (r + 1) * row - at < cols))
+            return true;
+    }
+    return false;
+}
+
 // A matrix argument: alignment to its element, a row stride that holds its
 // columns; an output's groups must lie apart.
 malib_status check_mat(const malib_mat* m, const char* what, int64_t rows, int64_t cols,
@@ -68,9 +86,7 @@ malib_status check_mat(const malib_mat* m, const char* what, int64_t rows, int64
         return set_error(MALIB_E_INVAL, "%s: negative group stride", what);
     if (m->row_stride > ((int64_t)1 << 40) || m->group_stride > ((int64_t)1 << 46))
         return set_error(MALIB_E_INVAL, "%s: stride too large", what);
-    if (output && groups > 1 && rows > 0 &&
-        m->group_stride < (rows - 1) * (rows > 1 ? m->row_stride : 0) + cols &&
-        (rows == 1 || m->row_stride < groups * cols || m->group_stride < cols))
+    if (output && groups_overlap(*m, rows, cols, groups))
         return set_error(MALIB_E_INVAL, "%s: the groups overlap", what);
     return MALIB_OK;
 }

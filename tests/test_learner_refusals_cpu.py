@@ -45,6 +45,28 @@ def test_linear_refuses(kw, word):
     assert word in L.malib_last_error()
 
 
+@pytest.mark.parametrize("groups, rows, row, group, apart", [
+    (2, 8, 8, 8, False),        # group 1's row r is group 0's row r + 1
+    (3, 8, 12, 6, False), (2, 8, 8, 5, False), (2, 3, 8, 16, False),
+    (2, 8, 8, 4, True), (3, 8, 12, 4, True), (2, 8, 9, 5, True), (2, 3, 8, 20, True),
+    (3, 8, 12, 8, True), (4, 8, 12, 8, False), (3, 8, 13, 9, True), (3, 2, 12, 8, True),
+    (2, 1, 8, 4, True), (2, 1, 8, 3, False), (2, 1 << 30, 1 << 40, 4, True),
+    (2, 1 << 30, 1 << 40, 1 << 40, False)])
+def test_linear_groups_of_outputs(groups, rows, row, group, apart):
+    """Groups of an output share no element, whatever their order in memory: dx of 4
+    columns, whose layer then lacks its workspace."""
+    L = M.lib()
+    if rows < 16:
+        places = {g * group + r * row + c for g in range(groups) for r in range(rows)
+                  for c in range(4)}
+        assert apart == (len(places) == groups * rows * 4)
+    d = B.LinearDesc(B.DT_F32, B.ACT_NONE, groups, rows, 4, 65536 if rows < 16 else 64)
+    m = C.byref(B.Mat(P, 65536, 0))
+    assert L.malib_linear_backward(C.byref(d), m, m, m, None, C.byref(B.Mat(P, row, group)), None,
+                                   None, None, 0, None) == B.E_INVAL
+    assert (b"workspace" if apart else b"dx: the groups overlap") in L.malib_last_error()
+
+
 def test_linear_desc_and_work_refused():
     L = M.lib()
     n = C.c_int64()
