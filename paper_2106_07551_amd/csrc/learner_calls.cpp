@@ -5,7 +5,8 @@
 // Every function takes device tensors as the binding's function of that name, and
 // the raw stream last.  It returns None, having launched nothing, for arguments that it does
 // not take (other types or layouts, what the library refuses, memory that cannot be
-// had): the binding's own checks then name the error.
+// had): the binding's own checks then name the error.  A launch that failed is raised: an
+// earlier one of the call may have run, over an input that is an output too.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -25,6 +26,9 @@ decltype(&malib_loss_work) p_loss_work;
 
 // An argument that these functions do not take.
 struct Other {};
+
+// A Python error that is set.
+struct Raised {};
 
 void need(bool ok)
 {
@@ -159,21 +163,42 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F fn)
     }
     try {
         return fn();
+    } catch (const Raised&) {
+        return nullptr;
     } catch (...) {   // (nothing may pass the C entry)
         PyErr_Clear();
     }
     return Py_NewRef(Py_None);
 }
 
-// The library's call without the interpreter's lock
-template <typename F>
-void call(F fn)
+// The error of a status as the binding raises it
+[[noreturn]] void raise_status(malib_status s)
 {
+    PyObject* m = PyImport_ImportModule("paper_2106_07551_amd.binding");
+    PyObject* r = m ? PyObject_CallMethod(m, "_check", "i", (int)s) : nullptr;
+    Py_XDECREF(m);
+    if (r) {
+        Py_DECREF(r);
+        PyErr_Format(PyExc_RuntimeError, "malib status %d", (int)s);
+    }
+    throw Raised();
+}
+
+// The library's call without the interpreter's lock.  `result`, made before it (behind it
+// nothing may become None), is returned.
+template <typename F>
+PyObject* call(PyObject* result, F fn)
+{
+    need(result != nullptr);
     malib_status s;
     Py_BEGIN_ALLOW_THREADS
     s = fn();
     Py_END_ALLOW_THREADS
-    need(s == MALIB_OK);
+    if (s == MALIB_OK)
+        return result;
+    Py_DECREF(result);
+    need(s != MALIB_E_INVAL && s != MALIB_E_UNSUPPORTED);   // checks, before the first launch
+    raise_status(s);
 }
 
 // load(path of the library)
@@ -264,11 +289,10 @@ PyObject* linear(PyObject*, PyObject* const* v, Py_ssize_t n)
             make(out, l, d.rows, d.out, *x);
         const malib_mat my = matrix(out.tensor(), l, d.rows, d.out);
         const Work work(ws, layer_work(l, 0), *x);
-        call([&] {
+        return call(out.object(), [&] {
             return p_linear(&d, &mx, &mw, (const float*)bias.ptr(), residual ? &mr : nullptr,
                             pre ? &mp : nullptr, &my, work.ptr, work.size, stream);
         });
-        return out.object();
     });
 }
 
@@ -312,12 +336,12 @@ PyObject* linear_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
                 db.make({d.out}, at::kFloat, *dy);
         }
         const Work work(ws, layer_work(l, 1), *dy);
-        call([&] {
+        PyObject* result = Py_BuildValue("(NNN)", dx.object(), dw.object(), db.object());
+        return call(result, [&] {
             return p_linear_backward(&d, &mdy, &mx, &mw, act ? &mp : nullptr,
                                      want[0] ? &mdx : nullptr, want[1] ? &mdw : nullptr,
                                      (float*)db.ptr(), work.ptr, work.size, stream);
         });
-        return Py_BuildValue("(NNN)", dx.object(), dw.object(), db.object());
     });
 }
 
@@ -400,14 +424,14 @@ PyObject* policy_loss(PyObject*, PyObject* const* v, Py_ssize_t n_args)
         if (grad)
             d.dlogits_stride = r.gradient(dx, *x);
         const Work work(ws, r.work(), *x);
-        call([&] {
+        PyObject* result = Py_BuildValue("(NNN)", total.object(), stats.object(), dx.object());
+        return call(result, [&] {
             return p_policy_loss(&d, x.ptr(), actions.ptr(), (const float*)old_logp.ptr(),
                                  (const float*)advantage.ptr(), (const float*)ref_logp.ptr(),
                                  ref.ptr(), (const uint8_t*)mask.ptr(),
                                  (const float*)weight.ptr(), (float*)total.ptr(),
                                  (float*)stats.ptr(), dx.ptr(), work.ptr, work.size, stream);
         });
-        return Py_BuildValue("(NNN)", total.object(), stats.object(), dx.object());
     });
 }
 
@@ -441,13 +465,13 @@ PyObject* distill_loss(PyObject*, PyObject* const* v, Py_ssize_t n_args)
         if (grad)
             d.dlogits_stride = r.gradient(dx, *x);
         const Work work(ws, r.work(), *x);
-        call([&] {
+        PyObject* result = Py_BuildValue("(NNN)", total.object(), loss.object(), dx.object());
+        return call(result, [&] {
             return p_distill_loss(&d, x.ptr(), (const int32_t*)idx.ptr(),
                                   (const float*)val.ptr(), (const uint8_t*)mask.ptr(),
                                   (const float*)weight.ptr(), (float*)total.ptr(),
                                   (float*)loss.ptr(), dx.ptr(), work.ptr, work.size, stream);
         });
-        return Py_BuildValue("(NNN)", total.object(), loss.object(), dx.object());
     });
 }
 

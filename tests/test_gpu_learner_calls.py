@@ -1,6 +1,10 @@
 """The native calls of the learner operators (csrc/learner_calls.cpp): what they take
 gives the same bits as the binding's own way to the library, and what they do not
 take is refused, or answered, by the binding as before."""
+import ctypes
+import os
+import subprocess
+
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -122,3 +126,64 @@ def test_refusals_name_the_argument():
                               work=torch.empty(16, device="cuda")), "work")):
         with pytest.raises(M.MalibError, match=word):
             fn()
+
+
+STAND_IN = r"""
+#include "malib.h"
+int calls, status;
+malib_status malib_linear_work(const malib_linear_desc* d, int32_t b, int64_t* n)
+{ *n = 0; return MALIB_OK; }
+malib_status malib_loss_work(int32_t t, int64_t r, int64_t a, int64_t* n) { *n = 0; return MALIB_OK; }
+malib_status malib_linear(const malib_linear_desc* d, const malib_mat* x, const malib_mat* w,
+    const float* bias, const malib_mat* residual, const malib_mat* pre, const malib_mat* y,
+    void* work, int64_t work_bytes, void* stream) { ++calls; return (malib_status)status; }
+malib_status malib_linear_backward(const malib_linear_desc* d, const malib_mat* dy,
+    const malib_mat* x, const malib_mat* w, const malib_mat* pre, const malib_mat* dx,
+    const malib_mat* dw, float* dbias, void* work, int64_t work_bytes, void* stream)
+{ ++calls; return (malib_status)status; }
+malib_status malib_policy_loss(const malib_policy_loss_desc* d, const void* logits,
+    const void* actions, const float* old_logp, const float* advantage, const float* ref_logp,
+    const void* ref_logits, const uint8_t* mask, const float* weight, float* total, float* stats,
+    void* dlogits, void* work, int64_t work_bytes, void* stream)
+{ ++calls; return (malib_status)status; }
+malib_status malib_distill_loss(const malib_distill_desc* d, const void* logits,
+    const int32_t* idx, const float* val, const uint8_t* mask, const float* weight, float* total,
+    float* loss, void* dlogits, void* work, int64_t work_bytes, void* stream)
+{ ++calls; return (malib_status)status; }
+"""
+
+
+def test_a_failed_launch_is_raised_once(tmp_path):
+    """A status from behind the checks (a stand-in library returns it and launches
+    nothing) is raised: the call is not made again, over a residual that is the output, say.
+    What the checks refuse is still the binding's to name."""
+    import paper_2106_07551_amd as M
+    B = M.binding
+    src, so = tmp_path / "stand_in.c", tmp_path / "stand_in.so"
+    src.write_text(STAND_IN)
+    include = os.path.join(os.path.dirname(os.path.dirname(B.LIB_PATH)), "include")
+    subprocess.run(["gcc", "-shared", "-fPIC", "-I", include, str(src), "-o", str(so)], check=True)
+    L = ctypes.CDLL(str(so))
+    calls, status = ctypes.c_int.in_dll(L, "calls"), ctypes.c_int.in_dll(L, "status")
+    x, w, y = rnd(9, 8), rnd(5, 8), rnd(9, 5)
+    act = torch.zeros(9, dtype=torch.int32, device="cuda")
+    old, before = rnd(9), y.clone()
+    whole = M.linear(x, w, residual=before)
+    fns = [lambda: M.linear(x, w, residual=y, out=y), lambda: M.linear_backward(y, x, w),
+           lambda: M.policy_loss(x, act, old, old),
+           lambda: M.distill_loss(x, act[:, None].contiguous(), old[:, None].contiguous())]
+    B._native().load(str(so))
+    try:
+        for code in (B.E_HIP, B.E_NOMEM):
+            status.value = code
+            for n, fn in enumerate(fns):
+                calls.value = 0
+                with pytest.raises(M.MalibError) as e:
+                    fn()
+                assert e.value.status == code and calls.value == 1, n
+                assert torch.equal(y, before)
+        status.value, calls.value = B.E_INVAL, 0
+        assert torch.equal(fns[0](), whole) and calls.value == 1
+    finally:
+        B._native().load(B.LIB_PATH)
+    assert M.linear(x, w).shape == (9, 5)
