@@ -684,6 +684,9 @@ def meta_sample_device(sigma, n_policies: int, n_envs: int, n_agents: int, seed:
 # These are called once per layer and step, often on small batches where the host's
 # share is the time: descriptions are packed into bytes (a tenth of a ctypes
 # structure's time), and checks name what they found only once one has failed.
+#
+# torch's autograd does not see them: tensors that require gradients are taken for
+# their values, outputs require none, and gradients are outputs of their own.
 
 _MAT = struct.Struct("@Pqq")                  # malib_mat
 _LINEAR = struct.Struct("@iiqqqq")            # malib_linear_desc
@@ -818,7 +821,8 @@ def linear(x, w, bias=None, *, act: int = ACT_NONE, residual=None, pre=None, out
     [out][in], or [groups][rows][in] and [groups][out][in] (x without the
     group dimension is shared by the groups); float32 or bfloat16, bias
     float32.  `pre` receives the values before the activation, which
-    linear_backward needs.  Returns [..][rows][out]."""
+    linear_backward needs.  Returns [..][rows][out], outside torch's autograd
+    graph: gradients are linear_backward's."""
     if stream is None and x.is_cuda:
         y = (_calls or _native()).linear(x, w, bias, act, residual, pre, out, work,
                                          _current_stream())
@@ -848,7 +852,7 @@ def linear_backward(dy, x, w, *, act: int = ACT_NONE, pre=None, want=(True, True
     """malib_linear_backward: (dx, dw, dbias) of linear for the gradient dy of
     its output; `pre` is what linear wrote there (needed with an activation).
     `want` leaves outputs out (None is returned for them).  The residual's
-    gradient is dy."""
+    gradient is dy.  Outside torch's autograd graph, as linear."""
     if stream is None and dy.is_cuda:
         out = (_calls or _native()).linear_backward(dy, x, w, act, pre, want, dx, dw, dbias, work,
                                                     _current_stream())
@@ -933,7 +937,8 @@ def policy_loss(logits, actions, old_logp, advantage, *, clip_low: float = 0.2,
     uint8, int32 or int64 [rows] (out of range: no action); mask: bool or uint8
     [rows][n_actions], legal entries.  Returns (total [1], stats [4][rows] =
     loss, log probability of the action, divergence and entropy of each row,
-    dlogits or None without `grad`)."""
+    dlogits or None without `grad`); total is outside torch's autograd graph,
+    dlogits is its gradient."""
     if stream is None and logits.is_cuda:
         out = (_calls or _native()).policy_loss(
             logits, actions, old_logp, advantage, clip_low, clip_high, kl_coef, entropy_coef,
@@ -981,7 +986,8 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
     """malib_distill_loss: distillation of teachers' top logits (teacher_idx
     int32 and teacher_logits float32 [rows][top], index -1 pads a list) into
     logits [rows][n_actions], and its gradient.  Returns (total [1], loss
-    [rows], dlogits or None without `grad`)."""
+    [rows], dlogits or None without `grad`); total is outside torch's autograd
+    graph, dlogits is its gradient."""
     if stream is None and logits.is_cuda:
         out = (_calls or _native()).distill_loss(
             logits, teacher_idx, teacher_logits, temperature, mask, weight, grad, total, loss,

@@ -401,7 +401,10 @@ GemmPlan gemm_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size, in
 // dW's and dx's plans of a backward pass, on the same tile where one launch is cheaper
 void backward_plans(int64_t groups, int64_t rows, int64_t in, int64_t out, int size, int loads,
                     GemmPlan& dw, GemmPlan& dx);
-// the forward's plan: up to kFewRows rows a kernel of its own (tile 0)
+// the forward's plan: up to kFewRows rows, as many as a 16x16 product takes, a kernel of
+// its own (tile 0).  Against tiles (us): 4096 -> 4096 bf16 with 1 row 8.5 and 12.3, with 16
+// rows 10.4 and 12.1; 8192 -> 8192 30.7 and 36.3, 39.2 and 36.7; fp32 62.8 and 77.9, 73.7
+// and 79.6; 256 -> 512 fp32 5.9 and 8.2 to 8.7.
 constexpr int kFewRows = 16;
 GemmPlan linear_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
 hipError_t launch_linear(int dtype, GemmArgs a, GemmPlan p, float* part, hipStream_t s);

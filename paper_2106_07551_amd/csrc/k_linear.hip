@@ -497,7 +497,7 @@ constexpr int wait_code(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4
 
 // Bound by the matrix cores where k is long (8192 x 4096 -> 4096 bf16 forward 241 us, 1.14
 // PFLOP/s, backward 488 us; 4096 x 2048 -> 2048 fp32 256 us, 134 TFLOP/s), by memory where
-// it is short (131072 x 256 -> 512 bf16 with z kept 84 us, 4.0 TB/s): LDS holds two stages
+// it is short (131072 x 256 -> 512 bf16 with z kept 84 to 94 us by machine, 4.0 to 3.6 TB/s): LDS holds two stages
 // of the largest tile, so one workgroup of it per CU, whose output phase nothing
 // overlaps.
 // One workgroup's tile of C, number `block` of `n_blocks` of this product.
@@ -955,7 +955,7 @@ int64_t split_sum_blocks(const GemmArgs& a, int shares)
     return (items * shares + kSumThreads - 1) / kSumThreads;
 }
 
-// Bound by memory: 131072 x 512 bf16 73 us (404 MB).  dz = dy act'(z) rounded to the layer's
+// Bound by memory: 131072 x 512 bf16 73 to 79 us by machine (404 MB).  dz = dy act'(z) rounded to the layer's
 // type (where there is an activation; the matrix cores take operands of that type), and
 // the column sums of the unrounded dz: a workgroup takes 32 chunks of columns
 // and a range of rows, eight rows at a time.

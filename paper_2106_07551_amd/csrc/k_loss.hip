@@ -1414,7 +1414,9 @@ __global__ void zero_total_kernel(float* total) { *total = 0.0f; }
 
 }  // namespace
 
-// Up to 31 actions a lane per row; up to 8 chunks of 16 bytes for each of 1024 threads
+// Up to 31 actions a lane per row (in fp32 with reference logits, against 4 or more
+// threads per row: 10^6 x 8 29 and 62 us, x 24 72 and 88, x 31 118 and 135; 100000 x 31
+// 19.6 and 19.0; 2000 x 8 12.2 and 11.6, x 31 14.1 and 12.1); up to 8 chunks of 16 bytes for each of 1024 threads
 // (65536 bf16 or 32768 fp32 entries) a row stays in the registers of as few threads as
 // hold it; above, and where a workgroup per row would leave half of the CUs idle, rows
 // are read twice, in parts where there are few.  Rows in registers against rows read
