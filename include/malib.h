@@ -679,6 +679,150 @@ malib_status malib_distill_loss(const malib_distill_desc* desc, const void* logi
 malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t n_actions,
                              int64_t* work_bytes);
 
+/*
+ * Log probabilities of given actions, with entropy and top alternatives: what
+ * malib_policy_loss takes as old or reference log probabilities and
+ * malib_distill_loss as a teacher's list.  With x a row's legal logits, T the
+ * temperature, m = max x, s = sum_j e^((x_j - m) / T) and p_j = e^((x_j - m) / T) / s:
+ *   l = log p[action] = (x[action] - m) / T - ln s,  H = -sum_j p_j log p_j
+ *  logits: [rows][n_actions] of `dtype`, rows logits_stride apart.
+ *  actions: device uint8, int32 or int64 [rows] (action_bytes 1, 4 or 8), or NULL.
+ *  mask: as in malib_policy_loss, or NULL.
+ *  stats: device fp32 [4][rows]: l, H, m and ln s of each row (m / T + ln s is the
+ *       logarithm of the sum of e^(x / T); in two parts its rounding does not grow
+ *       with the logits).
+ *  top_idx, top_logp: device int32 and fp32 [rows][top], 0 <= top <= 256 (unused with
+ *       0): the entries of largest logit, largest first, of equal ones (-0 equals 0)
+ *       the lowest index first, and their log probabilities.  Entries that are not
+ *       legal or are -inf are not listed; places behind the last entry hold -1 and 0.
+ * l is 0 where the action is not a legal entry in [0, n_actions) (255 and -1, say,
+ * stand for no action).  A row without a legal logit above -inf has l = H = ln s = 0 and
+ * m = -inf.  A legal NaN or +inf makes l, H, ln s and top_logp of its row NaN (l of an
+ * action that is not legal stays 0); NaNs are listed first.  Sums are formed in fp32 in an
+ * order fixed by the sizes.
+ * 0 <= rows < 2^31, 1 <= n_actions <= 2^24, rows * top < 2^40.  work: as
+ * malib_log_probs_work says, aligned to 16 bytes.
+ */
+typedef struct {
+    int32_t dtype;           /* MALIB_DT_* of logits, dlogits */
+    int32_t action_bytes;    /* 1, 4 or 8 */
+    int64_t rows, n_actions;
+    int64_t logits_stride, dlogits_stride, mask_stride;
+    int32_t top;
+    float temperature;       /* > 0, finite */
+} malib_log_probs_desc;
+
+malib_status malib_log_probs(const malib_log_probs_desc* desc, const void* logits,
+                             const void* actions, const uint8_t* mask, float* stats,
+                             int32_t* top_idx, float* top_logp, void* work, int64_t work_bytes,
+                             void* stream);
+
+/*
+ * The gradient of malib_log_probs: for dl and dH of each row,
+ *   dx_j = (dl ([j = action] - p_j) - dH p_j (log p_j + H)) / T.
+ *  stats: what malib_log_probs wrote for these logits, mask and temperature.
+ *  dlogp, dentropy: device fp32 [rows], each may be NULL (zero; actions may be NULL
+ *       without dlogp).  A row whose action is not a legal entry has no dl, whatever
+ *       dlogp holds there.
+ *  dlogits: [rows][n_actions] of `dtype`, rows dlogits_stride apart; may be logits itself
+ *       (same address and stride).
+ * Entries that are not legal or are -inf, and rows without any other, get zeros.  Lists
+ * have no gradient.  desc: `top` is not used.
+ */
+malib_status malib_log_probs_backward(const malib_log_probs_desc* desc, const void* logits,
+                                      const void* actions, const uint8_t* mask,
+                                      const float* stats, const float* dlogp,
+                                      const float* dentropy, void* dlogits, void* stream);
+
+/* Workspace bytes of malib_log_probs for these sizes.  Host only. */
+malib_status malib_log_probs_work(int32_t dtype, int64_t rows, int64_t n_actions, int32_t top,
+                                  int64_t* work_bytes);
+
+/*
+ * Dropout from the library's random stream: y = x k / q + residual, where k is 1 for the
+ * values that stay and 0 for the others, and q the probability of staying.  The mask is
+ * never stored: a value's k depends on its index in the matrix (row by row, strides
+ * aside), seed, step and layer alone, so the same call on dy (without the residual) is
+ * the backward pass.
+ * Value i has the 16 bits 16 (i mod 16) up of the Philox4x64-10 block (its words from the
+ * lowest) with counter (i / 16, step, 3 << 32 | layer, 0) and key (seed, 0), and stays where
+ * they are at least t = p 2^16, rounded to the nearest whole number: probabilities are
+ * multiples of 2^-16, and q = 1 - t 2^-16 exactly, so that y's mean is x.
+ *  p: 0 (every value stays) to 1 (none does: y is the residual, or zeros).
+ *  step: a number that the caller changes from call to call; device_step: device int64 [1]
+ *       added to it, or NULL (a captured graph then draws other masks in each replay once the
+ *       caller adds to it between replays, or within the graph).
+ *  layer: tells apart the layers of one step.
+ *  x, y: [rows][cols], strides in elements; y may be x itself; residual: [rows][cols] or
+ *       NULL, may be y itself (each: same address and stride).
+ * A value that does not stay counts as 0 even if it is infinite or NaN.  Formed in fp32,
+ * rounded once.  0 <= rows < 2^31, 1 <= cols <= 2^24.
+ */
+typedef struct {
+    int32_t dtype;           /* MALIB_DT_* of every matrix */
+    uint32_t layer;
+    int64_t rows, cols;
+    int64_t x_stride, residual_stride, y_stride;
+    uint64_t seed, step;
+    double p;
+} malib_dropout_desc;
+
+malib_status malib_dropout(const malib_dropout_desc* desc, const void* x, const void* residual,
+                           const int64_t* device_step, void* y, void* stream);
+
+/*
+ * Weights of frozen policies (teachers, references) in 4 bits: a weight is v s with v one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (codes 0 to 7, 8 added for a sign), and s the
+ * bf16 scale that `scale_group` weights (32, 64 or 128) along a row of W share.
+ *  codes: device uint8 [groups][ceil(out / 16)][ceil(in / 128)][64][16], contiguous, aligned to
+ *       16 bytes.  The code of weight (n, k) lies in byte (k % 128 / 32) 4 + k % 8 / 2 of
+ *       line (k % 32 / 8) 16 + n % 16 of block [n / 16][k / 128], in its low half for
+ *       even k: the order in which the matrix cores take it.
+ *  scales: device bf16 [groups][ceil(out / 16)][ceil(in / 128)][16][128 / scale_group],
+ *       contiguous, aligned to 8 bytes; weight (n, k) has scale [n / 16][k / 128][n % 16][k % 128 /
+ *       scale_group].
+ * Outputs beyond `out` and inputs beyond `in` are padding: malib_quantize_fp4 writes zeros
+ * there, and whatever they hold takes no part in a product.
+ * groups, rows, in, out: as in malib_linear_desc; groups * out * in <= 2^46.
+ */
+typedef struct {
+    int32_t dtype;           /* MALIB_DT_* of w, x, residual and y */
+    int32_t act;             /* MALIB_ACT_* (malib_linear_fp4) */
+    int64_t groups, rows, in, out;   /* rows: malib_linear_fp4 */
+    int32_t scale_group;     /* 32, 64 or 128 */
+    int32_t reserved;        /* 0 */
+} malib_fp4_desc;
+
+/*
+ * W [out][in] of each group in 4 bits: s = max |w| / 6 of the group of weights, rounded to
+ * bf16, and v the value nearest to w / s (halfway: the one of even code; beyond 6: 6).  The
+ * comparisons are exact.  A group of weights with an infinite one or a NaN gets a NaN as its
+ * scale, one whose scale rounds to 0 gets zeros.
+ */
+malib_status malib_quantize_fp4(const malib_fp4_desc* desc, const malib_mat* w, uint8_t* codes,
+                                uint16_t* scales, void* stream);
+
+/* The weights v s that codes and scales stand for, rounded to `dtype` (fp32: exact), into
+ * w [out][in] of each group. */
+malib_status malib_dequantize_fp4(const malib_fp4_desc* desc, const uint8_t* codes,
+                                  const uint16_t* scales, const malib_mat* w, void* stream);
+
+/*
+ * y = act(x W^T + b) + residual with W in 4 bits; the rest as in malib_linear.  Products
+ * are exact (x in bf16, or fp32 x in three bf16 parts), sums are formed in fp32, scales are
+ * applied to the fp32 sums of their weights.  The weights have no gradient, and x none from
+ * this call.  For a few rows of x at a time; the weights' codes are taken apart again for every
+ * 64 rows, so that for many rows malib_dequantize_fp4 and malib_linear take less time.
+ *  work: as malib_linear_fp4_work says, aligned to 16 bytes.
+ */
+malib_status malib_linear_fp4(const malib_fp4_desc* desc, const malib_mat* x,
+                              const uint8_t* codes, const uint16_t* scales, const float* bias,
+                              const malib_mat* residual, const malib_mat* y, void* work,
+                              int64_t work_bytes, void* stream);
+
+/* Workspace bytes of malib_linear_fp4 for this description.  Host only. */
+malib_status malib_linear_fp4_work(const malib_fp4_desc* desc, int64_t* work_bytes);
+
 /* Message for the last non-OK status returned on this thread. */
 const char* malib_last_error(void);
 

@@ -10,7 +10,8 @@ from .binding import (  # noqa: F401
     MalibError, ArgumentError, Population, Env, Trace, Traj, meta_sample,
     meta_sample_device, solve_fp, solve_alpharank, solve_lp,
     expansion_pairs, aggregate, linear, linear_backward,
-    policy_loss, distill_loss,
+    policy_loss, distill_loss, log_probs, log_probs_backward, dropout, dropout_backward,
+    quantize_fp4, dequantize_fp4, linear_fp4,
     debug_tanh_ref, debug_bf16, debug_philox,
     lib, LIB_PATH, POLICY_TABULAR, POLICY_MLP_F32, POLICY_MLP_BF16, ENV_MATRIX,
     ENV_ITER_MATRIX, ENV_PURSUIT, ENV_FEATURE, INIT_PER_ENV, INIT_SHARED, K_POLICY,

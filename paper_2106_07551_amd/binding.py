@@ -36,6 +36,8 @@ EXPORTS = [
     "malib_solve_alpharank", "malib_solve_lp",
     "malib_linear", "malib_linear_backward", "malib_linear_work",
     "malib_policy_loss", "malib_distill_loss", "malib_loss_work",
+    "malib_log_probs", "malib_log_probs_backward", "malib_log_probs_work", "malib_dropout",
+    "malib_quantize_fp4", "malib_dequantize_fp4", "malib_linear_fp4", "malib_linear_fp4_work",
 ]
 
 
@@ -101,6 +103,26 @@ class DistillDesc(C.Structure):
                 ("n_actions", C.c_int64), ("logits_stride", C.c_int64),
                 ("dlogits_stride", C.c_int64), ("mask_stride", C.c_int64),
                 ("temperature", C.c_float)]
+
+
+class LogProbsDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("action_bytes", C.c_int32), ("rows", C.c_int64),
+                ("n_actions", C.c_int64), ("logits_stride", C.c_int64),
+                ("dlogits_stride", C.c_int64), ("mask_stride", C.c_int64), ("top", C.c_int32),
+                ("temperature", C.c_float)]
+
+
+class DropoutDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("layer", C.c_uint32), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("x_stride", C.c_int64), ("residual_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("seed", C.c_uint64), ("step", C.c_uint64),
+                ("p", C.c_double)]
+
+
+class Fp4Desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("groups", C.c_int64),
+                ("rows", C.c_int64), ("inputs", C.c_int64), ("outputs", C.c_int64),
+                ("scale_group", C.c_int32), ("reserved", C.c_int32)]
 
 
 class EvalStats(C.Structure):
@@ -181,6 +203,22 @@ def lib():
         L.malib_distill_loss.restype = i32
         L.malib_loss_work.argtypes = [i32, i64, i64, C.POINTER(i64)]
         L.malib_loss_work.restype = i32
+        L.malib_log_probs.argtypes = [vp] * 8 + [i64, vp]
+        L.malib_log_probs.restype = i32
+        L.malib_log_probs_backward.argtypes = [vp] * 9
+        L.malib_log_probs_backward.restype = i32
+        L.malib_log_probs_work.argtypes = [i32, i64, i64, i32, C.POINTER(i64)]
+        L.malib_log_probs_work.restype = i32
+        L.malib_dropout.argtypes = [vp] * 6
+        L.malib_dropout.restype = i32
+        L.malib_quantize_fp4.argtypes = [vp] * 5
+        L.malib_quantize_fp4.restype = i32
+        L.malib_dequantize_fp4.argtypes = [vp] * 5
+        L.malib_dequantize_fp4.restype = i32
+        L.malib_linear_fp4.argtypes = [vp] * 8 + [i64, vp]
+        L.malib_linear_fp4.restype = i32
+        L.malib_linear_fp4_work.argtypes = [vp, C.POINTER(i64)]
+        L.malib_linear_fp4_work.restype = i32
         _lib = L
     return _lib
 
@@ -692,6 +730,9 @@ _MAT = struct.Struct("@Pqq")                  # malib_mat
 _LINEAR = struct.Struct("@iiqqqq")            # malib_linear_desc
 _POLICY_LOSS = struct.Struct("@iiqqqqqqffff")  # malib_policy_loss_desc
 _DISTILL = struct.Struct("@iiqqqqqf4x")        # malib_distill_desc
+_LOG_PROBS = struct.Struct("@iiqqqqqif")      # malib_log_probs_desc
+_DROPOUT = struct.Struct("@iIqqqqqQQd")        # malib_dropout_desc
+_FP4 = struct.Struct("@iiqqqqii")              # malib_fp4_desc
 
 
 _calls = None
@@ -1023,6 +1064,303 @@ def distill_loss(logits, teacher_idx, teacher_logits, *, temperature: float = 1.
         _ptr(weight), total.data_ptr(), loss.data_ptr(), _ptr(dlogits), wp, nbytes,
         _stream(stream)))
     return total, loss, dlogits
+
+
+def _here(t):
+    """The raw current stream of the device that is current where t lies on it (for the
+    native calls), else None."""
+    import torch
+    d = torch._C._cuda_getDevice()
+    return torch._C._cuda_getCurrentRawStream(d) if t.get_device() == d else None
+
+
+def _guard(t, stream, names, *tensors):
+    """Context of a launch over tensors that all have to lie on t's device, on a stream of
+    that device."""
+    import torch
+    _on_device(names, *tensors)
+    for u in tensors:
+        if u is not None and u.device != t.device:
+            what = next(n for n, v in zip(names.split(), tensors) if v is u)
+            raise ArgumentError(f"{what}: expected a tensor on {t.device}, got one on {u.device}")
+    if stream is not None and stream.device != t.device:
+        raise ArgumentError(f"stream: expected one of {t.device}, got one of {stream.device}")
+    return torch.cuda.device(t.device)
+
+
+def _scored(logits, actions, mask, dlogits):
+    """What both directions of log_probs check: (rows, n_actions, dtype code, bytes of an
+    action, strides of logits, dlogits and mask)."""
+    import torch
+    n, a, code, sl, sd, sm = _loss_args(logits, mask, None, dlogits)
+    if actions is None:
+        return n, a, code, 0, sl, sd, sm
+    if actions.dtype not in (torch.uint8, torch.int32, torch.int64):
+        raise ArgumentError(f"actions: expected dtype uint8, int32 or int64, got {actions.dtype}")
+    _check_buf(actions, None, n, False, "actions")
+    return n, a, code, actions.element_size(), sl, sd, sm
+
+
+def log_probs(logits, actions=None, *, temperature: float = 1.0, top: int = 0, mask=None,
+              stats=None, top_idx=None, top_logp=None, work=None, stream=None):
+    """malib_log_probs: log probabilities of `actions` (uint8, int32 or int64 [rows]; out of
+    range: no action) under logits [rows][n_actions] (float32 or bfloat16) over
+    `temperature`, the entropy of each row, and its `top` most likely entries.  Returns (stats
+    [4][rows] = log probability of the action, entropy, largest legal logit m and the
+    logarithm of the sum of e^((x - m) / temperature), top_idx int32 and top_logp
+    float32 [rows][top], -1 and 0 behind the last entry, or None without `top`): stats[0] is
+    policy_loss's old_logp or ref_logp, the lists are distill_loss's.  Outside torch's
+    autograd graph: gradients are log_probs_backward's."""
+    if stream is None and logits.is_cuda and (raw := _here(logits)) is not None:
+        out = (_calls or _native()).log_probs(logits, actions, temperature, top, mask, stats,
+                                              top_idx, top_logp, work, raw)
+        if out is not None:
+            return out
+    import torch
+    n, a, code, size, sl, _, sm = _scored(logits, actions, mask, None)
+    if not 0 <= top <= 256:
+        raise ArgumentError(f"top: expected 0 to 256, got {top}")
+    f32 = torch.float32
+    _check_buf(stats, f32, 4 * n, False, "stats")
+    _check_buf(top_idx, torch.int32, n * top, False, "top_idx")
+    _check_buf(top_logp, f32, n * top, False, "top_logp")
+    with _guard(logits, stream, "logits actions mask stats top_idx top_logp work", logits,
+                actions, mask, stats, top_idx, top_logp, work):
+        dev = logits.device
+        if stats is None:
+            stats = _empty((4, n), f32, dev, stream)
+        if top == 0:
+            top_idx = top_logp = None
+        if top and top_idx is None:
+            top_idx = _empty((n, top), torch.int32, dev, stream)
+        if top and top_logp is None:
+            top_logp = _empty((n, top), f32, dev, stream)
+        need = C.c_int64()
+        _check(lib().malib_log_probs_work(code, n, a, top, C.byref(need)))
+        wp, nbytes, work = _workspace(need.value, work, dev, stream)
+        d = _LOG_PROBS.pack(code, size, n, a, sl, 0, sm, top, temperature)
+        _check(lib().malib_log_probs(d, logits.data_ptr(), _ptr(actions), _ptr(mask),
+                                     stats.data_ptr(), _ptr(top_idx), _ptr(top_logp), wp, nbytes,
+                                     _stream(stream)))
+    return stats, top_idx, top_logp
+
+
+def log_probs_backward(logits, actions, stats, dlogp, dentropy=None, *, temperature: float = 1.0,
+                       mask=None, dlogits=None, stream=None):
+    """malib_log_probs_backward: the gradient of log_probs' logits for the gradients dlogp and
+    dentropy (float32 [rows], either may be None) of its first two rows of stats, which
+    are taken as log_probs returned them.  Returns dlogits (which may be logits
+    itself).  Outside torch's autograd graph."""
+    if stream is None and logits.is_cuda and (raw := _here(logits)) is not None:
+        out = (_calls or _native()).log_probs_backward(logits, actions, stats, dlogp, dentropy,
+                                                       temperature, mask, dlogits, raw)
+        if out is not None:
+            return out
+    import torch
+    n, a, code, size, sl, sd, sm = _scored(logits, actions, mask, dlogits)
+    f32 = torch.float32
+    _check_buf(stats, f32, 4 * n, False, "stats")
+    _check_buf(dlogp, f32, n, False, "dlogp")
+    _check_buf(dentropy, f32, n, False, "dentropy")
+    with _guard(logits, stream, "logits actions mask stats dlogp dentropy dlogits", logits,
+                actions, mask, stats, dlogp, dentropy, dlogits):
+        if dlogits is None:
+            dlogits, sd = _empty((n, a), logits.dtype, logits.device, stream), a
+        d = _LOG_PROBS.pack(code, size, n, a, sl, sd, sm, 0, temperature)
+        _check(lib().malib_log_probs_backward(
+            d, logits.data_ptr(), _ptr(actions), _ptr(mask), stats.data_ptr(), _ptr(dlogp),
+            _ptr(dentropy), dlogits.data_ptr(), _stream(stream)))
+    return dlogits
+
+
+def _flat_rows(t, like, what):
+    """(rows, cols, row stride) of a tensor whose values are taken in its own order: any
+    contiguous one, or [rows][cols] with contiguous rows."""
+    if t is None:
+        return 0, 0, 0
+    if t.shape != like.shape:
+        raise ArgumentError(f"{what}: expected shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if t.dtype is not like.dtype:
+        raise ArgumentError(f"{what}: expected dtype {like.dtype}, got {t.dtype}")
+    cols = t.shape[-1] if t.dim() else 1
+    rows = t.numel() // cols if cols else 0
+    if t.is_contiguous():
+        return rows, cols, cols
+    if t.dim() != 2 or (t.stride(1) != 1 and cols > 1):
+        raise ArgumentError(f"{what}: expected a contiguous tensor, or [rows][cols] with "
+                            f"contiguous rows, got strides {t.stride()}")
+    return rows, cols, t.stride(0) if rows > 1 else cols
+
+
+def _u64(v, what, top=64):
+    if not 0 <= v < 1 << top:
+        raise ArgumentError(f"{what}: expected a number in [0, 2^{top}), got {v}")
+    return v
+
+
+def dropout(x, p: float, seed: int, step: int = 0, *, layer: int = 0, residual=None, out=None,
+            device_step=None, stream=None):
+    """malib_dropout: x k / q + residual, where a value stays (k = 1) with probability q = 1 - p
+    (in steps of 2^-16) by the library's random stream, from its index, `seed`, `step`
+    (plus the int64 in `device_step`, a device tensor of one number) and `layer`
+    alone.  float32 or bfloat16; contiguous tensors of any shape, or [rows][cols] with
+    contiguous rows; `out` may be x or residual.  Outside torch's autograd graph: the
+    gradient is dropout_backward's, the residual's is dy."""
+    if stream is None and x.is_cuda and (raw := _here(x)) is not None:
+        y = (_calls or _native()).dropout(x, p, seed, step, layer, residual, out, device_step,
+                                          raw)
+        if y is not None:
+            return y
+    import torch
+    code = _dtype_code(x, "x")
+    rows, cols, sx = _flat_rows(x, x, "x")
+    _, _, sr = _flat_rows(residual, x, "residual")
+    _, _, sy = _flat_rows(out, x, "out")
+    _check_buf(device_step, torch.int64, 1, False, "device_step")
+    for v, what, top in ((seed, "seed", 64), (step, "step", 64), (layer, "layer", 32)):
+        _u64(v, what, top)
+    if not 0.0 <= p <= 1.0:
+        raise ArgumentError(f"p: expected a probability, got {p}")
+    with _guard(x, stream, "x residual out device_step", x, residual, out, device_step):
+        if out is None:
+            out, sy = _empty((tuple(x.shape),), x.dtype, x.device, stream), cols
+        if x.numel():
+            d = _DROPOUT.pack(code, layer, rows, cols, sx, sr, sy, seed, step, p)
+            _check(lib().malib_dropout(d, x.data_ptr(), _ptr(residual), _ptr(device_step),
+                                       out.data_ptr(), _stream(stream)))
+    return out
+
+
+def dropout_backward(dy, p: float, seed: int, step: int = 0, *, layer: int = 0, dx=None,
+                     device_step=None, stream=None):
+    """The gradient of dropout's x for the gradient dy of its output: dy k / q, with the mask
+    formed again from p, seed, step and layer.  dx may be dy itself."""
+    return dropout(dy, p, seed, step, layer=layer, out=dx, device_step=device_step,
+                   stream=stream)
+
+
+def _fp4_shape(n_out, n_in, group):
+    if group not in (32, 64, 128):
+        raise ArgumentError(f"group: expected 32, 64 or 128, got {group}")
+    tiles, blocks = (n_out + 15) // 16, (n_in + 127) // 128
+    return (tiles, blocks, 64, 16), (tiles, blocks, 16, 128 // group)
+
+
+def _fp4_held(codes, scales, G, n_out, n_in):
+    """Checks codes and scales of a layer; returns their scale group."""
+    import torch
+    per = scales.shape[-1] if scales.dim() else 0
+    if per not in (1, 2, 4):
+        raise ArgumentError(f"scales: expected 1, 2 or 4 in the last dimension, got shape "
+                            f"{tuple(scales.shape)}")
+    lead = () if G is None else (G,)
+    for t, shape, dt, align, what in zip(
+            (codes, scales), _fp4_shape(n_out, n_in, 128 // per),
+            (torch.uint8, torch.bfloat16), (16, 8), ("codes", "scales")):
+        if t.shape != lead + shape:
+            raise ArgumentError(f"{what}: expected shape {lead + shape}, got {tuple(t.shape)}")
+        _check_buf(t, dt, None, False, what)
+        if t.data_ptr() % align:
+            raise ArgumentError(f"{what}: expected to start on {align} bytes")
+    return 128 // per
+
+
+def quantize_fp4(w, group: int = 32, *, codes=None, scales=None, stream=None):
+    """malib_quantize_fp4: weights [out][in] or [groups][out][in] (float32 or bfloat16) in 4
+    bits, `group` (32, 64 or 128) weights of a row sharing a scale.  Returns (codes uint8
+    [..][ceil(out / 16)][ceil(in / 128)][64][16], scales bfloat16
+    [..][ceil(out / 16)][ceil(in / 128)][16][128 / group]), in the order that linear_fp4
+    takes."""
+    if stream is None and w.is_cuda and (raw := _here(w)) is not None:
+        out = (_calls or _native()).quantize_fp4(w, group, codes, scales, raw)
+        if out is not None:
+            return out
+    import torch
+    code = _dtype_code(w, "w")
+    if w.dim() not in (2, 3):
+        raise ArgumentError(f"w: expected [out][in] or [groups][out][in], got shape "
+                            f"{tuple(w.shape)}")
+    G, (n_out, n_in) = w.shape[0] if w.dim() == 3 else None, w.shape[-2:]
+    mw = _mat(w, w.dtype, G, n_out, n_in, "w")
+    sc, ss = _fp4_shape(n_out, n_in, group)
+    lead = () if G is None else (G,)
+    with _guard(w, stream, "w codes scales", w, codes, scales):
+        if codes is None:
+            codes = _empty((lead + sc,), torch.uint8, w.device, stream)
+        if scales is None:
+            scales = _empty((lead + ss,), torch.bfloat16, w.device, stream)
+        if _fp4_held(codes, scales, G, n_out, n_in) != group:
+            raise ArgumentError(f"scales: expected those of groups of {group}")
+        d = _FP4.pack(code, ACT_NONE, 1 if G is None else G, 0, n_in, n_out, group, 0)
+        _check(lib().malib_quantize_fp4(d, mw, codes.data_ptr(), scales.data_ptr(),
+                                        _stream(stream)))
+    return codes, scales
+
+
+def dequantize_fp4(codes, scales, n_out: int, n_in: int, *, dtype=None, out=None, stream=None):
+    """malib_dequantize_fp4: the weights [out][in] (or [groups][out][in]) that quantize_fp4's
+    codes and scales stand for, in `dtype` (bfloat16 unless `out` has another; float32 is
+    exact)."""
+    if stream is None and codes.is_cuda and (raw := _here(codes)) is not None:
+        w = (_calls or _native()).dequantize_fp4(codes, scales, n_out, n_in, dtype, out, raw)
+        if w is not None:
+            return w
+    import torch
+    G = codes.shape[0] if codes.dim() == 5 else None
+    group = _fp4_held(codes, scales, G, n_out, n_in)
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ArgumentError(f"dtype: expected float32 or bfloat16, got {dtype}")
+    with _guard(codes, stream, "codes scales out", codes, scales, out):
+        if out is None:
+            shape = (n_out, n_in) if G is None else (G, n_out, n_in)
+            out = _empty((shape,), dtype, codes.device, stream)
+        mw = _mat(out, dtype, G, n_out, n_in, "out", True)
+        d = _FP4.pack(DT_BF16 if dtype is torch.bfloat16 else DT_F32, ACT_NONE,
+                      1 if G is None else G, 0, n_in, n_out, group, 0)
+        _check(lib().malib_dequantize_fp4(d, codes.data_ptr(), scales.data_ptr(), mw,
+                                          _stream(stream)))
+    return out
+
+
+def linear_fp4(x, codes, scales, n_out: int, bias=None, *, act: int = ACT_NONE, residual=None,
+               out=None, work=None, stream=None):
+    """malib_linear_fp4: act(x w^T + bias) + residual with the weights of quantize_fp4, for
+    x [rows][in], or with weights of several policies [groups][rows][in] (x without the
+    group dimension is shared by the groups); float32 or bfloat16, bias float32.  For a few
+    rows of a frozen policy at a time; for hundreds of rows linear on dequantize_fp4's weights
+    takes less time.  Returns [..][rows][out]; nothing here has a gradient."""
+    if stream is None and x.is_cuda and (raw := _here(x)) is not None:
+        y = (_calls or _native()).linear_fp4(x, codes, scales, n_out, bias, act, residual, out,
+                                             work, raw)
+        if y is not None:
+            return y
+    code = _dtype_code(x, "x")
+    G = codes.shape[0] if codes.dim() == 5 else None
+    if x.dim() != 2 and (x.dim() != 3 or G is None):
+        raise ArgumentError(f"x: expected [rows][in] or, with weights per group, "
+                            f"[groups][rows][in], got shape {tuple(x.shape)}")
+    if act not in (ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU):
+        raise ArgumentError(f"act: unknown activation {act!r}")
+    (rows, n_in), dt = x.shape[-2:], x.dtype
+    group = _fp4_held(codes, scales, G, n_out, n_in)
+    mx = _mat(x, dt, G, rows, n_in, "x")
+    mr = _mat(residual, dt, G, rows, n_out, "residual")
+    _check_buf(bias, _f32(), n_out * (1 if G is None else G), False, "bias")
+    with _guard(x, stream, "x codes scales bias residual out work", x, codes, scales, bias,
+                residual, out, work):
+        if out is None:
+            out = _empty(((rows, n_out) if G is None else (G, rows, n_out),), dt, x.device,
+                         stream)
+        my = _mat(out, dt, G, rows, n_out, "out", True)
+        d = _FP4.pack(code, act, 1 if G is None else G, rows, n_in, n_out, group, 0)
+        need = C.c_int64()
+        _check(lib().malib_linear_fp4_work(d, C.byref(need)))
+        wp, nbytes, work = _workspace(need.value, work, x.device, stream)
+        _check(lib().malib_linear_fp4(d, mx, codes.data_ptr(), scales.data_ptr(), _ptr(bias), mr,
+                                      my, wp, nbytes, _stream(stream)))
+    return out
 
 
 def debug_tanh_ref(x, y=None, stream=None):

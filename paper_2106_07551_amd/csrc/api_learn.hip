@@ -467,4 +467,272 @@ malib_status malib_distill_loss(const malib_distill_desc* d, const void* logits,
     return MALIB_OK;
 }
 
+static malib_status check_log_probs(const malib_log_probs_desc* d)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    TRY(check_loss(d->dtype, d->rows, d->n_actions));
+    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature))
+        return set_error(MALIB_E_INVAL, "temperature must be positive and finite");
+    return MALIB_OK;
+}
+
+// Actions of either direction, and what both take of logits and mask.
+static malib_status check_scored(const malib_log_probs_desc* d, const void* logits,
+                                 const void* actions, const uint8_t* mask)
+{
+    if (!logits)
+        return set_error(MALIB_E_INVAL, "logits is NULL");
+    TRY(check_rows(logits, d->logits_stride, "logits", d->rows, d->n_actions,
+                   type_size(d->dtype), false));
+    if (mask)
+        TRY(check_rows(mask, d->mask_stride, "mask", d->rows, d->n_actions, 1, false));
+    if (actions) {
+        if (d->action_bytes != 1 && d->action_bytes != 4 && d->action_bytes != 8)
+            return set_error(MALIB_E_INVAL, "action_bytes must be 1, 4 or 8");
+        if ((uintptr_t)actions % d->action_bytes)
+            return set_error(MALIB_E_INVAL, "actions is not aligned to its elements");
+    }
+    return MALIB_OK;
+}
+
+static LogpArgs logp_args(const malib_log_probs_desc* d, const void* logits, const void* actions,
+                          const uint8_t* mask, const float* stats)
+{
+    LogpArgs a{};
+    a.logits = logits;
+    a.actions = actions;
+    a.mask = mask;
+    a.stats = const_cast<float*>(stats);
+    a.rows = d->rows;
+    a.logits_ld = d->logits_stride;
+    a.mask_ld = d->mask_stride;
+    a.dlogits_ld = d->dlogits_stride;
+    a.A = (int)d->n_actions;
+    a.action_bytes = d->action_bytes;
+    a.temperature = d->temperature;
+    return a;
+}
+
+static malib_status check_aligned(const void* p, const char* what, int bytes)
+{
+    if ((uintptr_t)p % bytes)
+        return set_error(MALIB_E_INVAL, "%s is not aligned to %d bytes", what, bytes);
+    return MALIB_OK;
+}
+
+static malib_status check_top(int64_t rows, int32_t top)
+{
+    if (top < 0 || top > 256)
+        return set_error(MALIB_E_INVAL, "top must be in [0, 256]");
+    if (rows * top >= (int64_t)1 << 40)
+        return set_error(MALIB_E_UNSUPPORTED, "rows * top must be below 2^40");
+    return MALIB_OK;
+}
+
+malib_status malib_log_probs_work(int32_t dtype, int64_t rows, int64_t A, int32_t top,
+                                  int64_t* work_bytes)
+{
+    TRY(check_loss(dtype, rows, A));
+    TRY(check_top(rows, top));
+    if (!work_bytes)
+        return set_error(MALIB_E_INVAL, "work_bytes is NULL");
+    *work_bytes = logp_plan(rows, A, top, type_size(dtype)).work_bytes;
+    return MALIB_OK;
+}
+
+malib_status malib_log_probs(const malib_log_probs_desc* d, const void* logits,
+                             const void* actions, const uint8_t* mask, float* stats,
+                             int32_t* top_idx, float* top_logp, void* work, int64_t work_bytes,
+                             void* stream)
+{
+    TRY(check_log_probs(d));
+    TRY(check_top(d->rows, d->top));
+    if (d->rows == 0)
+        return MALIB_OK;
+    TRY(check_scored(d, logits, actions, mask));
+    if (!stats)
+        return set_error(MALIB_E_INVAL, "stats is NULL");
+    if (d->top > 0 && (!top_idx || !top_logp))
+        return set_error(MALIB_E_INVAL, "top_idx and top_logp must not be NULL");
+    TRY(check_aligned(stats, "stats", 4));
+    TRY(check_aligned(top_idx, "top_idx", 4));
+    TRY(check_aligned(top_logp, "top_logp", 4));
+    const LogpPlan p = logp_plan(d->rows, d->n_actions, d->top, type_size(d->dtype));
+    TRY(check_work(work, work_bytes, p.work_bytes));
+    LogpArgs a = logp_args(d, logits, actions, mask, stats);
+    a.top = d->top;
+    a.top_idx = top_idx;
+    a.top_logp = top_logp;
+    HIP_TRY(launch_logp(a, d->dtype, p, work, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_log_probs_backward(const malib_log_probs_desc* d, const void* logits,
+                                      const void* actions, const uint8_t* mask,
+                                      const float* stats, const float* dlogp,
+                                      const float* dentropy, void* dlogits, void* stream)
+{
+    TRY(check_log_probs(d));
+    if (d->rows == 0)
+        return MALIB_OK;
+    TRY(check_scored(d, logits, actions, mask));
+    if (!stats || !dlogits)
+        return set_error(MALIB_E_INVAL, "stats and dlogits must not be NULL");
+    if (dlogp && !actions)
+        return set_error(MALIB_E_INVAL, "dlogp needs actions");
+    TRY(check_aligned(stats, "stats", 4));
+    TRY(check_aligned(dlogp, "dlogp", 4));
+    TRY(check_aligned(dentropy, "dentropy", 4));
+    TRY(check_rows(dlogits, d->dlogits_stride, "dlogits", d->rows, d->n_actions,
+                   type_size(d->dtype), true));
+    LogpArgs a = logp_args(d, logits, actions, mask, stats);
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    a.dlogits = dlogits;
+    HIP_TRY(launch_logp_grad(a, d->dtype, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_dropout(const malib_dropout_desc* d, const void* x, const void* residual,
+                           const int64_t* device_step, void* y, void* stream)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    if (d->dtype != MALIB_DT_F32 && d->dtype != MALIB_DT_BF16)
+        return set_error(MALIB_E_INVAL, "unknown dtype %d", d->dtype);
+    if (d->rows < 0 || d->rows > kMaxRows)
+        return set_error(MALIB_E_INVAL, "rows must be in [0, 2^31)");
+    if (d->cols < 1 || d->cols > kMaxWidth)
+        return set_error(MALIB_E_INVAL, "cols must be in [1, 2^24]");
+    if (!(d->p >= 0.0 && d->p <= 1.0))
+        return set_error(MALIB_E_INVAL, "p must be in [0, 1]");
+    if (d->rows == 0)
+        return MALIB_OK;
+    const int size = type_size(d->dtype);
+    if (!x || !y)
+        return set_error(MALIB_E_INVAL, "x and y must not be NULL");
+    TRY(check_rows(x, d->x_stride, "x", d->rows, d->cols, size, false));
+    TRY(check_rows(y, d->y_stride, "y", d->rows, d->cols, size, true));
+    if (residual)
+        TRY(check_rows(residual, d->residual_stride, "residual", d->rows, d->cols, size, false));
+    TRY(check_aligned(device_step, "device_step", 8));
+    DropoutArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.y = y;
+    a.device_step = device_step;
+    a.rows = d->rows;
+    a.cols = d->cols;
+    a.x_ld = d->x_stride;
+    a.residual_ld = d->residual_stride;
+    a.y_ld = d->y_stride;
+    a.seed = d->seed;
+    a.step = d->step;
+    a.layer = d->layer;
+    a.drop = (uint32_t)std::llrint(d->p * 65536.0);
+    a.scale = a.drop < 65536u ? (float)(65536.0 / (65536.0 - a.drop)) : 0.0f;
+    HIP_TRY(launch_dropout(a, d->dtype, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+static malib_status check_fp4(const malib_fp4_desc* d)
+{
+    if (!d)
+        return set_error(MALIB_E_INVAL, "desc is NULL");
+    const malib_linear_desc l{d->dtype, d->act, d->groups, d->rows, d->in, d->out};
+    TRY(check_linear(&l));
+    if (d->groups * d->out > kMaxValues / d->in)
+        return set_error(MALIB_E_UNSUPPORTED, "groups * out * in must be at most 2^46");
+    if (d->scale_group != 32 && d->scale_group != 64 && d->scale_group != 128)
+        return set_error(MALIB_E_INVAL, "scale_group must be 32, 64 or 128");
+    if (d->reserved != 0)
+        return set_error(MALIB_E_INVAL, "reserved must be 0");
+    return MALIB_OK;
+}
+
+static malib_status check_codes(const void* codes, const void* scales)
+{
+    if (!codes || !scales)
+        return set_error(MALIB_E_INVAL, "codes and scales must not be NULL");
+    TRY(check_aligned(codes, "codes", 16));
+    return check_aligned(scales, "scales", 8);
+}
+
+static Fp4Args fp4_args(const malib_fp4_desc* d, const uint8_t* codes, const uint16_t* scales)
+{
+    Fp4Args a{};
+    a.codes = const_cast<uint8_t*>(codes);
+    a.scales = const_cast<uint16_t*>(scales);
+    a.groups = (int)d->groups;
+    a.M = (int)d->rows;
+    a.N = (int)d->out;
+    a.K = (int)d->in;
+    a.scale_group = d->scale_group;
+    a.act = d->act;
+    a.tiles = (a.N + 15) / 16;
+    a.blocks_k = (a.K + 127) / 128;
+    return a;
+}
+
+malib_status malib_quantize_fp4(const malib_fp4_desc* d, const malib_mat* w, uint8_t* codes,
+                                uint16_t* scales, void* stream)
+{
+    TRY(check_fp4(d));
+    TRY(check_mat(w, "w", d->out, d->in, d->groups, type_size(d->dtype), false));
+    TRY(check_codes(codes, scales));
+    Fp4Args a = fp4_args(d, codes, scales);
+    a.w = arg(w);
+    HIP_TRY(launch_quantize_fp4(a, d->dtype, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_dequantize_fp4(const malib_fp4_desc* d, const uint8_t* codes,
+                                  const uint16_t* scales, const malib_mat* w, void* stream)
+{
+    TRY(check_fp4(d));
+    TRY(check_codes(codes, scales));
+    TRY(check_mat(w, "w", d->out, d->in, d->groups, type_size(d->dtype), true));
+    Fp4Args a = fp4_args(d, codes, scales);
+    a.w = arg(w);
+    HIP_TRY(launch_dequantize_fp4(a, d->dtype, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
+malib_status malib_linear_fp4_work(const malib_fp4_desc* d, int64_t* work_bytes)
+{
+    TRY(check_fp4(d));
+    if (!work_bytes)
+        return set_error(MALIB_E_INVAL, "work_bytes is NULL");
+    *work_bytes = fp4_plan(d->groups, d->rows, d->out, d->in, type_size(d->dtype)).part_bytes;
+    return MALIB_OK;
+}
+
+malib_status malib_linear_fp4(const malib_fp4_desc* d, const malib_mat* x,
+                              const uint8_t* codes, const uint16_t* scales, const float* bias,
+                              const malib_mat* residual, const malib_mat* y, void* work,
+                              int64_t work_bytes, void* stream)
+{
+    TRY(check_fp4(d));
+    if (d->rows == 0)
+        return MALIB_OK;
+    const int size = type_size(d->dtype);
+    TRY(check_mat(x, "x", d->rows, d->in, d->groups, size, false));
+    TRY(check_codes(codes, scales));
+    TRY(check_mat(y, "y", d->rows, d->out, d->groups, size, true));
+    if (residual)
+        TRY(check_mat(residual, "residual", d->rows, d->out, d->groups, size, false));
+    TRY(check_aligned(bias, "bias", 4));
+    const Fp4Plan p = fp4_plan(d->groups, d->rows, d->out, d->in, size);
+    TRY(check_work(work, work_bytes, p.part_bytes));
+    Fp4Args a = fp4_args(d, codes, scales);
+    a.x = arg(x);
+    a.res = arg(residual);
+    a.y = arg(y);
+    a.bias = bias;
+    a.part = (float*)work;
+    HIP_TRY(launch_linear_fp4(a, d->dtype, p, (hipStream_t)stream));
+    return MALIB_OK;
+}
+
 }  // extern "C"

@@ -11,7 +11,8 @@
 namespace malib {
 
 // Random-stream purposes (third counter word, high half).
-enum : uint32_t { kPurposeAction = 0, kPurposeReset = 1, kPurposeMeta = 2 };
+enum : uint32_t { kPurposeAction = 0, kPurposeReset = 1, kPurposeMeta = 2,
+                  kPurposeDropout = 3 };
 
 struct u64x4 {
     uint64_t x, y, z, w;

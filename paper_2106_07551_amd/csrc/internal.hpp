@@ -460,6 +460,68 @@ LossPlan loss_plan(int64_t rows, int64_t A, int top, int size);   // top: 0 for 
 hipError_t launch_loss(LossArgs a, int dtype, bool distill, const LossPlan& p, void* work,
                        hipStream_t s);
 
+// Log probabilities of given actions with top alternatives (k_logp.hip).
+struct LogpArgs {
+    const void* logits;        // [rows][A], rows logits_ld apart
+    const void* actions;       // action_bytes each, or null
+    const uint8_t* mask;       // legal entries, or null
+    float* stats;              // [4][rows] (an input of the gradient)
+    int32_t* top_idx;          // [rows][top]
+    float* top_logp;
+    const float *dlogp, *dentropy;   // gradient: [rows] or null
+    void* dlogits;
+    int64_t rows, logits_ld, mask_ld, dlogits_ld;
+    int A, top, action_bytes;
+    float temperature;
+    // set by the launchers
+    int splits, part_len, cap;   // cap: keys of a row in LDS
+    bool bf16;
+    void* part_stats;
+    uint64_t* part_keys;
+};
+enum { kLogpLane, kLogpRow, kLogpSplit };
+struct LogpPlan {
+    int variant, group, splits, part_len, cap;   // group: threads per row
+    int64_t blocks, stats_bytes, work_bytes;
+};
+LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size);
+hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hipStream_t s);
+hipError_t launch_logp_grad(const LogpArgs& a, int dtype, hipStream_t s);
+
+// Dropout from the random stream (k_dropout.hip).
+struct DropoutArgs {
+    const void *x, *residual;    // [rows][cols]; residual may be null
+    void* y;
+    const int64_t* device_step;  // or null
+    int64_t rows, cols, x_ld, residual_ld, y_ld;
+    uint64_t seed, step;
+    uint32_t layer, drop;        // a value is dropped where its 16 bits are below `drop`
+    float scale;
+};
+hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
+
+// Layers in 4 bits (k_fp4.hip).
+struct Fp4Args {
+    MatArg w, x, res, y;         // w: of quantising and its inverse
+    uint8_t* codes;
+    uint16_t* scales;
+    const float* bias;
+    float* part;                 // the splits' parts
+    int groups, M, N, K, scale_group, act;
+    int tiles, blocks_k;         // 16 outputs, 128 inputs
+    // set by the launcher
+    int first_group;
+    int splits, k_split;         // k_split: in blocks of 128 inputs
+};
+struct Fp4Plan {
+    int rows, tiles, splits, k_split;   // rows and output tiles (16 each) per workgroup
+    int64_t part_bytes;
+};
+Fp4Plan fp4_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
+hipError_t launch_quantize_fp4(const Fp4Args& a, int dtype, hipStream_t s);
+hipError_t launch_dequantize_fp4(const Fp4Args& a, int dtype, hipStream_t s);
+hipError_t launch_linear_fp4(Fp4Args a, int dtype, const Fp4Plan& p, hipStream_t s);
+
 // The message of malib_last_error and its status (api.hip).
 malib_status set_error(malib_status code, const char* fmt, ...);
 

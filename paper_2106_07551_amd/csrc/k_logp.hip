@@ -1,0 +1,896 @@
+// Log probabilities of given actions, the entropy and the top alternatives of rows of
+// logits, and the gradient of the first two.
+//
+// With x a row's legal logits, c = log2(e) / T and m = max x: s = sum_j 2^((x_j - m) c),
+// t = sum_j 2^((x_j - m) c) (x_j - m) c, and
+//   l = (x_a - m) / T - ln s,  H = ln s - ln2 t / s,
+//   dx_j = 2^((x_j - m) c) (c0 + c1 (x_j - m) c) + dl [j = a] / T.
+// A row is read once and stays in registers while its top entries are found: the sums
+// need the largest entry of every lane anyway, and the list lies among the entries that are
+// no less than the ceil(k / wavefronts)-th largest of a wavefront's lanes in every wavefront
+// (at least k entries are not less than the least of these).  Those few go to LDS,
+// where each finds its place by counting the larger ones.
+#include "rows.hpp"
+
+namespace malib {
+
+namespace {
+
+// ---------------------------------------------------------------- order of entries
+
+// The order of a list as whole numbers: the value's (NaN above everything, -0 as 0) in the
+// high half, the index reversed in the low one.  Entries up to kUnlisted are not listed.
+constexpr uint32_t kUnlisted = 0x007FFFFFu;   // of -inf
+constexpr uint32_t kAboveInf = 0xFF800000u;   // the values above are NaN
+constexpr float kLeastFinite = -3.402823466e38f;
+
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return x != x ? 0xFFFFFFFFu : b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k)
+{
+    return __uint_as_float(k >> 31 ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ __forceinline__ uint64_t entry_key(float x, int64_t index)
+{
+    return (uint64_t)order_of(x) << 32 | (uint32_t)~(uint32_t)index;
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float key_value(uint64_t k) { return value_of((uint32_t)(k >> 32)); }
+
+// ------------------------------------------------------------------ a row's scalars
+
+// The action of a row, -1 where it is not a legal entry
+__device__ __forceinline__ int row_action(const LogpArgs& a, int64_t row)
+{
+    if (!a.actions)
+        return -1;
+    const int64_t v = a.action_bytes == 1   ? (int64_t)((const uint8_t*)a.actions)[row]
+                      : a.action_bytes == 4 ? (int64_t)((const int32_t*)a.actions)[row]
+                                            : ((const int64_t*)a.actions)[row];
+    if (v < 0 || v >= a.A || (a.mask && a.mask[row * a.mask_ld + v] == 0))
+        return -1;
+    return (int)v;
+}
+
+struct RowOut {
+    float l, H, m, ln_s;
+};
+
+__device__ __forceinline__ RowOut row_finish(const LogpArgs& a, const Stats& st, int action,
+                                             float x_a)
+{
+    RowOut o{0.0f, 0.0f, st.m, 0.0f};
+    if (st.s != 0.0f) {
+        const float m = st.m == kNegInf ? 0.0f : st.m;   // (only NaN above -inf)
+        o.ln_s = logf(st.s);
+        o.H = o.ln_s - kLn2 * st.t / st.s;
+        if (action >= 0)
+            o.l = (x_a - m) / a.temperature - o.ln_s;
+    }
+    return o;
+}
+
+__device__ __forceinline__ void store_row(const LogpArgs& a, int64_t row, const RowOut& o)
+{
+    a.stats[row] = o.l;
+    a.stats[a.rows + row] = o.H;
+    a.stats[2 * a.rows + row] = o.m;
+    a.stats[3 * a.rows + row] = o.ln_s;
+}
+
+__device__ __forceinline__ float entry_logp(const LogpArgs& a, const RowOut& o, float x)
+{
+    return (x - (o.m == kNegInf ? 0.0f : o.m)) / a.temperature - o.ln_s;
+}
+
+// ------------------------------------------------ few actions: a lane per row
+
+// 64 rows per wavefront, as in the losses (rows.hpp): rows go through LDS in memory's own
+// order.  A list is found in as many rounds as it has places, each over the row's
+// entries in registers.
+template <typename E, int NA>
+__global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
+{
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int A = a.A, w = a.top < A ? a.top : A;   // w: places that entries can fill
+    float* bx = lds + wave * kLaneRows * (A + w);
+    float* bv = bx + kLaneRows * A;
+    const float c = kLog2e / a.temperature;
+    const int64_t tiles = (a.rows + kLaneThreads - 1) / kLaneThreads;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t r0 = tile * kLaneThreads + wave * kLaneRows;
+        const int64_t left = a.rows - r0;
+        const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
+        const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
+        const int64_t row = r0 + lane;
+        const int action = lane < n ? row_action(a, row) : -1;
+        wave_lds_sync();
+        rows_to_lds<false, false>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld,
+                                  (const E*)nullptr, 0, mask, a.mask_ld, n, A, bx, bx, lane);
+        wave_lds_sync();
+        float x[NA];
+        RowOut o{};
+        if (lane < n) {
+            float* xr = bx + lane * A;
+#pragma unroll
+            for (int j = 0; j < NA; ++j)
+                x[j] = kNegInf;
+            row_read(xr, A, x);
+            Stats st = empty_stats();
+#pragma unroll
+            for (int j = 0; j < NA; ++j)
+                st.m = fmaxf(st.m, x[j]);
+            const float m = st.m == kNegInf ? 0.0f : st.m;
+#pragma unroll
+            for (int q = 0; q < NA; q += 4) {
+                if (q >= A)
+                    break;
+#pragma unroll
+                for (int j = q; j < q + 4; ++j)
+                    add_entry<kPolicy>(st, x[j], 0.0f, m, 0.0f, c);
+            }
+            o = row_finish(a, st, action, action >= 0 ? xr[action] : 0.0f);
+            store_row(a, row, o);
+        }
+        if (w == 0)
+            continue;
+        wave_lds_sync();   // (the rows in bx have been read)
+        if (lane < n) {
+            uint32_t k[NA];
+#pragma unroll
+            for (int j = 0; j < NA; ++j)
+                k[j] = order_of(x[j]);
+            for (int p = 0; p < w; ++p) {
+                uint32_t best = kUnlisted;
+                int at = -1;
+#pragma unroll
+                for (int q = 0; q < NA; q += 4) {
+                    if (q >= A)
+                        break;
+#pragma unroll
+                    for (int j = q; j < q + 4; ++j) {
+                        at = k[j] > best ? j : at;
+                        best = k[j] > best ? k[j] : best;
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < NA; q += 4) {
+                    if (q >= A)
+                        break;
+#pragma unroll
+                    for (int j = q; j < q + 4; ++j)
+                        k[j] = j == at ? 0u : k[j];
+                }
+                bx[lane * w + p] = __uint_as_float((uint32_t)at);
+                bv[lane * w + p] = at < 0 ? 0.0f : entry_logp(a, o, value_of(best));
+            }
+        }
+        wave_lds_sync();
+        rows_from_lds<float>(bx, (float*)a.top_idx + r0 * a.top, a.top, n, w, lane);
+        rows_from_lds<float>(bv, a.top_logp + r0 * a.top, a.top, n, w, lane);
+        const int more = a.top - w;   // places that no entry can fill
+        for (int i = lane; i < n * more; i += 64) {
+            const int64_t to = (r0 + i / more) * a.top + w + i % more;
+            a.top_idx[to] = -1;
+            a.top_logp[to] = 0.0f;
+        }
+    }
+}
+
+// ------------------------------------------------------- a group of lanes per row
+
+// Sum of a whole number over the group, in every thread; `half`: which half of scratch is
+// next (see group_combine).
+template <int T>
+__device__ __forceinline__ int group_count(int v, float* scratch, int& half)
+{
+    float f = lanes_combine<(T < 64 ? T : 64)>((float)v, SumOp());   // (below 2^24: exact)
+    if constexpr (T > 64) {
+        float* h = scratch + half * kScratch;
+        if ((threadIdx.x & 63) == 0)
+            h[threadIdx.x >> 6] = f;
+        __syncthreads();
+        f = lanes_combine<T / 64>(h[threadIdx.x & (T / 64 - 1)], SumOp());
+        half ^= 1;
+    }
+    return (int)f;
+}
+
+// f(value, index in the row's part) for each entry in a lane's registers
+template <typename E, int T, int C, typename F>
+__device__ __forceinline__ void for_entries(u32x4 (&x)[C], int used, int lane, F f)
+{
+    constexpr int CH = kChunk<E>;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        if (i >= used)
+            break;
+        float v[CH];
+        unpack<E>(x[i], v);
+#pragma unroll
+        for (int e = 0; e < CH; ++e)
+            f(v[e], (lane + i * T) * CH + e);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// A value that at least k of the group's entries are not below, or the least finite
+// one: of each of its wavefronts (or parts of one) the j-th largest lane's, the least.
+constexpr int kBoundRounds = 16;
+template <int T>
+__device__ __forceinline__ float lower_bound(float m, int k, float* scratch, int& half)
+{
+    constexpr int TL = T < 64 ? T : 64, W = T / TL;
+    const int j = (k + W - 1) / W;
+    float bound = kLeastFinite;
+    if (j <= TL / 2 && j <= kBoundRounds) {   // (uniform)
+        const int lane = threadIdx.x & 63, first = lane & ~(TL - 1);
+        const uint64_t group = (TL == 64 ? ~0ull : (1ull << TL) - 1) << first;
+        for (int r = 0; r < j; ++r) {
+            bound = lanes_combine<TL>(m, MaxOp());
+            const uint64_t who = __ballot(m == bound) & group;
+            if (lane == __builtin_ctzll(who | 1ull << 63))   // (without NaN some lane is)
+                m = kNegInf;
+        }
+    }
+    if constexpr (W > 1) {
+        float* h = scratch + half * kScratch;
+        if ((threadIdx.x & 63) == 0)
+            h[threadIdx.x >> 6] = -bound;
+        __syncthreads();
+        bound = -lanes_combine<W>(h[threadIdx.x & (W - 1)], MaxOp());
+        half ^= 1;
+    }
+    return fmaxf(bound, kLeastFinite);
+}
+
+// The k first entries of a row's part in the order of lists: out(place, key) for each,
+// by any of the group's threads; returns how many there are.  m: the lane's largest
+// value; keys: LDS for `cap` >= k keys; *count: LDS, 0.  All threads of a workgroup come here
+// together (T > 64), or all lanes of a wavefront.
+template <typename E, int T, int C, typename F>
+__device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, float m, int k,
+                                          int64_t base, uint64_t* keys, int cap, int* count,
+                                          float* scratch, F out)
+{
+    int half = 0;
+    float at_least = lower_bound<T>(m, k, scratch, half);
+    int mine = 0;
+    for_entries<E, T, C>(x, used, lane, [&](float v, int) { mine += !(v < at_least); });
+    int slot = mine ? atomicAdd(count, mine) : 0;
+    group_sync<T>();
+    int n = *count;
+    bool is_nan = false;          // the least listed value is NaN
+    int index_below = 1 << 30;    // of the entries at that value, those with an index below
+    // Too many, by chance (a part of the row's entries in few lanes), by ties or since the
+    // list is long for so few lanes: the exact value of place k, bit by bit, then, where ties
+    // are too many, the index up to which they are listed.
+    // (Lanes of different rows share a wavefront: all go along, and keep what they had.)
+    bool search = n > cap;
+    if (T > 64 ? search : __any(search)) {
+        auto count_if = [&](auto pred) {
+            int v = 0;
+            for_entries<E, T, C>(x, used, lane, [&](float f, int i) { v += pred(f, i); });
+            return group_count<T>(v, scratch, half);
+        };
+        float at = at_least;
+        int above = count_if([&](float f, int) { return f > at || f != f; });
+        bool nan = false;
+        const bool deeper = above >= k;
+        if (T > 64 ? deeper : __any(search && deeper)) {
+            constexpr int kLast = sizeof(E) == 2 ? 16 : 0;   // (bf16 has no bits below)
+            uint32_t t = 0;
+            for (int b = 31; b >= kLast; --b) {
+                const uint32_t next = t | 1u << b;
+                const float v = value_of(next);
+                const bool beyond = next > kAboveInf;
+                if (count_if([&](float f, int) { return beyond ? f != f : !(f < v); }) >= k)
+                    t = next;
+            }
+            if (kLast > 0 && !(t >> 31))
+                t |= (1u << kLast) - 1u;
+            const bool tn = t > kAboveInf;
+            const float tv = value_of(t);
+            const int c = count_if([&](float f, int) { return tn ? false : f > tv || f != f; });
+            if (deeper) {
+                nan = tn;
+                at = tv;
+                above = c;
+            }
+        }
+        const int ties = count_if([&](float f, int) { return nan ? f != f : f == at; });
+        int below = 1 << 30;
+        const bool many = above + ties > cap;
+        if (T > 64 ? many : __any(search && many)) {
+            int lo = 0;
+            for (int b = 30 - __builtin_clz(T * C * kChunk<E>); b >= 0; --b) {
+                const int next = lo | 1 << b;
+                if (count_if([&](float f, int i) {
+                        return (nan ? f != f : f == at) && i < next;
+                    }) <= k - above)
+                    lo = next;
+            }
+            if (many)
+                below = lo;
+        }
+        if (search) {
+            at_least = at;
+            is_nan = nan;
+            index_below = below;
+        }
+        auto listed = [&](float f, int i) {
+            return is_nan ? f != f && i < index_below
+                          : f > at_least || f != f || (f == at_least && i < index_below);
+        };
+        mine = 0;
+        for_entries<E, T, C>(x, used, lane, [&](float f, int i) { mine += listed(f, i); });
+        group_sync<T>();
+        if (lane == 0)
+            *count = 0;
+        group_sync<T>();
+        slot = mine ? atomicAdd(count, mine) : 0;
+        group_sync<T>();
+        n = *count;
+    }
+    if (mine) {
+        for_entries<E, T, C>(x, used, lane, [&](float f, int i) {
+            const bool listed = is_nan ? f != f && i < index_below
+                                       : f > at_least || f != f ||
+                                             (f == at_least && i < index_below);
+            if (listed)
+                keys[slot++] = entry_key(f, base + i);
+        });
+    }
+    group_sync<T>();
+    for (int i = lane; i < n; i += T) {
+        const uint64_t key = keys[i];
+        int place = 0;
+        int q = 0;
+        for (; q + 4 <= n; q += 4) {
+            const uint64_t k0 = keys[q], k1 = keys[q + 1], k2 = keys[q + 2], k3 = keys[q + 3];
+            place += (k0 > key) + (k1 > key) + (k2 > key) + (k3 > key);
+        }
+        for (; q < n; ++q)
+            place += keys[q] > key;
+        if (place < k)
+            out(place, key);
+    }
+    return n < k ? n : k;
+}
+
+// Rows, or parts of rows (PART: their sums and lists go to the workspace), that fit the
+// registers of T threads, C chunks each.
+template <typename E, int T, int C, bool PART>
+__global__ __launch_bounds__(T <= 64 ? 256 : T) void logp_row_kernel(LogpArgs a)
+{
+    constexpr int ROWS = T <= 64 ? 256 / T : 1;
+    constexpr int CH = kChunk<E>;
+    extern __shared__ uint64_t all_keys[];
+    __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
+    __shared__ int counts[ROWS];
+    const int lane = threadIdx.x % T, slot = threadIdx.x / T;
+    uint64_t* keys = all_keys + (int64_t)slot * a.cap;
+    const float c = kLog2e / a.temperature;
+    const int64_t items = PART ? a.rows * a.splits : a.rows;
+    const int64_t tiles = (items + ROWS - 1) / ROWS;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t item = tile * ROWS + slot;
+        const bool live = item < items;
+        const int64_t row = PART ? item / a.splits : item;
+        const int part = PART ? (int)(item % a.splits) : 0;
+        const int64_t base = PART ? (int64_t)part * a.part_len : 0;
+        const int len = PART ? (int)(a.A - base < a.part_len ? a.A - base : a.part_len) : a.A;
+        const E* px = (const E*)a.logits + row * a.logits_ld + base;
+        const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld + base : nullptr;
+        // (the action's logit is asked for with the row's)
+        int action = -1;
+        float x_a = 0.0f;
+        if (!PART && live) {
+            action = row_action(a, row);
+            if (action >= 0)
+                x_a = to_f32(px[action]);
+        }
+        if (lane == 0)
+            counts[slot] = 0;
+        u32x4 x[C];
+        load_row<E, kPolicy, T, C>(len, live, px, (const E*)nullptr, pm, lane, x, nullptr);
+        const int used = (len + T * CH - 1) / (T * CH);
+        const Stats own = chunk_stats<E, kPolicy, C>(x, nullptr, used, c);
+        bool unused = true;
+        const Stats st = group_merge<T, kPolicy>(own, c, scratch, nullptr, unused);
+        RowOut o{};
+        if constexpr (PART) {
+            if (lane == 0 && live)
+                ((Stats*)a.part_stats)[item] = st;
+        } else {
+            o = row_finish(a, st, action, x_a);
+            if (lane == 0 && live)
+                store_row(a, row, o);
+        }
+        if (a.top == 0)
+            continue;
+        group_sync<T>();   // (T <= 64: the count)
+        keep_raw<kPolicy>(x, nullptr);
+        const int64_t at = item * a.top;
+        const int n = select_top<E, T, C>(
+            x, used, lane, own.m, a.top, base, keys, a.cap, counts + slot, scratch,
+            [&](int place, uint64_t key) {
+                if (!live)
+                    return;
+                if constexpr (PART) {
+                    a.part_keys[at + place] = key;
+                } else {
+                    a.top_idx[at + place] = key_index(key);
+                    a.top_logp[at + place] = entry_logp(a, o, key_value(key));
+                }
+            });
+        for (int i = n + lane; i < a.top && live; i += T) {
+            if constexpr (PART) {
+                a.part_keys[at + i] = 0;
+            } else {
+                a.top_idx[at + i] = -1;
+                a.top_logp[at + i] = 0.0f;
+            }
+        }
+        group_sync<T>();   // (keys, count and scratch are the next row's)
+    }
+}
+
+// ------------------------------------------------------------- parts of rows, merged
+
+// A workgroup per row: the parts' sums, and the first of their lists (each in order,
+// zeros behind its entries).  At least `top` entries are not below the j-th of every list,
+// j = ceil(top / lists), nor below the last place of any one list; with more lists than
+// places, nor below the top-th largest of their first entries.
+constexpr int kMergeThreads = 256, kMergeCap = 1024;
+constexpr int kMergeLists = 2;   // of a thread: logp_plan makes at most 512 parts
+
+__global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
+{
+    constexpr int T = kMergeThreads;
+    __shared__ float scratch[2 * kScratch];
+    __shared__ uint64_t keys[kMergeCap];
+    __shared__ uint64_t wave_key[T / 64];
+    __shared__ int total;
+    const int tid = threadIdx.x, top = a.top;
+    const float c = kLog2e / a.temperature;
+    auto block_max = [&](uint64_t v) {   // (ends with all having read wave_key)
+#pragma unroll
+        for (int o = 32; o; o >>= 1) {
+            const uint64_t u = __shfl_xor(v, o);
+            v = u > v ? u : v;
+        }
+        __syncthreads();
+        if ((tid & 63) == 0)
+            wave_key[tid >> 6] = v;
+        __syncthreads();
+        v = wave_key[0];
+        for (int i = 1; i < T / 64; ++i)
+            v = wave_key[i] > v ? wave_key[i] : v;
+        return v;
+    };
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int action = row_action(a, row);
+        const float x_a =
+            action < 0 ? 0.0f
+            : a.bf16   ? to_f32(((const bf16_t*)a.logits)[row * a.logits_ld + action])
+                       : ((const float*)a.logits)[row * a.logits_ld + action];
+        Stats st = empty_stats();
+        const Stats* parts = (const Stats*)a.part_stats + row * a.splits;
+        for (int i = tid; i < a.splits; i += T)
+            st = merge<kPolicy>(st, parts[i], c);
+        bool unused = true;
+        st = group_merge<T, kPolicy>(st, c, scratch, nullptr, unused);
+        const RowOut o = row_finish(a, st, action, x_a);
+        if (tid == 0)
+            store_row(a, row, o);
+        if (top == 0) {
+            __syncthreads();
+            continue;
+        }
+        const uint64_t* lists = a.part_keys + row * a.splits * top;
+        const int64_t to = row * top;
+        auto write = [&](int place, uint64_t key) {
+            a.top_idx[to + place] = key ? key_index(key) : -1;
+            a.top_logp[to + place] = key ? entry_logp(a, o, key_value(key)) : 0.0f;
+        };
+        // the bound: the largest last place, the least j-th (as the largest of ~key)
+        uint64_t last = 0, jth = 0;
+        const int j = (top + a.splits - 1) / a.splits;
+        for (int i = tid; i < a.splits; i += T) {
+            const uint64_t l = lists[(int64_t)i * top + top - 1];
+            const uint64_t f = ~lists[(int64_t)i * top + j - 1];
+            last = l > last ? l : last;
+            jth = f > jth ? f : jth;
+        }
+        last = block_max(last);
+        jth = ~block_max(jth);
+        uint64_t bound = last > jth ? last : jth;
+        if (a.splits > top && a.splits <= kMergeCap) {   // (j = 1)
+            for (int i = tid; i < a.splits; i += T)
+                keys[i] = lists[(int64_t)i * top];
+            __syncthreads();
+            uint64_t best = 0;
+            for (int i = tid; i < a.splits; i += T) {
+                const uint64_t key = keys[i];
+                int place = 0;
+                for (int q = 0; q < a.splits; ++q)
+                    place += keys[q] > key;
+                if (place == top - 1)
+                    best = key;
+            }
+            best = block_max(best);
+            bound = best > bound ? best : bound;
+        }
+        if (bound == 0)
+            bound = 1;   // (zeros are no entries)
+        if (tid == 0)
+            total = 0;
+        __syncthreads();
+        int mine = 0;
+        for (int i = tid; i < a.splits; i += T)
+            for (int p = 0; p < top && lists[(int64_t)i * top + p] >= bound; ++p)
+                ++mine;
+        int slot = mine ? atomicAdd(&total, mine) : 0;
+        __syncthreads();
+        const int n = total;
+        if (n <= kMergeCap) {
+            for (int i = tid; i < a.splits; i += T)
+                for (int p = 0; p < top; ++p) {
+                    const uint64_t key = lists[(int64_t)i * top + p];
+                    if (key < bound)
+                        break;
+                    keys[slot++] = key;
+                }
+            __syncthreads();
+            for (int i = tid; i < n; i += T) {
+                const uint64_t key = keys[i];
+                int place = 0;
+                for (int q = 0; q < n; ++q)
+                    place += keys[q] > key;
+                if (place < top)
+                    write(place, key);
+            }
+            for (int i = n + tid; i < top; i += T)
+                write(i, 0);
+        } else {   // place after place: the largest of the lists' next entries
+            int next[kMergeLists] = {};
+            for (int p = 0; p < top; ++p) {
+                uint64_t head[kMergeLists], best = 0;
+#pragma unroll
+                for (int q = 0; q < kMergeLists; ++q) {
+                    const int i = tid + q * T;
+                    head[q] = i < a.splits && next[q] < top ? lists[(int64_t)i * top + next[q]]
+                                                            : 0;
+                    best = head[q] > best ? head[q] : best;
+                }
+                best = block_max(best);
+#pragma unroll
+                for (int q = 0; q < kMergeLists; ++q)
+                    next[q] += head[q] == best;
+                if (tid == 0)
+                    write(p, best);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// --------------------------------------------------------------------- gradient
+
+// What a row's gradient needs: 2^d (c0 + c1 d) and, at the action, `at_action` more.
+struct GradRow {
+    RowGrad g;
+    int action;
+    bool some;
+};
+
+__device__ __forceinline__ GradRow grad_row(const LogpArgs& a, int64_t row)
+{
+    GradRow r{};
+    r.action = a.dlogp ? row_action(a, row) : -1;
+    const float H = a.stats[a.rows + row], m = a.stats[2 * a.rows + row];
+    const float ln_s = a.stats[3 * a.rows + row];
+    const float dl = r.action >= 0 ? a.dlogp[row] : 0.0f;
+    const float dh = a.dentropy ? a.dentropy[row] : 0.0f;
+    const float k = expf(-ln_s) / a.temperature;
+    r.some = m != kNegInf || ln_s != 0.0f;   // (only NaN above -inf: m is -inf, ln s NaN)
+    r.g.m = m == kNegInf ? 0.0f : m;
+    r.g.c0 = -k * (dl + dh * (H - ln_s));
+    r.g.c1 = -k * kLn2 * dh;
+    r.g.at_action = dl / a.temperature;
+    return r;
+}
+
+__device__ __forceinline__ float grad_at(const GradRow& r, float x, int j, float c)
+{
+    const float v = grad_entry<kPolicy>(r.g, x, 0.0f, c) + (j == r.action ? r.g.at_action : 0.0f);
+    return x == kNegInf || !r.some ? 0.0f : v;
+}
+
+// As the lane kernel above.
+template <typename E, int NA>
+__global__ __launch_bounds__(kLaneThreads) void logp_grad_lane_kernel(LogpArgs a)
+{
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int A = a.A;
+    float* bx = lds + wave * kLaneRows * A;
+    const float c = kLog2e / a.temperature;
+    const int64_t tiles = (a.rows + kLaneThreads - 1) / kLaneThreads;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t r0 = tile * kLaneThreads + wave * kLaneRows;
+        const int64_t left = a.rows - r0;
+        const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
+        const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
+        GradRow r{};
+        if (lane < n)
+            r = grad_row(a, r0 + lane);
+        wave_lds_sync();
+        rows_to_lds<false, false>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld,
+                                  (const E*)nullptr, 0, mask, a.mask_ld, n, A, bx, bx, lane);
+        wave_lds_sync();
+        if (lane < n) {
+            float* xr = bx + lane * A;
+            float x[NA];
+#pragma unroll
+            for (int j = 0; j < NA; ++j)
+                x[j] = kNegInf;
+            row_read(xr, A, x);
+#pragma unroll
+            for (int q = 0; q < NA; q += 4) {
+                if (q >= A)
+                    break;
+#pragma unroll
+                for (int j = q; j < q + 4; ++j)
+                    x[j] = grad_at(r, x[j], j, c);
+            }
+            row_write(xr, A, x);
+        }
+        wave_lds_sync();
+        rows_from_lds(bx, (E*)a.dlogits + r0 * a.dlogits_ld, a.dlogits_ld, n, A, lane);
+    }
+}
+
+// T lanes per row, or per part of one (splits > 1): every entry apart, in chunks of 16
+// bytes.
+constexpr int kGradThreads = 256, kGradUnroll = 4;
+
+template <typename E, int T>
+__global__ __launch_bounds__(kGradThreads) void logp_grad_kernel(LogpArgs a)
+{
+    constexpr int ROWS = kGradThreads / T, U = kGradUnroll, CH = kChunk<E>;
+    const int lane = threadIdx.x % T, slot = threadIdx.x / T;
+    const float c = kLog2e / a.temperature;
+    const int64_t items = a.rows * a.splits;
+    const int64_t tiles = (items + ROWS - 1) / ROWS;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t item = tile * ROWS + slot;
+        if (item >= items)
+            continue;
+        const int64_t row = a.splits > 1 ? item / a.splits : item;
+        const int64_t base = a.splits > 1 ? item % a.splits * a.part_len : 0;
+        const int len = a.splits > 1 && a.A - base > a.part_len ? a.part_len : (int)(a.A - base);
+        const GradRow r = grad_row(a, row);
+        const E* px = (const E*)a.logits + row * a.logits_ld + base;
+        E* po = (E*)a.dlogits + row * a.dlogits_ld + base;
+        const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld + base : nullptr;
+        for (int j0 = lane * CH; j0 < len; j0 += U * T * CH) {
+            u32x4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * T * CH;
+                x[u] = load_masked(px + j, len - j, pm ? pm + j : nullptr, j);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * T * CH;
+                if (j >= len)
+                    break;
+                float f[CH];
+                unpack<E>(x[u], f);
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    f[e] = grad_at(r, f[e], (int)base + j + e, c);
+                store_chunk(po + j, len - j, pack<E>(f));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------- launches
+
+template <typename E, bool PART>
+void launch_rows(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
+{
+    const unsigned nb = (unsigned)p.blocks;
+    const size_t lds = (size_t)a.cap * 8 * (p.group <= 64 ? 256 / p.group : 1);
+    if constexpr (!PART) {
+        switch (p.group) {
+        case 4:
+            logp_row_kernel<E, 4, 4, false><<<nb, 256, lds, s>>>(a);
+            return;
+        case 8:
+            logp_row_kernel<E, 8, 4, false><<<nb, 256, lds, s>>>(a);
+            return;
+        case 16:
+            logp_row_kernel<E, 16, 4, false><<<nb, 256, lds, s>>>(a);
+            return;
+        case 32:
+            logp_row_kernel<E, 32, 4, false><<<nb, 256, lds, s>>>(a);
+            return;
+        case 64:
+            logp_row_kernel<E, 64, 4, false><<<nb, 256, lds, s>>>(a);
+            return;
+        case 128:
+            logp_row_kernel<E, 128, 4, false><<<nb, 128, lds, s>>>(a);
+            return;
+        }
+    }
+    switch (p.group) {
+    case 256:
+        logp_row_kernel<E, 256, 4, PART><<<nb, 256, lds, s>>>(a);
+        return;
+    case 512:
+        logp_row_kernel<E, 512, 4, PART><<<nb, 512, lds, s>>>(a);
+        return;
+    case 1024:
+        logp_row_kernel<E, 1024, 4, PART><<<nb, 1024, lds, s>>>(a);
+        return;
+    default:
+        logp_row_kernel<E, 1024, 8, PART><<<nb, 1024, lds, s>>>(a);
+    }
+}
+
+template <typename E>
+hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
+{
+    if (p.variant == kLogpLane) {
+        const int w = a.top < a.A ? a.top : a.A;
+        const size_t lds = (size_t)kLaneThreads * 4 * (a.A + w);
+        const unsigned nb = (unsigned)p.blocks;
+        if (a.A <= 8)
+            logp_lane_kernel<E, 8><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 16)
+            logp_lane_kernel<E, 16><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 24)
+            logp_lane_kernel<E, 24><<<nb, kLaneThreads, lds, s>>>(a);
+        else
+            logp_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
+        return hipGetLastError();
+    }
+    if (p.variant == kLogpRow) {
+        launch_rows<E, false>(a, p, s);
+        return hipGetLastError();
+    }
+    launch_rows<E, true>(a, p, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return e;
+    logp_merge_kernel<<<(unsigned)std::min<int64_t>(a.rows, 4096), kMergeThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
+{
+    constexpr int64_t kCus = 256, CH = kChunk<E>;
+    a.splits = 1;
+    if (a.A <= kLaneMost) {
+        const unsigned nb = (unsigned)std::min<int64_t>(
+            2048, (a.rows + kLaneThreads - 1) / kLaneThreads);
+        const size_t lds = (size_t)kLaneThreads * 4 * a.A;
+        if (a.A <= 8)
+            logp_grad_lane_kernel<E, 8><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 16)
+            logp_grad_lane_kernel<E, 16><<<nb, kLaneThreads, lds, s>>>(a);
+        else if (a.A <= 24)
+            logp_grad_lane_kernel<E, 24><<<nb, kLaneThreads, lds, s>>>(a);
+        else
+            logp_grad_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
+        return hipGetLastError();
+    }
+    const int64_t chunks = (a.A + CH - 1) / CH;
+    int T = 4;
+    while (T < kGradThreads && T * 2 < chunks)
+        T *= 2;
+    if (T == kGradThreads && a.rows < 8 * kCus) {   // parts of at least a round of the loop
+        const int64_t want = 8 * kCus / a.rows;
+        a.splits = (int)std::max<int64_t>(
+            1, std::min<int64_t>(want, chunks / (kGradThreads * kGradUnroll)));
+        const int64_t per = (chunks + a.splits - 1) / a.splits;
+        a.part_len = (int)(per * CH);
+        a.splits = (int)((chunks + per - 1) / per);
+    }
+    const int64_t tiles = (a.rows * a.splits + kGradThreads / T - 1) / (kGradThreads / T);
+    const unsigned nb = (unsigned)std::min<int64_t>(65536, tiles);
+    switch (T) {
+    case 4:
+        logp_grad_kernel<E, 4><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    case 8:
+        logp_grad_kernel<E, 8><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    case 16:
+        logp_grad_kernel<E, 16><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    case 32:
+        logp_grad_kernel<E, 32><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    case 64:
+        logp_grad_kernel<E, 64><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    case 128:
+        logp_grad_kernel<E, 128><<<nb, kGradThreads, 0, s>>>(a);
+        break;
+    default:
+        logp_grad_kernel<E, 256><<<nb, kGradThreads, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// As the losses' plan (k_loss.hip): a lane per row up to 31 actions, rows in as few
+// threads' registers as hold them, rows in parts where they do not fit or where there are
+// fewer than half as many as CUs.
+LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
+{
+    constexpr int64_t kCus = 256;
+    LogpPlan p{};
+    const int64_t ch = 16 / size;
+    p.splits = 1;
+    int64_t per = 1;   // rows per workgroup
+    if (A <= kLaneMost) {
+        p.variant = kLogpLane;
+        per = kLaneThreads;
+    } else if (A <= 256 * 4 * ch || (A <= 1024 * 8 * ch && rows >= kCus / 2)) {
+        p.variant = kLogpRow;
+        p.group = 4;
+        while (p.group * 4 * ch < A || (p.group < 64 && p.group * 8 < top))
+            p.group *= 2;   // (2048: 1024 threads with 8 chunks)
+        per = p.group <= 64 ? 256 / p.group : 1;
+    } else {
+        p.variant = kLogpSplit;
+        const int64_t chunks = (A + ch - 1) / ch;
+        // as many parts as fill the CUs twice, of at least 512 chunks (8 KB), at most what fits
+        const int64_t want = std::max<int64_t>(1, 2 * kCus / std::max<int64_t>(1, rows));
+        const int64_t parts = std::max(std::min(want, std::max<int64_t>(1, chunks / 512)),
+                                       (chunks + 8191) / 8192);
+        const int64_t each = (chunks + parts - 1) / parts;
+        p.group = 256;
+        while (p.group * 4 < each)
+            p.group *= 2;
+        p.part_len = (int)(each * ch);
+        p.splits = (int)((chunks + each - 1) / each);
+    }
+    p.cap = std::max(top, p.group <= 64 ? std::max(64, 4 * p.group) : 1024);
+    p.blocks = std::min<int64_t>(4096, (rows * p.splits + per - 1) / per);
+    if (p.variant == kLogpSplit) {
+        p.stats_bytes = (rows * p.splits * (int64_t)sizeof(Stats) + 255) / 256 * 256;
+        p.work_bytes = p.stats_bytes + rows * p.splits * top * 8;
+    }
+    return p;
+}
+
+hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hipStream_t s)
+{
+    a.bf16 = dtype == MALIB_DT_BF16;
+    a.splits = p.splits;
+    a.part_len = p.part_len;
+    a.cap = a.top > 0 ? p.cap : 0;
+    a.part_stats = work;
+    a.part_keys = (uint64_t*)((char*)work + p.stats_bytes);
+    return a.bf16 ? launch_as<bf16_t>(a, p, s) : launch_as<float>(a, p, s);
+}
+
+hipError_t launch_logp_grad(const LogpArgs& a, int dtype, hipStream_t s)
+{
+    return dtype == MALIB_DT_BF16 ? launch_grad_as<bf16_t>(a, s) : launch_grad_as<float>(a, s);
+}
+
+}  // namespace malib

@@ -11,6 +11,7 @@
 
 #include <ATen/ATen.h>
 #include <dlfcn.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "malib.h"
@@ -23,6 +24,14 @@ decltype(&malib_linear_work) p_linear_work;
 decltype(&malib_policy_loss) p_policy_loss;
 decltype(&malib_distill_loss) p_distill_loss;
 decltype(&malib_loss_work) p_loss_work;
+decltype(&malib_log_probs) p_log_probs;
+decltype(&malib_log_probs_backward) p_log_probs_backward;
+decltype(&malib_log_probs_work) p_log_probs_work;
+decltype(&malib_dropout) p_dropout;
+decltype(&malib_quantize_fp4) p_quantize_fp4;
+decltype(&malib_dequantize_fp4) p_dequantize_fp4;
+decltype(&malib_linear_fp4) p_linear_fp4;
+decltype(&malib_linear_fp4_work) p_linear_fp4_work;
 
 // An argument that these functions do not take.
 struct Other {};
@@ -201,7 +210,8 @@ PyObject* call(PyObject* result, F fn)
     raise_status(s);
 }
 
-// load(path of the library)
+// load(path of the library): the losses and layers have to be there; calls of what is not
+// are left to the binding
 PyObject* load(PyObject*, PyObject* path)
 {
     const char* p = PyUnicode_AsUTF8(path);
@@ -215,6 +225,15 @@ PyObject* load(PyObject*, PyObject* path)
         p_distill_loss = (decltype(p_distill_loss))dlsym(h, "malib_distill_loss");
         p_loss_work = (decltype(p_loss_work))dlsym(h, "malib_loss_work");
         p_linear = (decltype(p_linear))dlsym(h, "malib_linear");
+        p_log_probs = (decltype(p_log_probs))dlsym(h, "malib_log_probs");
+        p_log_probs_backward =
+            (decltype(p_log_probs_backward))dlsym(h, "malib_log_probs_backward");
+        p_log_probs_work = (decltype(p_log_probs_work))dlsym(h, "malib_log_probs_work");
+        p_dropout = (decltype(p_dropout))dlsym(h, "malib_dropout");
+        p_quantize_fp4 = (decltype(p_quantize_fp4))dlsym(h, "malib_quantize_fp4");
+        p_dequantize_fp4 = (decltype(p_dequantize_fp4))dlsym(h, "malib_dequantize_fp4");
+        p_linear_fp4 = (decltype(p_linear_fp4))dlsym(h, "malib_linear_fp4");
+        p_linear_fp4_work = (decltype(p_linear_fp4_work))dlsym(h, "malib_linear_fp4_work");
     }
     if (!h || !p_linear || !p_linear_backward || !p_linear_work || !p_policy_loss ||
         !p_distill_loss || !p_loss_work) {
@@ -475,12 +494,305 @@ PyObject* distill_loss(PyObject*, PyObject* const* v, Py_ssize_t n_args)
     });
 }
 
+// ------------------------------------------------ log probabilities, dropout, 4 bits
+//
+// These launch on the current device: tensors of another one are left to the binding.
+void same_device(const at::Tensor& x, std::initializer_list<const Arg*> others)
+{
+    for (const Arg* a : others)
+        need(!*a || (*a)->device() == x.device());
+}
+
+// Actions, and what both directions take beside them
+malib_log_probs_desc scored(const Rows& r, const Arg& actions, PyObject* temperature)
+{
+    malib_log_probs_desc d{};
+    d.dtype = r.dtype;
+    d.rows = r.n;
+    d.n_actions = r.a;
+    d.logits_stride = r.logits;
+    d.mask_stride = r.mask;
+    d.temperature = real(temperature);
+    if (actions) {
+        const auto at = actions->scalar_type();
+        d.action_bytes = at == at::kByte ? 1 : at == at::kInt ? 4 : at == at::kLong ? 8 : 0;
+        need(d.action_bytes != 0);
+        buffer(actions, at, r.n);
+    }
+    return d;
+}
+
+// log_probs(logits, actions, temperature, top, mask, stats, top_idx, top_logp, work, stream)
+//   -> (stats, top_idx, top_logp)
+PyObject* log_probs(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 10, [&]() -> PyObject* {
+        need(p_log_probs && p_log_probs_work);
+        const Arg x(v[0]), actions(v[1]), mask(v[4]), none(Py_None), ws(v[8]);
+        const Rows r(x, mask, none);
+        malib_log_probs_desc d = scored(r, actions, v[2]);
+        const int64_t top = integer(v[3]);
+        need(top >= 0 && top <= 256);
+        d.top = (int32_t)top;
+        Out stats{Arg(v[5])}, idx{Arg(top ? v[6] : Py_None)}, val{Arg(top ? v[7] : Py_None)};
+        same_device(*x, {&actions, &mask, &stats.given, &idx.given, &val.given, &ws});
+        buffer(stats.given, at::kFloat, 4 * r.n);
+        buffer(idx.given, at::kInt, r.n * top);
+        buffer(val.given, at::kFloat, r.n * top);
+        if (!stats.given)
+            stats.make({4, r.n}, at::kFloat, *x);
+        if (top && !idx.given)
+            idx.make({r.n, top}, at::kInt, *x);
+        if (top && !val.given)
+            val.make({r.n, top}, at::kFloat, *x);
+        int64_t bytes = 0;
+        need(p_log_probs_work(d.dtype, r.n, r.a, d.top, &bytes) == MALIB_OK);
+        const Work work(ws, bytes, *x);
+        void* stream = (void*)integer(v[9]);
+        PyObject* result = Py_BuildValue("(NNN)", stats.object(), idx.object(), val.object());
+        return call(result, [&] {
+            return p_log_probs(&d, x.ptr(), actions.ptr(), (const uint8_t*)mask.ptr(),
+                               (float*)stats.ptr(), (int32_t*)idx.ptr(), (float*)val.ptr(),
+                               work.ptr, work.size, stream);
+        });
+    });
+}
+
+// log_probs_backward(logits, actions, stats, dlogp, dentropy, temperature, mask, dlogits,
+//   stream) -> dlogits
+PyObject* log_probs_backward(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 9, [&]() -> PyObject* {
+        need(p_log_probs_backward != nullptr);
+        const Arg x(v[0]), actions(v[1]), stats(v[2]), dlogp(v[3]), dentropy(v[4]), mask(v[6]),
+            none(Py_None);
+        const Rows r(x, mask, none);
+        malib_log_probs_desc d = scored(r, actions, v[5]);
+        need((bool)stats);
+        buffer(stats, at::kFloat, 4 * r.n);
+        buffer(dlogp, at::kFloat, r.n);
+        buffer(dentropy, at::kFloat, r.n);
+        Out dx{Arg(v[7])};
+        same_device(*x, {&actions, &stats, &dlogp, &dentropy, &mask, &dx.given});
+        d.dlogits_stride = r.gradient(dx, *x);
+        void* stream = (void*)integer(v[8]);
+        return call(dx.object(), [&] {
+            return p_log_probs_backward(&d, x.ptr(), actions.ptr(), (const uint8_t*)mask.ptr(),
+                                        (const float*)stats.ptr(), (const float*)dlogp.ptr(),
+                                        (const float*)dentropy.ptr(), dx.ptr(), stream);
+        });
+    });
+}
+
+// Row stride of a tensor whose values are taken in its own order
+int64_t flat_stride(const at::Tensor& t, const at::Tensor& like, int64_t rows, int64_t cols)
+{
+    need(t.scalar_type() == like.scalar_type() && t.sizes() == like.sizes());
+    if (t.is_contiguous())
+        return cols;
+    need(t.dim() == 2 && (t.stride(1) == 1 || cols <= 1));
+    return rows > 1 ? t.stride(0) : cols;
+}
+
+uint64_t whole64(PyObject* o)
+{
+    const uint64_t v = PyLong_Check(o) ? PyLong_AsUnsignedLongLong(o) : ~0ull;
+    need(PyLong_Check(o) && !(v == ~0ull && PyErr_Occurred()));
+    return v;
+}
+
+// dropout(x, p, seed, step, layer, residual, out, device_step, stream) -> out
+PyObject* dropout(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 9, [&]() -> PyObject* {
+        need(p_dropout != nullptr);
+        const Arg x(v[0]), residual(v[5]), device_step(v[7]);
+        need(x && x->dim() >= 1 && x->numel() > 0);
+        malib_dropout_desc d{};
+        d.dtype = type_code(*x);
+        d.cols = x->size(-1);
+        d.rows = x->numel() / d.cols;
+        d.p = PyFloat_AsDouble(v[1]);
+        need(!(d.p == -1.0 && PyErr_Occurred()));
+        d.seed = whole64(v[2]);
+        d.step = whole64(v[3]);
+        const uint64_t layer = whole64(v[4]);
+        need(layer <= 0xFFFFFFFFull);
+        d.layer = (uint32_t)layer;
+        Out out{Arg(v[6])};
+        same_device(*x, {&residual, &out.given, &device_step});
+        buffer(device_step, at::kLong, 1);
+        d.x_stride = flat_stride(*x, *x, d.rows, d.cols);
+        if (residual)
+            d.residual_stride = flat_stride(*residual, *x, d.rows, d.cols);
+        if (!out.given)
+            out.make(x->sizes(), x->scalar_type(), *x);
+        d.y_stride = flat_stride(out.tensor(), *x, d.rows, d.cols);
+        void* stream = (void*)integer(v[8]);
+        return call(out.object(), [&] {
+            return p_dropout(&d, x.ptr(), residual.ptr(), (const int64_t*)device_step.ptr(),
+                             out.ptr(), stream);
+        });
+    });
+}
+
+// A layer in 4 bits
+struct Fp4 {
+    malib_fp4_desc d{};
+    bool grouped;
+    int64_t tiles, blocks;
+
+    Fp4(int dtype, bool grouped_, int64_t groups, int64_t rows, int64_t out, int64_t in,
+        int64_t scale_group)
+        : grouped(grouped_), tiles((out + 15) / 16), blocks((in + 127) / 128)
+    {
+        need(scale_group == 32 || scale_group == 64 || scale_group == 128);
+        d.dtype = dtype;
+        d.groups = groups;
+        d.rows = rows;
+        d.out = out;
+        d.in = in;
+        d.scale_group = (int32_t)scale_group;
+    }
+    void check(const at::Tensor& t, at::ScalarType type, int64_t a, int64_t b) const
+    {
+        const auto s = t.sizes();
+        need(t.scalar_type() == type && t.is_contiguous() && (int)s.size() == 4 + grouped);
+        need(!grouped || s[0] == d.groups);
+        need(s[grouped] == tiles && s[1 + grouped] == blocks && s[2 + grouped] == a &&
+             s[3 + grouped] == b);
+    }
+    void held(const at::Tensor& codes, const at::Tensor& scales) const
+    {
+        check(codes, at::kByte, 64, 16);
+        check(scales, at::kBFloat16, 16, 128 / d.scale_group);
+    }
+    void make(Out& o, at::ScalarType type, int64_t a, int64_t b, const at::Tensor& like) const
+    {
+        if (grouped)
+            o.make({d.groups, tiles, blocks, a, b}, type, like);
+        else
+            o.make({tiles, blocks, a, b}, type, like);
+    }
+    malib_mat mat(const at::Tensor& t, at::ScalarType type, int64_t rows, int64_t cols) const
+    {
+        return matrix(t, type, grouped, d.groups, rows, cols);
+    }
+};
+
+// quantize_fp4(w, group, codes, scales, stream) -> (codes, scales)
+PyObject* quantize_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 5, [&]() -> PyObject* {
+        need(p_quantize_fp4 != nullptr);
+        const Arg w(v[0]);
+        need(w && (w->dim() == 2 || w->dim() == 3));
+        const bool grouped = w->dim() == 3;
+        const Fp4 l(type_code(*w), grouped, grouped ? w->size(0) : 1, 0, w->size(-2), w->size(-1),
+                    integer(v[1]));
+        const malib_mat m = l.mat(*w, w->scalar_type(), l.d.out, l.d.in);
+        Out codes{Arg(v[2])}, scales{Arg(v[3])};
+        same_device(*w, {&codes.given, &scales.given});
+        if (!codes.given)
+            l.make(codes, at::kByte, 64, 16, *w);
+        if (!scales.given)
+            l.make(scales, at::kBFloat16, 16, 128 / l.d.scale_group, *w);
+        l.held(codes.tensor(), scales.tensor());
+        void* stream = (void*)integer(v[4]);
+        PyObject* result = Py_BuildValue("(NN)", codes.object(), scales.object());
+        return call(result, [&] {
+            return p_quantize_fp4(&l.d, &m, (uint8_t*)codes.ptr(), (uint16_t*)scales.ptr(),
+                                  stream);
+        });
+    });
+}
+
+// dequantize_fp4(codes, scales, n_out, n_in, dtype, out, stream) -> out
+PyObject* dequantize_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 7, [&]() -> PyObject* {
+        need(p_dequantize_fp4 != nullptr);
+        const Arg codes(v[0]), scales(v[1]);
+        need((bool)codes && (bool)scales && scales->dim() >= 1);
+        need(v[4] == Py_None || THPDtype_Check(v[4]));
+        Out out{Arg(v[5])};
+        const at::ScalarType type = v[4] != Py_None ? ((THPDtype*)v[4])->scalar_type
+                                    : out.given     ? out.given->scalar_type()
+                                                    : at::kBFloat16;
+        need(type == at::kFloat || type == at::kBFloat16);
+        const int64_t per = scales->size(-1);
+        need(per == 1 || per == 2 || per == 4);
+        const bool grouped = codes->dim() == 5;
+        const Fp4 l(type == at::kBFloat16 ? MALIB_DT_BF16 : MALIB_DT_F32, grouped,
+                    grouped ? codes->size(0) : 1, 0, integer(v[2]), integer(v[3]), 128 / per);
+        l.held(*codes, *scales);
+        same_device(*codes, {&scales, &out.given});
+        if (!out.given && grouped)
+            out.make({l.d.groups, l.d.out, l.d.in}, type, *codes);
+        else if (!out.given)
+            out.make({l.d.out, l.d.in}, type, *codes);
+        const malib_mat m = l.mat(out.tensor(), type, l.d.out, l.d.in);
+        void* stream = (void*)integer(v[6]);
+        return call(out.object(), [&] {
+            return p_dequantize_fp4(&l.d, (const uint8_t*)codes.ptr(),
+                                    (const uint16_t*)scales.ptr(), &m, stream);
+        });
+    });
+}
+
+// linear_fp4(x, codes, scales, n_out, bias, act, residual, out, work, stream) -> out
+PyObject* linear_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
+{
+    return guarded(n_args, 10, [&]() -> PyObject* {
+        need(p_linear_fp4 && p_linear_fp4_work);
+        const Arg x(v[0]), codes(v[1]), scales(v[2]), bias(v[4]), residual(v[6]), ws(v[8]);
+        need(x && codes && scales && scales->dim() >= 1);
+        const int64_t per = scales->size(-1), act = integer(v[5]);
+        need(per == 1 || per == 2 || per == 4);
+        need(act >= MALIB_ACT_NONE && act <= MALIB_ACT_SILU);
+        const bool grouped = codes->dim() == 5;
+        need(x->dim() == 2 + grouped);   // (a shared x is the binding's)
+        Fp4 l(type_code(*x), grouped, grouped ? codes->size(0) : 1, x->size(-2), integer(v[3]),
+              x->size(-1), 128 / per);
+        l.d.act = (int32_t)act;
+        l.held(*codes, *scales);
+        const at::ScalarType type = x->scalar_type();
+        Out out{Arg(v[7])};
+        same_device(*x, {&codes, &scales, &bias, &residual, &out.given, &ws});
+        const malib_mat mx = l.mat(*x, type, l.d.rows, l.d.in);
+        malib_mat mr{};
+        if (residual)
+            mr = l.mat(*residual, type, l.d.rows, l.d.out);
+        buffer(bias, at::kFloat, l.d.out * l.d.groups);
+        if (!out.given && grouped)
+            out.make({l.d.groups, l.d.rows, l.d.out}, type, *x);
+        else if (!out.given)
+            out.make({l.d.rows, l.d.out}, type, *x);
+        const malib_mat my = l.mat(out.tensor(), type, l.d.rows, l.d.out);
+        int64_t bytes = 0;
+        need(p_linear_fp4_work(&l.d, &bytes) == MALIB_OK);
+        const Work work(ws, bytes, *x);
+        void* stream = (void*)integer(v[9]);
+        return call(out.object(), [&] {
+            return p_linear_fp4(&l.d, &mx, (const uint8_t*)codes.ptr(),
+                                (const uint16_t*)scales.ptr(), (const float*)bias.ptr(),
+                                residual ? &mr : nullptr, &my, work.ptr, work.size, stream);
+        });
+    });
+}
+
 PyMethodDef methods[] = {
     {"load", load, METH_O, nullptr},
     {"linear", (PyCFunction)(void (*)())linear, METH_FASTCALL, nullptr},
     {"linear_backward", (PyCFunction)(void (*)())linear_backward, METH_FASTCALL, nullptr},
     {"policy_loss", (PyCFunction)(void (*)())policy_loss, METH_FASTCALL, nullptr},
     {"distill_loss", (PyCFunction)(void (*)())distill_loss, METH_FASTCALL, nullptr},
+    {"log_probs", (PyCFunction)(void (*)())log_probs, METH_FASTCALL, nullptr},
+    {"log_probs_backward", (PyCFunction)(void (*)())log_probs_backward, METH_FASTCALL, nullptr},
+    {"dropout", (PyCFunction)(void (*)())dropout, METH_FASTCALL, nullptr},
+    {"quantize_fp4", (PyCFunction)(void (*)())quantize_fp4, METH_FASTCALL, nullptr},
+    {"dequantize_fp4", (PyCFunction)(void (*)())dequantize_fp4, METH_FASTCALL, nullptr},
+    {"linear_fp4", (PyCFunction)(void (*)())linear_fp4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_learner_calls", nullptr, -1, methods,
