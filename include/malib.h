@@ -794,8 +794,8 @@ typedef struct {
 } malib_fp4_desc;
 
 /*
- * W [out][in] of each group in 4 bits: s = max |w| / 6 of the group of weights, rounded to
- * bf16, and v the value nearest to w / s (halfway: the one of even code; beyond 6: 6).  The
+ * W [out][in] of each group in 4 bits: s = max |w| / 6 of the group of weights (as the fp32
+ * product with 1 / 6), rounded to bf16, and v the value nearest to w / s (halfway: the one of even code; beyond 6: 6).  The
  * comparisons are exact.  A group of weights with an infinite one or a NaN gets a NaN as its
  * scale, one whose scale rounds to 0 gets zeros.
  */

@@ -37,6 +37,7 @@ __device__ __forceinline__ float scale_value(uint16_t s)
 // ------------------------------------------------------------- weights to codes and back
 
 constexpr int kPackThreads = 256;
+constexpr float kSixth = 1.0f / 6.0f;   // of the largest magnitude: a group's scale
 
 // A wavefront per block of 16 outputs x 128 inputs; a lane has output lane & 15 and, of
 // each 32 inputs, the eight from 8 (lane >> 4) on.
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
         for (int j = 0; j < 4; ++j) {
             const uint16_t s = most[j] >= 0x7F800000u
                                    ? (uint16_t)0x7FC0u
-                                   : from_f32<bf16_t>(__uint_as_float(most[j]) / 6.0f).b;
+                                   : from_f32<bf16_t>(__uint_as_float(most[j]) * kSixth).b;
             if (j * 32 / a.scale_group == h)
                 scale = s;
             uint32_t c = 0;

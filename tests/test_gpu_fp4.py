@@ -46,7 +46,8 @@ def quantized64(w, group):
     n, k = w.shape
     full = torch.nn.functional.pad(w, (0, -k % group)).reshape(n, -1, group)
     most = full.abs().amax(-1)
-    s = (most.float() / 6).bfloat16().double()
+    sixth = torch.tensor(1 / 6, dtype=torch.float32, device=w.device)
+    s = (most.float() * sixth).bfloat16().double()
     s = torch.where(torch.isfinite(full).all(-1), s, float("nan"))
     r = full.abs() / torch.where(s > 0, s, 1.0)[..., None]
     best = torch.zeros_like(r)
