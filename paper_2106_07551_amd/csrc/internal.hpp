@@ -474,14 +474,14 @@ struct LogpArgs {
     int A, top, action_bytes;
     float temperature;
     // set by the launchers
-    int splits, part_len, cap;   // cap: keys of a row in LDS
+    int splits, part_len;
     bool bf16;
     void* part_stats;
     uint64_t* part_keys;
 };
-enum { kLogpLane, kLogpRow, kLogpSplit };
+enum { kLogpLane, kLogpShort, kLogpWave, kLogpGroup };
 struct LogpPlan {
-    int variant, group, splits, part_len, cap;   // group: threads per row
+    int variant, group, splits, part_len;   // group: threads per row (kLogpShort)
     int64_t blocks, stats_bytes, work_bytes;
 };
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size);

@@ -5,11 +5,12 @@
 // t = sum_j 2^((x_j - m) c) (x_j - m) c, and
 //   l = (x_a - m) / T - ln s,  H = ln s - ln2 t / s,
 //   dx_j = 2^((x_j - m) c) (c0 + c1 (x_j - m) c) + dl [j = a] / T.
-// A row is read once and stays in registers while its top entries are found: the sums
-// need the largest entry of every lane anyway, and the list lies among the entries that are
-// no less than the ceil(k / wavefronts)-th largest of a wavefront's lanes in every wavefront
-// (at least k entries are not less than the least of these).  Those few go to LDS,
-// where each finds its place by counting the larger ones.
+// Lists: rows of up to kShortMost entries stay in the registers of a few lanes, which
+// find one place after the other, or, for longer lists, in LDS, where a wavefront finds the value
+// of the last place bit by bit.  Longer rows stream through a wavefront or a workgroup, whose
+// sums need the largest entry of every chunk of 16 bytes anyway: chunks with an entry that
+// can still be listed (one per hundreds) go to LDS, and the bound for that rises as the
+// row goes by.
 #include "rows.hpp"
 
 namespace malib {
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
     }
 }
 
-// ------------------------------------------------------- a group of lanes per row
+// ------------------------------------------------ the exact search, in registers
 
 // Sum of a whole number over the group, in every thread; `half`: which half of scratch is
 // next (see group_combine).
@@ -362,81 +363,564 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
     return n < k ? n : k;
 }
 
-// Rows, or parts of rows (PART: their sums and lists go to the workspace), that fit the
-// registers of T threads, C chunks each.
-template <typename E, int T, int C, bool PART>
-__global__ __launch_bounds__(T <= 64 ? 256 : T) void logp_row_kernel(LogpArgs a)
+// --------------------------------------------- short rows: 4 to 32 lanes per row
+
+// Rows of up to kShortMost entries, C chunks a lane.
+constexpr int kShortMost = 512, kShortThreads = 256, kShortC = 4;
+
+// Rounds of a group of T lanes cost their wavefront about 85 instructions for 64 / T rows, a
+// list by the whole wavefront 200 to 300 and what its places take, for one row.
+constexpr int rounds_most(int T) { return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : 6; }
+
+struct MaxU32 {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const
+    {
+        return a > b ? a : b;
+    }
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v)
 {
-    constexpr int ROWS = T <= 64 ? 256 / T : 1;
-    constexpr int CH = kChunk<E>;
-    extern __shared__ uint64_t all_keys[];
-    __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
-    __shared__ int counts[ROWS];
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
+}
+
+// The largest of N lanes' numbers (N up to 64), in each; as lanes_combine
+template <int N>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v)
+{
+    const MaxU32 op;
+    if constexpr (N >= 2)
+        v = op(v, dpp_u32<0xB1>(v));
+    if constexpr (N >= 4)
+        v = op(v, dpp_u32<0x4E>(v));
+    if constexpr (N >= 8)
+        v = op(v, dpp_u32<0x141>(v));
+    if constexpr (N >= 16)
+        v = op(v, dpp_u32<0x140>(v));
+    if constexpr (N >= 32)
+        v = op(v, (uint32_t)__shfl_xor((int)v, 16));
+    if constexpr (N >= 64)
+        v = op(v, (uint32_t)__shfl_xor((int)v, 32));
+    return v;
+}
+
+// A list place after place by the row's T lanes.  bf16: order and index fit one number.
+template <typename E, int T>
+__device__ __forceinline__ void list_by_rounds(const LogpArgs& a, u32x4 (&x)[kShortC], int lane,
+                                               int64_t row, bool live, const RowOut& o)
+{
+    constexpr int CH = kChunk<E>, N = kShortC * CH;
+    constexpr bool kOne = sizeof(E) == 2;
+    uint32_t k[N];
+#pragma unroll
+    for (int i = 0; i < kShortC; ++i) {
+        float v[CH];
+        unpack<E>(x[i], v);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+            const uint32_t key = order_of(v[e]);
+            const uint32_t at = (lane + i * T) * CH + e;
+            k[i * CH + e] = key <= kUnlisted ? 0u : kOne ? (key & 0xFFFF0000u) | (0xFFFFu - at)
+                                                         : key;
+        }
+    }
+    int idx = -1;
+    float val = 0.0f;
+    for (int p = 0; p < a.top; ++p) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            best = k[i] > best ? k[i] : best;
+        best = lanes_max<T>(best);
+        uint32_t at = 0;   // 65535 less the index
+        if constexpr (kOne) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                k[i] = k[i] == best ? 0u : k[i];
+            at = best & 0xFFFFu;
+        } else {
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i)
+                at = k[i] == best ? 0xFFFFu - ((lane + i / CH * T) * CH + i % CH) : at;
+            at = lanes_max<T>(at);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                k[i] = at == 0xFFFFu - ((lane + i / CH * T) * CH + i % CH) ? 0u : k[i];
+        }
+        if (p % T == lane) {
+            // (bf16: a NaN's order lost its low half, which leaves a NaN)
+            const uint32_t order = kOne ? (best >> 31 ? best & 0xFFFF0000u : best | 0xFFFFu) : best;
+            idx = best ? (int)(0xFFFFu - at) : -1;
+            val = best ? entry_logp(a, o, value_of(order)) : 0.0f;
+        }
+        if ((p + 1) % T == 0 || p + 1 == a.top) {
+            const int64_t to = row * a.top + p - p % T + lane;
+            if (live && lane <= p % T) {
+                a.top_idx[to] = idx;
+                a.top_logp[to] = val;
+            }
+        }
+    }
+}
+
+// A list by a wavefront: the row's entries in LDS, lane l takes every 64th.  keys: LDS for
+// kShortMost keys.
+template <typename E, int T>
+__device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, uint64_t* keys,
+                                             int lane, int64_t row, const RowOut& o)
+{
+    constexpr int N = T * kShortC * kChunk<E> / 64;
+    uint32_t k[N];
+    int listed = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        k[i] = order_of(to_f32(from[lane + 64 * i]));
+        k[i] = k[i] <= kUnlisted ? 0u : k[i];
+        listed += __popcll(__ballot(k[i] != 0));
+    }
+    const int most = a.top;
+    uint32_t t = 1;       // the least order that is listed
+    int ties = kShortMost;   // how many entries of that order
+    if (listed > most) {
+        auto count = [&](uint32_t c) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                n += __popcll(__ballot(k[i] >= c));
+            return n;
+        };
+        t = 0;
+        for (int b = 31; b >= 16; --b)
+            if (count(t | 1u << b) >= most)
+                t |= 1u << b;
+        int n = sizeof(E) == 4 ? count(t) : 0;
+        if (sizeof(E) == 4 && n > most + 16) {
+            for (int b = 15; b >= 0; --b)
+                if (count(t | 1u << b) >= most)
+                    t |= 1u << b;
+            n = 0;
+        }
+        if (sizeof(E) == 2 && !(t >> 31))
+            t |= 0xFFFFu;
+        if (sizeof(E) == 2 && t > kAboveInf)
+            t = 0xFFFFFFFFu;
+        if (n == 0)   // t is an entry's
+            ties = most - count(t + 1 > t ? t + 1 : 0xFFFFFFFFu) * (t != 0xFFFFFFFFu);
+    }
+    int n = 0, tied = 0;
+    const uint64_t before = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint64_t same = __ballot(k[i] == t);
+        const bool in = k[i] > t || (k[i] == t && tied + __popcll(same & before) < ties);
+        const uint64_t who = __ballot(in);
+        if (in)
+            keys[n + __popcll(who & before)] = (uint64_t)k[i] << 32 | (uint32_t)~(lane + 64 * i);
+        n += __popcll(who);
+        tied += __popcll(same);
+    }
+    wave_lds_sync();
+    const int64_t to = row * most;
+    for (int i = lane; i < n; i += 64) {
+        const uint64_t key = keys[i];
+        int place = 0;
+#pragma unroll 4
+        for (int q = 0; q < n; ++q)
+            place += keys[q] > key;
+        if (place < most) {
+            a.top_idx[to + place] = key_index(key);
+            a.top_logp[to + place] = entry_logp(a, o, key_value(key));
+        }
+    }
+    for (int i = n + lane; i < most; i += 64) {
+        a.top_idx[to + i] = -1;
+        a.top_logp[to + i] = 0.0f;
+    }
+    wave_lds_sync();
+}
+
+template <typename E, int T>
+__global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
+{
+    constexpr int ROWS = kShortThreads / T, C = kShortC, CH = kChunk<E>;
+    extern __shared__ u32x4 staged[];   // lists by wavefronts: rows, then keys
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
-    uint64_t* keys = all_keys + (int64_t)slot * a.cap;
+    const int wave = threadIdx.x >> 6, wl = threadIdx.x & 63;
     const float c = kLog2e / a.temperature;
-    const int64_t items = PART ? a.rows * a.splits : a.rows;
-    const int64_t tiles = (items + ROWS - 1) / ROWS;
+    const int64_t tiles = (a.rows + ROWS - 1) / ROWS;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t item = tile * ROWS + slot;
-        const bool live = item < items;
+        const int64_t row = tile * ROWS + slot;
+        const bool live = row < a.rows;
+        const E* px = (const E*)a.logits + row * a.logits_ld;
+        const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld : nullptr;
+        // (the action's logit is asked for with the row's)
+        const int action = live ? row_action(a, row) : -1;
+        const float x_a = action >= 0 ? to_f32(px[action]) : 0.0f;
+        u32x4 x[C];
+        load_row<E, kPolicy, T, C>(a.A, live, px, (const E*)nullptr, pm, lane, x, nullptr);
+        const int used = (a.A + T * CH - 1) / (T * CH);
+        bool unused = true;
+        const Stats st = group_merge<T, kPolicy>(chunk_stats<E, kPolicy, C>(x, nullptr, used, c),
+                                                 c, nullptr, nullptr, unused);
+        const RowOut o = row_finish(a, st, action, x_a);
+        if (lane == 0 && live)
+            store_row(a, row, o);
+        if (a.top == 0)
+            continue;
+        if (a.top <= rounds_most(T)) {
+            list_by_rounds<E, T>(a, x, lane, row, live, o);
+            continue;
+        }
+        u32x4* mine = staged + wave * 64 * C;
+        uint64_t* keys = (uint64_t*)(staged + kShortThreads * C) + wave * kShortMost;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            mine[wl / T * T * C + lane + i * T] = x[i];
+        wave_lds_sync();
+        for (int r = 0; r < 64 / T; ++r) {
+            const int64_t at = tile * ROWS + wave * (64 / T) + r;
+            if (at >= a.rows)
+                break;
+            RowOut of = o;
+            of.m = __shfl(o.m, r * T);
+            of.ln_s = __shfl(o.ln_s, r * T);
+            list_by_wave<E, T>(a, (const E*)(mine + r * T * C), keys, wl, at, of);
+        }
+    }
+}
+
+// -------------------------------------------------------------- long rows, streamed
+
+// T threads per row, or per part of one (PART: its sums and list go to the workspace): a
+// wavefront (lists of up to kWaveTop places) or a workgroup.  They go through the row in tiles
+// of U chunks each.  A chunk with an entry that is not below `bound` goes to LDS; the first
+// tile's bound is the least of its wavefronts' j-th largest chunks' maxima, j = ceil(k /
+// wavefronts).  After tiles 1, 2, 4, 8, ... and the last one the chunks' entries join the
+// list's candidates, which are cut to about k, the bound becoming the last one's value: each
+// time about as many come in as stay.  (Values are cut by the high half of their order: bf16
+// exactly.)  Where LDS does not hold them (entries that rise along the row, many equal ones) or a
+// NaN is about, the row's list is made in a second pass by the exact search, tile by
+// tile.
+constexpr int kStreamU = 4, kWaveTop = 64;
+template <int T>
+struct StreamSize {
+    static constexpr int kChunks = T == 64 ? 160 : 512, kKeys = T == 64 ? 256 : 1024;
+    static constexpr int kRows = T == 64 ? 4 : 1;   // per workgroup
+};
+
+template <int T>
+struct Candidates {
+    u32x4 raw[StreamSize<T>::kChunks];
+    uint64_t keys[StreamSize<T>::kKeys];
+    int at[StreamSize<T>::kChunks];   // first index of each chunk
+    float scratch[T > 64 ? 2 * kScratch : 1];
+    int n_raw, n_keys;
+    float bound;
+    bool over;
+};
+
+// The largest 16-bit prefix of an order that at least k of the wavefront's entries are not below
+// (up to that of +inf), as the lowest value with it, from `lo` on, which at least k are
+// not below.  count(v): how many are not below v.
+template <typename F>
+__device__ __forceinline__ uint32_t prefix_bound(uint32_t lo, uint32_t hi, int k, F count)
+{
+    while (hi - lo > 1) {   // (uniform)
+        const uint32_t mid = (lo + hi) / 2;
+        if (count(mid) >= k)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+constexpr uint32_t kLeastPrefix = 0x0080u, kInfPrefix = 0xFF80u;   // of the least finite value
+// the lowest value of a prefix
+__device__ __forceinline__ float prefix_value(uint32_t p) { return value_of(p << 16); }
+
+// The chunks' entries become candidates; the candidates are cut to k or a few more.
+template <typename E, int T>
+__device__ __forceinline__ void tighten(Candidates<T>& l, int lane, int k)
+{
+    using S = StreamSize<T>;
+    constexpr int CH = kChunk<E>;
+    group_sync<T>();
+    const int chunks = l.n_raw;
+    if (chunks > S::kChunks) {   // (uniform over the group)
+        l.over = true;
+        return;
+    }
+    const float bound = l.bound;
+    for (int i = lane; i < chunks * CH; i += T) {
+        const float v = to_f32(((const E*)l.raw)[i]);
+        if (!(v < bound)) {
+            const int slot = atomicAdd(&l.n_keys, 1);
+            if (slot < S::kKeys)
+                l.keys[slot] = entry_key(v, l.at[i / CH] + i % CH);
+        }
+    }
+    group_sync<T>();
+    const int n = l.n_keys;
+    if (n > S::kKeys) {
+        l.over = true;
+        return;
+    }
+    if (n > k) {
+        if (T == 64 || lane < 64) {
+            auto count = [&](uint32_t p) {
+                int m = 0;
+                for (int i = 0; i < n; i += 64)
+                    m += __popcll(__ballot(i + lane < n &&
+                                            (uint32_t)(l.keys[i + lane] >> 32) >= p << 16));
+                return m;
+            };
+            const uint32_t p = prefix_bound(kLeastPrefix, kInfPrefix + 1, k, count);
+            int kept = 0;
+            for (int i = 0; i < n; i += 64) {
+                const uint64_t key = i + lane < n ? l.keys[i + lane] : 0;
+                const bool in = (uint32_t)(key >> 32) >= p << 16;
+                const uint64_t who = __ballot(in);
+                wave_lds_sync();
+                if (in)
+                    l.keys[kept + __popcll(who & ((1ull << lane) - 1))] = key;
+                wave_lds_sync();
+                kept += __popcll(who);
+            }
+            if (lane == 0) {
+                l.n_keys = kept;
+                l.bound = fmaxf(bound, prefix_value(p));
+            }
+        }
+    }
+    if (lane == 0)
+        l.n_raw = 0;
+    group_sync<T>();
+}
+
+// The exact list of a row's part, tile by tile, into l.keys in order; returns its length.
+template <typename E, int T>
+__device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* px,
+                                                    const uint8_t* pm, int len, int64_t base,
+                                                    int k, int lane)
+{
+    constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH;
+    uint64_t* best = (uint64_t*)l.raw;   // the list so far, and behind it the tile's
+    uint64_t* more = best + k;
+    static_assert(sizeof(l.raw) >= 16 * (T == 64 ? kWaveTop : 256), "two lists");
+    int n = 0;
+    for (int64_t j0 = 0; j0 < len; j0 += TILE) {
+        u32x4 x[U];
+        float m = kNegInf;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t j = j0 + (lane + u * T) * CH;
+            x[u] = load_masked(px + j, len - j < CH ? (int)(len - j) : CH, pm ? pm + j : nullptr,
+                               j);
+            float v[CH];
+            unpack<E>(x[u], v);
+#pragma unroll
+            for (int e = 0; e < CH; ++e)
+                m = fmaxf(m, v[e]);
+        }
+        group_sync<T>();
+        if (lane == 0)
+            l.n_keys = 0;
+        group_sync<T>();
+        const int got = select_top<E, T, U>(x, U, lane, m, k, base + j0, l.keys,
+                                            StreamSize<T>::kKeys, &l.n_keys, l.scratch,
+                                            [&](int place, uint64_t key) { more[place] = key; });
+        group_sync<T>();
+        for (int i = lane; i < n + got; i += T) {   // merged through l.keys
+            const uint64_t key = i < n ? best[i] : more[i - n];
+            int place = 0;
+            for (int q = 0; q < n; ++q)
+                place += best[q] > key;
+            for (int q = 0; q < got; ++q)
+                place += more[q] > key;
+            if (place < k)
+                l.keys[place] = key;
+        }
+        n = n + got < k ? n + got : k;
+        group_sync<T>();
+        for (int i = lane; i < n; i += T)
+            best[i] = l.keys[i];
+        group_sync<T>();
+    }
+    for (int i = lane; i < n; i += T)
+        l.keys[i] = best[i];
+    group_sync<T>();
+    return n;
+}
+
+template <typename E, int T, bool PART>
+__global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
+{
+    using S = StreamSize<T>;
+    constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH, W = T / 64;
+    extern __shared__ u32x4 lists[];
+    __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
+    const int lane = threadIdx.x % T, slot = threadIdx.x / T;
+    Candidates<T>& l = ((Candidates<T>*)lists)[slot];
+    const float c = kLog2e / a.temperature;
+    const int k = a.top;
+    const int64_t items = PART ? a.rows * a.splits : a.rows;
+    for (int64_t item = (int64_t)blockIdx.x * S::kRows + slot; item < items;
+         item += (int64_t)gridDim.x * S::kRows) {   // (a wavefront's, or a workgroup's, alone)
         const int64_t row = PART ? item / a.splits : item;
         const int part = PART ? (int)(item % a.splits) : 0;
         const int64_t base = PART ? (int64_t)part * a.part_len : 0;
         const int len = PART ? (int)(a.A - base < a.part_len ? a.A - base : a.part_len) : a.A;
         const E* px = (const E*)a.logits + row * a.logits_ld + base;
         const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld + base : nullptr;
-        // (the action's logit is asked for with the row's)
         int action = -1;
         float x_a = 0.0f;
-        if (!PART && live) {
+        if (!PART) {
             action = row_action(a, row);
             if (action >= 0)
                 x_a = to_f32(px[action]);
         }
-        if (lane == 0)
-            counts[slot] = 0;
-        u32x4 x[C];
-        load_row<E, kPolicy, T, C>(len, live, px, (const E*)nullptr, pm, lane, x, nullptr);
-        const int used = (len + T * CH - 1) / (T * CH);
-        const Stats own = chunk_stats<E, kPolicy, C>(x, nullptr, used, c);
+        if (k > 0 && lane == 0) {
+            l.n_raw = l.n_keys = 0;
+            l.over = false;
+            l.bound = kLeastFinite;
+        }
+        Stats st = empty_stats();
+        float bound = 0.0f;
+        int next = 0, tile = 0;
+        for (int j0 = 0; j0 < len; j0 += TILE, ++tile) {
+            u32x4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + (lane + u * T) * CH;
+                x[u] = load_masked(px + j, len - j, pm ? pm + j : nullptr, j);
+            }
+            float top[U];   // of each chunk
+            Stats own = empty_stats();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[CH];
+                unpack<E>(x[u], v);
+                top[u] = v[0];
+#pragma unroll
+                for (int e = 1; e < CH; ++e)
+                    top[u] = fmaxf(top[u], v[e]);
+                own.m = fmaxf(own.m, top[u]);
+            }
+            const float m = own.m == kNegInf ? 0.0f : own.m;
+            keep_raw<kPolicy>(x, nullptr);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[CH];
+                unpack<E>(x[u], v);
+#pragma unroll
+                for (int e = 0; e < CH; ++e)
+                    add_entry<kPolicy>(own, v[e], 0.0f, m, 0.0f, c);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            st = tile == 0 ? own : merge<kPolicy>(st, own, c);
+            if (k == 0)
+                continue;
+            if (tile == 0) {
+                const int j = (k + W - 1) / W;
+                auto count = [&](uint32_t p) {
+                    const float v = prefix_value(p);
+                    int n = 0;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        n += __popcll(__ballot(top[u] >= v));
+                    return n;
+                };
+                bound = prefix_value(
+                    count(kLeastPrefix) < j
+                        ? kLeastPrefix
+                        : prefix_bound(kLeastPrefix, kInfPrefix + 1, j, count));
+                if constexpr (W > 1) {
+                    if ((lane & 63) == 0)
+                        scratch[lane >> 6] = bound;
+                    __syncthreads();
+                    bound = scratch[0];
+#pragma unroll
+                    for (int i = 1; i < W; ++i)
+                        bound = fminf(bound, scratch[i]);
+                }
+                bound = fmaxf(bound, kLeastFinite);
+                if (lane == 0)
+                    l.bound = bound;
+                group_sync<T>();   // (and the counts are 0 before others add)
+            }
+            bool any = false;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                any = any || top[u] >= bound;
+            if (any) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (top[u] >= bound) {
+                        const int to = atomicAdd(&l.n_raw, 1);
+                        if (to < S::kChunks) {
+                            l.raw[to] = x[u];
+                            l.at[to] = (int)base + j0 + (lane + u * T) * CH;
+                        }
+                    }
+            }
+            if (tile == next || j0 + TILE >= len) {
+                tighten<E, T>(l, lane, k);
+                if (l.over) {   // (no later chunk counts)
+                    bound = -kNegInf;
+                    next = 1 << 30;
+                } else {
+                    bound = l.bound;
+                    next = 2 * next + 1;
+                }
+            }
+        }
         bool unused = true;
-        const Stats st = group_merge<T, kPolicy>(own, c, scratch, nullptr, unused);
+        st = group_merge<T, kPolicy>(st, c, scratch, nullptr, unused);
         RowOut o{};
         if constexpr (PART) {
-            if (lane == 0 && live)
+            if (lane == 0)
                 ((Stats*)a.part_stats)[item] = st;
         } else {
             o = row_finish(a, st, action, x_a);
-            if (lane == 0 && live)
+            if (lane == 0)
                 store_row(a, row, o);
         }
-        if (a.top == 0)
+        if (k == 0)
             continue;
-        group_sync<T>();   // (T <= 64: the count)
-        keep_raw<kPolicy>(x, nullptr);
-        const int64_t at = item * a.top;
-        const int n = select_top<E, T, C>(
-            x, used, lane, own.m, a.top, base, keys, a.cap, counts + slot, scratch,
-            [&](int place, uint64_t key) {
-                if (!live)
-                    return;
+        int n = l.n_keys;
+        bool sorted = false;
+        if (l.over || st.s != st.s) {
+            n = exact_list<E, T>(l, px, pm, len, base, k, lane);
+            sorted = true;
+        }
+        const int64_t to = item * k;
+        for (int i = lane; i < n; i += T) {
+            const uint64_t key = l.keys[i];
+            int place = sorted ? i : 0;
+            if (!sorted) {
+#pragma unroll 4
+                for (int q = 0; q < n; ++q)
+                    place += l.keys[q] > key;
+            }
+            if (place < k) {
                 if constexpr (PART) {
-                    a.part_keys[at + place] = key;
+                    a.part_keys[to + place] = key;
                 } else {
-                    a.top_idx[at + place] = key_index(key);
-                    a.top_logp[at + place] = entry_logp(a, o, key_value(key));
+                    a.top_idx[to + place] = key_index(key);
+                    a.top_logp[to + place] = entry_logp(a, o, key_value(key));
                 }
-            });
-        for (int i = n + lane; i < a.top && live; i += T) {
-            if constexpr (PART) {
-                a.part_keys[at + i] = 0;
-            } else {
-                a.top_idx[at + i] = -1;
-                a.top_logp[at + i] = 0.0f;
             }
         }
-        group_sync<T>();   // (keys, count and scratch are the next row's)
+        for (int i = n + lane; i < k; i += T) {
+            if constexpr (PART) {
+                a.part_keys[to + i] = 0;
+            } else {
+                a.top_idx[to + i] = -1;
+                a.top_logp[to + i] = 0.0f;
+            }
+        }
+        group_sync<T>();   // (lists and scratch are the next row's)
     }
 }
 
@@ -447,7 +931,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void logp_row_kernel(LogpArgs a)
 // j = ceil(top / lists), nor below the last place of any one list; with more lists than
 // places, nor below the top-th largest of their first entries.
 constexpr int kMergeThreads = 256, kMergeCap = 1024;
-constexpr int kMergeLists = 2;   // of a thread: logp_plan makes at most 512 parts
+constexpr int kMergeLists = 2;   // of a thread, at most
 
 __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
 {
@@ -704,55 +1188,20 @@ __global__ __launch_bounds__(kGradThreads) void logp_grad_kernel(LogpArgs a)
 
 // ---------------------------------------------------------------------- launches
 
-template <typename E, bool PART>
-void launch_rows(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
+template <typename E, int T, bool PART>
+void launch_stream(const LogpArgs& a, unsigned nb, hipStream_t s)
 {
-    const unsigned nb = (unsigned)p.blocks;
-    const size_t lds = (size_t)a.cap * 8 * (p.group <= 64 ? 256 / p.group : 1);
-    if constexpr (!PART) {
-        switch (p.group) {
-        case 4:
-            logp_row_kernel<E, 4, 4, false><<<nb, 256, lds, s>>>(a);
-            return;
-        case 8:
-            logp_row_kernel<E, 8, 4, false><<<nb, 256, lds, s>>>(a);
-            return;
-        case 16:
-            logp_row_kernel<E, 16, 4, false><<<nb, 256, lds, s>>>(a);
-            return;
-        case 32:
-            logp_row_kernel<E, 32, 4, false><<<nb, 256, lds, s>>>(a);
-            return;
-        case 64:
-            logp_row_kernel<E, 64, 4, false><<<nb, 256, lds, s>>>(a);
-            return;
-        case 128:
-            logp_row_kernel<E, 128, 4, false><<<nb, 128, lds, s>>>(a);
-            return;
-        }
-    }
-    switch (p.group) {
-    case 256:
-        logp_row_kernel<E, 256, 4, PART><<<nb, 256, lds, s>>>(a);
-        return;
-    case 512:
-        logp_row_kernel<E, 512, 4, PART><<<nb, 512, lds, s>>>(a);
-        return;
-    case 1024:
-        logp_row_kernel<E, 1024, 4, PART><<<nb, 1024, lds, s>>>(a);
-        return;
-    default:
-        logp_row_kernel<E, 1024, 8, PART><<<nb, 1024, lds, s>>>(a);
-    }
+    const size_t lds = a.top > 0 ? sizeof(Candidates<T>) * StreamSize<T>::kRows : 0;
+    logp_stream_kernel<E, T, PART><<<nb, 256, lds, s>>>(a);
 }
 
 template <typename E>
 hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
 {
+    const unsigned nb = (unsigned)p.blocks;
     if (p.variant == kLogpLane) {
         const int w = a.top < a.A ? a.top : a.A;
         const size_t lds = (size_t)kLaneThreads * 4 * (a.A + w);
-        const unsigned nb = (unsigned)p.blocks;
         if (a.A <= 8)
             logp_lane_kernel<E, 8><<<nb, kLaneThreads, lds, s>>>(a);
         else if (a.A <= 16)
@@ -761,17 +1210,30 @@ hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
             logp_lane_kernel<E, 24><<<nb, kLaneThreads, lds, s>>>(a);
         else
             logp_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
-        return hipGetLastError();
+    } else if (p.variant == kLogpShort) {
+        const size_t lds = a.top > rounds_most(p.group)
+                               ? (size_t)kShortThreads * kShortC * 16 +
+                                     kShortThreads / 64 * kShortMost * 8
+                               : 0;
+        if (p.group == 4)
+            logp_short_kernel<E, 4><<<nb, kShortThreads, lds, s>>>(a);
+        else if (p.group == 8)
+            logp_short_kernel<E, 8><<<nb, kShortThreads, lds, s>>>(a);
+        else if (p.group == 16)
+            logp_short_kernel<E, 16><<<nb, kShortThreads, lds, s>>>(a);
+        else if constexpr (sizeof(E) == 4)   // (bf16 rows of kShortMost fit 16 lanes)
+            logp_short_kernel<E, 32><<<nb, kShortThreads, lds, s>>>(a);
+    } else if (p.variant == kLogpWave) {
+        launch_stream<E, 64, false>(a, nb, s);
+    } else if (p.splits == 1) {
+        launch_stream<E, 256, false>(a, nb, s);
+    } else {
+        launch_stream<E, 256, true>(a, nb, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+        logp_merge_kernel<<<(unsigned)std::min<int64_t>(a.rows, 4096), kMergeThreads, 0, s>>>(a);
     }
-    if (p.variant == kLogpRow) {
-        launch_rows<E, false>(a, p, s);
-        return hipGetLastError();
-    }
-    launch_rows<E, true>(a, p, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
-        return e;
-    logp_merge_kernel<<<(unsigned)std::min<int64_t>(a.rows, 4096), kMergeThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -835,42 +1297,39 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 
 }  // namespace
 
-// As the losses' plan (k_loss.hip): a lane per row up to 31 actions, rows in as few
-// threads' registers as hold them, rows in parts where they do not fit or where there are
-// fewer than half as many as CUs.
+// Up to 31 entries a lane per row, up to kShortMost a few lanes, above a wavefront where there are
+// rows enough and short lists, else a workgroup, or several where there are fewer rows
+// than fill the CUs: of at least a tile (16 KB) each.
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 {
     constexpr int64_t kCus = 256;
     LogpPlan p{};
-    const int64_t ch = 16 / size;
+    const int64_t ch = 16 / size, chunks = (A + ch - 1) / ch;
     p.splits = 1;
     int64_t per = 1;   // rows per workgroup
     if (A <= kLaneMost) {
         p.variant = kLogpLane;
         per = kLaneThreads;
-    } else if (A <= 256 * 4 * ch || (A <= 1024 * 8 * ch && rows >= kCus / 2)) {
-        p.variant = kLogpRow;
+    } else if (A <= kShortMost) {
+        p.variant = kLogpShort;
         p.group = 4;
-        while (p.group * 4 * ch < A || (p.group < 64 && p.group * 8 < top))
-            p.group *= 2;   // (2048: 1024 threads with 8 chunks)
-        per = p.group <= 64 ? 256 / p.group : 1;
-    } else {
-        p.variant = kLogpSplit;
-        const int64_t chunks = (A + ch - 1) / ch;
-        // as many parts as fill the CUs twice, of at least 512 chunks (8 KB), at most what fits
-        const int64_t want = std::max<int64_t>(1, 2 * kCus / std::max<int64_t>(1, rows));
-        const int64_t parts = std::max(std::min(want, std::max<int64_t>(1, chunks / 512)),
-                                       (chunks + 8191) / 8192);
-        const int64_t each = (chunks + parts - 1) / parts;
-        p.group = 256;
-        while (p.group * 4 < each)
+        while (p.group * kShortC * ch < A)
             p.group *= 2;
+        per = kShortThreads / p.group;
+    } else if (top <= kWaveTop && rows >= 8 * kCus && chunks <= 1024) {
+        p.variant = kLogpWave;
+        per = StreamSize<64>::kRows;
+    } else {
+        p.variant = kLogpGroup;
+        const int64_t want = (8 * kCus + rows - 1) / std::max<int64_t>(1, rows);
+        const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(
+            {want, (int64_t)kMergeThreads * kMergeLists, chunks / (256 * kStreamU)}));
+        const int64_t each = (chunks + parts - 1) / parts;
         p.part_len = (int)(each * ch);
         p.splits = (int)((chunks + each - 1) / each);
     }
-    p.cap = std::max(top, p.group <= 64 ? std::max(64, 4 * p.group) : 1024);
-    p.blocks = std::min<int64_t>(4096, (rows * p.splits + per - 1) / per);
-    if (p.variant == kLogpSplit) {
+    p.blocks = std::min<int64_t>(1 << 20, (rows * p.splits + per - 1) / per);
+    if (p.splits > 1) {
         p.stats_bytes = (rows * p.splits * (int64_t)sizeof(Stats) + 255) / 256 * 256;
         p.work_bytes = p.stats_bytes + rows * p.splits * top * 8;
     }
@@ -882,7 +1341,6 @@ hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hip
     a.bf16 = dtype == MALIB_DT_BF16;
     a.splits = p.splits;
     a.part_len = p.part_len;
-    a.cap = a.top > 0 ? p.cap : 0;
     a.part_stats = work;
     a.part_keys = (uint64_t*)((char*)work + p.stats_bytes);
     return a.bf16 ? launch_as<bf16_t>(a, p, s) : launch_as<float>(a, p, s);
