@@ -811,17 +811,13 @@ malib_status malib_dequantize_fp4(const malib_fp4_desc* desc, const uint8_t* cod
  * y = act(x W^T + b) + residual with W in 4 bits; the rest as in malib_linear.  Products
  * are exact (x in bf16, or fp32 x in three bf16 parts), sums are formed in fp32, scales are
  * applied to the fp32 sums of their weights.  The weights have no gradient, and x none from
- * this call.  For a few rows of x at a time; the weights' codes are taken apart again for every
- * 64 rows, so that for many rows malib_dequantize_fp4 and malib_linear take less time.
- *  work: as malib_linear_fp4_work says, aligned to 16 bytes.
+ * this call.  For a few rows of x at a time: the weights' codes are taken apart again for every 16
+ * or 32 rows, so that for hundreds of rows malib_dequantize_fp4 and malib_linear take less time.
+ * No workspace.
  */
 malib_status malib_linear_fp4(const malib_fp4_desc* desc, const malib_mat* x,
                               const uint8_t* codes, const uint16_t* scales, const float* bias,
-                              const malib_mat* residual, const malib_mat* y, void* work,
-                              int64_t work_bytes, void* stream);
-
-/* Workspace bytes of malib_linear_fp4 for this description.  Host only. */
-malib_status malib_linear_fp4_work(const malib_fp4_desc* desc, int64_t* work_bytes);
+                              const malib_mat* residual, const malib_mat* y, void* stream);
 
 /* Message for the last non-OK status returned on this thread. */
 const char* malib_last_error(void);

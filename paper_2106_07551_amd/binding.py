@@ -37,7 +37,7 @@ EXPORTS = [
     "malib_linear", "malib_linear_backward", "malib_linear_work",
     "malib_policy_loss", "malib_distill_loss", "malib_loss_work",
     "malib_log_probs", "malib_log_probs_backward", "malib_log_probs_work", "malib_dropout",
-    "malib_quantize_fp4", "malib_dequantize_fp4", "malib_linear_fp4", "malib_linear_fp4_work",
+    "malib_quantize_fp4", "malib_dequantize_fp4", "malib_linear_fp4",
 ]
 
 
@@ -215,10 +215,8 @@ def lib():
         L.malib_quantize_fp4.restype = i32
         L.malib_dequantize_fp4.argtypes = [vp] * 5
         L.malib_dequantize_fp4.restype = i32
-        L.malib_linear_fp4.argtypes = [vp] * 8 + [i64, vp]
+        L.malib_linear_fp4.argtypes = [vp] * 8
         L.malib_linear_fp4.restype = i32
-        L.malib_linear_fp4_work.argtypes = [vp, C.POINTER(i64)]
-        L.malib_linear_fp4_work.restype = i32
         _lib = L
     return _lib
 
@@ -1325,7 +1323,7 @@ def dequantize_fp4(codes, scales, n_out: int, n_in: int, *, dtype=None, out=None
 
 
 def linear_fp4(x, codes, scales, n_out: int, bias=None, *, act: int = ACT_NONE, residual=None,
-               out=None, work=None, stream=None):
+               out=None, stream=None):
     """malib_linear_fp4: act(x w^T + bias) + residual with the weights of quantize_fp4, for
     x [rows][in], or with weights of several policies [groups][rows][in] (x without the
     group dimension is shared by the groups); float32 or bfloat16, bias float32.  For a few
@@ -1333,7 +1331,7 @@ def linear_fp4(x, codes, scales, n_out: int, bias=None, *, act: int = ACT_NONE, 
     takes less time.  Returns [..][rows][out]; nothing here has a gradient."""
     if stream is None and x.is_cuda and (raw := _here(x)) is not None:
         y = (_calls or _native()).linear_fp4(x, codes, scales, n_out, bias, act, residual, out,
-                                             work, raw)
+                                             raw)
         if y is not None:
             return y
     code = _dtype_code(x, "x")
@@ -1348,18 +1346,15 @@ def linear_fp4(x, codes, scales, n_out: int, bias=None, *, act: int = ACT_NONE, 
     mx = _mat(x, dt, G, rows, n_in, "x")
     mr = _mat(residual, dt, G, rows, n_out, "residual")
     _check_buf(bias, _f32(), n_out * (1 if G is None else G), False, "bias")
-    with _guard(x, stream, "x codes scales bias residual out work", x, codes, scales, bias,
-                residual, out, work):
+    with _guard(x, stream, "x codes scales bias residual out", x, codes, scales, bias, residual,
+                out):
         if out is None:
             out = _empty(((rows, n_out) if G is None else (G, rows, n_out),), dt, x.device,
                          stream)
         my = _mat(out, dt, G, rows, n_out, "out", True)
         d = _FP4.pack(code, act, 1 if G is None else G, rows, n_in, n_out, group, 0)
-        need = C.c_int64()
-        _check(lib().malib_linear_fp4_work(d, C.byref(need)))
-        wp, nbytes, work = _workspace(need.value, work, x.device, stream)
         _check(lib().malib_linear_fp4(d, mx, codes.data_ptr(), scales.data_ptr(), _ptr(bias), mr,
-                                      my, wp, nbytes, _stream(stream)))
+                                      my, _stream(stream)))
     return out
 
 

@@ -699,19 +699,9 @@ malib_status malib_dequantize_fp4(const malib_fp4_desc* d, const uint8_t* codes,
     return MALIB_OK;
 }
 
-malib_status malib_linear_fp4_work(const malib_fp4_desc* d, int64_t* work_bytes)
-{
-    TRY(check_fp4(d));
-    if (!work_bytes)
-        return set_error(MALIB_E_INVAL, "work_bytes is NULL");
-    *work_bytes = fp4_plan(d->groups, d->rows, d->out, d->in, type_size(d->dtype)).part_bytes;
-    return MALIB_OK;
-}
-
 malib_status malib_linear_fp4(const malib_fp4_desc* d, const malib_mat* x,
                               const uint8_t* codes, const uint16_t* scales, const float* bias,
-                              const malib_mat* residual, const malib_mat* y, void* work,
-                              int64_t work_bytes, void* stream)
+                              const malib_mat* residual, const malib_mat* y, void* stream)
 {
     TRY(check_fp4(d));
     if (d->rows == 0)
@@ -723,14 +713,12 @@ malib_status malib_linear_fp4(const malib_fp4_desc* d, const malib_mat* x,
     if (residual)
         TRY(check_mat(residual, "residual", d->rows, d->out, d->groups, size, false));
     TRY(check_aligned(bias, "bias", 4));
-    const Fp4Plan p = fp4_plan(d->groups, d->rows, d->out, d->in, size);
-    TRY(check_work(work, work_bytes, p.part_bytes));
     Fp4Args a = fp4_args(d, codes, scales);
     a.x = arg(x);
     a.res = arg(residual);
     a.y = arg(y);
     a.bias = bias;
-    a.part = (float*)work;
+    const Fp4Plan p = fp4_plan(d->groups, d->rows, d->out, d->in, size);
     HIP_TRY(launch_linear_fp4(a, d->dtype, p, (hipStream_t)stream));
     return MALIB_OK;
 }

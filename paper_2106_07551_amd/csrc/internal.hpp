@@ -497,6 +497,8 @@ struct DropoutArgs {
     uint64_t seed, step;
     uint32_t layer, drop;        // a value is dropped where its 16 bits are below `drop`
     float scale;
+    // set by the launcher
+    double inv_cols;
 };
 hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
 
@@ -506,16 +508,13 @@ struct Fp4Args {
     uint8_t* codes;
     uint16_t* scales;
     const float* bias;
-    float* part;                 // the splits' parts
     int groups, M, N, K, scale_group, act;
     int tiles, blocks_k;         // 16 outputs, 128 inputs
     // set by the launcher
     int first_group;
-    int splits, k_split;         // k_split: in blocks of 128 inputs
 };
 struct Fp4Plan {
-    int rows, tiles, splits, k_split;   // rows and output tiles (16 each) per workgroup
-    int64_t part_bytes;
+    int rows, tiles;   // tiles of 16 rows and of 16 outputs per workgroup
 };
 Fp4Plan fp4_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
 hipError_t launch_quantize_fp4(const Fp4Args& a, int dtype, hipStream_t s);

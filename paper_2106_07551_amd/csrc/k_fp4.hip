@@ -7,6 +7,8 @@
 // too, and a scale goes onto the fp32 sum of its weights' products.
 #include "internal.hpp"
 
+#include <type_traits>
+
 #include "act.hpp"
 #include "chunk.hpp"
 #include "device.hpp"
@@ -52,15 +54,30 @@ struct BlockOf {
 };
 
 // Nearest value's code: the comparisons with the borders between values are exact (a
-// border times a bf16 scale fits fp32), ties go to the even code.
-__device__ __forceinline__ uint32_t code_of(float w, float s)
-{
-    const float m = __builtin_fabsf(w);
-    uint32_t c = (m > s * 0.25f) + (m >= s * 0.75f) + (m > s * 1.25f) + (m >= s * 1.75f) +
-                 (m > s * 2.5f) + (m >= s * 3.5f) + (m > s * 5.0f);
-    c = s > 0.0f ? c : 0u;
-    return c && w < 0.0f ? c | 8u : c;
-}
+// border times a bf16 scale fits fp32), ties go to the even code.  Bit by bit from the highest: the
+// borders below codes 4, 2 and 6 belong to the upper code, the others to the lower.
+struct Borders {
+    float b[8];   // b[c]: below code c
+    __device__ __forceinline__ explicit Borders(float s)
+    {
+        const float t = s == 0.0f ? __builtin_inff() : s;   // (NaN: no comparison holds)
+        b[1] = t * 0.25f;
+        b[2] = t * 0.75f;
+        b[3] = t * 1.25f;
+        b[4] = t * 1.75f;
+        b[5] = t * 2.5f;
+        b[6] = t * 3.5f;
+        b[7] = t * 5.0f;
+    }
+    __device__ __forceinline__ uint32_t code(float w) const
+    {
+        const float m = __builtin_fabsf(w);
+        const bool c2 = m >= b[4], c1 = m >= (c2 ? b[6] : b[2]);
+        const bool c0 = m > (c2 ? (c1 ? b[7] : b[5]) : (c1 ? b[3] : b[1]));
+        const uint32_t c = (c2 ? 4u : 0u) | (c1 ? 2u : 0u) | (c0 ? 1u : 0u);
+        return c && w < 0.0f ? c | 8u : c;
+    }
+};
 
 template <typename E>
 __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
@@ -120,10 +137,11 @@ __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
                                    : from_f32<bf16_t>(__uint_as_float(most[j]) * kSixth).b;
             if (j * 32 / a.scale_group == h)
                 scale = s;
+            const Borders borders(scale_value(s));
             uint32_t c = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                c |= code_of(v[j][e], scale_value(s)) << (4 * e);
+                c |= borders.code(v[j][e]) << (4 * e);
             codes[j] = c;
         }
         *(u32x4*)(a.codes + i * 1024 + lane * 16) = codes;
@@ -183,48 +201,106 @@ __device__ __forceinline__ void split_parts(const u32x4 (&raw)[8 / kChunk<E>],
     if constexpr (sizeof(E) == 2) {
         out[0] = __builtin_bit_cast(bf16x8, raw[0]);
     } else {
-        uint32_t part[3][4];
+        uint32_t b[3][8];
+        float check = 0.0f;   // NaN where any input is inf or NaN
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t b[2][3];
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t x = raw[i / 4][i % 4];
+            const float rest = __uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u);
+            const float mid = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
+            b[0][i] = x;
+            b[1][i] = __float_as_uint(rest);
+            b[2][i] = __float_as_uint(rest - mid);
+            check += rest;
+        }
+        if (__any(check != check)) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t x = raw[i / 2][2 * (i % 2) + e];
-                const bool special = (x & 0x7F800000u) == 0x7F800000u;
-                const float f = __uint_as_float(x);
-                const float hi = __uint_as_float(x & 0xFFFF0000u);
-                const float rest = special ? 0.0f : f - hi;
-                const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-                b[e][0] = f != f ? 0x7FC00000u : x;
-                b[e][1] = mid;
-                b[e][2] = __float_as_uint(rest - __uint_as_float(mid));
+            for (int i = 0; i < 8; ++i) {
+                const float f = __uint_as_float(b[0][i]);
+                if (f - f != 0.0f) {   // inf or NaN: the first part alone
+                    b[0][i] = f != f ? 0x7FC00000u : b[0][i];
+                    b[1][i] = b[2][i] = 0;
+                }
             }
-#pragma unroll
-            for (int p = 0; p < 3; ++p)
-                part[p][i] = b[0][p] >> 16 | (b[1][p] & 0xFFFF0000u);
         }
 #pragma unroll
-        for (int p = 0; p < 3; ++p)
-            out[p] = __builtin_bit_cast(bf16x8, u32x4{part[p][0], part[p][1], part[p][2],
-                                                      part[p][3]});
+        for (int p = 0; p < 3; ++p) {
+            u32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)   // the high halves of two
+                v[i] = __builtin_amdgcn_perm(b[p][2 * i + 1], b[p][2 * i], 0x07060302u);
+            out[p] = __builtin_bit_cast(bf16x8, v);
+        }
     }
 }
 
-// A workgroup takes 16 MT rows of x and 16 NT outputs, each of its wavefronts a share of the
-// blocks of 128 inputs; the shares are added through LDS in their order.  Rows and
-// outputs that do not exist repeat the last row, or use the padding's codes: their
-// results are not written.
+// The scales of an output in a block, two in a register
+template <int PER>
+__device__ __forceinline__ void load_scales(const uint16_t* p, uint32_t (&s)[(PER + 1) / 2])
+{
+    if constexpr (PER == 4) {
+        const uint64_t v = *(const uint64_t*)p;
+        s[0] = (uint32_t)v;
+        s[1] = (uint32_t)(v >> 32);
+    } else if constexpr (PER == 2) {
+        s[0] = *(const uint32_t*)p;
+    } else {
+        s[0] = *p;
+    }
+}
+// (padding's scales may hold anything)
+template <int PER>
+__device__ __forceinline__ float scale_of(const uint32_t (&s)[(PER + 1) / 2], int i, bool there)
+{
+    const uint32_t v = s[i / 2];
+    return there ? __uint_as_float(i % 2 ? v & 0xFFFF0000u : v << 16) : 0.0f;
+}
+
+// Output n of rows m .. m + 3: the sum of COUNT shares, `stride` apart in LDS, and the epilogue.
+template <typename E, int COUNT>
+__device__ __forceinline__ void finish_tile(const Fp4Args& a, int64_t g, int64_t m, int64_t n,
+                                            const f32x4* part, int stride)
+{
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const f32x4 f = part[i * stride];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] += f[e];
+    }
+    if (n >= a.N)
+        return;
+    if (a.bias) {
+        const float b = a.bias[g * a.N + n];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] += b;
+    }
+    activate(a.act, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (m + e < a.M) {
+            if (a.res.p)
+                v[e] += to_f32(((const E*)a.res.p)[g * a.res.gs + (m + e) * a.res.ld + n]);
+            ((E*)const_cast<void*>(a.y.p))[g * a.y.gs + (m + e) * a.y.ld + n] = from_f32<E>(v[e]);
+        }
+}
+
+// A workgroup takes 16 rows of x and 16 NT outputs, each of its wavefronts a share of the blocks
+// of 128 inputs, straight from memory to registers, a block ahead of the products; the shares
+// are added through LDS in their order.  Rows and outputs that do not exist repeat the last
+// row, or use the padding's codes: their results are not written.
 constexpr int kWaves = 8;
 
-template <typename E, int SG, int MT, int NT>
+template <typename E, int SG, int NT>
 __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
 {
     constexpr int CH = kChunk<E>, P = kParts<E>, PER = 128 / SG;
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t g = a.first_group + blockIdx.z;
-    const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
-    const int64_t t0 = (int64_t)blockIdx.x * NT;
+    const int64_t m0 = (int64_t)blockIdx.y * 16, t0 = (int64_t)blockIdx.x * NT;
     const uint8_t* codes[NT];
     const uint16_t* scales[NT];
 #pragma unroll
@@ -234,129 +310,256 @@ __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
         codes[t] = a.codes + first * 1024 + lane * 16;
         scales[t] = a.scales + (first * 16 + r) * PER;
     }
-    const E* x[MT];
+    const int64_t row = m0 + r < a.M ? m0 + r : a.M - 1;
+    const E* x = (const E*)a.x.p + g * a.x.gs + row * a.x.ld + h * 8;
+    f32x4 acc[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t m = m0 + t * 16 + r;
-        x[t] = (const E*)a.x.p + g * a.x.gs + (m < a.M ? m : a.M - 1) * a.x.ld + h * 8;
-    }
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto block = [&](int64_t kb, bool whole) {
+    for (int t = 0; t < NT; ++t)
+        acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Block {
         u32x4 c[NT];
-        float s[NT][PER];
+        uint32_t s[NT][(PER + 1) / 2];   // two scales each
+        u32x4 raw[4][8 / CH];
+    };
+    auto load = [&](Block& b, int64_t kb, bool whole) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            c[t] = *(const u32x4*)(codes[t] + kb * 1024);
-            const uint16_t* p = scales[t] + kb * 16 * PER;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                s[t][i] = whole || kb * 128 + i * SG < a.K ? scale_value(p[i]) : 0.0f;
+            b.c[t] = *(const u32x4*)(codes[t] + kb * 1024);
+            load_scales<PER>(scales[t] + kb * 16 * PER, b.s[t]);
         }
-        u32x4 raw[MT][4][8 / CH];
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int q = 0; q < 8; q += CH) {
-                    const int64_t k = kb * 128 + j * 32 + q;
-                    if (whole) {
-                        raw[t][j][q / CH] = *(const u32x4_any*)(x[t] + k);
-                    } else {
-                        const int64_t left = a.K - k - h * 8;
-                        raw[t][j][q / CH] = u32x4{0, 0, 0, 0};
-                        if (left > 0)
-                            raw[t][j][q / CH] =
-                                load_chunk(x[t] + k, left < CH ? (int)left : CH, k + h * 8);
-                    }
+            for (int q = 0; q < 8; q += CH) {
+                const int64_t k = kb * 128 + j * 32 + q;
+                if (whole) {
+                    b.raw[j][q / CH] = *(const u32x4_any*)(x + k);
+                } else {
+                    const int64_t left = a.K - k - h * 8;
+                    b.raw[j][q / CH] = u32x4{0, 0, 0, 0};
+                    if (left > 0)
+                        b.raw[j][q / CH] =
+                            load_chunk(x + k, left < CH ? (int)left : CH, k + h * 8);
                 }
-        f32x4 sum[MT][NT];
+            }
+    };
+    auto multiply = [&](const Block& b, int64_t kb, bool whole) {
+        f32x4 sum[NT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            bf16x8 w[NT];
+            bf16x8 xp[P];
+            split_parts<E>(b.raw[j], xp);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                w[t] = __builtin_bit_cast(bf16x8, code_values(c[t][j]));
+            for (int t = 0; t < NT; ++t) {
+                const bf16x8 w = __builtin_bit_cast(bf16x8, code_values(b.c[t][j]));
+                const float s = scale_of<PER>(b.s[t], j * 32 / SG,
+                                              whole || kb * 128 + j * 32 / SG * SG < a.K);
+                if (j * 32 % SG == 0)
+                    sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                bf16x8 xp[P];
-                split_parts<E>(raw[i][j], xp);
+                for (int p = P - 1; p >= 0; --p)
+                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[p], w, sum[t], 0, 0, 0);
+                if ((j * 32 + 32) % SG == 0) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if (j * 32 % SG == 0)
-                        sum[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int p = P - 1; p >= 0; --p)
-                        sum[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[p], w[t], sum[i][t],
-                                                                            0, 0, 0);
-                    if ((j * 32 + 32) % SG == 0) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][t][e] = __builtin_fmaf(sum[i][t][e], s[t][j * 32 / SG],
-                                                          acc[i][t][e]);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        acc[t][e] = __builtin_fmaf(sum[t][e], s, acc[t][e]);
                 }
             }
         }
     };
     const int64_t whole = a.K / 128;
     int64_t kb = wave;
-    for (; kb < whole; kb += kWaves)
-        block(kb, true);
-    if (kb < a.blocks_k)
-        block(kb, false);
-    __shared__ f32x4 part[kWaves][MT * NT][64];
+    if (kb < whole) {
+        Block now, next;
+        load(now, kb, true);
+        for (; kb + kWaves < whole; kb += kWaves) {
+            load(next, kb + kWaves, true);
+            multiply(now, kb, true);
+            now = next;
+        }
+        multiply(now, kb, true);
+        kb += kWaves;
+    }
+    if (kb < a.blocks_k) {
+        Block b;
+        load(b, kb, false);
+        multiply(b, kb, false);
+    }
+    __shared__ f32x4 part[kWaves][NT][64];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        part[wave][t][lane] = acc[t];
+    __syncthreads();
+    if (wave < NT)
+        finish_tile<E, kWaves>(a, g, m0 + 4 * h, (t0 + wave) * 16 + r, &part[0][wave][lane],
+                               NT * 64);
+}
+
+// More rows, bf16: a workgroup takes 32 rows and 64 outputs.  Rows go through LDS, a wavefront's
+// own 32 x 128 at a time (whole lines of memory, where a 16-row operand takes half ones);
+// 16-byte chunk c of row m lies at c ^ (m mod 16), so that a wavefront's reads of one
+// operand fall into different banks.
+constexpr int kTallWaves = 4, kTallRows = 32, kTallTiles = 4;
+
+template <int SG>
+__global__ __launch_bounds__(kTallWaves * 64) void tall_fp4_kernel(Fp4Args a)
+{
+    constexpr int NT = kTallTiles, MT = kTallRows / 16, PER = 128 / SG, IN = kTallRows / 4;
+    const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t g = a.first_group + blockIdx.z;
+    const int64_t m0 = (int64_t)blockIdx.y * kTallRows, t0 = (int64_t)blockIdx.x * NT;
+    __shared__ u32x4 lds[kTallWaves][kTallRows * 16];
+    u32x4* staged = lds[wave];
+    const uint8_t* codes[NT];
+    const uint16_t* scales[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t tile = t0 + t < a.tiles ? t0 + t : a.tiles - 1;
+        const int64_t first = (g * a.tiles + tile) * a.blocks_k;
+        codes[t] = a.codes + first * 1024 + lane * 16;
+        scales[t] = a.scales + (first * 16 + r) * PER;
+    }
+    // on the way to LDS a lane has chunk r of rows 4 i + h
+    const bf16_t* x[IN];
+#pragma unroll
+    for (int i = 0; i < IN; ++i) {
+        const int64_t m = m0 + 4 * i + h;
+        x[i] = (const bf16_t*)a.x.p + g * a.x.gs + (m < a.M ? m : a.M - 1) * a.x.ld + r * 8;
+    }
+    f32x4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-            part[wave][i * NT + j][lane] = acc[i][j];
-    __syncthreads();
-    // lane: output r of a tile, its rows 4 h .. 4 h + 3
-    for (int q = wave; q < MT * NT; q += kWaves) {
-        const int64_t n = (t0 + q % NT) * 16 + r, m = m0 + q / NT * 16 + 4 * h;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < NT; ++t)
+            acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Block {
+        u32x4 c[NT], raw[IN];
+        uint32_t s[NT][(PER + 1) / 2];
+    };
+    auto load = [&](Block& b, int64_t kb, auto whole) {
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) {
-            const f32x4 t = part[i][q][lane];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] += t[e];
+        for (int t = 0; t < NT; ++t) {
+            b.c[t] = *(const u32x4*)(codes[t] + kb * 1024);
+            load_scales<PER>(scales[t] + kb * 16 * PER, b.s[t]);
         }
-        if (n >= a.N)
-            continue;
-        if (a.bias) {
-            const float b = a.bias[g * a.N + n];
+        if constexpr (whole()) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] += b;
+            for (int i = 0; i < IN; ++i)
+                b.raw[i] = *(const u32x4_any*)(x[i] + kb * 128);
+        } else {
+            const int64_t left = a.K - kb * 128 - r * 8;
+#pragma unroll
+            for (int i = 0; i < IN; ++i)
+                b.raw[i] = left > 0 ? load_chunk(x[i] + kb * 128, left < 8 ? (int)left : 8,
+                                                 kb * 128 + r * 8)
+                                    : u32x4{0, 0, 0, 0};
         }
-        activate(a.act, v);
+    };
+    using Whole = std::true_type;
+    using Short = std::false_type;
+    // `b` holds block kb; block `next` (whole) takes its place
+    auto step = [&](Block& b, int64_t kb, int64_t next, auto whole, auto more) {
+        wave_lds_sync();   // (the last block's operands have been read)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (m + e < a.M) {
-                if (a.res.p)
-                    v[e] += to_f32(((const E*)a.res.p)[g * a.res.gs + (m + e) * a.res.ld + n]);
-                ((E*)const_cast<void*>(a.y.p))[g * a.y.gs + (m + e) * a.y.ld + n] =
-                    from_f32<E>(v[e]);
+        for (int i = 0; i < IN; ++i) {
+            const int m = 4 * i + h;
+            staged[m * 16 + (r ^ (m & 15))] = b.raw[i];
+        }
+        wave_lds_sync();
+        u32x4 c[NT];
+        uint32_t s[NT][(PER + 1) / 2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            c[t] = b.c[t];
+#pragma unroll
+            for (int i = 0; i < (PER + 1) / 2; ++i)
+                s[t][i] = b.s[t][i];
+        }
+        if constexpr (more())
+            load(b, next, Whole());
+        f32x4 sum[MT][NT];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 xp[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                xp[i] = __builtin_bit_cast(bf16x8, staged[(i * 16 + r) * 16 + ((j * 4 + h) ^ r)]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const bf16x8 w = __builtin_bit_cast(bf16x8, code_values(c[t][j]));
+                const float sc = scale_of<PER>(s[t], j * 32 / SG,
+                                               whole() || kb * 128 + j * 32 / SG * SG < a.K);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if (j * 32 % SG == 0)
+                        sum[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    sum[i][t] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[i], w, sum[i][t], 0, 0, 0);
+                    if ((j * 32 + 32) % SG == 0) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[i][t][e] = __builtin_fmaf(sum[i][t][e], sc, acc[i][t][e]);
+                    }
+                }
             }
+        }
+    };
+    // whole blocks, two ahead (behind the last one it is loaded again), then the short one
+    const int64_t whole = a.K / 128, last = whole - 1;
+    int64_t kb = wave;
+    if (kb < whole) {
+        Block even, odd;
+        load(even, kb, Whole());
+        load(odd, kb + kTallWaves < whole ? kb + kTallWaves : last, Whole());
+        for (; kb + kTallWaves < whole; kb += 2 * kTallWaves) {
+            const int64_t n0 = kb + 2 * kTallWaves, n1 = n0 + kTallWaves;
+            step(even, kb, n0 < whole ? n0 : last, Whole(), Whole());
+            step(odd, kb + kTallWaves, n1 < whole ? n1 : last, Whole(), Whole());
+        }
+        if (kb < whole) {
+            step(even, kb, 0, Whole(), Short());
+            kb += kTallWaves;
+        }
     }
+    if (kb == whole && whole < a.blocks_k) {
+        Block b;
+        load(b, kb, Short());
+        step(b, kb, 0, Short(), Short());
+    }
+    static_assert(sizeof lds == sizeof(f32x4) * kTallWaves * MT * NT * 64, "");
+    f32x4* part = (f32x4*)lds;   // [wavefront][tile][lane], each wavefront's over its own rows
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            part[(wave * MT * NT + i * NT + t) * 64 + lane] = acc[i][t];
+    __syncthreads();
+    for (int q = wave; q < MT * NT; q += kTallWaves)
+        finish_tile<bf16_t, kTallWaves>(a, g, m0 + q / NT * 16 + 4 * h, (t0 + q % NT) * 16 + r,
+                                        part + q * 64 + lane, MT * NT * 64);
 }
 
-template <typename E, int MT, int NT>
+template <typename E, int NT>
 void launch_tiles(const Fp4Args& a, dim3 grid, hipStream_t s)
 {
     if (a.scale_group == 32)
-        linear_fp4_kernel<E, 32, MT, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 32, NT><<<grid, kWaves * 64, 0, s>>>(a);
     else if (a.scale_group == 64)
-        linear_fp4_kernel<E, 64, MT, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 64, NT><<<grid, kWaves * 64, 0, s>>>(a);
     else
-        linear_fp4_kernel<E, 128, MT, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 128, NT><<<grid, kWaves * 64, 0, s>>>(a);
+}
+
+void launch_tall(const Fp4Args& a, dim3 grid, hipStream_t s)
+{
+    if (a.scale_group == 32)
+        tall_fp4_kernel<32><<<grid, kTallWaves * 64, 0, s>>>(a);
+    else if (a.scale_group == 64)
+        tall_fp4_kernel<64><<<grid, kTallWaves * 64, 0, s>>>(a);
+    else
+        tall_fp4_kernel<128><<<grid, kTallWaves * 64, 0, s>>>(a);
 }
 
 template <typename E>
@@ -380,12 +583,14 @@ hipError_t launch_linear_as(Fp4Args a, const Fp4Plan& p, hipStream_t s)
             b.first_group = (int)g;
             const dim3 grid((unsigned)nt, (unsigned)((b.M + 16 * p.rows - 1) / (16 * p.rows)),
                             (unsigned)std::min<int64_t>(groups, a.groups - g));
-            if (p.rows == 1)
-                launch_tiles<E, 1, 1>(b, grid, s);
-            else if (p.rows == 2)
-                launch_tiles<E, 2, 1>(b, grid, s);
+            if (p.rows == 2)
+                launch_tall(b, grid, s);
+            else if (p.tiles == 4)
+                launch_tiles<E, 4>(b, grid, s);
+            else if (p.tiles == 2)
+                launch_tiles<E, 2>(b, grid, s);
             else
-                launch_tiles<E, 4, 1>(b, grid, s);
+                launch_tiles<E, 1>(b, grid, s);
         }
     }
     return hipGetLastError();
@@ -402,12 +607,25 @@ hipError_t launch_pack(const Fp4Args& a, F kernel, hipStream_t s)
 
 }  // namespace
 
+// bf16 rows through LDS against straight to registers (us, groups of 128 and of 32 weights): 96 rows
+// x 4096 -> 4096 9.4 and 13.6, 15.6 and 14.6; 128 rows x 8192 -> 8192 25.4 and 44.2, 37.9 and
+// 48.8; 256 x 512 -> 16384 15.7 and 25.5, 18.8 and 22.8; but 48 x 4096 -> 4096 9.8 and 8.1, 15.5
+// and 9.0, and with few blocks of inputs for each wavefront 256 x 16384 <- 512 23.9 and 21.1, 43.8
+// and 24.8.  Straight to registers, as many tiles as leave a workgroup for most CUs: 1 row x 8192 ->
+// 8192 with 1, 2, 4 tiles 9.1, 8.5, 11.0; 16 rows 19.2, 12.5, 14.6; 32 rows 34.8, 21.8, 15.3.
 Fp4Plan fp4_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
 {
+    constexpr int64_t kFill = 192;   // workgroups
     Fp4Plan p{};
-    p.rows = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    p.tiles = 1;
-    p.splits = 1;
+    p.tiles = 4;
+    p.rows = 1;
+    if (size == 2 && M > 64 && K >= 2048) {
+        p.rows = kTallRows / 16;
+        return p;
+    }
+    const int64_t tiles = (N + 15) / 16, blocks = (M + 15) / 16 * groups;
+    while (p.tiles > 1 && (tiles + p.tiles - 1) / p.tiles * blocks < kFill)
+        p.tiles /= 2;
     return p;
 }
 

@@ -363,14 +363,14 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
     return n < k ? n : k;
 }
 
-// --------------------------------------------- short rows: 4 to 32 lanes per row
+// --------------------------------------------- short rows: 4 to 64 lanes per row
 
 // Rows of up to kShortMost entries, C chunks a lane.
-constexpr int kShortMost = 512, kShortThreads = 256, kShortC = 4;
+constexpr int kShortMost = 1024, kShortThreads = 256, kShortC = 4;
 
 // Rounds of a group of T lanes cost their wavefront about 85 instructions for 64 / T rows, a
 // list by the whole wavefront 200 to 300 and what its places take, for one row.
-constexpr int rounds_most(int T) { return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : 6; }
+constexpr int rounds_most(int T) { return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : T == 32 ? 6 : 3; }
 
 struct MaxU32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const
@@ -465,7 +465,7 @@ __device__ __forceinline__ void list_by_rounds(const LogpArgs& a, u32x4 (&x)[kSh
 }
 
 // A list by a wavefront: the row's entries in LDS, lane l takes every 64th.  keys: LDS for
-// kShortMost keys.
+// as many keys.
 template <typename E, int T>
 __device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, uint64_t* keys,
                                              int lane, int64_t row, const RowOut& o)
@@ -482,7 +482,28 @@ __device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, u
     const int most = a.top;
     uint32_t t = 1;       // the least order that is listed
     int ties = kShortMost;   // how many entries of that order
-    if (listed > most) {
+    bool search = listed > most;
+    if (search && N > 1 && most <= 32) {
+        // at least `most` lanes' largest entries are not below t: about as many entries as that
+        // (one count a step, not N) as long as they lie in different lanes
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            m = k[i] > m ? k[i] : m;
+        uint32_t low = 0;
+        for (int b = 31; b >= 16; --b)
+            if (__popcll(__ballot(m >= (low | 1u << b))) >= most)
+                low |= 1u << b;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            n += __popcll(__ballot(k[i] >= low));
+        if (low > kUnlisted && n <= 2 * most + 32) {
+            t = low;
+            search = false;
+        }
+    }
+    if (search) {
         auto count = [&](uint32_t c) {
             int n = 0;
 #pragma unroll
@@ -573,7 +594,7 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
             continue;
         }
         u32x4* mine = staged + wave * 64 * C;
-        uint64_t* keys = (uint64_t*)(staged + kShortThreads * C) + wave * kShortMost;
+        uint64_t* keys = (uint64_t*)(staged + kShortThreads * C) + wave * (T * C * CH);
 #pragma unroll
         for (int i = 0; i < C; ++i)
             mine[wl / T * T * C + lane + i * T] = x[i];
@@ -596,7 +617,7 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
 // wavefront (lists of up to kWaveTop places) or a workgroup.  They go through the row in tiles
 // of U chunks each.  A chunk with an entry that is not below `bound` goes to LDS; the first
 // tile's bound is the least of its wavefronts' j-th largest chunks' maxima, j = ceil(k /
-// wavefronts).  After tiles 1, 2, 4, 8, ... and the last one the chunks' entries join the
+// wavefronts).  After 2, 4, 8, ... tiles (long lists: after the first, too) and the last one the chunks' entries join the
 // list's candidates, which are cut to about k, the bound becoming the last one's value: each
 // time about as many come in as stay.  (Values are cut by the high half of their order: bf16
 // exactly.)  Where LDS does not hold them (entries that rise along the row, many equal ones) or a
@@ -620,13 +641,24 @@ struct Candidates {
     bool over;
 };
 
-// The largest 16-bit prefix of an order that at least k of the wavefront's entries are not below
-// (up to that of +inf), as the lowest value with it, from `lo` on, which at least k are
-// not below.  count(v): how many are not below v.
+// The largest 16-bit prefix of an order, from `lo` (which at least k entries are not below) to
+// that of +inf, that at least k of the wavefront's entries are not below.  count(p): how many
+// are not below the lowest value of prefix p.  The steps double, then halve: the result lies
+// near lo.
 template <typename F>
-__device__ __forceinline__ uint32_t prefix_bound(uint32_t lo, uint32_t hi, int k, F count)
+__device__ __forceinline__ uint32_t prefix_bound(uint32_t lo, int k, F count)
 {
-    while (hi - lo > 1) {   // (uniform)
+    uint32_t hi = 0xFF81u, step = 1;   // behind +inf's
+    while (lo + step < hi) {   // (uniform)
+        const uint32_t p = lo + step;
+        if (count(p) < k)
+            hi = p;
+        else {
+            lo = p;
+            step *= 2;
+        }
+    }
+    while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
         if (count(mid) >= k)
             lo = mid;
@@ -635,7 +667,21 @@ __device__ __forceinline__ uint32_t prefix_bound(uint32_t lo, uint32_t hi, int k
     }
     return lo;
 }
-constexpr uint32_t kLeastPrefix = 0x0080u, kInfPrefix = 0xFF80u;   // of the least finite value
+// The same from the least finite value's prefix, halving alone
+template <typename F>
+__device__ __forceinline__ uint32_t halved_bound(int k, F count)
+{
+    uint32_t lo = 0x0080u, hi = 0xFF81u;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (count(mid) >= k)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+constexpr uint32_t kLeastPrefix = 0x0080u;   // of the least finite value
 // the lowest value of a prefix
 __device__ __forceinline__ float prefix_value(uint32_t p) { return value_of(p << 16); }
 
@@ -668,14 +714,23 @@ __device__ __forceinline__ void tighten(Candidates<T>& l, int lane, int k)
     }
     if (n > k) {
         if (T == 64 || lane < 64) {
+            constexpr int R = 4;   // keys of a lane in registers
+            uint32_t order[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                order[r] =
+                    r * 64 + lane < n ? (uint32_t)(l.keys[r * 64 + lane] >> 32) : kUnlisted;
             auto count = [&](uint32_t p) {
                 int m = 0;
-                for (int i = 0; i < n; i += 64)
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    m += __popcll(__ballot(order[r] >= p << 16));
+                for (int i = R * 64; i < n; i += 64)
                     m += __popcll(__ballot(i + lane < n &&
-                                            (uint32_t)(l.keys[i + lane] >> 32) >= p << 16));
+                                           (uint32_t)(l.keys[i + lane] >> 32) >= p << 16));
                 return m;
             };
-            const uint32_t p = prefix_bound(kLeastPrefix, kInfPrefix + 1, k, count);
+            const uint32_t p = prefix_bound(order_of(bound) >> 16, k, count);
             int kept = 0;
             for (int i = 0; i < n; i += 64) {
                 const uint64_t key = i + lane < n ? l.keys[i + lane] : 0;
@@ -787,7 +842,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
         }
         Stats st = empty_stats();
         float bound = 0.0f;
-        int next = 0, tile = 0;
+        int next = 4 * k <= S::kChunks ? 1 : 0, tile = 0;   // (the tile of the next cut)
         for (int j0 = 0; j0 < len; j0 += TILE, ++tile) {
             u32x4 x[U];
 #pragma unroll
@@ -797,8 +852,12 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
             }
             float top[U];   // of each chunk
             Stats own = empty_stats();
+            const int here = (len - j0 + T * CH - 1) / (T * CH);   // rounds with any chunk
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                top[u] = kNegInf;
+                if (u >= here)
+                    continue;
                 float v[CH];
                 unpack<E>(x[u], v);
                 top[u] = v[0];
@@ -811,6 +870,8 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
             keep_raw<kPolicy>(x, nullptr);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (u >= here)
+                    break;
                 float v[CH];
                 unpack<E>(x[u], v);
 #pragma unroll
@@ -834,7 +895,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
                 bound = prefix_value(
                     count(kLeastPrefix) < j
                         ? kLeastPrefix
-                        : prefix_bound(kLeastPrefix, kInfPrefix + 1, j, count));
+                        : halved_bound(j, count));
                 if constexpr (W > 1) {
                     if ((lane & 63) == 0)
                         scratch[lane >> 6] = bound;
@@ -899,7 +960,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
             const uint64_t key = l.keys[i];
             int place = sorted ? i : 0;
             if (!sorted) {
-#pragma unroll 4
+#pragma unroll 8
                 for (int q = 0; q < n; ++q)
                     place += l.keys[q] > key;
             }
@@ -1015,22 +1076,26 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
         if (tid == 0)
             total = 0;
         __syncthreads();
-        int mine = 0;
-        for (int i = tid; i < a.splits; i += T)
-            for (int p = 0; p < top && lists[(int64_t)i * top + p] >= bound; ++p)
-                ++mine;
-        int slot = mine ? atomicAdd(&total, mine) : 0;
+        // kSide places of every list at a time, until none of them reaches the bound
+        constexpr int kSide = 16;
+        for (int p0 = 0; p0 < top; p0 += kSide) {
+            bool any = false;
+            for (int i = tid; i < a.splits * kSide; i += T) {
+                const int p = p0 + i % kSide;
+                const uint64_t key = p < top ? lists[(int64_t)(i / kSide) * top + p] : 0;
+                if (key >= bound) {
+                    any = true;
+                    const int slot = atomicAdd(&total, 1);
+                    if (slot < kMergeCap)
+                        keys[slot] = key;
+                }
+            }
+            if (!__syncthreads_or(any))
+                break;
+        }
         __syncthreads();
         const int n = total;
         if (n <= kMergeCap) {
-            for (int i = tid; i < a.splits; i += T)
-                for (int p = 0; p < top; ++p) {
-                    const uint64_t key = lists[(int64_t)i * top + p];
-                    if (key < bound)
-                        break;
-                    keys[slot++] = key;
-                }
-            __syncthreads();
             for (int i = tid; i < n; i += T) {
                 const uint64_t key = keys[i];
                 int place = 0;
@@ -1213,7 +1278,7 @@ hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
     } else if (p.variant == kLogpShort) {
         const size_t lds = a.top > rounds_most(p.group)
                                ? (size_t)kShortThreads * kShortC * 16 +
-                                     kShortThreads / 64 * kShortMost * 8
+                                     (size_t)kShortThreads / 64 * p.group * kShortC * kChunk<E> * 8
                                : 0;
         if (p.group == 4)
             logp_short_kernel<E, 4><<<nb, kShortThreads, lds, s>>>(a);
@@ -1221,8 +1286,10 @@ hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
             logp_short_kernel<E, 8><<<nb, kShortThreads, lds, s>>>(a);
         else if (p.group == 16)
             logp_short_kernel<E, 16><<<nb, kShortThreads, lds, s>>>(a);
-        else if constexpr (sizeof(E) == 4)   // (bf16 rows of kShortMost fit 16 lanes)
+        else if (p.group == 32)
             logp_short_kernel<E, 32><<<nb, kShortThreads, lds, s>>>(a);
+        else if constexpr (sizeof(E) == 4)   // (bf16 rows of kShortMost fit 32 lanes)
+            logp_short_kernel<E, 64><<<nb, kShortThreads, lds, s>>>(a);
     } else if (p.variant == kLogpWave) {
         launch_stream<E, 64, false>(a, nb, s);
     } else if (p.splits == 1) {

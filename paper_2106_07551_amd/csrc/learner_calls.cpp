@@ -31,7 +31,6 @@ decltype(&malib_dropout) p_dropout;
 decltype(&malib_quantize_fp4) p_quantize_fp4;
 decltype(&malib_dequantize_fp4) p_dequantize_fp4;
 decltype(&malib_linear_fp4) p_linear_fp4;
-decltype(&malib_linear_fp4_work) p_linear_fp4_work;
 
 // An argument that these functions do not take.
 struct Other {};
@@ -233,7 +232,6 @@ PyObject* load(PyObject*, PyObject* path)
         p_quantize_fp4 = (decltype(p_quantize_fp4))dlsym(h, "malib_quantize_fp4");
         p_dequantize_fp4 = (decltype(p_dequantize_fp4))dlsym(h, "malib_dequantize_fp4");
         p_linear_fp4 = (decltype(p_linear_fp4))dlsym(h, "malib_linear_fp4");
-        p_linear_fp4_work = (decltype(p_linear_fp4_work))dlsym(h, "malib_linear_fp4_work");
     }
     if (!h || !p_linear || !p_linear_backward || !p_linear_work || !p_policy_loss ||
         !p_distill_loss || !p_loss_work) {
@@ -740,12 +738,12 @@ PyObject* dequantize_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
     });
 }
 
-// linear_fp4(x, codes, scales, n_out, bias, act, residual, out, work, stream) -> out
+// linear_fp4(x, codes, scales, n_out, bias, act, residual, out, stream) -> out
 PyObject* linear_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
 {
-    return guarded(n_args, 10, [&]() -> PyObject* {
-        need(p_linear_fp4 && p_linear_fp4_work);
-        const Arg x(v[0]), codes(v[1]), scales(v[2]), bias(v[4]), residual(v[6]), ws(v[8]);
+    return guarded(n_args, 9, [&]() -> PyObject* {
+        need(p_linear_fp4 != nullptr);
+        const Arg x(v[0]), codes(v[1]), scales(v[2]), bias(v[4]), residual(v[6]);
         need(x && codes && scales && scales->dim() >= 1);
         const int64_t per = scales->size(-1), act = integer(v[5]);
         need(per == 1 || per == 2 || per == 4);
@@ -758,7 +756,7 @@ PyObject* linear_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
         l.held(*codes, *scales);
         const at::ScalarType type = x->scalar_type();
         Out out{Arg(v[7])};
-        same_device(*x, {&codes, &scales, &bias, &residual, &out.given, &ws});
+        same_device(*x, {&codes, &scales, &bias, &residual, &out.given});
         const malib_mat mx = l.mat(*x, type, l.d.rows, l.d.in);
         malib_mat mr{};
         if (residual)
@@ -769,14 +767,11 @@ PyObject* linear_fp4(PyObject*, PyObject* const* v, Py_ssize_t n_args)
         else if (!out.given)
             out.make({l.d.rows, l.d.out}, type, *x);
         const malib_mat my = l.mat(out.tensor(), type, l.d.rows, l.d.out);
-        int64_t bytes = 0;
-        need(p_linear_fp4_work(&l.d, &bytes) == MALIB_OK);
-        const Work work(ws, bytes, *x);
-        void* stream = (void*)integer(v[9]);
+        void* stream = (void*)integer(v[8]);
         return call(out.object(), [&] {
             return p_linear_fp4(&l.d, &mx, (const uint8_t*)codes.ptr(),
                                 (const uint16_t*)scales.ptr(), (const float*)bias.ptr(),
-                                residual ? &mr : nullptr, &my, work.ptr, work.size, stream);
+                                residual ? &mr : nullptr, &my, stream);
         });
     });
 }

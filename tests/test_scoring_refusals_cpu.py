@@ -98,7 +98,7 @@ def _fp4(call, *, dtype=B.DT_F32, act=0, groups=1, rows=2, n_in=40, n_out=20, gr
     if call == "dequantize":
         return L.malib_dequantize_fp4(C.byref(d), codes, scales, w, None)
     out = None if y is None else C.byref(B.Mat(y, n_out if yld is None else yld, gs))
-    return L.malib_linear_fp4(C.byref(d), w, codes, scales, bias, None, out, None, 0, None)
+    return L.malib_linear_fp4(C.byref(d), w, codes, scales, bias, None, out, None)
 
 
 @pytest.mark.parametrize("call", ["quantize", "dequantize", "linear"])
@@ -184,7 +184,7 @@ def test_binding_refuses(call, word):
 
 @pytest.mark.parametrize("name, n", [("log_probs", 10), ("log_probs_backward", 9), ("dropout", 9),
                                      ("quantize_fp4", 5), ("dequantize_fp4", 7),
-                                     ("linear_fp4", 10)])
+                                     ("linear_fp4", 9)])
 def test_native_calls_leave_what_they_do_not_take(name, n):
     call = getattr(B._native(), name)
     with pytest.raises(TypeError):
