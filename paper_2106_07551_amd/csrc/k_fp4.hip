@@ -57,23 +57,25 @@ struct BlockOf {
 // border times a bf16 scale fits fp32), ties go to the even code.  Bit by bit from the highest: the
 // borders below codes 4, 2 and 6 belong to the upper code, the others to the lower.
 struct Borders {
-    float b[8];   // b[c]: below code c
+    float b1, b2, b3, b4, b5, b6, b7;   // below each code
     __device__ __forceinline__ explicit Borders(float s)
     {
         const float t = s == 0.0f ? __builtin_inff() : s;   // (NaN: no comparison holds)
-        b[1] = t * 0.25f;
-        b[2] = t * 0.75f;
-        b[3] = t * 1.25f;
-        b[4] = t * 1.75f;
-        b[5] = t * 2.5f;
-        b[6] = t * 3.5f;
-        b[7] = t * 5.0f;
+        b1 = t * 0.25f;
+        b2 = t * 0.75f;
+        b3 = t * 1.25f;
+        b4 = t * 1.75f;
+        b5 = t * 2.5f;
+        b6 = t * 3.5f;
+        b7 = t * 5.0f;
     }
     __device__ __forceinline__ uint32_t code(float w) const
     {
         const float m = __builtin_fabsf(w);
-        const bool c2 = m >= b[4], c1 = m >= (c2 ? b[6] : b[2]);
-        const bool c0 = m > (c2 ? (c1 ? b[7] : b[5]) : (c1 ? b[3] : b[1]));
+        const bool c2 = m >= b4;
+        const float second = c2 ? b6 : b2, low = c2 ? b5 : b1, high = c2 ? b7 : b3;
+        const bool c1 = m >= second;
+        const bool c0 = m > (c1 ? high : low);
         const uint32_t c = (c2 ? 4u : 0u) | (c1 ? 2u : 0u) | (c0 ? 1u : 0u);
         return c && w < 0.0f ? c | 8u : c;
     }
