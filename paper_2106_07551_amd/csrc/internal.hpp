@@ -474,6 +474,7 @@ struct LogpArgs {
     int A, top, action_bytes;
     float temperature;
     // set by the launchers
+    float inv_t;
     int splits, part_len;
     bool bf16;
     void* part_stats;
@@ -481,7 +482,7 @@ struct LogpArgs {
 };
 enum { kLogpLane, kLogpShort, kLogpWave, kLogpGroup };
 struct LogpPlan {
-    int variant, group, splits, part_len;   // group: threads per row (kLogpShort)
+    int variant, group, chunks, splits, part_len;   // kLogpShort: threads per row, chunks each
     int64_t blocks, stats_bytes, work_bytes;
 };
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size);

@@ -3,7 +3,7 @@
 //
 // With x a row's legal logits, c = log2(e) / T and m = max x: s = sum_j 2^((x_j - m) c),
 // t = sum_j 2^((x_j - m) c) (x_j - m) c, and
-//   l = (x_a - m) / T - ln s,  H = ln s - ln2 t / s,
+//   l = (x_a - m) / T - ln s (as a product with 1 / T),  H = ln s - ln2 t / s,
 //   dx_j = 2^((x_j - m) c) (c0 + c1 (x_j - m) c) + dl [j = a] / T.
 // Lists: rows of up to kShortMost entries stay in the registers of a few lanes, which
 // find one place after the other, or, for longer lists, in LDS, where a wavefront finds the value
@@ -41,19 +41,47 @@ __device__ __forceinline__ uint64_t entry_key(float x, int64_t index)
 __device__ __forceinline__ int key_index(uint64_t k) { return (int)~(uint32_t)k; }
 __device__ __forceinline__ float key_value(uint64_t k) { return value_of((uint32_t)(k >> 32)); }
 
+// How many of the n keys in LDS are larger; zeros behind them up to a multiple of kPad (which
+// are not larger than any).
+constexpr int kPad = 8;
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ int place_of(const uint64_t* keys, int n, uint64_t key)
+{
+    int place = 0;
+    for (int q = 0; q < n; q += kPad) {
+        u64x2 k[kPad / 2];
+#pragma unroll
+        for (int i = 0; i < kPad / 2; ++i)
+            k[i] = *(const u64x2*)(keys + q + 2 * i);
+#pragma unroll
+        for (int i = 0; i < kPad / 2; ++i)
+            place += (k[i][0] > key) + (k[i][1] > key);
+    }
+    return place;
+}
+
 // ------------------------------------------------------------------ a row's scalars
 
-// The action of a row, -1 where it is not a legal entry
-__device__ __forceinline__ int row_action(const LogpArgs& a, int64_t row)
+// The action of a row as it is, -1 without one
+__device__ __forceinline__ int64_t given_action(const LogpArgs& a, int64_t row)
 {
     if (!a.actions)
         return -1;
-    const int64_t v = a.action_bytes == 1   ? (int64_t)((const uint8_t*)a.actions)[row]
-                      : a.action_bytes == 4 ? (int64_t)((const int32_t*)a.actions)[row]
-                                            : ((const int64_t*)a.actions)[row];
+    return a.action_bytes == 1   ? (int64_t)((const uint8_t*)a.actions)[row]
+           : a.action_bytes == 4 ? (int64_t)((const int32_t*)a.actions)[row]
+                                 : ((const int64_t*)a.actions)[row];
+}
+// -1 where it is not a legal entry
+__device__ __forceinline__ int legal_action(const LogpArgs& a, int64_t row, int64_t v)
+{
     if (v < 0 || v >= a.A || (a.mask && a.mask[row * a.mask_ld + v] == 0))
         return -1;
     return (int)v;
+}
+__device__ __forceinline__ int row_action(const LogpArgs& a, int64_t row)
+{
+    return legal_action(a, row, given_action(a, row));
 }
 
 struct RowOut {
@@ -69,7 +97,7 @@ __device__ __forceinline__ RowOut row_finish(const LogpArgs& a, const Stats& st,
         o.ln_s = logf(st.s);
         o.H = o.ln_s - kLn2 * st.t / st.s;
         if (action >= 0)
-            o.l = (x_a - m) / a.temperature - o.ln_s;
+            o.l = (x_a - m) * a.inv_t - o.ln_s;
     }
     return o;
 }
@@ -84,7 +112,7 @@ __device__ __forceinline__ void store_row(const LogpArgs& a, int64_t row, const 
 
 __device__ __forceinline__ float entry_logp(const LogpArgs& a, const RowOut& o, float x)
 {
-    return (x - (o.m == kNegInf ? 0.0f : o.m)) / a.temperature - o.ln_s;
+    return (x - (o.m == kNegInf ? 0.0f : o.m)) * a.inv_t - o.ln_s;
 }
 
 // ------------------------------------------------ few actions: a lane per row
@@ -108,11 +136,13 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
         const int n = left < kLaneRows ? (left > 0 ? (int)left : 0) : kLaneRows;
         const uint8_t* mask = a.mask ? a.mask + r0 * a.mask_ld : nullptr;
         const int64_t row = r0 + lane;
-        const int action = lane < n ? row_action(a, row) : -1;
+        const int64_t given = lane < n ? given_action(a, row) : -1;
         wave_lds_sync();
         rows_to_lds<false, false>((const E*)a.logits + r0 * a.logits_ld, a.logits_ld,
                                   (const E*)nullptr, 0, mask, a.mask_ld, n, A, bx, bx, lane);
         wave_lds_sync();
+        // (asked for behind the rows, in the caches by now)
+        const int action = lane < n ? legal_action(a, row, given) : -1;
         float x[NA];
         RowOut o{};
         if (lane < n) {
@@ -365,12 +395,18 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
 
 // --------------------------------------------- short rows: 4 to 64 lanes per row
 
-// Rows of up to kShortMost entries, C chunks a lane.
-constexpr int kShortMost = 1024, kShortThreads = 256, kShortC = 4;
+// Rows of up to kShortMost entries, C chunks a lane: 4, or 1 where there are few rows, whose lanes
+// then have less to do one after the other.
+constexpr int kShortMost = 1024, kShortThreads = 256;
 
 // Rounds of a group of T lanes cost their wavefront about 85 instructions for 64 / T rows, a
 // list by the whole wavefront 200 to 300 and what its places take, for one row.
-constexpr int rounds_most(int T) { return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : T == 32 ? 6 : 3; }
+constexpr int rounds_most(int T, int C)
+{
+    if (C == 1)
+        return T <= 8 ? 40 : T == 16 ? 20 : T == 32 ? 10 : 6;
+    return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : T == 32 ? 6 : 3;
+}
 
 struct MaxU32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const
@@ -406,15 +442,15 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 }
 
 // A list place after place by the row's T lanes.  bf16: order and index fit one number.
-template <typename E, int T>
-__device__ __forceinline__ void list_by_rounds(const LogpArgs& a, u32x4 (&x)[kShortC], int lane,
+template <typename E, int T, int C>
+__device__ __forceinline__ void list_by_rounds(const LogpArgs& a, u32x4 (&x)[C], int lane,
                                                int64_t row, bool live, const RowOut& o)
 {
-    constexpr int CH = kChunk<E>, N = kShortC * CH;
+    constexpr int CH = kChunk<E>, N = C * CH;
     constexpr bool kOne = sizeof(E) == 2;
     uint32_t k[N];
 #pragma unroll
-    for (int i = 0; i < kShortC; ++i) {
+    for (int i = 0; i < C; ++i) {
         float v[CH];
         unpack<E>(x[i], v);
 #pragma unroll
@@ -465,17 +501,17 @@ __device__ __forceinline__ void list_by_rounds(const LogpArgs& a, u32x4 (&x)[kSh
 }
 
 // A list by a wavefront: the row's entries in LDS, lane l takes every 64th.  keys: LDS for
-// as many keys.
-template <typename E, int T>
+// as many keys and kPad more.
+template <typename E, int T, int C>
 __device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, uint64_t* keys,
                                              int lane, int64_t row, const RowOut& o)
 {
-    constexpr int N = T * kShortC * kChunk<E> / 64;
+    constexpr int COUNT = T * C * kChunk<E>, N = (COUNT + 63) / 64;
     uint32_t k[N];
     int listed = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        k[i] = order_of(to_f32(from[lane + 64 * i]));
+        k[i] = COUNT >= 64 || lane < COUNT ? order_of(to_f32(from[lane + 64 * i])) : 0u;
         k[i] = k[i] <= kUnlisted ? 0u : k[i];
         listed += __popcll(__ballot(k[i] != 0));
     }
@@ -541,14 +577,13 @@ __device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, u
         n += __popcll(who);
         tied += __popcll(same);
     }
+    if (lane < kPad)
+        keys[n + lane] = 0;
     wave_lds_sync();
     const int64_t to = row * most;
     for (int i = lane; i < n; i += 64) {
         const uint64_t key = keys[i];
-        int place = 0;
-#pragma unroll 4
-        for (int q = 0; q < n; ++q)
-            place += keys[q] > key;
+        const int place = place_of(keys, n, key);
         if (place < most) {
             a.top_idx[to + place] = key_index(key);
             a.top_logp[to + place] = entry_logp(a, o, key_value(key));
@@ -561,10 +596,10 @@ __device__ __forceinline__ void list_by_wave(const LogpArgs& a, const E* from, u
     wave_lds_sync();
 }
 
-template <typename E, int T>
+template <typename E, int T, int C>
 __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
 {
-    constexpr int ROWS = kShortThreads / T, C = kShortC, CH = kChunk<E>;
+    constexpr int ROWS = kShortThreads / T, CH = kChunk<E>;
     extern __shared__ u32x4 staged[];   // lists by wavefronts: rows, then keys
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
     const int wave = threadIdx.x >> 6, wl = threadIdx.x & 63;
@@ -575,11 +610,12 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
         const bool live = row < a.rows;
         const E* px = (const E*)a.logits + row * a.logits_ld;
         const uint8_t* pm = a.mask ? a.mask + row * a.mask_ld : nullptr;
-        // (the action's logit is asked for with the row's)
-        const int action = live ? row_action(a, row) : -1;
-        const float x_a = action >= 0 ? to_f32(px[action]) : 0.0f;
+        const int64_t given = live ? given_action(a, row) : -1;
         u32x4 x[C];
         load_row<E, kPolicy, T, C>(a.A, live, px, (const E*)nullptr, pm, lane, x, nullptr);
+        keep_raw<kPolicy>(x, nullptr);   // (asked for behind the row, in the caches by now)
+        const int action = live ? legal_action(a, row, given) : -1;
+        const float x_a = action >= 0 ? to_f32(px[action]) : 0.0f;
         const int used = (a.A + T * CH - 1) / (T * CH);
         bool unused = true;
         const Stats st = group_merge<T, kPolicy>(chunk_stats<E, kPolicy, C>(x, nullptr, used, c),
@@ -589,12 +625,12 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
             store_row(a, row, o);
         if (a.top == 0)
             continue;
-        if (a.top <= rounds_most(T)) {
-            list_by_rounds<E, T>(a, x, lane, row, live, o);
+        if (a.top <= rounds_most(T, C)) {
+            list_by_rounds<E, T, C>(a, x, lane, row, live, o);
             continue;
         }
         u32x4* mine = staged + wave * 64 * C;
-        uint64_t* keys = (uint64_t*)(staged + kShortThreads * C) + wave * (T * C * CH);
+        uint64_t* keys = (uint64_t*)(staged + kShortThreads * C) + wave * (T * C * CH + kPad);
 #pragma unroll
         for (int i = 0; i < C; ++i)
             mine[wl / T * T * C + lane + i * T] = x[i];
@@ -606,7 +642,7 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
             RowOut of = o;
             of.m = __shfl(o.m, r * T);
             of.ln_s = __shfl(o.ln_s, r * T);
-            list_by_wave<E, T>(a, (const E*)(mine + r * T * C), keys, wl, at, of);
+            list_by_wave<E, T, C>(a, (const E*)(mine + r * T * C), keys, wl, at, of);
         }
     }
 }
@@ -633,7 +669,7 @@ struct StreamSize {
 template <int T>
 struct Candidates {
     u32x4 raw[StreamSize<T>::kChunks];
-    uint64_t keys[StreamSize<T>::kKeys];
+    uint64_t keys[StreamSize<T>::kKeys + kPad];
     int at[StreamSize<T>::kChunks];   // first index of each chunk
     float scratch[T > 64 ? 2 * kScratch : 1];
     int n_raw, n_keys;
@@ -751,6 +787,9 @@ __device__ __forceinline__ void tighten(Candidates<T>& l, int lane, int k)
     if (lane == 0)
         l.n_raw = 0;
     group_sync<T>();
+    if (lane < kPad)   // (for place_of; before the next candidates, or the last barrier)
+        l.keys[l.n_keys + lane] = 0;
+    group_sync<T>();
 }
 
 // The exact list of a row's part, tile by tile, into l.keys in order; returns its length.
@@ -808,8 +847,10 @@ __device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* p
     return n;
 }
 
-template <typename E, int T, bool PART>
-__global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
+// LIST: top > 0.  (Without lists the sums alone need no more than four wavefronts a SIMD, and
+// registers for the next tile's loads: 4096 x 65536 bf16 108 us, with six 122.)
+template <typename E, int T, bool PART, bool LIST>
+__global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs a)
 {
     using S = StreamSize<T>;
     constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH, W = T / 64;
@@ -818,7 +859,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
     const int lane = threadIdx.x % T, slot = threadIdx.x / T;
     Candidates<T>& l = ((Candidates<T>*)lists)[slot];
     const float c = kLog2e / a.temperature;
-    const int k = a.top;
+    const int k = LIST ? a.top : 0;
     const int64_t items = PART ? a.rows * a.splits : a.rows;
     for (int64_t item = (int64_t)blockIdx.x * S::kRows + slot; item < items;
          item += (int64_t)gridDim.x * S::kRows) {   // (a wavefront's, or a workgroup's, alone)
@@ -880,10 +921,18 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
                 __builtin_amdgcn_sched_barrier(0);
             }
             st = tile == 0 ? own : merge<kPolicy>(st, own, c);
-            if (k == 0)
+            if constexpr (!LIST)
                 continue;
             if (tile == 0) {
                 const int j = (k + W - 1) / W;
+                // (entries instead of chunks where the list is long for so few)
+                auto entries = [&](uint32_t p) {
+                    const float v = prefix_value(p);
+                    int n = 0;
+                    for_entries<E, T, U>(x, here, lane,
+                                         [&](float f, int) { n += __popcll(__ballot(f >= v)); });
+                    return n;
+                };
                 auto count = [&](uint32_t p) {
                     const float v = prefix_value(p);
                     int n = 0;
@@ -892,10 +941,13 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
                         n += __popcll(__ballot(top[u] >= v));
                     return n;
                 };
-                bound = prefix_value(
-                    count(kLeastPrefix) < j
-                        ? kLeastPrefix
-                        : halved_bound(j, count));
+                const int chunks = count(kLeastPrefix);
+                uint32_t p = kLeastPrefix;
+                if (chunks >= 3 * j)
+                    p = halved_bound(j, count);
+                else if (entries(kLeastPrefix) >= j)
+                    p = halved_bound(j, entries);
+                bound = prefix_value(p);
                 if constexpr (W > 1) {
                     if ((lane & 63) == 0)
                         scratch[lane >> 6] = bound;
@@ -947,7 +999,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
             if (lane == 0)
                 store_row(a, row, o);
         }
-        if (k == 0)
+        if constexpr (!LIST)
             continue;
         int n = l.n_keys;
         bool sorted = false;
@@ -958,12 +1010,7 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
         const int64_t to = item * k;
         for (int i = lane; i < n; i += T) {
             const uint64_t key = l.keys[i];
-            int place = sorted ? i : 0;
-            if (!sorted) {
-#pragma unroll 8
-                for (int q = 0; q < n; ++q)
-                    place += l.keys[q] > key;
-            }
+            const int place = sorted ? i : place_of(l.keys, n, key);
             if (place < k) {
                 if constexpr (PART) {
                     a.part_keys[to + place] = key;
@@ -991,14 +1038,14 @@ __global__ __launch_bounds__(256, 6) void logp_stream_kernel(LogpArgs a)
 // zeros behind its entries).  At least `top` entries are not below the j-th of every list,
 // j = ceil(top / lists), nor below the last place of any one list; with more lists than
 // places, nor below the top-th largest of their first entries.
-constexpr int kMergeThreads = 256, kMergeCap = 1024;
+constexpr int kMergeThreads = 256, kMergeCap = 1024, kMergeAll = 512;
 constexpr int kMergeLists = 2;   // of a thread, at most
 
 __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
 {
     constexpr int T = kMergeThreads;
     __shared__ float scratch[2 * kScratch];
-    __shared__ uint64_t keys[kMergeCap];
+    __shared__ __align__(16) uint64_t keys[kMergeCap + kPad];
     __shared__ uint64_t wave_key[T / 64];
     __shared__ int total;
     const int tid = threadIdx.x, top = a.top;
@@ -1019,17 +1066,30 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
         return v;
     };
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const int action = row_action(a, row);
-        const float x_a =
-            action < 0 ? 0.0f
-            : a.bf16   ? to_f32(((const bf16_t*)a.logits)[row * a.logits_ld + action])
-                       : ((const float*)a.logits)[row * a.logits_ld + action];
+        // (everything that is known to be needed is asked for at once)
+        const int64_t given = given_action(a, row);
+        const uint64_t* lists = a.part_keys + row * a.splits * top;
+        const bool all = a.splits * top <= kMergeAll;
+        uint64_t own[kMergeAll / T];
+#pragma unroll
+        for (int i = 0; i < kMergeAll / T; ++i)
+            own[i] = all && tid + i * T < a.splits * top ? lists[tid + i * T] : 0;
         Stats st = empty_stats();
         const Stats* parts = (const Stats*)a.part_stats + row * a.splits;
         for (int i = tid; i < a.splits; i += T)
             st = merge<kPolicy>(st, parts[i], c);
+        const int action = legal_action(a, row, given);
+        const float x_a =
+            action < 0 ? 0.0f
+            : a.bf16   ? to_f32(((const bf16_t*)a.logits)[row * a.logits_ld + action])
+                       : ((const float*)a.logits)[row * a.logits_ld + action];
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < kMergeAll / T; ++i)
+                keys[tid + i * T] = own[i];   // (zeros behind the last one)
+        }
         bool unused = true;
-        st = group_merge<T, kPolicy>(st, c, scratch, nullptr, unused);
+        st = group_merge<T, kPolicy>(st, c, scratch, nullptr, unused);   // (with barriers)
         const RowOut o = row_finish(a, st, action, x_a);
         if (tid == 0)
             store_row(a, row, o);
@@ -1037,12 +1097,27 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
             __syncthreads();
             continue;
         }
-        const uint64_t* lists = a.part_keys + row * a.splits * top;
         const int64_t to = row * top;
         auto write = [&](int place, uint64_t key) {
             a.top_idx[to + place] = key ? key_index(key) : -1;
             a.top_logp[to + place] = key ? entry_logp(a, o, key_value(key)) : 0.0f;
         };
+        if (all) {   // (zeros are no entries)
+            const int n = a.splits * top;
+#pragma unroll
+            for (int i = 0; i < kMergeAll / T; ++i) {
+                if (tid + i * T >= n)
+                    continue;
+                const int place = place_of(keys, n, own[i]);
+                if (own[i] != 0 && place < top)
+                    write(place, own[i]);
+            }
+            const int entries = place_of(keys, n, 0);
+            for (int i = entries + tid; i < top; i += T)
+                write(i, 0);
+            __syncthreads();
+            continue;
+        }
         // the bound: the largest last place, the least j-th (as the largest of ~key)
         uint64_t last = 0, jth = 0;
         const int j = (top + a.splits - 1) / a.splits;
@@ -1056,16 +1131,13 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
         jth = ~block_max(jth);
         uint64_t bound = last > jth ? last : jth;
         if (a.splits > top && a.splits <= kMergeCap) {   // (j = 1)
-            for (int i = tid; i < a.splits; i += T)
-                keys[i] = lists[(int64_t)i * top];
+            for (int i = tid; i < a.splits + kPad; i += T)
+                keys[i] = i < a.splits ? lists[(int64_t)i * top] : 0;
             __syncthreads();
             uint64_t best = 0;
             for (int i = tid; i < a.splits; i += T) {
                 const uint64_t key = keys[i];
-                int place = 0;
-                for (int q = 0; q < a.splits; ++q)
-                    place += keys[q] > key;
-                if (place == top - 1)
+                if (place_of(keys, a.splits, key) == top - 1)
                     best = key;
             }
             best = block_max(best);
@@ -1096,11 +1168,12 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
         __syncthreads();
         const int n = total;
         if (n <= kMergeCap) {
+            if (tid < kPad)
+                keys[n + tid] = 0;
+            __syncthreads();
             for (int i = tid; i < n; i += T) {
                 const uint64_t key = keys[i];
-                int place = 0;
-                for (int q = 0; q < n; ++q)
-                    place += keys[q] > key;
+                const int place = place_of(keys, n, key);
                 if (place < top)
                     write(place, key);
             }
@@ -1253,11 +1326,29 @@ __global__ __launch_bounds__(kGradThreads) void logp_grad_kernel(LogpArgs a)
 
 // ---------------------------------------------------------------------- launches
 
+template <typename E, int C>
+void launch_short(const LogpArgs& a, int T, unsigned nb, size_t lds, hipStream_t s)
+{
+    if (T == 4)
+        logp_short_kernel<E, 4, C><<<nb, kShortThreads, lds, s>>>(a);
+    else if (T == 8)
+        logp_short_kernel<E, 8, C><<<nb, kShortThreads, lds, s>>>(a);
+    else if (T == 16)
+        logp_short_kernel<E, 16, C><<<nb, kShortThreads, lds, s>>>(a);
+    else if (T == 32)
+        logp_short_kernel<E, 32, C><<<nb, kShortThreads, lds, s>>>(a);
+    else if constexpr (sizeof(E) == 4 || C == 1)   // (4 chunks: bf16 rows fit 32 lanes)
+        logp_short_kernel<E, 64, C><<<nb, kShortThreads, lds, s>>>(a);
+}
+
 template <typename E, int T, bool PART>
 void launch_stream(const LogpArgs& a, unsigned nb, hipStream_t s)
 {
-    const size_t lds = a.top > 0 ? sizeof(Candidates<T>) * StreamSize<T>::kRows : 0;
-    logp_stream_kernel<E, T, PART><<<nb, 256, lds, s>>>(a);
+    if (a.top == 0)
+        logp_stream_kernel<E, T, PART, false><<<nb, 256, 0, s>>>(a);
+    else
+        logp_stream_kernel<E, T, PART, true>
+            <<<nb, 256, sizeof(Candidates<T>) * StreamSize<T>::kRows, s>>>(a);
 }
 
 template <typename E>
@@ -1276,20 +1367,15 @@ hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
         else
             logp_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
     } else if (p.variant == kLogpShort) {
-        const size_t lds = a.top > rounds_most(p.group)
-                               ? (size_t)kShortThreads * kShortC * 16 +
-                                     (size_t)kShortThreads / 64 * p.group * kShortC * kChunk<E> * 8
+        const size_t lds = a.top > rounds_most(p.group, p.chunks)
+                               ? (size_t)kShortThreads * p.chunks * 16 +
+                                     (size_t)kShortThreads / 64 *
+                                         (p.group * p.chunks * kChunk<E> + kPad) * 8
                                : 0;
-        if (p.group == 4)
-            logp_short_kernel<E, 4><<<nb, kShortThreads, lds, s>>>(a);
-        else if (p.group == 8)
-            logp_short_kernel<E, 8><<<nb, kShortThreads, lds, s>>>(a);
-        else if (p.group == 16)
-            logp_short_kernel<E, 16><<<nb, kShortThreads, lds, s>>>(a);
-        else if (p.group == 32)
-            logp_short_kernel<E, 32><<<nb, kShortThreads, lds, s>>>(a);
-        else if constexpr (sizeof(E) == 4)   // (bf16 rows of kShortMost fit 32 lanes)
-            logp_short_kernel<E, 64><<<nb, kShortThreads, lds, s>>>(a);
+        if (p.chunks == 1)
+            launch_short<E, 1>(a, p.group, nb, lds, s);
+        else
+            launch_short<E, 4>(a, p.group, nb, lds, s);
     } else if (p.variant == kLogpWave) {
         launch_stream<E, 64, false>(a, nb, s);
     } else if (p.splits == 1) {
@@ -1366,7 +1452,12 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 
 // Up to 31 entries a lane per row, up to kShortMost a few lanes, above a wavefront where there are
 // rows enough and short lists, else a workgroup, or several where there are fewer rows
-// than fill the CUs: of at least a tile (16 KB) each.
+// than fill the CUs: of at least a tile (16 KB) each.  Few rows: a chunk per lane, while that takes
+// no more threads than fill the CUs a few times (us, lists of 6 places, against a lane per row: fp32
+// 4096 x 18 5.4 and 10.0, 65536 x 18 10.4 and 10.8, 131072 x 18 16.6 and 12.9; against four chunks per
+// lane: 4096 x 60 5.3 and 7.0, 65536 x 60 15.7 and 12.6, 4096 x 250 7.7 and 7.7, 16384 x 250 18.7 and
+// 13.0; bf16 131072 x 18 12.4 and 12.5, 4096 x 250 6.3 and 8.2, 16384 x 250 11.9 and 9.9).
+constexpr int64_t kFewLane = 1 << 19, kFewShort = 1 << 18;
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 {
     constexpr int64_t kCus = 256;
@@ -1374,13 +1465,18 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
     const int64_t ch = 16 / size, chunks = (A + ch - 1) / ch;
     p.splits = 1;
     int64_t per = 1;   // rows per workgroup
-    if (A <= kLaneMost) {
+    int64_t lanes = 4;   // of a row, a chunk each
+    while (lanes < chunks && lanes < 128)
+        lanes *= 2;
+    const bool few = lanes <= 64 && rows * lanes <= (A <= kLaneMost ? kFewLane : kFewShort);
+    if (A <= kLaneMost && !few) {
         p.variant = kLogpLane;
         per = kLaneThreads;
     } else if (A <= kShortMost) {
         p.variant = kLogpShort;
+        p.chunks = few ? 1 : 4;
         p.group = 4;
-        while (p.group * kShortC * ch < A)
+        while (p.group * p.chunks * ch < A)
             p.group *= 2;
         per = kShortThreads / p.group;
     } else if (top <= kWaveTop && rows >= 8 * kCus && chunks <= 1024) {
@@ -1406,6 +1502,7 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hipStream_t s)
 {
     a.bf16 = dtype == MALIB_DT_BF16;
+    a.inv_t = 1.0f / a.temperature;
     a.splits = p.splits;
     a.part_len = p.part_len;
     a.part_stats = work;
