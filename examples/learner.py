@@ -4,10 +4,11 @@ A team game's population fills its payoff table and the meta-solver mixes its
 policies.  A learner then trains a best response to the mixture from
 trajectory records (linear layers, clipped policy loss with a divergence from
 the policy it started as) and distils the mixture's own policies into one
-student from their top logits.  Both join the population, and the new cells of
+student from their top logits, with dropout if asked for, and from teachers held
+in 4 bits if asked for.  Both join the population, and the new cells of
 the table are simulated.
 
-    python examples/learner.py [--envs N] [--steps K] [--policies P]
+    python examples/learner.py [--envs N] [--steps K] [--policies P] [--dropout p] [--teacher-bits 4]
 """
 from __future__ import annotations
 
@@ -40,13 +41,18 @@ class Net:
     def refresh(self):
         self.half = [w.bfloat16() for w in self.w]
 
-    def forward(self, obs):
+    def forward(self, obs, drop=None):
+        """The logits; drop: (p, seed, step) of dropout behind the hidden layers."""
         self.x = [obs]
         self.pre = []
+        self.drop = drop
         for l in range(2):
             pre = torch.empty((obs.shape[0], self.w[l].shape[0]), dtype=torch.bfloat16,
                               device="cuda")
-            self.x.append(M.linear(self.x[l], self.half[l], self.b[l], act=M.ACT_RELU, pre=pre))
+            y = M.linear(self.x[l], self.half[l], self.b[l], act=M.ACT_RELU, pre=pre)
+            if drop:
+                M.dropout(y, *drop, layer=l, out=y)
+            self.x.append(y)
             self.pre.append(pre)
         self.x[2] = self.x[2].float()
         return M.linear(self.x[2], self.half[2].float(), self.b[2])
@@ -57,6 +63,8 @@ class Net:
         grads = [(dw, db)]
         dy = dy.bfloat16()
         for l in (1, 0):
+            if self.drop:
+                M.dropout_backward(dy, *self.drop, layer=l, dx=dy)
             dy, dw, db = M.linear_backward(dy, self.x[l], self.half[l], act=M.ACT_RELU,
                                            pre=self.pre[l], want=(l > 0, True, True))
             grads.append((dw.float(), db))
@@ -66,19 +74,44 @@ class Net:
         self.refresh()
 
 
-def mixture_lists(nets_w, nets_b, obs, policy_of_row, top):
-    """The top logits of each row's policy: every policy's logits on all rows
-    (one grouped call per layer), then each row's own."""
-    h = obs
-    for l in range(2):
-        h = M.linear(h, nets_w[l].bfloat16(), nets_b[l], act=M.ACT_RELU)
-    logits = M.linear(h.float(), nets_w[2].bfloat16().float(), nets_b[2])
-    own = logits[policy_of_row, torch.arange(obs.shape[0], device="cuda")]
-    val, idx = torch.topk(own, top, dim=1)
-    return idx.int(), val
+class Teachers:
+    """The mixture's policies, frozen: weights [policy][out][in] in bf16 or in 4 bits, all
+    policies' logits in one grouped call per layer."""
+
+    FEW = 256    # rows that the layers in 4 bits take as they are
+
+    def __init__(self, weights, biases, bits=16):
+        self.b = biases
+        self.shapes = [w.shape[1:] for w in weights]
+        self.w = [M.quantize_fp4(w) if bits == 4 else w.bfloat16() for w in weights]
+        self.bits = bits
+
+    def layer(self, l, x, act):
+        if self.bits == 16:
+            return M.linear(x, self.w[l].to(x.dtype), self.b[l], act=act)
+        if x.shape[-2] <= self.FEW:
+            return M.linear_fp4(x, *self.w[l], self.shapes[l][0], self.b[l], act=act)
+        return M.linear(x, M.dequantize_fp4(*self.w[l], *self.shapes[l], dtype=x.dtype),
+                        self.b[l], act=act)
+
+    def logits(self, obs):
+        h = obs
+        for l in range(2):
+            h = self.layer(l, h, M.ACT_RELU)
+        return self.layer(2, h.float(), M.ACT_NONE)
 
 
-def run(n_envs=512, horizon=8, policies=6, steps=20, top=6, rate=3.0, say=print):
+def mixture_lists(teachers, obs, policy_of_row, top):
+    """The top entries of each row's policy: every policy's logits on all rows, then
+    each row's own (log probabilities are logits less a number of the row's, which
+    distillation does not see)."""
+    own = teachers.logits(obs)[policy_of_row, torch.arange(obs.shape[0], device="cuda")]
+    _, idx, val = M.log_probs(own, top=top)
+    return idx, val
+
+
+def run(n_envs=512, horizon=8, policies=6, steps=20, top=6, rate=3.0, dropout=0.0, teacher_bits=16,
+        say=print):
     wl = W.team_variant(4, d=256, P=policies, n_envs=n_envs, horizon=horizon)
     env = IO.make_env(wl)
     ws = [torch.from_numpy(w).cuda() for w in wl.weights]
@@ -118,9 +151,8 @@ def run(n_envs=512, horizon=8, policies=6, steps=20, top=6, rate=3.0, say=print)
         old = None
         for _ in range(2):
             logits = net.forward(traj.obs)
-            if old is None:   # log probabilities under the policy that acted (the loss
-                # itself is not used yet, so any old values do)
-                old = M.policy_loss(logits, actions, adv, adv, grad=False)[1][1]
+            if old is None:   # log probabilities under the policy that acted
+                old = M.log_probs(logits, actions)[0][0]
             total, stats, dlogits = M.policy_loss(logits, actions, old, adv, kl_coef=0.02,
                                                   entropy_coef=0.002, ref_logits=ref_logits)
             net.backward(dlogits, rate)
@@ -132,11 +164,12 @@ def run(n_envs=512, horizon=8, policies=6, steps=20, top=6, rate=3.0, say=print)
     obs = traj.obs
     teacher = M.meta_sample_device(sigma, policies, obs.shape[0], 2, wl.seed + 99,
                                    seat_row=[0, 0])[:, 0].long()
-    idx, val = mixture_lists(ws, bs, obs, teacher, top)
+    idx, val = mixture_lists(Teachers(ws, bs, teacher_bits), obs, teacher, top)
     student = Net([w.mean(0) for w in ws], [b.mean(0) for b in bs])
     losses = []
-    for _ in range(steps):
-        total, _, dlogits = M.distill_loss(student.forward(obs), idx, val, temperature=2.0)
+    for step in range(steps):
+        drop = (dropout, wl.seed, step) if dropout else None
+        total, _, dlogits = M.distill_loss(student.forward(obs, drop), idx, val, temperature=2.0)
         student.backward(dlogits, rate)
         losses.append(float(total))
     say(f"student: distillation loss {losses[0]:.4f} -> {losses[-1]:.4f}")
@@ -162,5 +195,8 @@ if __name__ == "__main__":
     ap.add_argument("--envs", type=int, default=2048)
     ap.add_argument("--steps", type=int, default=30)
     ap.add_argument("--policies", type=int, default=6)
+    ap.add_argument("--dropout", type=float, default=0.0)
+    ap.add_argument("--teacher-bits", type=int, choices=(4, 16), default=16)
     a = ap.parse_args()
-    run(n_envs=a.envs, steps=a.steps, policies=a.policies)
+    run(n_envs=a.envs, steps=a.steps, policies=a.policies, dropout=a.dropout,
+        teacher_bits=a.teacher_bits)

@@ -709,7 +709,7 @@ typedef struct {
     int64_t rows, n_actions;
     int64_t logits_stride, dlogits_stride, mask_stride;
     int32_t top;
-    float temperature;       /* > 0, finite */
+    float temperature;       /* in [2^-100, 2^100] */
 } malib_log_probs_desc;
 
 malib_status malib_log_probs(const malib_log_probs_desc* desc, const void* logits,

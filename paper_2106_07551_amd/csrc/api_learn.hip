@@ -472,8 +472,8 @@ static malib_status check_log_probs(const malib_log_probs_desc* d)
     if (!d)
         return set_error(MALIB_E_INVAL, "desc is NULL");
     TRY(check_loss(d->dtype, d->rows, d->n_actions));
-    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature))
-        return set_error(MALIB_E_INVAL, "temperature must be positive and finite");
+    if (!(d->temperature >= 0x1p-100f && d->temperature <= 0x1p100f))   // (1 / T is taken)
+        return set_error(MALIB_E_INVAL, "temperature must be in [2^-100, 2^100]");
     return MALIB_OK;
 }
 

@@ -38,7 +38,9 @@ def view(t, pad, shift=0):
 def close(got, ref, bound, what, eps=U):
     got = got.double()
     assert got.shape == ref.shape, what
-    same = (got == ref) | (torch.isnan(got) & torch.isnan(ref))
+    # (a finite l below -2^128, of an entry at the type's lowest value over T < 1, is -inf in fp32)
+    same = (got == ref) | (torch.isnan(got) & torch.isnan(ref)) | \
+        (torch.isinf(got) & (got == ref.float()))
     tol = bound + 1.01 * eps * ref.abs() + 1e-36
     ok = same | ((got - ref).abs() <= tol)
     assert ok.all(), (what, float(torch.nan_to_num(((got - ref).abs() / tol)[~ok]).max()))
@@ -164,6 +166,25 @@ def test_lists_of_every_kind(dtype, a, n):
     for top in (1, 6, 40, 256) if a < 4000 else (5, 64, 256):
         check(x, act, top=top, what="kinds")
     check(x, act, what="no lists")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("a, n", [(1, 140000), (5, 140000), (18, 140000), (24, 70001), (31, 70001),
+                                  (33, 33000), (100, 20000), (250, 9000), (500, 5000),
+                                  (777, 4500), (1024, 4500), (1025, 2049), (2048, 2050),
+                                  (3001, 2049), (8192, 2048)])
+def test_many_rows_of_every_kind(dtype, a, n):
+    """As above where there are rows for the whole card: 60 rows, each many times."""
+    g = torch.Generator(device="cuda").manual_seed(a + n)
+    lane = next((t for t in (4, 8, 16, 32) if t * 32 >= a), 64)
+    some = torch.stack([row_of(KINDS[r % 12], a, lane, dtype, g) for r in range(60)])
+    x = some[torch.randint(0, 60, (n,), generator=g, device="cuda")]
+    act = torch.randint(-1, a + 1, (n,), generator=g, device="cuda", dtype=torch.int64)
+    mask = torch.rand((n, a), generator=g, device="cuda") < 0.9
+    for top in (1, 5, 64) if a < 9 else (0, 1, 6, 33, 64, 100):
+        check(x, act, top=top, what="many")
+    check(x, act, top=6, mask=mask, T=0.7, what="many, mask")
+    check(view(x, 3, 1), act, top=6, mask=view(mask, 1), what="many, apart")
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
