@@ -47,9 +47,17 @@ struct BlockOf {
     int64_t g, tile, kb;
     __device__ __forceinline__ BlockOf(const Fp4Args& a, int64_t i)
     {
-        kb = i % a.blocks_k;
-        tile = i / a.blocks_k % a.tiles;
-        g = i / a.blocks_k / a.tiles;
+        int64_t q = i;
+        if (i >> 31 == 0) {   // (uniform; 64-bit divisions take far longer)
+            q = (uint32_t)i / (uint32_t)a.blocks_k;
+            kb = i - q * a.blocks_k;
+            g = (uint32_t)q / (uint32_t)a.tiles;
+        } else {
+            q = i / a.blocks_k;
+            kb = i - q * a.blocks_k;
+            g = q / a.tiles;
+        }
+        tile = q - g * a.tiles;
     }
 };
 
@@ -76,10 +84,40 @@ struct Borders {
         const float second = c2 ? b6 : b2, low = c2 ? b5 : b1, high = c2 ? b7 : b3;
         const bool c1 = m >= second;
         const bool c0 = m > (c1 ? high : low);
-        const uint32_t c = (c2 ? 4u : 0u) | (c1 ? 2u : 0u) | (c0 ? 1u : 0u);
-        return c && w < 0.0f ? c | 8u : c;
+        uint32_t c = c2;
+        c = c + c + c1;
+        c = c + c + c0;
+        return c | (__float_as_uint(w) >> 28 & 8u);   // (-0 is a code, too)
     }
 };
+
+// The codes of eight weights.  bf16: a weight and a border of 3 bits times a bf16 scale are
+// equal or differ by 2^-11 of themselves at least, so their quotient, formed to a few
+// units in its last place and then rounded to 14 bits, lies on a border where it should and on the
+// right side of it elsewhere: gfx950's own conversion (nearest, ties to the even code) takes it
+// from there.
+template <typename E>
+__device__ __forceinline__ uint32_t codes_of(const float (&w)[8], float s)
+{
+    uint32_t c = 0;
+    if (sizeof(E) == 2 && s >= 0x1p-120f && s <= 0x1p120f) {
+        const float inv = __builtin_amdgcn_rcpf(s);
+        float q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            q[e] = __uint_as_float((__float_as_uint(w[e] * inv) + 0x100u) & 0xFFFFFE00u);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[0], q[1], 1.0f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[2], q[3], 1.0f, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[4], q[5], 1.0f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[6], q[7], 1.0f, 3);
+        return c;
+    }
+    const Borders borders(s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        c |= borders.code(w[e]) << (4 * e);
+    return c;
+}
 
 template <typename E>
 __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
@@ -88,7 +126,8 @@ __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int per = 128 / a.scale_group;   // scales of an output in a block
     const int64_t n_blocks = (int64_t)a.groups * a.tiles * a.blocks_k;
-    for (int64_t i = (int64_t)blockIdx.x * (kPackThreads / 64) + (threadIdx.x >> 6); i < n_blocks;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t i = (int64_t)blockIdx.x * (kPackThreads / 64) + wave; i < n_blocks;
          i += (int64_t)gridDim.x * (kPackThreads / 64)) {
         const BlockOf at(a, i);
         const int64_t n = at.tile * 16 + r, k0 = at.kb * 128 + h * 8;
@@ -139,12 +178,7 @@ __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
                                    : from_f32<bf16_t>(__uint_as_float(most[j]) * kSixth).b;
             if (j * 32 / a.scale_group == h)
                 scale = s;
-            const Borders borders(scale_value(s));
-            uint32_t c = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                c |= borders.code(v[j][e]) << (4 * e);
-            codes[j] = c;
+            codes[j] = codes_of<E>(v[j], scale_value(s));
         }
         *(u32x4*)(a.codes + i * 1024 + lane * 16) = codes;
         if (h < per)
@@ -159,7 +193,8 @@ __global__ __launch_bounds__(kPackThreads) void dequantize_kernel(Fp4Args a)
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int per = 128 / a.scale_group;
     const int64_t n_blocks = (int64_t)a.groups * a.tiles * a.blocks_k;
-    for (int64_t i = (int64_t)blockIdx.x * (kPackThreads / 64) + (threadIdx.x >> 6); i < n_blocks;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t i = (int64_t)blockIdx.x * (kPackThreads / 64) + wave; i < n_blocks;
          i += (int64_t)gridDim.x * (kPackThreads / 64)) {
         const BlockOf at(a, i);
         const int64_t n = at.tile * 16 + r, k0 = at.kb * 128 + h * 8;

@@ -1450,7 +1450,10 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 
 }  // namespace
 
-// Up to 31 entries a lane per row, up to kShortMost a few lanes, above a wavefront where there are
+// Up to 31 entries a lane per row, up to kShortMost a few lanes (for up to half as many in all
+// cases: us, 65536 rows of 1024 bf16, few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and
+// 76, 97 and 82, 184 and 157; of 512: 28 and 73, 42 and 80, 95 and 126; fp32 1024 without
+// lists 48 and 39), above a wavefront where there are
 // rows enough and short lists, else a workgroup, or several where there are fewer rows
 // than fill the CUs: of at least a tile (16 KB) each.  Few rows: a chunk per lane, while that takes
 // no more threads than fill the CUs a few times (us, lists of 6 places, against a lane per row: fp32
@@ -1472,7 +1475,8 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
     if (A <= kLaneMost && !few) {
         p.variant = kLogpLane;
         per = kLaneThreads;
-    } else if (A <= kShortMost) {
+    } else if (A <= kShortMost && !(A > kShortMost / 2 && rows >= 8 * kCus &&
+                                    (top == 0 || (top > 6 && top <= kWaveTop)))) {
         p.variant = kLogpShort;
         p.chunks = few ? 1 : 4;
         p.group = 4;
