@@ -515,7 +515,9 @@ struct Fp4Args {
     int first_group;
 };
 struct Fp4Plan {
-    int rows, tiles;   // tiles of 16 rows and of 16 outputs per workgroup
+    // tiles of 16 rows and of 16 outputs of a wavefront (of a workgroup where rows is 2); how many
+    // wavefronts of a workgroup have outputs of their own
+    int rows, tiles, apart;
 };
 Fp4Plan fp4_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size);
 hipError_t launch_quantize_fp4(const Fp4Args& a, int dtype, hipStream_t s);

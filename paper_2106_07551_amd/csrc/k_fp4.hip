@@ -324,20 +324,25 @@ __device__ __forceinline__ void finish_tile(const Fp4Args& a, int64_t g, int64_t
         }
 }
 
-// A workgroup takes 16 rows of x and 16 NT outputs, each of its wavefronts a share of the blocks
-// of 128 inputs, straight from memory to registers, a block ahead of the products; the shares
-// are added through LDS in their order.  Rows and outputs that do not exist repeat the last
+// A wavefront takes 16 rows of x, 16 NT outputs and a share of the blocks of 128 inputs, straight
+// from memory to registers, a block ahead of the products.  WK = 8: a workgroup's wavefronts
+// share the inputs, and their sums are added through LDS in their order; WK = 1 (few blocks of
+// inputs): each has outputs of its own.  Rows and outputs that do not exist repeat the last
 // row, or use the padding's codes: their results are not written.
 constexpr int kWaves = 8;
 
-template <typename E, int SG, int NT>
+template <typename E, int SG, int NT, int WK>
 __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
 {
     constexpr int CH = kChunk<E>, P = kParts<E>, PER = 128 / SG;
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t g = a.first_group + blockIdx.z;
-    const int64_t m0 = (int64_t)blockIdx.y * 16, t0 = (int64_t)blockIdx.x * NT;
+    const int64_t m0 = (int64_t)blockIdx.y * 16;
+    const int64_t t0 = (WK == 1 ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x) * NT;
+    const int share = WK == 1 ? 0 : wave;
+    if (WK == 1 && t0 >= a.tiles)
+        return;
     const uint8_t* codes[NT];
     const uint16_t* scales[NT];
 #pragma unroll
@@ -405,31 +410,38 @@ __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
         }
     };
     const int64_t whole = a.K / 128;
-    int64_t kb = wave;
+    int64_t kb = share;
     if (kb < whole) {
         Block now, next;
         load(now, kb, true);
-        for (; kb + kWaves < whole; kb += kWaves) {
-            load(next, kb + kWaves, true);
+        for (; kb + WK < whole; kb += WK) {
+            load(next, kb + WK, true);
             multiply(now, kb, true);
             now = next;
         }
         multiply(now, kb, true);
-        kb += kWaves;
+        kb += WK;
     }
     if (kb < a.blocks_k) {
         Block b;
         load(b, kb, false);
         multiply(b, kb, false);
     }
-    __shared__ f32x4 part[kWaves][NT][64];
+    // lane: output r of a tile, its rows 4 h .. 4 h + 3
+    if constexpr (WK == 1) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-        part[wave][t][lane] = acc[t];
-    __syncthreads();
-    if (wave < NT)
-        finish_tile<E, kWaves>(a, g, m0 + 4 * h, (t0 + wave) * 16 + r, &part[0][wave][lane],
-                               NT * 64);
+        for (int t = 0; t < NT; ++t)
+            finish_tile<E, 1>(a, g, m0 + 4 * h, (t0 + t) * 16 + r, &acc[t], 0);
+    } else {
+        __shared__ f32x4 part[kWaves][NT][64];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            part[wave][t][lane] = acc[t];
+        __syncthreads();
+        if (wave < NT)
+            finish_tile<E, kWaves>(a, g, m0 + 4 * h, (t0 + wave) * 16 + r, &part[0][wave][lane],
+                                   NT * 64);
+    }
 }
 
 // More rows, bf16: a workgroup takes 32 rows and 64 outputs.  Rows go through LDS, a wavefront's
@@ -578,15 +590,15 @@ __global__ __launch_bounds__(kTallWaves * 64) void tall_fp4_kernel(Fp4Args a)
                                         part + q * 64 + lane, MT * NT * 64);
 }
 
-template <typename E, int NT>
+template <typename E, int NT, int WK>
 void launch_tiles(const Fp4Args& a, dim3 grid, hipStream_t s)
 {
     if (a.scale_group == 32)
-        linear_fp4_kernel<E, 32, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 32, NT, WK><<<grid, kWaves * 64, 0, s>>>(a);
     else if (a.scale_group == 64)
-        linear_fp4_kernel<E, 64, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 64, NT, WK><<<grid, kWaves * 64, 0, s>>>(a);
     else
-        linear_fp4_kernel<E, 128, NT><<<grid, kWaves * 64, 0, s>>>(a);
+        linear_fp4_kernel<E, 128, NT, WK><<<grid, kWaves * 64, 0, s>>>(a);
 }
 
 void launch_tall(const Fp4Args& a, dim3 grid, hipStream_t s)
@@ -604,7 +616,7 @@ hipError_t launch_linear_as(Fp4Args a, const Fp4Plan& p, hipStream_t s)
 {
     // at most 2^22 workgroups a launch (and 65535 blocks of rows)
     constexpr int64_t kMost = (int64_t)1 << 22;
-    const int64_t nt = (a.tiles + p.tiles - 1) / p.tiles;
+    const int64_t nt = (a.tiles + p.tiles * p.apart - 1) / (p.tiles * p.apart);
     const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(a.groups, kMost / nt));
     const int64_t per =
         std::max<int64_t>(1, std::min<int64_t>(65535, kMost / (nt * groups))) * 16 * p.rows;
@@ -622,12 +634,16 @@ hipError_t launch_linear_as(Fp4Args a, const Fp4Plan& p, hipStream_t s)
                             (unsigned)std::min<int64_t>(groups, a.groups - g));
             if (p.rows == 2)
                 launch_tall(b, grid, s);
+            else if (p.apart > 1 && p.tiles == 4)
+                launch_tiles<E, 4, 1>(b, grid, s);
+            else if (p.apart > 1)
+                launch_tiles<E, 1, 1>(b, grid, s);
             else if (p.tiles == 4)
-                launch_tiles<E, 4>(b, grid, s);
+                launch_tiles<E, 4, kWaves>(b, grid, s);
             else if (p.tiles == 2)
-                launch_tiles<E, 2>(b, grid, s);
+                launch_tiles<E, 2, kWaves>(b, grid, s);
             else
-                launch_tiles<E, 1>(b, grid, s);
+                launch_tiles<E, 1, kWaves>(b, grid, s);
         }
     }
     return hipGetLastError();
@@ -647,22 +663,31 @@ hipError_t launch_pack(const Fp4Args& a, F kernel, hipStream_t s)
 // bf16 rows through LDS against straight to registers (us, groups of 128 and of 32 weights): 96 rows
 // x 4096 -> 4096 9.4 and 13.6, 15.6 and 14.6; 128 rows x 8192 -> 8192 25.4 and 44.2, 37.9 and
 // 48.8; 256 x 512 -> 16384 15.7 and 25.5, 18.8 and 22.8; but 48 x 4096 -> 4096 9.8 and 8.1, 15.5
-// and 9.0, and with few blocks of inputs for each wavefront 256 x 16384 <- 512 23.9 and 21.1, 43.8
-// and 24.8.  Straight to registers, as many tiles as leave a workgroup for most CUs: 1 row x 8192 ->
-// 8192 with 1, 2, 4 tiles 9.1, 8.5, 11.0; 16 rows 19.2, 12.5, 14.6; 32 rows 34.8, 21.8, 15.3.
+// and 9.0, and with few workgroups 256 x 16384 -> 512 23.9 and 21.1, 43.8 and 24.8, 112 x 11504 ->
+// 1856 41 and 19 (groups of 32).  Straight to registers, as many
+// tiles as leave a workgroup for most CUs: 1 row x 8192 -> 8192 with 1, 2, 4 tiles 9.1, 8.5, 11.0; 16
+// rows 19.2, 12.5, 14.6; 32 rows 34.8, 21.8, 15.3.  Wavefronts with outputs of their own
+// where there is one block of inputs: 21 x 58 x 112 -> 2624 fp32 12 and 41; with four 16 x 512 -> 512
+// bf16 6.4 and 3.5.
+constexpr int64_t kApartMost = 128;
 Fp4Plan fp4_plan(int64_t groups, int64_t M, int64_t N, int64_t K, int size)
 {
     constexpr int64_t kFill = 192;   // workgroups
     Fp4Plan p{};
     p.tiles = 4;
-    p.rows = 1;
-    if (size == 2 && M > 64 && K >= 2048) {
-        p.rows = kTallRows / 16;
-        return p;
-    }
+    p.rows = p.apart = 1;
     const int64_t tiles = (N + 15) / 16, blocks = (M + 15) / 16 * groups;
-    while (p.tiles > 1 && (tiles + p.tiles - 1) / p.tiles * blocks < kFill)
-        p.tiles /= 2;
+    if (size == 2 && M > 64 && K >= 512 &&
+        (tiles + 3) / 4 * ((M + kTallRows - 1) / kTallRows) * groups >= kFill) {
+        p.rows = kTallRows / 16;
+    } else if (K <= kApartMost) {
+        p.apart = kWaves;
+        if ((tiles + 4 * kWaves - 1) / (4 * kWaves) * blocks < kFill)
+            p.tiles = 1;
+    } else {
+        while (p.tiles > 1 && (tiles + p.tiles - 1) / p.tiles * blocks < kFill)
+            p.tiles /= 2;
+    }
     return p;
 }
 

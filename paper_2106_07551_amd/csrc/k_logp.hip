@@ -1454,7 +1454,8 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 // cases: us, 65536 rows of 1024 bf16, few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and
 // 76, 97 and 82, 184 and 157; of 512: 28 and 73, 42 and 80, 95 and 126; fp32 1024 without
 // lists 48 and 39), above a wavefront where there are
-// rows enough and short lists, else a workgroup, or several where there are fewer rows
+// rows enough and short lists (700 rows of 3000 bf16, lists of 3 and 64 places 8.6 and 14.0, a
+// workgroup 10.4 and 12.5; 1657 rows of 1553 fp32 9.2 and 14.2, 16.3 and 18.9), else a workgroup, or several where there are fewer rows
 // than fill the CUs: of at least a tile (16 KB) each.  Few rows: a chunk per lane, while that takes
 // no more threads than fill the CUs a few times (us, lists of 6 places, against a lane per row: fp32
 // 4096 x 18 5.4 and 10.0, 65536 x 18 10.4 and 10.8, 131072 x 18 16.6 and 12.9; against four chunks per
@@ -1483,7 +1484,8 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
         while (p.group * p.chunks * ch < A)
             p.group *= 2;
         per = kShortThreads / p.group;
-    } else if (top <= kWaveTop && rows >= 8 * kCus && chunks <= 1024) {
+    } else if (top <= kWaveTop && chunks <= 1024 &&
+               rows >= (chunks > 512 ? 8 : top > 32 ? 4 : 1) * kCus) {
         p.variant = kLogpWave;
         per = StreamSize<64>::kRows;
     } else {
