@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
 constexpr int kTallWaves = 4, kTallRows = 32, kTallTiles = 4;
 
 template <int SG>
-__global__ __launch_bounds__(kTallWaves * 64) void tall_fp4_kernel(Fp4Args a)
+__global__ __launch_bounds__(kTallWaves * 64, SG == 64 ? 1 : 2) void tall_fp4_kernel(Fp4Args a)
 {
     constexpr int NT = kTallTiles, MT = kTallRows / 16, PER = 128 / SG, IN = kTallRows / 4;
     const int lane = threadIdx.x & 63, r = lane & 15, h = lane >> 4;
