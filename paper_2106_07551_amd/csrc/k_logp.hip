@@ -653,12 +653,17 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
 // wavefront (lists of up to kWaveTop places) or a workgroup.  They go through the row in tiles
 // of U chunks each.  A chunk with an entry that is not below `bound` goes to LDS; the first
 // tile's bound is the least of its wavefronts' j-th largest chunks' maxima, j = ceil(k /
-// wavefronts).  After 2, 4, 8, ... tiles (long lists: after the first, too) and the last one the chunks' entries join the
-// list's candidates, which are cut to about k, the bound becoming the last one's value: each
-// time about as many come in as stay.  (Values are cut by the high half of their order: bf16
-// exactly.)  Where LDS does not hold them (entries that rise along the row, many equal ones) or a
-// NaN is about, the row's list is made in a second pass by the exact search, tile by
-// tile.
+// wavefronts).  After 2, 8, 32, ... tiles (long lists: 1, 2, 4, ...) and the last one the chunks'
+// entries join the list's candidates, which are cut to about k, the bound becoming the last one's
+// value: three times as many (as many) come in from one cut to the next.  Values are cut by the
+// high half of their order (bf16 exactly).  Where LDS does not hold them (entries that rise along
+// the row, many equal ones) or a NaN is about, the row's list is made in a second pass by the exact
+// search, tile by tile, which passes over tiles that add nothing: 4096 x 65536 bf16 equal entries
+// 1.3 ms, entries that rise 2.5 ms.
+// Bound by memory without lists: 4096 x 65536 bf16 103 us, 5.2 TB/s; with 64 places 130 to 142 us:
+// the cuts' and the first tile's barriers leave their workgroups without loads on the way, and the
+// registers of the lists' code keep more workgroups out (tiles half as wide for eight a CU 144
+// us, the next tile's loads ahead of the cuts 154 us).
 constexpr int kStreamU = 4, kWaveTop = 64;
 template <int T>
 struct StreamSize {
@@ -818,6 +823,14 @@ __device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* p
                 m = fmaxf(m, v[e]);
         }
         group_sync<T>();
+        if (n == k) {   // (later entries are listed above the last one's value alone)
+            const float last = key_value(best[k - 1]);
+            bool above = false;
+            for_entries<E, T, U>(x, U, lane, [&](float f, int) { above |= !(f <= last); });
+            above &= last == last;
+            if (T > 64 ? __syncthreads_or(above) == 0 : __ballot(above) == 0)
+                continue;
+        }
         if (lane == 0)
             l.n_keys = 0;
         group_sync<T>();
@@ -883,7 +896,10 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
         }
         Stats st = empty_stats();
         float bound = 0.0f;
-        int next = 4 * k <= S::kChunks ? 1 : 0, tile = 0;   // (the tile of the next cut)
+        // (the tile of the next cut: each comes when three times as many tiles as before it, or
+        // as many, have gone by)
+        const bool seldom = 4 * k <= S::kChunks;
+        int next = seldom ? 1 : 0, tile = 0;
         for (int j0 = 0; j0 < len; j0 += TILE, ++tile) {
             u32x4 x[U];
 #pragma unroll
@@ -962,19 +978,20 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                     l.bound = bound;
                 group_sync<T>();   // (and the counts are 0 before others add)
             }
-            bool any = false;
+            int mine = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                any = any || top[u] >= bound;
-            if (any) {
+                mine += top[u] >= bound;
+            if (mine) {
+                int to = atomicAdd(&l.n_raw, mine);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (top[u] >= bound) {
-                        const int to = atomicAdd(&l.n_raw, 1);
                         if (to < S::kChunks) {
                             l.raw[to] = x[u];
                             l.at[to] = (int)base + j0 + (lane + u * T) * CH;
                         }
+                        ++to;
                     }
             }
             if (tile == next || j0 + TILE >= len) {
@@ -984,7 +1001,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                     next = 1 << 30;
                 } else {
                     bound = l.bound;
-                    next = 2 * next + 1;
+                    next = seldom ? 4 * next + 3 : 2 * next + 1;
                 }
             }
         }
