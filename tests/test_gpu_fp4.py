@@ -296,3 +296,33 @@ def test_no_rows():
     import paper_2106_07551_amd as M
     codes, scales = M.quantize_fp4(torch.randn((20, 40), device="cuda"))
     assert M.linear_fp4(torch.empty((0, 40), device="cuda"), codes, scales, 20).shape == (0, 20)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("groups, rows, n, k", [(3, 17, 40, 200), (2, 70, 4000, 600)])
+def test_rows_beyond_32_bits(dtype, groups, rows, n, k):
+    """Rows of x, y and the residual and policies of x that are far apart (no difference to the
+    result at all), and weights that are."""
+    import paper_2106_07551_amd as M
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    apart = ((1 << 32) // (rows * groups) + 1) | 1
+
+    def far(t):
+        lead, (r, c) = t.shape[0], t.shape[1:]
+        wide = torch.empty((lead * r - 1) * apart + c, dtype=t.dtype, device="cuda")
+        return wide.as_strided(t.shape, (r * apart, apart, 1)).copy_(t)
+
+    w = torch.randn((groups, n, k), generator=g, device="cuda").to(dtype)
+    x = torch.randn((groups, rows, k), generator=g, device="cuda").to(dtype)
+    res = torch.randn((groups, rows, n), generator=g, device="cuda").to(dtype)
+    codes, scales = M.quantize_fp4(w)
+    y = check(x, codes, scales, n, residual=res)
+    assert torch.equal(M.linear_fp4(far(x), codes, scales, n, residual=far(res),
+                                    out=far(torch.zeros_like(res))), y)
+    if n < 100:
+        apart = (1 << 32) // (n * groups) + 1
+        c, s = M.quantize_fp4(far(w))
+        assert torch.equal(c, codes) and torch.equal(s.view(torch.int16), scales.view(torch.int16))
+        plain = M.dequantize_fp4(codes, scales, n, k, dtype=dtype)
+        assert torch.equal(M.dequantize_fp4(codes, scales, n, k, dtype=dtype,
+                                            out=far(torch.zeros_like(plain))), plain)

@@ -242,6 +242,45 @@ def test_indices_beyond_24_bits_of_a_row():
     check(x, torch.tensor([a - 1], device="cuda"), top=4)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("a, n", [(9000, 2048), (40000, 260), (300000, 3)])
+def test_equal_entries_and_a_few_others(dtype, a, n):
+    """Equal entries with a few others anywhere: the exact search, part by part."""
+    g = torch.Generator(device="cuda").manual_seed(a)
+    x = torch.zeros((n, a), device="cuda")
+    others = torch.tensor([1.0, -1.0, 0.0, 3e38, -math.inf, math.inf, math.nan, 2.0],
+                          device="cuda")
+    for r in range(0, n, max(1, n // 64)):
+        at = torch.randint(0, a, (r % 7,), generator=g, device="cuda")
+        x[r, at] = others[torch.randint(0, 3 + r % 6, (r % 7,), generator=g, device="cuda")]
+    act = torch.randint(0, a, (n,), generator=g, device="cuda")
+    for top in (1, 7, 64, 200):
+        check(x.to(dtype), act, top=top, what="equal")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("a, n, apart", [(18, 9, 1 << 28), (300, 5, 1 << 29), (5000, 5, 1 << 29),
+                                         (70000, 17, (1 << 27) + 1)])
+def test_rows_beyond_32_bits(dtype, a, n, apart):
+    """Rows whose offsets in elements (of logits, mask and dlogits) do not fit 31 bits."""
+    import paper_2106_07551_amd as M
+    g = torch.Generator(device="cuda").manual_seed(a)
+    wide = torch.empty((n - 1) * apart + a, dtype=dtype, device="cuda")
+    x = wide.as_strided((n, a), (apart, 1))
+    x.copy_(torch.randn((n, a), generator=g, device="cuda") * 3)
+    mask = torch.empty((n - 1) * apart + a, dtype=torch.uint8, device="cuda") \
+        .as_strided((n, a), (apart, 1))
+    mask.copy_(torch.rand((n, a), generator=g, device="cuda") < 0.8)
+    act = torch.randint(0, a, (n,), generator=g, device="cuda")
+    stats = check(x, act, top=9, mask=mask, what="far apart")
+    near, legal = x.contiguous(), mask.contiguous()
+    assert torch.equal(M.log_probs(near, act, top=9, mask=legal)[0], stats)
+    dl, dh = torch.randn((2, n), generator=g, device="cuda")
+    ref = M.log_probs_backward(near, act, stats, dl, dh, mask=legal)
+    assert M.log_probs_backward(x, act, stats, dl, dh, mask=mask, dlogits=x) is x
+    assert torch.equal(x, ref)
+
+
 @pytest.mark.parametrize("n, a", [(0, 5), (0, 5000), (1, 1)])
 def test_no_rows_and_one_entry(n, a):
     import paper_2106_07551_amd as M
