@@ -4,6 +4,8 @@
 // A thread takes 16 consecutive values (in the matrix's own order, whatever its
 // strides), which share one block of the stream: 16 bits each.  Bound by memory: with 32 bits
 // a value the stream's 64-bit products would take longer than the values' transfer.
+// 131072 x 512 bf16 with a residual, 402 MB: 68 us, 5.9 TB/s (two thirds of it are reads, which
+// are faster than a copy).  5003 x 777 fp32, rows apart, 31 MB: 9 us, 3.5 TB/s.
 #include "internal.hpp"
 
 #include "chunk.hpp"

@@ -119,7 +119,8 @@ __device__ __forceinline__ float entry_logp(const LogpArgs& a, const RowOut& o, 
 
 // 64 rows per wavefront, as in the losses (rows.hpp): rows go through LDS in memory's own
 // order.  A list is found in as many rounds as it has places, each over the row's
-// entries in registers.
+// entries in registers.  Bound by their instructions: 131072 x 18 fp32, 6 places 12 us, of
+// which 5 are the transfer (17.8 MB at the copy's rate: 3.7).
 template <typename E, int NA>
 __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
 {
@@ -396,7 +397,8 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
 // --------------------------------------------- short rows: 4 to 64 lanes per row
 
 // Rows of up to kShortMost entries, C chunks a lane: 4, or 1 where there are few rows, whose lanes
-// then have less to do one after the other.
+// then have less to do one after the other.  Few rows are bound by latency (192 x 18 fp32 4.6
+// us), many by the lists' instructions (65536 x 512 bf16 with one place 28 us, 2.4 TB/s).
 constexpr int kShortMost = 1024, kShortThreads = 256;
 
 // Rounds of a group of T lanes cost their wavefront about 85 instructions for 64 / T rows, a
@@ -659,11 +661,11 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
 // high half of their order (bf16 exactly).  Where LDS does not hold them (entries that rise along
 // the row, many equal ones) or a NaN is about, the row's list is made in a second pass by the exact
 // search, tile by tile, which passes over tiles that add nothing: 4096 x 65536 bf16 equal entries
-// 1.3 ms, entries that rise 2.5 ms.
-// Bound by memory without lists: 4096 x 65536 bf16 103 us, 5.2 TB/s; with 64 places 130 to 142 us:
-// the cuts' and the first tile's barriers leave their workgroups without loads on the way, and the
-// registers of the lists' code keep more workgroups out (tiles half as wide for eight a CU 144
-// us, the next tile's loads ahead of the cuts 154 us).
+// 1.2 ms, entries that rise 2.5 ms.
+// Bound by memory without lists: 4096 x 65536 bf16 102 us, 5.3 TB/s; with 64 places 131 us: the
+// cuts' and the first tile's barriers leave their workgroups without loads on the way, and the
+// registers of the lists' code keep more workgroups out (tiles half as wide for eight a CU, or the
+// next tile's loads ahead of the cuts, took longer).
 constexpr int kStreamU = 4, kWaveTop = 64;
 template <int T>
 struct StreamSize {
@@ -681,6 +683,15 @@ struct Candidates {
     float bound;
     bool over;
 };
+
+// A number of which nothing is formed ahead: what hangs on a lane's alone would be, before the
+// loops over rows and tiles, and in registers that are not there (4096 x 65536 bf16 wrote 57 MB
+// of them to memory; 16384 x 8192 fp32, 8 places, takes 124 us for 131).
+__device__ __forceinline__ int apart(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
 // The largest 16-bit prefix of an order, from `lo` (which at least k entries are not below) to
 // that of +inf, that at least k of the wavefront's entries are not below.  count(p): how many
@@ -828,7 +839,20 @@ __device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* p
             bool above = false;
             for_entries<E, T, U>(x, U, lane, [&](float f, int) { above |= !(f <= last); });
             above &= last == last;
-            if (T > 64 ? __syncthreads_or(above) == 0 : __ballot(above) == 0)
+            // (__syncthreads_or here costs every row of the kernel: 4096 x 65536 bf16 142 us
+            // for 130)
+            bool some = __ballot(above) != 0;
+            if constexpr (T > 64) {
+                if (lane == 0)
+                    l.n_keys = 0;
+                group_sync<T>();
+                if (some && (lane & 63) == 0)
+                    l.n_keys = 1;
+                group_sync<T>();
+                some = l.n_keys != 0;
+                group_sync<T>();
+            }
+            if (!some)
                 continue;
         }
         if (lane == 0)
@@ -869,13 +893,16 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
     constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH, W = T / 64;
     extern __shared__ u32x4 lists[];
     __shared__ float scratch[T > 64 ? 2 * kScratch : 1];
-    const int lane = threadIdx.x % T, slot = threadIdx.x / T;
+    // (in fp32 a row is said to be the whole workgroup's: 16384 x 8192, 8 places 133 us, else 149;
+    // bf16 rows, and wavefronts', take longer by it: 4096 x 65536, 64 places 157 and 135)
+    const int slot = T > 64 && sizeof(E) == 4 ? 0 : threadIdx.x / T;
     Candidates<T>& l = ((Candidates<T>*)lists)[slot];
     const float c = kLog2e / a.temperature;
     const int k = LIST ? a.top : 0;
     const int64_t items = PART ? a.rows * a.splits : a.rows;
     for (int64_t item = (int64_t)blockIdx.x * S::kRows + slot; item < items;
          item += (int64_t)gridDim.x * S::kRows) {   // (a wavefront's, or a workgroup's, alone)
+        const int lane = apart(threadIdx.x % T);
         const int64_t row = PART ? item / a.splits : item;
         const int part = PART ? (int)(item % a.splits) : 0;
         const int64_t base = PART ? (int64_t)part * a.part_len : 0;
@@ -890,7 +917,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                 x_a = to_f32(px[action]);
         }
         if (k > 0 && lane == 0) {
-            l.n_raw = l.n_keys = 0;
+            l.n_raw = l.n_keys = apart(0);
             l.over = false;
             l.bound = kLeastFinite;
         }
@@ -995,7 +1022,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                     }
             }
             if (tile == next || j0 + TILE >= len) {
-                tighten<E, T>(l, lane, k);
+                tighten<E, T>(l, apart(lane), k);
                 if (l.over) {   // (no later chunk counts)
                     bound = -kNegInf;
                     next = 1 << 30;
@@ -1020,12 +1047,13 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
             continue;
         int n = l.n_keys;
         bool sorted = false;
+        const int own = apart(lane);
         if (l.over || st.s != st.s) {
-            n = exact_list<E, T>(l, px, pm, len, base, k, lane);
+            n = exact_list<E, T>(l, px, pm, len, base, k, own);
             sorted = true;
         }
         const int64_t to = item * k;
-        for (int i = lane; i < n; i += T) {
+        for (int i = own; i < n; i += T) {
             const uint64_t key = l.keys[i];
             const int place = sorted ? i : place_of(l.keys, n, key);
             if (place < k) {
@@ -1037,7 +1065,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                 }
             }
         }
-        for (int i = n + lane; i < k; i += T) {
+        for (int i = n + own; i < k; i += T) {
             if constexpr (PART) {
                 a.part_keys[to + i] = 0;
             } else {
@@ -1054,7 +1082,8 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
 // A workgroup per row: the parts' sums, and the first of their lists (each in order,
 // zeros behind its entries).  At least `top` entries are not below the j-th of every list,
 // j = ceil(top / lists), nor below the last place of any one list; with more lists than
-// places, nor below the top-th largest of their first entries.
+// places, nor below the top-th largest of their first entries.  Bound by latency, a chain of
+// loads, barriers and stores: 3 x 131071 bf16, 40 places 6 us, the parts before it 9.6.
 constexpr int kMergeThreads = 256, kMergeCap = 1024, kMergeAll = 512;
 constexpr int kMergeLists = 2;   // of a thread, at most
 
@@ -1296,7 +1325,7 @@ __global__ __launch_bounds__(kLaneThreads) void logp_grad_lane_kernel(LogpArgs a
 }
 
 // T lanes per row, or per part of one (splits > 1): every entry apart, in chunks of 16
-// bytes.
+// bytes.  Bound by memory: 2047 x 50001 bf16, 410 MB, 90 us, 4.5 TB/s.
 constexpr int kGradThreads = 256, kGradUnroll = 4;
 
 template <typename E, int T>
@@ -1467,17 +1496,18 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 
 }  // namespace
 
-// Up to 31 entries a lane per row, up to kShortMost a few lanes (for up to half as many in all
-// cases: us, 65536 rows of 1024 bf16, few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and
-// 76, 97 and 82, 184 and 157; of 512: 28 and 73, 42 and 80, 95 and 126; fp32 1024 without
-// lists 48 and 39), above a wavefront where there are
-// rows enough and short lists (700 rows of 3000 bf16, lists of 3 and 64 places 8.6 and 14.0, a
-// workgroup 10.4 and 12.5; 1657 rows of 1553 fp32 9.2 and 14.2, 16.3 and 18.9), else a workgroup, or several where there are fewer rows
-// than fill the CUs: of at least a tile (16 KB) each.  Few rows: a chunk per lane, while that takes
-// no more threads than fill the CUs a few times (us, lists of 6 places, against a lane per row: fp32
-// 4096 x 18 5.4 and 10.0, 65536 x 18 10.4 and 10.8, 131072 x 18 16.6 and 12.9; against four chunks per
-// lane: 4096 x 60 5.3 and 7.0, 65536 x 60 15.7 and 12.6, 4096 x 250 7.7 and 7.7, 16384 x 250 18.7 and
-// 13.0; bf16 131072 x 18 12.4 and 12.5, 4096 x 250 6.3 and 8.2, 16384 x 250 11.9 and 9.9).
+// Up to 31 entries a lane per row; up to kShortMost a few lanes.  From half of that on, with many
+// rows and without lists or with more than 6 places, a wavefront (us, 65536 rows of 1024 bf16,
+// few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and 76, 97 and 82, 184 and 157; of
+// 512: 28 and 73, 42 and 80, 95 and 126; fp32 1024 without lists 48 and 39).  Above, a wavefront
+// where there are rows enough and short lists (700 rows of 3000 bf16, lists of 3 and 64 places 8.6
+// and 14.0, a workgroup 10.4 and 12.5; 1657 rows of 1553 fp32 9.2 and 14.2, a workgroup 16.3 and
+// 18.9), else a workgroup, or several where there are fewer rows than fill the CUs: of at least a
+// tile (16 KB) each.  Few rows: a chunk per lane, while that takes no more threads than fill the
+// CUs a few times (us, lists of 6 places, against a lane per row: fp32 4096 x 18 5.4 and 10.0,
+// 65536 x 18 10.4 and 10.8, 131072 x 18 16.6 and 12.9; against four chunks per lane: 4096 x 60
+// 5.3 and 7.0, 65536 x 60 15.7 and 12.6, 4096 x 250 7.7 and 7.7, 16384 x 250 18.7 and 13.0; bf16
+// 131072 x 18 12.4 and 12.5, 4096 x 250 6.3 and 8.2, 16384 x 250 11.9 and 9.9).
 constexpr int64_t kFewLane = 1 << 19, kFewShort = 1 << 18;
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 {
