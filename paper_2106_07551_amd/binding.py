@@ -1201,8 +1201,8 @@ def dropout(x, p: float, seed: int, step: int = 0, *, layer: int = 0, residual=N
     """malib_dropout: x k / q + residual, where a value stays (k = 1) with probability q = 1 - p
     (in steps of 2^-16) by the library's random stream, from its index, `seed`, `step`
     (plus the int64 in `device_step`, a device tensor of one number) and `layer`
-    alone.  float32 or bfloat16; contiguous tensors of any shape, or [rows][cols] with
-    contiguous rows; `out` may be x or residual.  Outside torch's autograd graph: the
+    alone.  float32 or bfloat16; contiguous tensors of any shape (the last dimension up to
+    2^24), or [rows][cols] with contiguous rows; `out` may be x or residual.  Outside torch's autograd graph: the
     gradient is dropout_backward's, the residual's is dy."""
     if stream is None and x.is_cuda and (raw := _here(x)) is not None:
         y = (_calls or _native()).dropout(x, p, seed, step, layer, residual, out, device_step,
