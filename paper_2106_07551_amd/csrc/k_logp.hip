@@ -172,12 +172,18 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
             continue;
         wave_lds_sync();   // (the rows in bx have been read)
         if (lane < n) {
+            // bf16: order and index fit one number (2M x 18, 6 places 78 us, as in fp32 86; fp32
+            // with the index looked for behind the maximum took 5% longer)
+            constexpr bool kOne = sizeof(E) == 2;
             uint32_t k[NA];
 #pragma unroll
-            for (int j = 0; j < NA; ++j)
+            for (int j = 0; j < NA; ++j) {
                 k[j] = order_of(x[j]);
+                if (kOne)
+                    k[j] = k[j] <= kUnlisted ? 0u : (k[j] & 0xFFFF0000u) | (31u - j);
+            }
             for (int p = 0; p < w; ++p) {
-                uint32_t best = kUnlisted;
+                uint32_t best = kOne ? 0u : kUnlisted;
                 int at = -1;
 #pragma unroll
                 for (int q = 0; q < NA; q += 4) {
@@ -185,7 +191,8 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
                         break;
 #pragma unroll
                     for (int j = q; j < q + 4; ++j) {
-                        at = k[j] > best ? j : at;
+                        if (!kOne)
+                            at = k[j] > best ? j : at;
                         best = k[j] > best ? k[j] : best;
                     }
                 }
@@ -195,7 +202,11 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
                         break;
 #pragma unroll
                     for (int j = q; j < q + 4; ++j)
-                        k[j] = j == at ? 0u : k[j];
+                        k[j] = (kOne ? k[j] == best : j == at) ? 0u : k[j];
+                }
+                if (kOne && best) {   // (a NaN's order lost its low half, which leaves a NaN)
+                    at = 31 - (int)(best & 31u);
+                    best = best >> 31 ? best & 0xFFFF0000u : best | 0xFFFFu;
                 }
                 bx[lane * w + p] = __uint_as_float((uint32_t)at);
                 bv[lane * w + p] = at < 0 ? 0.0f : entry_logp(a, o, value_of(best));
