@@ -809,9 +809,10 @@ malib_status malib_dequantize_fp4(const malib_fp4_desc* desc, const uint8_t* cod
 
 /*
  * y = act(x W^T + b) + residual with W in 4 bits; the rest as in malib_linear.  Products
- * are exact (x in bf16, or fp32 x in three bf16 parts), sums are formed in fp32, scales are
- * applied to the fp32 sums of their weights.  The weights have no gradient, and x none from
- * this call.  For a few rows of x at a time: the weights' codes are taken apart again for every 16
+ * are exact (x in bf16, or fp32 x in three bf16 parts: bits below 2^-133 do not count), sums are
+ * formed in fp32, scales are applied to the fp32 sums of their weights; a sum that leaves fp32 without
+ * its scale is formed again, scaled down, so that results that fit fp32 are finite.  The weights
+ * have no gradient, and x none from this call.  For a few rows of x at a time: the weights' codes are taken apart again for every 16
  * or 32 rows, so that for hundreds of rows malib_dequantize_fp4 and malib_linear take less time.
  * No workspace.
  */

@@ -20,14 +20,14 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// The bf16 values of eight codes
-__device__ __forceinline__ u32x4 code_values(uint32_t c)
+// The bf16 values of eight codes, times a power of two
+__device__ __forceinline__ u32x4 code_values(uint32_t c, float times = 1.0f)
 {
     u32x4 v;
-    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.0f, 0));
-    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.0f, 1));
-    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.0f, 2));
-    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.0f, 3));
+    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, times, 0));
+    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, times, 1));
+    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, times, 2));
+    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, times, 3));
     return v;
 }
 
@@ -325,6 +325,75 @@ __device__ __forceinline__ void finish_tile(const Fp4Args& a, int64_t g, int64_t
         }
 }
 
+// Whether a wavefront's sums are not all finite
+template <int N>
+__device__ __forceinline__ bool beyond_fp32(const f32x4 (&acc)[N])
+{
+    f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};   // NaN where a sum is inf or NaN
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            zero[e] = __builtin_fmaf(acc[t][e], 0.0f, zero[e]);
+    const bool beyond = (zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f;
+    return __builtin_expect(__ballot(beyond) != 0, false);
+}
+
+// A sum without its scale can leave fp32 where their product would not: it has up to 128 terms of
+// up to 6 |x| (one of |x| = 1e38 does, or 128 of 1e36).  A tile's sums (of 16 rows from m0 on,
+// blocks kb, kb + step, ..) that are not finite are formed again from the codes' values times
+// kSmall, with which no sum of finite terms leaves fp32.  The others stay as they are: inputs below
+// 2^-116 would lose bits by kSmall.  (Finite sums pay for the look at them: 0.6% over 84 sizes.)
+constexpr float kSmall = 0x1p-10f;
+static_assert(128 * 6 * kSmall < 1.0f, "");
+
+template <typename E, int SG>
+__device__ __forceinline__ f32x4 mended(const Fp4Args& a, int64_t g, int64_t m0, int64_t tile,
+                                        int64_t kb, int step, int lane, f32x4 acc)
+{
+    constexpr int CH = kChunk<E>, P = kParts<E>, PER = 128 / SG;
+    asm volatile("" : "+v"(lane));   // (no address of the loops before is kept for this one)
+    const int r = lane & 15, h = lane >> 4;
+    tile = tile < a.tiles ? tile : a.tiles - 1;
+    const int64_t first = (g * a.tiles + tile) * a.blocks_k, row = m0 + r < a.M ? m0 + r : a.M - 1;
+    const E* x = (const E*)a.x.p + g * a.x.gs + row * a.x.ld;
+    f32x4 again = {0.0f, 0.0f, 0.0f, 0.0f}, sum = again;
+    for (; kb < a.blocks_k; kb += step) {
+        const u32x4 codes = *(const u32x4*)(a.codes + (first + kb) * 1024 + lane * 16);
+        uint32_t scales[(PER + 1) / 2];
+        load_scales<PER>(a.scales + ((first + kb) * 16 + r) * PER, scales);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4 raw[8 / CH];
+#pragma unroll
+            for (int q = 0; q < 8; q += CH) {
+                const int64_t k = kb * 128 + j * 32 + h * 8 + q, left = a.K - k;
+                raw[q / CH] = left > 0 ? load_chunk(x + k, left < CH ? (int)left : CH, k)
+                                       : u32x4{0, 0, 0, 0};
+            }
+            bf16x8 xp[P];
+            split_parts<E>(raw, xp);
+            const bf16x8 w = __builtin_bit_cast(bf16x8, code_values(codes[j], kSmall));
+            if (j * 32 % SG == 0)
+                sum = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xp[p], w, sum, 0, 0, 0);
+            if ((j * 32 + 32) % SG == 0) {
+                const float s =
+                    scale_of<PER>(scales, j * 32 / SG, kb * 128 + j * 32 / SG * SG < a.K);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    again[e] = __builtin_fmaf(sum[e] * s, 1.0f / kSmall, again[e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        acc[e] = acc[e] - acc[e] != 0.0f ? again[e] : acc[e];
+    return acc;
+}
+
 // A wavefront takes 16 rows of x, 16 NT outputs and a share of the blocks of 128 inputs, straight
 // from memory to registers, a block ahead of the products.  WK = 8: a workgroup's wavefronts
 // share the inputs, and their sums are added through LDS in their order; WK = 1 (few blocks of
@@ -430,7 +499,13 @@ __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
         multiply(b, kb, false);
     }
     // lane: output r of a tile, its rows 4 h .. 4 h + 3
+    const bool beyond = beyond_fp32(acc);
     if constexpr (WK == 1) {
+        if (beyond) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                acc[t] = mended<E, SG>(a, g, m0, t0 + t, share, WK, lane, acc[t]);
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
             finish_tile<E, 1>(a, g, m0 + 4 * h, (t0 + t) * 16 + r, &acc[t], 0);
@@ -439,6 +514,11 @@ __global__ __launch_bounds__(kWaves * 64) void linear_fp4_kernel(Fp4Args a)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
             part[wave][t][lane] = acc[t];
+        if (beyond) {
+            for (int t = 0; t < NT; ++t)
+                part[wave][t][lane] =
+                    mended<E, SG>(a, g, m0, t0 + t, share, WK, lane, part[wave][t][lane]);
+        }
         __syncthreads();
         if (wave < NT)
             finish_tile<E, kWaves>(a, g, m0 + 4 * h, (t0 + wave) * 16 + r, &part[0][wave][lane],
@@ -580,6 +660,7 @@ __global__ __launch_bounds__(kTallWaves * 64, SG == 64 ? 1 : 2) void tall_fp4_ke
         load(b, kb, Short());
         step(b, kb, 0, Short(), Short());
     }
+    static_assert(MT == 2, "");
     static_assert(sizeof lds == sizeof(f32x4) * kTallWaves * MT * NT * 64, "");
     f32x4* part = (f32x4*)lds;   // [wavefront][tile][lane], each wavefront's over its own rows
     wave_lds_sync();
@@ -588,6 +669,13 @@ __global__ __launch_bounds__(kTallWaves * 64, SG == 64 ? 1 : 2) void tall_fp4_ke
 #pragma unroll
         for (int t = 0; t < NT; ++t)
             part[(wave * MT * NT + i * NT + t) * 64 + lane] = acc[i][t];
+    if (beyond_fp32(acc[0]) || beyond_fp32(acc[1])) {
+        for (int q = 0; q < MT * NT; ++q) {
+            f32x4& sums = part[(wave * MT * NT + q) * 64 + lane];
+            sums = mended<bf16_t, SG>(a, g, m0 + q / NT * 16, t0 + q % NT, wave, kTallWaves, lane,
+                                      sums);
+        }
+    }
     __syncthreads();
     for (int q = wave; q < MT * NT; q += kTallWaves)
         finish_tile<bf16_t, kTallWaves>(a, g, m0 + q / NT * 16 + 4 * h, (t0 + q % NT) * 16 + r,
