@@ -795,9 +795,10 @@ typedef struct {
 
 /*
  * W [out][in] of each group in 4 bits: s = max |w| / 6 of the group of weights (as the fp32
- * product with 1 / 6), rounded to bf16, and v the value nearest to w / s (halfway: the one of even code; beyond 6: 6).  The
- * comparisons are exact.  A group of weights with an infinite one or a NaN gets a NaN as its
- * scale, one whose scale rounds to 0 gets zeros.
+ * product with 1 / 6), rounded to bf16, at most 85 x 2^119 (so that 6 s is finite), and v the value
+ * nearest to w / s (halfway: the one of even code; beyond 6: 6).  The comparisons are exact.  A
+ * group of weights with an infinite one or a NaN gets a NaN as its scale, one whose scale rounds to
+ * 0 gets zeros.
  */
 malib_status malib_quantize_fp4(const malib_fp4_desc* desc, const malib_mat* w, uint8_t* codes,
                                 uint16_t* scales, void* stream);

@@ -40,6 +40,9 @@ __device__ __forceinline__ float scale_value(uint16_t s)
 
 constexpr int kPackThreads = 256;
 constexpr float kSixth = 1.0f / 6.0f;   // of the largest magnitude: a group's scale
+// The largest scale (85 x 2^119) whose product with 6 fits fp32, and bf16: with the next one, that
+// of fp32 weights beyond 1023 x 2^118 (bf16's end before it), they would come back infinite
+constexpr uint16_t kMostScale = 0x7E2A;
 
 // A wavefront per block of 16 outputs x 128 inputs; a lane has output lane & 15 and, of
 // each 32 inputs, the eight from 8 (lane >> 4) on.  Bound by memory, without a second round of
@@ -174,9 +177,11 @@ __global__ __launch_bounds__(kPackThreads) void quantize_kernel(Fp4Args a)
         uint16_t scale = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint16_t s = most[j] >= 0x7F800000u
-                                   ? (uint16_t)0x7FC0u
-                                   : from_f32<bf16_t>(__uint_as_float(most[j]) * kSixth).b;
+            uint16_t s = from_f32<bf16_t>(__uint_as_float(most[j]) * kSixth).b;
+            if (sizeof(E) == 4 && s > kMostScale)
+                s = kMostScale;
+            if (most[j] >= 0x7F800000u)
+                s = 0x7FC0u;
             if (j * 32 / a.scale_group == h)
                 scale = s;
             codes[j] = codes_of<E>(v[j], scale_value(s));
