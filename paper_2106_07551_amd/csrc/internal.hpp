@@ -474,7 +474,7 @@ struct LogpArgs {
     int A, top, action_bytes;
     float temperature;
     // set by the launchers
-    float inv_t;
+    float two_over_t;
     int splits, part_len;
     bool bf16;
     void* part_stats;

@@ -3,7 +3,7 @@
 //
 // With x a row's legal logits, c = log2(e) / T and m = max x: s = sum_j 2^((x_j - m) c),
 // t = sum_j 2^((x_j - m) c) (x_j - m) c, and
-//   l = (x_a - m) / T - ln s (as a product with 1 / T),  H = ln s - ln2 t / s,
+//   l = (x_a - m) / T - ln s (as a product with 2 / T),  H = ln s - ln2 t / s,
 //   dx_j = 2^((x_j - m) c) (c0 + c1 (x_j - m) c) + dl [j = a] / T.
 // Lists: rows of up to kShortMost entries stay in the registers of a few lanes, which
 // find one place after the other, or, for longer lists, in LDS, where a wavefront finds the value
@@ -88,6 +88,13 @@ struct RowOut {
     float l, H, m, ln_s;
 };
 
+// (x - m) / T, of halves: x - m itself can leave fp32 where the result does not (3e38 and -3e38
+// with T = 4)
+__device__ __forceinline__ float below_max(const LogpArgs& a, float x, float m)
+{
+    return __builtin_fmaf(0.5f, x, -0.5f * m) * a.two_over_t;
+}
+
 __device__ __forceinline__ RowOut row_finish(const LogpArgs& a, const Stats& st, int action,
                                              float x_a)
 {
@@ -97,7 +104,7 @@ __device__ __forceinline__ RowOut row_finish(const LogpArgs& a, const Stats& st,
         o.ln_s = logf(st.s);
         o.H = o.ln_s - kLn2 * st.t / st.s;
         if (action >= 0)
-            o.l = (x_a - m) * a.inv_t - o.ln_s;
+            o.l = below_max(a, x_a, m) - o.ln_s;
     }
     return o;
 }
@@ -112,7 +119,7 @@ __device__ __forceinline__ void store_row(const LogpArgs& a, int64_t row, const 
 
 __device__ __forceinline__ float entry_logp(const LogpArgs& a, const RowOut& o, float x)
 {
-    return (x - (o.m == kNegInf ? 0.0f : o.m)) * a.inv_t - o.ln_s;
+    return below_max(a, x, o.m == kNegInf ? 0.0f : o.m) - o.ln_s;
 }
 
 // ------------------------------------------------ few actions: a lane per row
@@ -1566,7 +1573,7 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hipStream_t s)
 {
     a.bf16 = dtype == MALIB_DT_BF16;
-    a.inv_t = 1.0f / a.temperature;
+    a.two_over_t = 2.0f / a.temperature;
     a.splits = p.splits;
     a.part_len = p.part_len;
     a.part_stats = work;
