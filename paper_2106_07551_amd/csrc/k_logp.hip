@@ -676,10 +676,13 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
 // wavefronts).  After 2, 8, 32, ... tiles (long lists: 1, 2, 4, ...) and the last one the chunks'
 // entries join the list's candidates, which are cut to about k, the bound becoming the last one's
 // value: three times as many (as many) come in from one cut to the next.  Values are cut by the
-// high half of their order (bf16 exactly).  Where LDS does not hold them (entries that rise along
-// the row, many equal ones) or a NaN is about, the row's list is made in a second pass by the exact
-// search, tile by tile, which passes over tiles that add nothing: 4096 x 65536 bf16 equal entries
-// 1.2 ms, entries that rise 2.5 ms.
+// high half of their order (bf16 exactly).  Where LDS does not hold them, the row's list is made in
+// a second pass, from its end on, in which a tile that brings too many gets a bound of its own
+// (4096 x 65536 bf16, 64 places, a first tile without entries or of low ones: 270 us); or, where a
+// tile's own entries are too alike for that or a NaN is about, by the exact search, tile by tile,
+// which passes over tiles that add nothing (many equal entries: 1.1 ms; entries that rise: 1.8 ms;
+// fp32 entries that share the high half of their order, as all from 300 up to 302 do: 16384 x 8192
+// of 300 +- 0.5, 64 places, 0.77 ms, around 0 0.16).
 // Bound by memory without lists: 4096 x 65536 bf16 102 us, 5.3 TB/s; with 64 places 131 us: the
 // cuts' and the first tile's barriers leave their workgroups without loads on the way, and the
 // registers of the lists' code keep more workgroups out (tiles half as wide for eight a CU, or the
@@ -826,11 +829,129 @@ __device__ __forceinline__ void tighten(Candidates<T>& l, int lane, int k)
     group_sync<T>();
 }
 
+// A row's part once more where LDS did not hold what the first pass asked for: candidates are cut
+// before they are too many, and a tile that alone brings too many gets a bound of its own.  The
+// last tile comes first: the first pass was misled by the first.  False where that does not help.
+template <typename E, int T>
+__device__ __forceinline__ bool careful_list(Candidates<T>& l, const E* px, const uint8_t* pm,
+                                             int len, int64_t base, int k, int lane)
+{
+    using S = StreamSize<T>;
+    constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH, W = T / 64;
+    group_sync<T>();   // (all have read what the first pass left)
+    if (lane == 0) {   // (the first pass' bound holds)
+        l.n_raw = l.n_keys = 0;
+        l.over = false;
+    }
+    group_sync<T>();
+    int before = 0;   // chunks of the tiles before this one
+    for (int j0 = (len - 1) / TILE * TILE; j0 >= 0; j0 -= TILE) {
+        u32x4 x[U];
+        float top[U];   // of each chunk
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + (lane + u * T) * CH;
+            x[u] = load_masked(px + j, len - j, pm ? pm + j : nullptr, j);
+            float v[CH];
+            unpack<E>(x[u], v);
+            top[u] = kNegInf;
+#pragma unroll
+            for (int e = 0; e < CH; ++e)
+                top[u] = fmaxf(top[u], v[e]);
+        }
+        keep_raw<kPolicy>(x, nullptr);
+        auto add = [&]() {
+            const float bound = l.bound;
+            int mine = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                mine += top[u] >= bound;
+            int to = mine ? atomicAdd(&l.n_raw, mine) : 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (top[u] >= bound) {
+                    if (to < S::kChunks) {
+                        l.raw[to] = x[u];
+                        l.at[to] = (int)base + j0 + (lane + u * T) * CH;
+                    }
+                    ++to;
+                }
+            group_sync<T>();
+        };
+        add();
+        const int keys = l.n_keys;
+        int n = l.n_raw;   // (uniform: no one adds or cuts before all have passed another barrier)
+        if (n * CH + keys > S::kKeys) {
+            auto entries = [&](uint32_t p) {
+                const float v = prefix_value(p);
+                int n = 0;
+                for_entries<E, T, U>(x, U, lane,
+                                     [&](float f, int) { n += __popcll(__ballot(f >= v)); });
+                return n;
+            };
+            auto chunks = [&](uint32_t p) {
+                const float v = prefix_value(p);
+                int n = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    n += __popcll(__ballot(top[u] >= v));
+                return n;
+            };
+            // of each wavefront the j-th largest chunk's maximum (or entry, of few chunks), the
+            // least; wavefronts with fewer entries than j leave the k to the others
+            const int any = chunks(kLeastPrefix);
+            const int own = any >= 3 * k ? any : entries(kLeastPrefix);
+            int j = k, with = own >= k;
+            if constexpr (W > 1) {
+                if ((lane & 63) == 0)
+                    l.scratch[lane >> 6] = (float)own;
+                __syncthreads();
+                with = W;
+                do {
+                    j = (k + with - 1) / with;
+                    with = 0;
+                    for (int i = 0; i < W; ++i)
+                        with += (int)l.scratch[i] >= j;
+                } while (with > 0 && with * j < k);
+            }
+            float bound = any >= 3 * j ? prefix_value(halved_bound(j, chunks))
+                          : own >= j   ? prefix_value(halved_bound(j, entries))
+                                       : -kNegInf;
+            if constexpr (W > 1) {
+                if ((lane & 63) == 0)
+                    l.scratch[kScratch + (lane >> 6)] = bound;
+                __syncthreads();
+                for (int i = 0; i < W; ++i)
+                    bound = fminf(bound, l.scratch[kScratch + i]);
+            }
+            if (with > 0 && bound > l.bound) {
+                group_sync<T>();   // (all have read the counts and the bound)
+                if (lane == 0) {
+                    l.n_raw = before;
+                    l.bound = bound;
+                }
+                group_sync<T>();
+                add();
+                n = l.n_raw;
+            }
+        }
+        if (n * CH + keys > S::kKeys / 2 || j0 == 0) {
+            tighten<E, T>(l, lane, k);
+            if (l.over)
+                return false;
+            before = 0;
+        } else {
+            before = n;
+            group_sync<T>();
+        }
+    }
+    return true;
+}
+
 // The exact list of a row's part, tile by tile, into l.keys in order; returns its length.
 template <typename E, int T>
-__device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* px,
-                                                    const uint8_t* pm, int len, int64_t base,
-                                                    int k, int lane)
+__device__ __forceinline__ int exact_list(Candidates<T>& l, const E* px, const uint8_t* pm, int len,
+                                          int64_t base, int k, int lane)
 {
     constexpr int U = kStreamU, CH = kChunk<E>, TILE = T * U * CH;
     uint64_t* best = (uint64_t*)l.raw;   // the list so far, and behind it the tile's
@@ -900,6 +1021,41 @@ __device__ __attribute__((noinline)) int exact_list(Candidates<T>& l, const E* p
         l.keys[i] = best[i];
     group_sync<T>();
     return n;
+}
+
+template <typename V>
+using InLds = __attribute__((address_space(3))) V;
+template <typename V>
+using InGlobal = __attribute__((address_space(1))) V;
+
+// The list of a row's part in a second pass, into l.keys in order; returns its length.  (A call of
+// its own leaves the first pass its registers.  Its pointers say what memory they are of, which a
+// call forgets: a first tile without entries, as above, 540 us.)
+template <typename E, int T>
+__device__ __attribute__((noinline)) int list_again(InLds<Candidates<T>>* lists,
+                                                    InGlobal<const E>* logits,
+                                                    InGlobal<const uint8_t>* mask, int len,
+                                                    int64_t base, int k, int lane, bool any_nan)
+{
+    Candidates<T>& l = *(Candidates<T>*)lists;
+    const E* px = (const E*)logits;
+    const uint8_t* pm = (const uint8_t*)mask;
+    if (any_nan || !careful_list<E, T>(l, px, pm, len, base, k, lane))
+        return exact_list<E, T>(l, px, pm, len, base, k, lane);
+    uint64_t* best = (uint64_t*)l.raw;
+    const int n = l.n_keys;
+    for (int i = lane; i < n; i += T) {
+        const uint64_t key = l.keys[i];
+        const int place = place_of(l.keys, n, key);
+        if (place < k)
+            best[place] = key;
+    }
+    group_sync<T>();
+    const int listed = n < k ? n : k;
+    for (int i = lane; i < listed; i += T)
+        l.keys[i] = best[i];
+    group_sync<T>();
+    return listed;
 }
 
 // LIST: top > 0.  (Without lists the sums alone need no more than four wavefronts a SIMD, and
@@ -985,7 +1141,10 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
             if constexpr (!LIST)
                 continue;
             if (tile == 0) {
-                const int j = (k + W - 1) / W;
+                // wavefronts that a row's end leaves 32 chunks at least: the others have too few
+                // (parts have a tile at least, but for the last one)
+                const int with = PART ? W : max(1, min(W, (a.A + 32 * CH) / (64 * CH)));
+                const int j = (k + with - 1) / with;
                 // (entries instead of chunks where the list is long for so few)
                 auto entries = [&](uint32_t p) {
                     const float v = prefix_value(p);
@@ -1016,7 +1175,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                     bound = scratch[0];
 #pragma unroll
                     for (int i = 1; i < W; ++i)
-                        bound = fminf(bound, scratch[i]);
+                        bound = i < with ? fminf(bound, scratch[i]) : bound;
                 }
                 bound = fmaxf(bound, kLeastFinite);
                 if (lane == 0)
@@ -1066,8 +1225,9 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
         int n = l.n_keys;
         bool sorted = false;
         const int own = apart(lane);
-        if (l.over || st.s != st.s) {
-            n = exact_list<E, T>(l, px, pm, len, base, k, own);
+        if (__builtin_expect(l.over || st.s != st.s, false)) {
+            n = list_again<E, T>((InLds<Candidates<T>>*)&l, (InGlobal<const E>*)px,
+                                 (InGlobal<const uint8_t>*)pm, len, base, k, own, st.s != st.s);
             sorted = true;
         }
         const int64_t to = item * k;
