@@ -700,8 +700,8 @@ malib_status malib_loss_work(int32_t dtype, int64_t rows, int64_t n_actions,
  * m = -inf.  A legal NaN or +inf makes l, H, ln s and top_logp of its row NaN (l of an
  * action that is not legal stays 0); NaNs are listed first.  Sums are formed in fp32 in an
  * order fixed by the sizes.
- * 0 <= rows < 2^31, 1 <= n_actions <= 2^24, rows * top < 2^40.  work: as
- * malib_log_probs_work says, aligned to 16 bytes.
+ * 0 <= rows < 2^31, 1 <= n_actions <= 2^24.  work: as malib_log_probs_work says, aligned to
+ * 16 bytes.
  */
 typedef struct {
     int32_t dtype;           /* MALIB_DT_* of logits, dlogits */

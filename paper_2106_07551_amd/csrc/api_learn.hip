@@ -521,12 +521,10 @@ static malib_status check_aligned(const void* p, const char* what, int bytes)
     return MALIB_OK;
 }
 
-static malib_status check_top(int64_t rows, int32_t top)
+static malib_status check_top(int32_t top)
 {
     if (top < 0 || top > 256)
         return set_error(MALIB_E_INVAL, "top must be in [0, 256]");
-    if (rows * top >= (int64_t)1 << 40)
-        return set_error(MALIB_E_UNSUPPORTED, "rows * top must be below 2^40");
     return MALIB_OK;
 }
 
@@ -534,7 +532,7 @@ malib_status malib_log_probs_work(int32_t dtype, int64_t rows, int64_t A, int32_
                                   int64_t* work_bytes)
 {
     TRY(check_loss(dtype, rows, A));
-    TRY(check_top(rows, top));
+    TRY(check_top(top));
     if (!work_bytes)
         return set_error(MALIB_E_INVAL, "work_bytes is NULL");
     *work_bytes = logp_plan(rows, A, top, type_size(dtype)).work_bytes;
@@ -547,7 +545,7 @@ malib_status malib_log_probs(const malib_log_probs_desc* d, const void* logits,
                              void* stream)
 {
     TRY(check_log_probs(d));
-    TRY(check_top(d->rows, d->top));
+    TRY(check_top(d->top));
     if (d->rows == 0)
         return MALIB_OK;
     TRY(check_scored(d, logits, actions, mask));

@@ -233,12 +233,13 @@ __global__ __launch_bounds__(kLaneThreads) void logp_lane_kernel(LogpArgs a)
 
 // ------------------------------------------------ the exact search, in registers
 
-// Sum of a whole number over the group, in every thread; `half`: which half of scratch is
-// next (see group_combine).
+// Sum of a whole number over the group (a wavefront or a workgroup, as all below), in every
+// thread; `half`: which half of scratch is next (see group_combine).
 template <int T>
 __device__ __forceinline__ int group_count(int v, float* scratch, int& half)
 {
-    float f = lanes_combine<(T < 64 ? T : 64)>((float)v, SumOp());   // (below 2^24: exact)
+    static_assert(T >= 64, "");
+    float f = lanes_combine<64>((float)v, SumOp());   // (below 2^24: exact)
     if constexpr (T > 64) {
         float* h = scratch + half * kScratch;
         if ((threadIdx.x & 63) == 0)
@@ -269,20 +270,19 @@ __device__ __forceinline__ void for_entries(u32x4 (&x)[C], int used, int lane, F
 }
 
 // A value that at least k of the group's entries are not below, or the least finite
-// one: of each of its wavefronts (or parts of one) the j-th largest lane's, the least.
+// one: of each of its wavefronts the j-th largest lane's, the least.
 constexpr int kBoundRounds = 16;
 template <int T>
 __device__ __forceinline__ float lower_bound(float m, int k, float* scratch, int& half)
 {
-    constexpr int TL = T < 64 ? T : 64, W = T / TL;
+    constexpr int W = T / 64;
     const int j = (k + W - 1) / W;
     float bound = kLeastFinite;
-    if (j <= TL / 2 && j <= kBoundRounds) {   // (uniform)
-        const int lane = threadIdx.x & 63, first = lane & ~(TL - 1);
-        const uint64_t group = (TL == 64 ? ~0ull : (1ull << TL) - 1) << first;
+    if (j <= kBoundRounds) {   // (uniform)
+        const int lane = threadIdx.x & 63;
         for (int r = 0; r < j; ++r) {
-            bound = lanes_combine<TL>(m, MaxOp());
-            const uint64_t who = __ballot(m == bound) & group;
+            bound = lanes_combine<64>(m, MaxOp());
+            const uint64_t who = __ballot(m == bound);
             if (lane == __builtin_ctzll(who | 1ull << 63))   // (without NaN some lane is)
                 m = kNegInf;
         }
@@ -319,19 +319,14 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
     // Too many, by chance (a part of the row's entries in few lanes), by ties or since the
     // list is long for so few lanes: the exact value of place k, bit by bit, then, where ties
     // are too many, the index up to which they are listed.
-    // (Lanes of different rows share a wavefront: all go along, and keep what they had.)
-    bool search = n > cap;
-    if (T > 64 ? search : __any(search)) {
+    if (n > cap) {   // (uniform, as all counts)
         auto count_if = [&](auto pred) {
             int v = 0;
             for_entries<E, T, C>(x, used, lane, [&](float f, int i) { v += pred(f, i); });
             return group_count<T>(v, scratch, half);
         };
-        float at = at_least;
-        int above = count_if([&](float f, int) { return f > at || f != f; });
-        bool nan = false;
-        const bool deeper = above >= k;
-        if (T > 64 ? deeper : __any(search && deeper)) {
+        int above = count_if([&](float f, int) { return f > at_least || f != f; });
+        if (above >= k) {
             constexpr int kLast = sizeof(E) == 2 ? 16 : 0;   // (bf16 has no bits below)
             uint32_t t = 0;
             for (int b = 31; b >= kLast; --b) {
@@ -343,34 +338,23 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
             }
             if (kLast > 0 && !(t >> 31))
                 t |= (1u << kLast) - 1u;
-            const bool tn = t > kAboveInf;
-            const float tv = value_of(t);
-            const int c = count_if([&](float f, int) { return tn ? false : f > tv || f != f; });
-            if (deeper) {
-                nan = tn;
-                at = tv;
-                above = c;
-            }
+            is_nan = t > kAboveInf;
+            at_least = value_of(t);
+            above = count_if(
+                [&](float f, int) { return is_nan ? false : f > at_least || f != f; });
         }
-        const int ties = count_if([&](float f, int) { return nan ? f != f : f == at; });
-        int below = 1 << 30;
-        const bool many = above + ties > cap;
-        if (T > 64 ? many : __any(search && many)) {
+        const int ties =
+            count_if([&](float f, int) { return is_nan ? f != f : f == at_least; });
+        if (above + ties > cap) {
             int lo = 0;
             for (int b = 30 - __builtin_clz(T * C * kChunk<E>); b >= 0; --b) {
                 const int next = lo | 1 << b;
                 if (count_if([&](float f, int i) {
-                        return (nan ? f != f : f == at) && i < next;
+                        return (is_nan ? f != f : f == at_least) && i < next;
                     }) <= k - above)
                     lo = next;
             }
-            if (many)
-                below = lo;
-        }
-        if (search) {
-            at_least = at;
-            is_nan = nan;
-            index_below = below;
+            index_below = lo;
         }
         auto listed = [&](float f, int i) {
             return is_nan ? f != f && i < index_below
@@ -1264,6 +1248,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
 // loads, barriers and stores: 3 x 131071 bf16, 40 places 6 us, the parts before it 9.6.
 constexpr int kMergeThreads = 256, kMergeCap = 1024, kMergeAll = 512;
 constexpr int kMergeLists = 2;   // of a thread, at most
+static_assert(kMergeThreads * kMergeLists <= kMergeCap, "");   // (a key of each list fits)
 
 __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
 {
@@ -1354,7 +1339,7 @@ __global__ __launch_bounds__(kMergeThreads) void logp_merge_kernel(LogpArgs a)
         last = block_max(last);
         jth = ~block_max(jth);
         uint64_t bound = last > jth ? last : jth;
-        if (a.splits > top && a.splits <= kMergeCap) {   // (j = 1)
+        if (a.splits > top) {   // (j = 1)
             for (int i = tid; i < a.splits + kPad; i += T)
                 keys[i] = i < a.splits ? lists[(int64_t)i * top] : 0;
             __syncthreads();
