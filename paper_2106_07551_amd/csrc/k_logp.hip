@@ -403,13 +403,24 @@ __device__ __forceinline__ int select_top(u32x4 (&x)[C], int used, int lane, flo
 // us), many by the lists' instructions (65536 x 512 bf16 with one place 28 us, 2.4 TB/s).
 constexpr int kShortMost = 1024, kShortThreads = 256;
 
-// Rounds of a group of T lanes cost their wavefront about 85 instructions for 64 / T rows, a
-// list by the whole wavefront 200 to 300 and what its places take, for one row.
+// The places up to which a group of T lanes with C chunks each finds a list by rounds: their time
+// rises with every place, that of a list by the whole wavefront hardly (us, lists by rounds and by
+// the wavefront at the last size of rounds here and behind it.  1024 rows, C = 1: fp32 x 63, 14
+// and 20 places 5.9 and 6.3, 7.1 and 6.5; x 127, 6 and 8 4.8 and 4.8, 5.3 and 4.9; x 255, 2 and 3
+// 4.1 and 4.3, 4.4 and 4.3; bf16 x 127, 20 and 28 6.8 and 7.6, 8.2 and 8.1; x 255, 10 and 14 5.6
+// and 5.7, 6.5 and 5.7; x 511, 4 and 6 4.8 and 4.9, 5.4 and 5.0.  65536 rows, C = 4: fp32 x 63, 28
+// and 40 28.4 and 29.0, 38.1 and 32.2; x 127, 10 and 14 24.0 and 28.4, 29.9 and 28.8; x 255, 6 and
+// 8 32.7 and 34.4, 37.8 and 35.2; x 511, 4 and 6 51.8 and 57.0, 62.5 and 57.6; bf16 x 127, 40 and
+// 56 37.7 and 43.0, 49.3 and 47.7; x 255, 20 and 28 37.8 and 38.7, 47.9 and 42.3; x 511, 14 and 20
+// 54.0 and 56.2, 67.5 and 58.5; 2040 x 1023, 10 and 14 9.0 and 9.6, 10.6 and 9.8, fp32 3 and 4 6.2
+// and 6.7, 6.9 and 6.8).
+template <typename E>
 constexpr int rounds_most(int T, int C)
 {
-    if (C == 1)
-        return T <= 8 ? 40 : T == 16 ? 20 : T == 32 ? 10 : 6;
-    return T == 4 ? 40 : T == 8 ? 20 : T == 16 ? 10 : T == 32 ? 6 : 3;
+    const int i = T == 4 ? 0 : T == 8 ? 1 : T == 16 ? 2 : T == 32 ? 3 : 4;
+    constexpr int one[2][5] = {{40, 40, 17, 6, 2}, {56, 56, 27, 10, 4}};
+    constexpr int four[2][5] = {{28, 13, 6, 5, 3}, {50, 20, 15, 11, 11}};
+    return C == 1 ? one[sizeof(E) == 2][i] : four[sizeof(E) == 2][i];
 }
 
 struct MaxU32 {
@@ -629,7 +640,7 @@ __global__ __launch_bounds__(kShortThreads) void logp_short_kernel(LogpArgs a)
             store_row(a, row, o);
         if (a.top == 0)
             continue;
-        if (a.top <= rounds_most(T, C)) {
+        if (a.top <= rounds_most<E>(T, C)) {
             list_by_rounds<E, T, C>(a, x, lane, row, live, o);
             continue;
         }
@@ -1490,6 +1501,7 @@ __global__ __launch_bounds__(kLaneThreads) void logp_grad_lane_kernel(LogpArgs a
 // T lanes per row, or per part of one (splits > 1): every entry apart, in chunks of 16
 // bytes.  Bound by memory: 2047 x 50001 bf16, 410 MB, 90 us, 4.5 TB/s.
 constexpr int kGradThreads = 256, kGradUnroll = 4;
+constexpr int64_t kFewGrad = 1 << 17;   // threads
 
 template <typename E, int T>
 __global__ __launch_bounds__(kGradThreads) void logp_grad_kernel(LogpArgs a)
@@ -1576,7 +1588,7 @@ hipError_t launch_as(const LogpArgs& a, const LogpPlan& p, hipStream_t s)
         else
             logp_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
     } else if (p.variant == kLogpShort) {
-        const size_t lds = a.top > rounds_most(p.group, p.chunks)
+        const size_t lds = a.top > rounds_most<E>(p.group, p.chunks)
                                ? (size_t)kShortThreads * p.chunks * 16 +
                                      (size_t)kShortThreads / 64 *
                                          (p.group * p.chunks * kChunk<E> + kPad) * 8
@@ -1618,9 +1630,14 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
             logp_grad_lane_kernel<E, 32><<<nb, kLaneThreads, lds, s>>>(a);
         return hipGetLastError();
     }
+    // Lanes of four chunks each, a round of the loop, or of two where that leaves the CUs few
+    // threads (us, two and four: bf16 65536 x 1000 53 and 43, 65536 x 250 17.5 and 15.4, 4096 x
+    // 2000 10.3 and 9.0, fp32 65536 x 1000 101 and 98; but bf16 4096 x 500 5.3 and 5.5, 200 x 1000
+    // 4.2 and 4.7, 4096 x 100 4.5 and 4.8).  Few wide rows in parts (against one each: fp32 3 x
+    // 131071 4.4 and 35, 40 x 20000 5.0 and 8.3, 300 x 131071 59 and 70, 1500 x 20000 39 and 39).
     const int64_t chunks = (a.A + CH - 1) / CH;
     int T = 4;
-    while (T < kGradThreads && T * 2 < chunks)
+    while (T < kGradThreads && T * (a.rows * T >= kFewGrad ? 4 : 2) < chunks)
         T *= 2;
     if (T == kGradThreads && a.rows < 8 * kCus) {   // parts of at least a round of the loop
         const int64_t want = 8 * kCus / a.rows;
@@ -1660,17 +1677,18 @@ hipError_t launch_grad_as(LogpArgs a, hipStream_t s)
 }  // namespace
 
 // Up to 31 entries a lane per row; up to kShortMost a few lanes.  From half of that on, with many
-// rows and without lists or with more than 6 places, a wavefront (us, 65536 rows of 1024 bf16,
-// few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and 76, 97 and 82, 184 and 157; of
-// 512: 28 and 73, 42 and 80, 95 and 126; fp32 1024 without lists 48 and 39).  Above, a wavefront
-// where there are rows enough and short lists (700 rows of 3000 bf16, lists of 3 and 64 places 8.6
-// and 14.0, a workgroup 10.4 and 12.5; 1657 rows of 1553 fp32 9.2 and 14.2, a workgroup 16.3 and
-// 18.9), else a workgroup, or several where there are fewer rows than fill the CUs: of at least a
-// tile (16 KB) each.  Few rows: a chunk per lane, while that takes no more threads than fill the
-// CUs a few times (us, lists of 6 places, against a lane per row: fp32 4096 x 18 5.4 and 10.0,
-// 65536 x 18 10.4 and 10.8, 131072 x 18 16.6 and 12.9; against four chunks per lane: 4096 x 60
-// 5.3 and 7.0, 65536 x 60 15.7 and 12.6, 4096 x 250 7.7 and 7.7, 16384 x 250 18.7 and 13.0; bf16
-// 131072 x 18 12.4 and 12.5, 4096 x 250 6.3 and 8.2, 16384 x 250 11.9 and 9.9).
+// rows and, in fp32, without lists, or with more than 6 places, a wavefront (us, 65536 rows of
+// 1024 bf16, few lanes and a wavefront, lists of 1, 8 and 64 places: 51 and 76, 97 and 82, 184 and
+// 157; of 512: 28 and 73, 42 and 80, 95 and 126; without lists 29 and 37, 8192 x 640 5.2 and 7.4,
+// fp32 46 and 40, 6.8 and 5.7).  Above, a wavefront where there are rows enough and short lists
+// (700 rows of 3000 bf16, lists of 3 and 64 places 8.6 and 14.0, a workgroup 10.4 and 12.5; 1657
+// rows of 1553 fp32 9.2 and 14.2, a workgroup 16.3 and 18.9), else a workgroup, or several where
+// there are fewer rows than fill the CUs: of at least a tile (16 KB) each.  Few rows: a chunk per
+// lane, while that takes no more threads than fill the CUs a few times (us, lists of 6 places,
+// against a lane per row: fp32 4096 x 18 5.4 and 10.0, 65536 x 18 10.4 and 10.8, 131072 x 18 16.6
+// and 12.9; against four chunks per lane: 4096 x 60 5.3 and 7.0, 65536 x 60 15.7 and 12.6, 4096 x
+// 250 7.7 and 7.7, 16384 x 250 18.7 and 13.0; bf16 131072 x 18 12.4 and 12.5, 4096 x 250 6.3 and
+// 8.2, 16384 x 250 11.9 and 9.9).
 constexpr int64_t kFewLane = 1 << 19, kFewShort = 1 << 18;
 LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
 {
@@ -1686,8 +1704,9 @@ LogpPlan logp_plan(int64_t rows, int64_t A, int top, int size)
     if (A <= kLaneMost && !few) {
         p.variant = kLogpLane;
         per = kLaneThreads;
-    } else if (A <= kShortMost && !(A > kShortMost / 2 && rows >= 8 * kCus &&
-                                    (top == 0 || (top > 6 && top <= kWaveTop)))) {
+    } else if (A <= kShortMost &&
+               !(A > kShortMost / 2 && rows >= 8 * kCus &&
+                 (top == 0 ? size == 4 : top > 6 && top <= kWaveTop))) {
         p.variant = kLogpShort;
         p.chunks = few ? 1 : 4;
         p.group = 4;
