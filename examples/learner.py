@@ -78,7 +78,10 @@ class Teachers:
     """The mixture's policies, frozen: weights [policy][out][in] in bf16 or in 4 bits, all
     policies' logits in one grouped call per layer."""
 
-    FEW = 256    # rows that the layers in 4 bits take as they are
+    # Rows of all policies that the layers in 4 bits take as they are (us, and with the weights in
+    # full width first: one policy's 512 -> 512 bf16, 2048 rows 7.7 and 11.0, 16384 38 and 22, four
+    # policies' 512 rows 7.6 and 11.4, 2048 22.4 and 17.4; of 256 -> 512 the limit lies at 3000)
+    FEW = 4096
 
     def __init__(self, weights, biases, bits=16):
         self.b = biases
@@ -89,7 +92,7 @@ class Teachers:
     def layer(self, l, x, act):
         if self.bits == 16:
             return M.linear(x, self.w[l].to(x.dtype), self.b[l], act=act)
-        if x.shape[-2] <= self.FEW:
+        if len(self.b[l]) * x.shape[-2] <= self.FEW:
             return M.linear_fp4(x, *self.w[l], self.shapes[l][0], self.b[l], act=act)
         return M.linear(x, M.dequantize_fp4(*self.w[l], *self.shapes[l], dtype=x.dtype),
                         self.b[l], act=act)

@@ -33,7 +33,8 @@
  *    flag on the population handle that the next malib_payoff_eval reports
  *    as MALIB_E_DEVICE.
  *  - Results depend only on (inputs, seed, env_offset + local env index):
- *    they are independent of launch geometry, batching and streams.
+ *    they are independent of launch geometry, batching (malib_dropout's mask
+ *    aside, which counts from a call's own first value) and streams.
  *  - A handle must not be used from two threads at once.
  */
 #ifndef MALIB_H
@@ -752,7 +753,9 @@ malib_status malib_log_probs_work(int32_t dtype, int64_t rows, int64_t n_actions
  *  step: a number that the caller changes from call to call; device_step: device int64 [1]
  *       added to it, or NULL (a captured graph then draws other masks in each replay once the
  *       caller adds to it between replays, or within the graph).
- *  layer: tells apart the layers of one step.
+ *  layer: tells apart the layers of one step.  The index counts from this call's first value: parts
+ *       of a batch in calls of their own need a layer or a seed each (the same ones give every part
+ *       the same mask), and do not draw the mask of the undivided batch.
  *  x, y: [rows][cols], strides in elements; y may be x itself; residual: [rows][cols] or
  *       NULL, may be y itself (each: same address and stride).
  * A value that does not stay counts as 0 even if it is infinite or NaN.  Formed in fp32,
@@ -809,13 +812,17 @@ malib_status malib_dequantize_fp4(const malib_fp4_desc* desc, const uint8_t* cod
                                   const uint16_t* scales, const malib_mat* w, void* stream);
 
 /*
- * y = act(x W^T + b) + residual with W in 4 bits; the rest as in malib_linear.  Products
- * are exact (x in bf16, or fp32 x in three bf16 parts: bits below 2^-133 do not count), sums are
- * formed in fp32, scales are applied to the fp32 sums of their weights; a sum that leaves fp32 without
- * its scale is formed again, scaled down, so that results that fit fp32 are finite.  The weights
- * have no gradient, and x none from this call.  For a few rows of x at a time: the weights' codes are taken apart again for every 16
- * or 32 rows, so that for hundreds of rows malib_dequantize_fp4 and malib_linear take less time.
- * No workspace.
+ * y = act(x W^T + b) + residual with W in 4 bits; the rest as in malib_linear.  Products are
+ * exact (x in bf16, or fp32 x in three bf16 parts: bits below 2^-133 do not count), sums are
+ * formed in fp32, scales are applied to the fp32 sums of their weights; a sum that leaves fp32
+ * without its scale is formed again, scaled down, so that results that fit fp32 are finite.  The
+ * weights have no gradient, and x none from this call.  The weights' codes are taken apart again
+ * for every 16 or 32 rows: for many rows (of all groups) malib_dequantize_fp4 and malib_linear
+ * take less time, in bf16 from 500 to 1000 rows on in wide layers (8192 -> 8192, groups of 32
+ * weights: 384 rows 82 and 97 us, 768 166 and 145; 4096 -> 4096: 768 rows 45 and 56, 2048 117
+ * and 79), from 4000 on in narrow ones (512 -> 512); in fp32 only where there are few inputs
+ * (512 -> 8192: 512 rows 57 and 58, 1024 115 and 87; 4096 -> 4096 at no number of rows up to
+ * 4096).  No workspace.
  */
 malib_status malib_linear_fp4(const malib_fp4_desc* desc, const malib_mat* x,
                               const uint8_t* codes, const uint16_t* scales, const float* bias,

@@ -1201,9 +1201,10 @@ def dropout(x, p: float, seed: int, step: int = 0, *, layer: int = 0, residual=N
     """malib_dropout: x k / q + residual, where a value stays (k = 1) with probability q = 1 - p
     (in steps of 2^-16) by the library's random stream, from its index, `seed`, `step`
     (plus the int64 in `device_step`, a device tensor of one number) and `layer`
-    alone.  float32 or bfloat16; contiguous tensors of any shape (the last dimension up to
-    2^24), or [rows][cols] with contiguous rows; `out` may be x or residual.  Outside torch's autograd graph: the
-    gradient is dropout_backward's, the residual's is dy."""
+    alone.  The index is that in x: parts of a batch in calls of their own need a layer or seed
+    each.  float32 or bfloat16; contiguous tensors of any shape (the last dimension up to 2^24), or
+    [rows][cols] with contiguous rows; `out` may be x or residual.  Outside torch's autograd
+    graph: the gradient is dropout_backward's, the residual's is dy."""
     if stream is None and x.is_cuda and (raw := _here(x)) is not None:
         y = (_calls or _native()).dropout(x, p, seed, step, layer, residual, out, device_step,
                                           raw)
@@ -1326,9 +1327,10 @@ def linear_fp4(x, codes, scales, n_out: int, bias=None, *, act: int = ACT_NONE, 
                out=None, stream=None):
     """malib_linear_fp4: act(x w^T + bias) + residual with the weights of quantize_fp4, for
     x [rows][in], or with weights of several policies [groups][rows][in] (x without the
-    group dimension is shared by the groups); float32 or bfloat16, bias float32.  For a few
-    rows of a frozen policy at a time; for hundreds of rows linear on dequantize_fp4's weights
-    takes less time.  Returns [..][rows][out]; nothing here has a gradient."""
+    group dimension is shared by the groups); float32 or bfloat16, bias float32.  For up to
+    hundreds of bfloat16 rows (of all policies) of a wide layer, or thousands of a narrow one or in
+    float32; for more linear on dequantize_fp4's weights takes less time.  Returns
+    [..][rows][out]; nothing here has a gradient."""
     if stream is None and x.is_cuda and (raw := _here(x)) is not None:
         y = (_calls or _native()).linear_fp4(x, codes, scales, n_out, bias, act, residual, out,
                                              raw)
