@@ -476,6 +476,7 @@ struct LogpArgs {
     // set by the launchers
     float two_over_t;
     int splits, part_len;
+    int tile_waves, wave_places;   // of a streaming workgroup's first tile, and of each of them
     bool bf16;
     void* part_stats;
     uint64_t* part_keys;

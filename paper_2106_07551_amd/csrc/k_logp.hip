@@ -1136,10 +1136,7 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
             if constexpr (!LIST)
                 continue;
             if (tile == 0) {
-                // wavefronts that a row's end leaves 32 chunks at least: the others have too few
-                // (parts have a tile at least, but for the last one)
-                const int with = PART ? W : max(1, min(W, (a.A + 32 * CH) / (64 * CH)));
-                const int j = (k + with - 1) / with;
+                const int j = T > 64 ? a.wave_places : k;
                 // (entries instead of chunks where the list is long for so few)
                 auto entries = [&](uint32_t p) {
                     const float v = prefix_value(p);
@@ -1165,12 +1162,12 @@ __global__ __launch_bounds__(256, LIST ? 6 : 4) void logp_stream_kernel(LogpArgs
                 bound = prefix_value(p);
                 if constexpr (W > 1) {
                     if ((lane & 63) == 0)
-                        scratch[lane >> 6] = bound;
+                        scratch[lane >> 6] = (lane >> 6) < a.tile_waves ? bound : -kNegInf;
                     __syncthreads();
                     bound = scratch[0];
 #pragma unroll
                     for (int i = 1; i < W; ++i)
-                        bound = i < with ? fminf(bound, scratch[i]) : bound;
+                        bound = fminf(bound, scratch[i]);
                 }
                 bound = fmaxf(bound, kLeastFinite);
                 if (lane == 0)
@@ -1740,6 +1737,11 @@ hipError_t launch_logp(LogpArgs a, int dtype, const LogpPlan& p, void* work, hip
     a.two_over_t = 2.0f / a.temperature;
     a.splits = p.splits;
     a.part_len = p.part_len;
+    // wavefronts of a streaming workgroup that a row's end leaves 32 chunks at least: the others
+    // have too few for a bound (parts have a tile, but for the last one)
+    const int64_t chunks = p.splits > 1 ? 1024 : (a.A * (a.bf16 ? 2 : 4) + 15) / 16;
+    a.tile_waves = (int)std::max<int64_t>(1, std::min<int64_t>(4, (chunks + 32) / 64));
+    a.wave_places = (a.top + a.tile_waves - 1) / a.tile_waves;
     a.part_stats = work;
     a.part_keys = (uint64_t*)((char*)work + p.stats_bytes);
     return a.bf16 ? launch_as<bf16_t>(a, p, s) : launch_as<float>(a, p, s);
